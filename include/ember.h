@@ -399,6 +399,130 @@ int ember_lmhead_step(void* W, int w_dtype, int64_t ldw,
                       void* ws, size_t ws_bytes, hipStream_t stream);
 
 /*
+ * The final norm: a residual addition, a root-mean-square norm and, where the
+ * rows go to an 8-bit head, their rounding to 8 bits, in one pass.  For each of
+ * T rows of D columns
+ *
+ *   s = x + r                                  (r: the residual stream; may be NULL)
+ *   rstd = 1 / sqrt(mean_j s_j^2 + eps)
+ *   y_j = s_j rstd gain_j
+ *   a = max_j |y_j|,  qscale = a / 127,  q_j = rint(y_j 127 / a)
+ *
+ * Arithmetic is fp32 and y is formed from the unrounded sum.  Outputs, each
+ * NULL if it is not wanted, at least one of Y and Q:
+ *   S (T x D, x_dtype)   the sum, with R only; it may be X or R itself (same ld);
+ *   Y (T x D, y_dtype)   the norm's output (the H of ember_lmhead_step); it may
+ *                        be X itself (same dtype and ld) where S is not;
+ *   Q (T x D, int8) and qscale (T), both or neither: y in 8 bits, codes in
+ *                        [-127, 127], one scale a row.  A row whose a is below
+ *                        1e-36 (zeros among them) has codes and scale 0; one
+ *                        that holds an infinity or a NaN has codes 0 and scale
+ *                        NaN, which makes its logits NaN;
+ *   rstd (T)             kept for the gradient.
+ * X, R (x_dtype), S, Y: layout rules of W and G.  Q: 16-byte aligned, ldq a
+ * multiple of 16; columns D..ldq-1 are not written.  gain: D values of
+ * gain_dtype, 16-byte aligned.  0 <= T <= EMBER_MAX_TOKENS (0: nothing to do, the
+ * pointers may be NULL), 1 <= D <= EMBER_NORM_MAX_D, eps >= 0 and finite.
+ */
+#define EMBER_NORM_MAX_D ((int64_t)32768)
+
+int ember_rmsnorm(const void* X, int x_dtype, int64_t ldx, const void* R, int64_t ldr,
+                  const void* gain, int gain_dtype, float eps, int64_t T, int64_t D,
+                  void* S, int64_t lds, void* Y, int y_dtype, int64_t ldy,
+                  int8_t* Q, int64_t ldq, float* qscale, float* rstd, hipStream_t stream);
+
+/*
+ * The norm's gradient.  S (T x D, x_dtype) is the sum the forward call stored
+ * (or its X, without R) and rstd what it wrote; dY (T x D, x_dtype) the gradient
+ * of Y; dS (T x D, x_dtype, may be NULL) a gradient that reaches the sum by
+ * another way, such as the residual stream.  With u = dy gain:
+ *
+ *   dx_j = rstd u_j - rstd^3 mean_k(u_k s_k) s_j + ds_j    -> dX (T x D, x_dtype)
+ *   dgain_j = sum_t dy_tj s_tj rstd_t                      -> dgain (D, fp32)
+ *
+ * dX is the gradient of X and of R; it may be dY, dS or S itself (same ld).  dgain is
+ * overwritten (zeros for T = 0); its sum has an order fixed by T and D.  The
+ * workspace (device, 256-byte aligned, ember_rmsnorm_grad_workspace_bytes of at
+ * least T tokens and this D) needs no initialisation.
+ */
+int ember_rmsnorm_grad_workspace_bytes(int64_t max_tokens, int64_t D, size_t* bytes);
+
+int ember_rmsnorm_grad(const void* dY, int64_t lddy, const void* S, int x_dtype, int64_t lds,
+                       const void* gain, int gain_dtype, const float* rstd, const void* dS, int64_t ldds,
+                       int64_t T, int64_t D, void* dX, int64_t lddx, float* dgain,
+                       void* ws, size_t ws_bytes, hipStream_t stream);
+
+/*
+ * Rows of a table in 8 bits, as the norm writes Q and qscale, from the rows
+ * themselves: what ember_logits_q8 reads as Wq and wscale.  1 <= D <=
+ * EMBER_NORM_MAX_D, 0 <= rows <= EMBER_MAX_V.
+ */
+int ember_quantize_rows(const void* X, int x_dtype, int64_t ldx, int64_t rows, int64_t D,
+                        int8_t* Q, int64_t ldq, float* qscale, hipStream_t stream);
+
+/*
+ * Logits of an LM head held in 8 bits, for T tokens:
+ *
+ *   Y_tv = (sum_k Xq_tk Wq_vk) xscale_t wscale_v + bias_v
+ *
+ * Xq (T x D) and Wq (V x D) are int8 codes with one fp32 scale a row (xscale: T,
+ * wscale: V), bias (V, fp32) may be NULL, Y is T x V of y_dtype.  The sum over D
+ * is exact (int32), the scaling fp32, and the result is rounded once to y_dtype.
+ * Layout: bases 16-byte aligned, ldx and ldw multiples of 16, Y as W and G.  The
+ * padding of Xq and Wq (columns D..ld-1) is not used.  0 <= T <=
+ * EMBER_MAX_TOKENS (0: nothing to do), 1 <= V <= EMBER_MAX_V,
+ * 1 <= D <= EMBER_NORM_MAX_D.
+ */
+int ember_logits_q8(const int8_t* Xq, int64_t ldx, const float* xscale,
+                    const int8_t* Wq, int64_t ldw, const float* wscale, const float* bias,
+                    int64_t T, int64_t V, int64_t D, void* Y, int y_dtype, int64_t ldy, hipStream_t stream);
+
+/*
+ * Global gradient norm and clipping.  Over all n_grads tensors together
+ *
+ *   norm = sqrt(sum g^2),   factor = max_norm / norm if norm > max_norm, else 1
+ *   dst = factor src        (rounded once to dst_dtype)
+ *
+ * and out[0] = norm, out[1] = factor (device, fp32), with no host read: the
+ * tables' steps can follow on the stream at once.  A norm that is NaN or
+ * infinite gives factor 1.  Squares are summed in float64 in a fixed order.
+ *
+ * One ember_grad per tensor: rows x cols elements, row i at element i * ld;
+ *   src, src_dtype, lds   the gradient, aligned to its element size (views at
+ *                         any element of a bucket are fine);
+ *   dst, dst_dtype, ldd   where it goes: src itself (same dtype and ld; in
+ *                         place, and then nothing is written when factor is 1) or
+ *                         other memory, of either dtype;
+ *   rows_dev              NULL, or a device int64 (8-byte aligned) that says how
+ *                         many of the rows hold a gradient (ember_coalesce_rows
+ *                         writes it); the others are neither read nor written.
+ *                         A value outside [0, rows] counts as the nearer end.
+ * Tensors must not overlap each other's memory.  rows, cols >= 0 (an empty
+ * tensor's pointers may be NULL), rows * cols <= 2^42, 0 <= n_grads <=
+ * EMBER_MAX_GRADS, max_norm >= 0 (infinite: only the norm, and copies).  The
+ * workspace (device, 256-byte aligned, ember_clip_workspace_bytes(n_grads))
+ * needs no initialisation.  grads is read before the call returns.
+ */
+#define EMBER_MAX_GRADS ((int64_t)(1 << 16))
+
+typedef struct {
+    const void* src;
+    int src_dtype;
+    int64_t lds;
+    void* dst;
+    int dst_dtype;
+    int64_t ldd;
+    int64_t rows;
+    int64_t cols;
+    const int64_t* rows_dev;
+} ember_grad;
+
+int ember_clip_workspace_bytes(int64_t n_grads, size_t* bytes);
+
+int ember_clip_grads(const ember_grad* grads, int64_t n_grads, float max_norm, float* out,
+                     void* ws, size_t ws_bytes, hipStream_t stream);
+
+/*
  * Device status of the most recent step enqueued with this workspace.
  * Synchronises `stream`, then sets *device_status to EMBER_OK or
  * EMBER_ERR_INDEX.  Returns EMBER_OK, EMBER_ERR_ARG or EMBER_ERR_HIP.

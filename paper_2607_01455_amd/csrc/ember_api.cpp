@@ -274,6 +274,75 @@ hipError_t run_phase(const std::vector<const StepArgs*>& order, Key key, Launch 
     return hipSuccess;
 }
 
+// ---------------------------------------------------------------------------
+// norm, 8-bit rows and logits, clipping
+// ---------------------------------------------------------------------------
+
+int check_tokens(int64_t T, int64_t D) {
+    return T < 0 || T > EMBER_MAX_TOKENS || D < 1 || D > EMBER_NORM_MAX_D ? EMBER_ERR_SHAPE : EMBER_OK;
+}
+
+int check_gain(const void* gain, int dtype) {
+    if (!dtype_ok(dtype)) return EMBER_ERR_DTYPE;
+    if (gain == nullptr) return EMBER_ERR_ARG;
+    return aligned(gain, 16) ? EMBER_OK : EMBER_ERR_ALIGN;
+}
+
+// Rows of codes and their scales; both NULL where that is allowed.
+int check_codes(const int8_t* q, int64_t ld, const float* scale, int64_t D, bool may_be_null) {
+    if (q == nullptr && scale == nullptr && may_be_null) return EMBER_OK;
+    if (q == nullptr || scale == nullptr) return EMBER_ERR_ARG;
+    if (ld < D) return EMBER_ERR_SHAPE;
+    return aligned(q, 16) && ld % 16 == 0 && aligned(scale, 4) ? EMBER_OK : EMBER_ERR_ALIGN;
+}
+
+// Memory a call writes, and memory it reads.  An output with the base, the
+// stride and the element size of an input takes its place element for element,
+// which the kernels allow where elem is set on both.
+struct Output {
+    const void* p;
+    size_t bytes, elem;
+    int64_t ld;
+};
+struct Input {
+    Span span;
+    const void* p;
+    size_t elem;
+    int64_t ld;
+};
+bool bad_overlap(const Output* outs, int n_out, const Input* ins, int n_in) {
+    for (int i = 0; i < n_out; ++i) {
+        if (outs[i].p == nullptr) continue;
+        const Span o = span_of(outs[i].p, outs[i].bytes);
+        for (int j = 0; j < i; ++j)
+            if (outs[j].p != nullptr && overlap(o, span_of(outs[j].p, outs[j].bytes))) return true;
+        for (int j = 0; j < n_in; ++j) {
+            const bool same = outs[i].elem != 0 && ins[j].p == outs[i].p && ins[j].elem == outs[i].elem &&
+                              ins[j].ld == outs[i].ld;
+            if (!same && overlap(o, ins[j].span)) return true;
+        }
+    }
+    return false;
+}
+
+int check_grad(const ember_grad& g) {
+    if (g.rows < 0 || g.cols < 0) return EMBER_ERR_SHAPE;
+    if (!dtype_ok(g.src_dtype) || !dtype_ok(g.dst_dtype)) return EMBER_ERR_DTYPE;
+    if (g.rows == 0 || g.cols == 0) return EMBER_OK;
+    if (g.cols > ((int64_t)1 << 42) / g.rows) return EMBER_ERR_SHAPE;
+    if (g.rows > 1 && (g.lds < g.cols || g.ldd < g.cols)) return EMBER_ERR_SHAPE;
+    if (g.src == nullptr || g.dst == nullptr) return EMBER_ERR_ARG;
+    if (!aligned(g.src, dtype_size(g.src_dtype)) || !aligned(g.dst, dtype_size(g.dst_dtype)) ||
+        (g.rows_dev != nullptr && !aligned(g.rows_dev, 8)))
+        return EMBER_ERR_ALIGN;
+    if (g.src == g.dst)
+        return g.src_dtype == g.dst_dtype && (g.rows == 1 || g.lds == g.ldd) ? EMBER_OK : EMBER_ERR_ARG;
+    const auto span = [&](const void* p, int dtype, int64_t ld) {
+        return span_of(p, matrix_bytes(g.rows, g.rows == 1 ? g.cols : ld, g.cols, dtype));
+    };
+    return overlap(span(g.src, g.src_dtype, g.lds), span(g.dst, g.dst_dtype, g.ldd)) ? EMBER_ERR_ARG : EMBER_OK;
+}
+
 } // namespace
 
 extern "C" {
@@ -713,6 +782,157 @@ int ember_coalesce_rows(const int64_t* tok, int64_t n_tok, const void* U, int u_
     a.n_out = n_out;
     a.ws = static_cast<char*>(ws);
     hipError_t e = timed("ember_coalesce", stream, [&] { return ember::launch_coalesce(a, stream); });
+    return e == hipSuccess ? EMBER_OK : EMBER_ERR_HIP;
+}
+
+int ember_rmsnorm(const void* X, int x_dtype, int64_t ldx, const void* R, int64_t ldr, const void* gain,
+                  int gain_dtype, float eps, int64_t T, int64_t D, void* S, int64_t lds, void* Y, int y_dtype,
+                  int64_t ldy, int8_t* Q, int64_t ldq, float* qscale, float* rstd, hipStream_t stream) {
+    int st = check_tokens(T, D);
+    if (st == EMBER_OK) st = check_matrix(X, x_dtype, ldx, D, T == 0);
+    if (st == EMBER_OK && R != nullptr) st = check_matrix(R, x_dtype, ldr, D, false);
+    if (st == EMBER_OK && S != nullptr) st = check_matrix(S, x_dtype, lds, D, false);
+    if (st == EMBER_OK && Y != nullptr) st = check_matrix(Y, y_dtype, ldy, D, false);
+    if (st == EMBER_OK) st = check_codes(Q, ldq, qscale, D, true);
+    if (st == EMBER_OK) st = check_gain(gain, gain_dtype);
+    if (st == EMBER_OK && (!(eps >= 0.0f) || !std::isfinite(eps))) st = EMBER_ERR_ARG;
+    if (st == EMBER_OK && T > 0 && Y == nullptr && Q == nullptr) st = EMBER_ERR_ARG;
+    if (st == EMBER_OK && S != nullptr && R == nullptr) st = EMBER_ERR_ARG;
+    if (st == EMBER_OK && rstd != nullptr && !aligned(rstd, 4)) st = EMBER_ERR_ALIGN;
+    if (st != EMBER_OK || T == 0) return st;
+    const size_t es = dtype_size(x_dtype);
+    const Span x = span_of(X, matrix_bytes(T, ldx, D, x_dtype));
+    const Span r = R ? span_of(R, matrix_bytes(T, ldr, D, x_dtype)) : span_of(nullptr, 0);
+    // a row's outputs may take the place of its inputs, element for element;
+    // any other overlap of an output would be read or written by another row
+    const Output outs[] = {
+        {S, S ? matrix_bytes(T, lds, D, x_dtype) : 0, es, lds},
+        {Y, Y ? matrix_bytes(T, ldy, D, y_dtype) : 0, Y ? dtype_size(y_dtype) : 0, ldy},
+        {Q, Q ? (size_t)(T - 1) * (size_t)ldq + (size_t)D : 0, 1, ldq},
+        {qscale, Q ? (size_t)T * 4 : 0, 0, 0},
+        {rstd, rstd ? (size_t)T * 4 : 0, 0, 0},
+    };
+    const Input ins[] = {{x, X, es, ldx}, {r, R, es, ldr},
+                         {span_of(gain, (size_t)D * dtype_size(gain_dtype)), nullptr, 0, 0}};
+    if (bad_overlap(outs, 5, ins, 3)) return EMBER_ERR_ARG;
+    const ember::NormArgs a{X, x_dtype, ldx, R, ldr, gain, gain_dtype, eps, T, D, S, lds, Y, y_dtype, ldy,
+                            Q, ldq, qscale, rstd};
+    const hipError_t e = timed("ember_rmsnorm", stream, [&] { return ember::launch_rmsnorm(a, stream); });
+    return e == hipSuccess ? EMBER_OK : EMBER_ERR_HIP;
+}
+
+int ember_rmsnorm_grad_workspace_bytes(int64_t max_tokens, int64_t D, size_t* bytes) {
+    if (bytes == nullptr) return EMBER_ERR_ARG;
+    const int st = check_tokens(max_tokens, D);
+    if (st != EMBER_OK) return st;
+    *bytes = ember::norm_grad_ws_bytes(max_tokens, D);
+    return EMBER_OK;
+}
+
+int ember_rmsnorm_grad(const void* dY, int64_t lddy, const void* S, int x_dtype, int64_t lds, const void* gain,
+                       int gain_dtype, const float* rstd, const void* dS, int64_t ldds, int64_t T, int64_t D,
+                       void* dX, int64_t lddx, float* dgain, void* ws, size_t ws_bytes, hipStream_t stream) {
+    int st = check_tokens(T, D);
+    if (st == EMBER_OK) st = check_matrix(dY, x_dtype, lddy, D, T == 0);
+    if (st == EMBER_OK) st = check_matrix(S, x_dtype, lds, D, T == 0);
+    if (st == EMBER_OK) st = check_matrix(dX, x_dtype, lddx, D, T == 0);
+    if (st == EMBER_OK && dS != nullptr) st = check_matrix(dS, x_dtype, ldds, D, false);
+    if (st == EMBER_OK) st = check_gain(gain, gain_dtype);
+    if (st == EMBER_OK && ((T > 0 && rstd == nullptr) || dgain == nullptr || ws == nullptr)) st = EMBER_ERR_ARG;
+    if (st == EMBER_OK && (!aligned(rstd, 4) || !aligned(dgain, 4) || !aligned(ws, 256))) st = EMBER_ERR_ALIGN;
+    if (st == EMBER_OK && ws_bytes < ember::norm_grad_ws_bytes(T, D)) st = EMBER_ERR_WORKSPACE;
+    if (st != EMBER_OK) return st;
+    const size_t es = dtype_size(x_dtype);
+    const Output outs[] = {
+        {T ? dX : nullptr, T ? matrix_bytes(T, lddx, D, x_dtype) : 0, es, lddx},
+        {dgain, (size_t)D * 4, 0, 0},
+        {ws, ember::norm_grad_ws_bytes(T, D), 0, 0},
+    };
+    const Input ins[] = {
+        {span_of(dY, matrix_bytes(T, lddy, D, x_dtype)), dY, es, lddy},
+        {span_of(S, matrix_bytes(T, lds, D, x_dtype)), S, es, lds},
+        {span_of(dS, dS ? matrix_bytes(T, ldds, D, x_dtype) : 0), dS, es, ldds},
+        {span_of(gain, (size_t)D * dtype_size(gain_dtype)), nullptr, 0, 0},
+        {span_of(rstd, (size_t)T * 4), nullptr, 0, 0},
+    };
+    if (bad_overlap(outs, 3, ins, 5)) return EMBER_ERR_ARG;
+    const ember::NormGradArgs a{dY, lddy, S, x_dtype, lds, gain, gain_dtype, rstd, dS, ldds, T, D, dX, lddx, dgain,
+                                static_cast<char*>(ws)};
+    const hipError_t e = timed("ember_rmsnorm_grad", stream, [&] { return ember::launch_rmsnorm_grad(a, stream); });
+    return e == hipSuccess ? EMBER_OK : EMBER_ERR_HIP;
+}
+
+int ember_quantize_rows(const void* X, int x_dtype, int64_t ldx, int64_t rows, int64_t D, int8_t* Q, int64_t ldq,
+                        float* qscale, hipStream_t stream) {
+    if (rows < 0 || rows > EMBER_MAX_V || D < 1 || D > EMBER_NORM_MAX_D) return EMBER_ERR_SHAPE;
+    int st = check_matrix(X, x_dtype, ldx, D, rows == 0);
+    if (st == EMBER_OK) st = check_codes(Q, ldq, qscale, D, rows == 0);
+    if (st == EMBER_OK && rows > 0 && Q == nullptr) st = EMBER_ERR_ARG;
+    if (st != EMBER_OK || rows == 0) return st;
+    const Output outs[] = {{Q, (size_t)(rows - 1) * (size_t)ldq + (size_t)D, 1, ldq},
+                           {qscale, (size_t)rows * 4, 0, 0}};
+    const Input ins[] = {{span_of(X, matrix_bytes(rows, ldx, D, x_dtype)), nullptr, 0, 0}};
+    if (bad_overlap(outs, 2, ins, 1)) return EMBER_ERR_ARG;
+    ember::NormArgs a{};
+    a.X = X;
+    a.x_dtype = x_dtype;
+    a.ldx = ldx;
+    a.T = rows;
+    a.D = D;
+    a.Q = Q;
+    a.ldq = ldq;
+    a.qscale = qscale;
+    const hipError_t e = timed("ember_quantize_rows", stream, [&] { return ember::launch_rmsnorm(a, stream); });
+    return e == hipSuccess ? EMBER_OK : EMBER_ERR_HIP;
+}
+
+int ember_logits_q8(const int8_t* Xq, int64_t ldx, const float* xscale, const int8_t* Wq, int64_t ldw,
+                    const float* wscale, const float* bias, int64_t T, int64_t V, int64_t D, void* Y, int y_dtype,
+                    int64_t ldy, hipStream_t stream) {
+    int st = check_tokens(T, D);
+    if (st == EMBER_OK && (V < 1 || V > EMBER_MAX_V)) st = EMBER_ERR_SHAPE;
+    if (st == EMBER_OK) st = check_codes(Xq, ldx, xscale, D, T == 0);
+    if (st == EMBER_OK && T > 0 && Xq == nullptr) st = EMBER_ERR_ARG;
+    if (st == EMBER_OK) st = check_codes(Wq, ldw, wscale, D, false);
+    if (st == EMBER_OK && Wq == nullptr) st = EMBER_ERR_ARG;
+    if (st == EMBER_OK) st = check_matrix(Y, y_dtype, ldy, V, T == 0);
+    if (st == EMBER_OK && bias != nullptr && !aligned(bias, 4)) st = EMBER_ERR_ALIGN;
+    if (st != EMBER_OK || T == 0) return st;
+    const Output outs[] = {{Y, matrix_bytes(T, ldy, V, y_dtype), 0, 0}};
+    const Input ins[] = {
+        {span_of(Xq, (size_t)(T - 1) * (size_t)ldx + (size_t)D), nullptr, 0, 0},
+        {span_of(Wq, (size_t)(V - 1) * (size_t)ldw + (size_t)D), nullptr, 0, 0},
+        {span_of(xscale, (size_t)T * 4), nullptr, 0, 0},
+        {span_of(wscale, (size_t)V * 4), nullptr, 0, 0},
+        {span_of(bias, bias ? (size_t)V * 4 : 0), nullptr, 0, 0},
+    };
+    if (bad_overlap(outs, 1, ins, 5)) return EMBER_ERR_ARG;
+    const ember::LogitsArgs a{Xq, ldx, xscale, Wq, ldw, wscale, bias, T, V, D, Y, y_dtype, ldy};
+    const hipError_t e = timed("ember_logits_q8", stream, [&] { return ember::launch_logits(a, stream); });
+    return e == hipSuccess ? EMBER_OK : EMBER_ERR_HIP;
+}
+
+int ember_clip_workspace_bytes(int64_t n_grads, size_t* bytes) {
+    if (bytes == nullptr) return EMBER_ERR_ARG;
+    if (n_grads < 0 || n_grads > EMBER_MAX_GRADS) return EMBER_ERR_SHAPE;
+    *bytes = ember::clip_ws_bytes(n_grads);
+    return EMBER_OK;
+}
+
+int ember_clip_grads(const ember_grad* grads, int64_t n_grads, float max_norm, float* out, void* ws,
+                     size_t ws_bytes, hipStream_t stream) {
+    if (n_grads < 0 || n_grads > EMBER_MAX_GRADS) return EMBER_ERR_SHAPE;
+    if ((n_grads > 0 && grads == nullptr) || out == nullptr || ws == nullptr || !(max_norm >= 0.0f))
+        return EMBER_ERR_ARG;
+    for (int64_t i = 0; i < n_grads; ++i) {
+        const int st = check_grad(grads[i]);
+        if (st != EMBER_OK) return st;
+    }
+    if (!aligned(out, 4) || !aligned(ws, 256)) return EMBER_ERR_ALIGN;
+    if (ws_bytes < ember::clip_ws_bytes(n_grads)) return EMBER_ERR_WORKSPACE;
+    const hipError_t e = timed("ember_clip_grads", stream, [&] {
+        return ember::launch_clip(grads, n_grads, max_norm, out, static_cast<char*>(ws), stream);
+    });
     return e == hipSuccess ? EMBER_OK : EMBER_ERR_HIP;
 }
 

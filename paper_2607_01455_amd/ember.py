@@ -33,7 +33,9 @@ EXPORTED = ("ember_workspace_bytes", "ember_init_state", "ember_step_dense",
             "ember_step_sparse_rows", "ember_rowonly_init_state", "ember_rowonly_step_dense",
             "ember_rowonly_step_sparse_rows", "ember_step_sparse_rows_devn",
             "ember_rowonly_step_sparse_rows_devn", "ember_coalesce_workspace_bytes", "ember_coalesce_rows",
-            "ember_lmhead_step", "ember_step_multi", "ember_get_error", "ember_strerror",
+            "ember_lmhead_step", "ember_rmsnorm", "ember_rmsnorm_grad_workspace_bytes", "ember_rmsnorm_grad",
+            "ember_quantize_rows", "ember_logits_q8", "ember_clip_workspace_bytes", "ember_clip_grads",
+            "ember_step_multi", "ember_get_error", "ember_strerror",
             "ember_profile_enable", "ember_profile_collect", "ember_stream_probe",
             "ember_set_barrier_wait_ticks",
             "ember_step_sparse_rows_static")
@@ -58,6 +60,13 @@ class TableStep(ctypes.Structure):
                 ("V", ctypes.c_int64), ("D", ctypes.c_int64), ("t", ctypes.c_int64),
                 ("lr", ctypes.c_float), ("beta2", ctypes.c_float), ("eps", ctypes.c_float),
                 ("maximize", ctypes.c_int), ("ws", ctypes.c_void_p), ("ws_bytes", ctypes.c_size_t)]
+
+
+class Grad(ctypes.Structure):
+    """One tensor of ember_clip_grads (the C struct ember_grad)."""
+    _fields_ = [("src", ctypes.c_void_p), ("src_dtype", ctypes.c_int), ("lds", ctypes.c_int64),
+                ("dst", ctypes.c_void_p), ("dst_dtype", ctypes.c_int), ("ldd", ctypes.c_int64),
+                ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("rows_dev", ctypes.c_void_p)]
 
 
 class _KernelStat(ctypes.Structure):
@@ -88,6 +97,14 @@ def _load(path: str = _LIB_PATH) -> ctypes.CDLL:
     lib.ember_coalesce_rows.argtypes = [vp, i64, vp, i32, i64, i64, i64, vp, vp, i32, i64, vp, vp, sz, vp]
     lib.ember_lmhead_step.argtypes = [vp, i32, i64, vp, i64, vp, i64, i64, vp, i32, i64, vp, vp, i64, i64, i64,
                                       f32, f32, f32, i32, vp, sz, vp]
+    lib.ember_rmsnorm.argtypes = [vp, i32, i64, vp, i64, vp, i32, f32, i64, i64, vp, i64, vp, i32, i64, vp, i64,
+                                  vp, vp, vp]
+    lib.ember_rmsnorm_grad_workspace_bytes.argtypes = [i64, i64, ctypes.POINTER(sz)]
+    lib.ember_rmsnorm_grad.argtypes = [vp, i64, vp, i32, i64, vp, i32, vp, vp, i64, i64, i64, vp, i64, vp, vp, sz, vp]
+    lib.ember_quantize_rows.argtypes = [vp, i32, i64, i64, i64, vp, i64, vp, vp]
+    lib.ember_logits_q8.argtypes = [vp, i64, vp, vp, i64, vp, vp, i64, i64, i64, vp, i32, i64, vp]
+    lib.ember_clip_workspace_bytes.argtypes = [i64, ctypes.POINTER(sz)]
+    lib.ember_clip_grads.argtypes = [ctypes.POINTER(Grad), i64, f32, vp, vp, sz, vp]
     lib.ember_step_multi.argtypes = [ctypes.POINTER(TableStep), i32, vp]
     lib.ember_get_error.argtypes = [vp, vp, ctypes.POINTER(i32)]
     lib.ember_strerror.argtypes = [i32]
@@ -336,6 +353,198 @@ def ember_lmhead_step(W: torch.Tensor, dY: torch.Tensor, H: torch.Tensor, G: tor
                                  _ptr(G), _dtype(G), _ld(G), _ptr(r), _ptr(c), V, D, int(t), float(lr),
                                  float(beta2), float(eps), int(bool(maximize)), _ptr(ws),
                                  ws.numel() * ws.element_size(), _stream(W)), "ember_lmhead_step")
+
+
+def _shaped(what: str, t: torch.Tensor | None, shape, dtype=None) -> None:
+    """Refuses a tensor the C entry point would index past its end: those know
+    pointers and the sizes they are given, not what memory lies behind them."""
+    if t is None:
+        return
+    if t.shape != shape:
+        raise ValueError(f"{what}: shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{what}: {t.dtype}, expected {dtype}")
+    if len(shape) == 1 and shape[0] > 1 and t.stride(0) != 1:
+        raise TypeError(f"{what}: a contiguous tensor is required")
+
+
+def ember_rmsnorm(X: torch.Tensor, gain: torch.Tensor, eps: float = 1e-6, R: torch.Tensor | None = None,
+                  S: torch.Tensor | None = None, Y: torch.Tensor | None = None, Q: torch.Tensor | None = None,
+                  qscale: torch.Tensor | None = None, rstd: torch.Tensor | None = None) -> None:
+    """S = X + R and its root-mean-square norm with gains, to Y and, in 8 bits
+    with one scale a row, to (Q, qscale); rstd is kept for the gradient."""
+    shape = X.shape
+    T, D = shape
+    rows = (T,)
+    _shaped("gain", gain, (D,))
+    _shaped("R", R, shape, X.dtype)
+    _shaped("S", S, shape, X.dtype)
+    _shaped("Y", Y, shape)
+    _shaped("Q", Q, shape, torch.int8)
+    _shaped("qscale", qscale, rows, torch.float32)
+    _shaped("rstd", rstd, rows, torch.float32)
+    _check(LIB.ember_rmsnorm(_ptr(X), _dtype(X), _ld(X), _ptr(R), 0 if R is None else _ld(R), _ptr(gain),
+                             _dtype(gain), eps, T, D, _ptr(S), 0 if S is None else _ld(S), _ptr(Y),
+                             EMBER_F32 if Y is None else _dtype(Y), 0 if Y is None else _ld(Y), _ptr(Q),
+                             0 if Q is None else _ld(Q), _ptr(qscale), _ptr(rstd), _stream(X)), "ember_rmsnorm")
+
+
+def ember_rmsnorm_grad_workspace_bytes(max_tokens: int, D: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(LIB.ember_rmsnorm_grad_workspace_bytes(int(max_tokens), int(D), ctypes.byref(out)),
+           "ember_rmsnorm_grad_workspace_bytes")
+    return out.value
+
+
+def ember_rmsnorm_grad(dY: torch.Tensor, S: torch.Tensor, gain: torch.Tensor, rstd: torch.Tensor,
+                       dX: torch.Tensor, dgain: torch.Tensor, ws: torch.Tensor,
+                       dS: torch.Tensor | None = None) -> None:
+    """Gradient of ember_rmsnorm: dX (of X and of R) and dgain from dY, the sum S
+    and rstd of the forward call, plus dS, the sum's gradient by other ways."""
+    shape = S.shape
+    T, D = shape
+    _shaped("dY", dY, shape, S.dtype)
+    _shaped("dX", dX, shape, S.dtype)
+    _shaped("dS", dS, shape, S.dtype)
+    _shaped("gain", gain, (D,))
+    _shaped("rstd", rstd, (T,), torch.float32)
+    _shaped("dgain", dgain, (D,), torch.float32)
+    _check(LIB.ember_rmsnorm_grad(_ptr(dY), _ld(dY), _ptr(S), _dtype(S), _ld(S), _ptr(gain), _dtype(gain),
+                                  _ptr(rstd), _ptr(dS), 0 if dS is None else _ld(dS), T, D, _ptr(dX), _ld(dX),
+                                  _ptr(dgain), _ptr(ws), ws.numel() * ws.element_size(), _stream(dgain)),
+           "ember_rmsnorm_grad")
+
+
+def ember_quantize_rows(X: torch.Tensor, Q: torch.Tensor, qscale: torch.Tensor) -> None:
+    """Rows of X in 8 bits: codes Q and one scale a row."""
+    rows, D = X.shape
+    _shaped("Q", Q, X.shape, torch.int8)
+    _shaped("qscale", qscale, (rows,), torch.float32)
+    _check(LIB.ember_quantize_rows(_ptr(X), _dtype(X), _ld(X), rows, D, _ptr(Q), _ld(Q), _ptr(qscale),
+                                   _stream(X)), "ember_quantize_rows")
+
+
+def ember_logits_q8(Xq: torch.Tensor, xscale: torch.Tensor, Wq: torch.Tensor, wscale: torch.Tensor,
+                    Y: torch.Tensor, bias: torch.Tensor | None = None) -> None:
+    """Y = (Xq Wq^T) xscale wscale + bias: logits of T tokens from 8-bit hidden
+    states and an 8-bit table, each with one scale a row."""
+    T, D = Xq.shape
+    V = Wq.shape[0]
+    _shaped("Xq", Xq, (T, D), torch.int8)
+    _shaped("Wq", Wq, (V, D), torch.int8)
+    _shaped("xscale", xscale, (T,), torch.float32)
+    _shaped("wscale", wscale, (V,), torch.float32)
+    _shaped("bias", bias, (V,), torch.float32)
+    _shaped("Y", Y, (T, V))
+    _check(LIB.ember_logits_q8(_ptr(Xq), _ld(Xq), _ptr(xscale), _ptr(Wq), _ld(Wq), _ptr(wscale), _ptr(bias),
+                               T, V, D, _ptr(Y), _dtype(Y), _ld(Y), _stream(Wq)), "ember_logits_q8")
+
+
+def ember_clip_workspace_bytes(n_grads: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(LIB.ember_clip_workspace_bytes(int(n_grads), ctypes.byref(out)), "ember_clip_workspace_bytes")
+    return out.value
+
+
+def grad_entry(src: torch.Tensor, dst: torch.Tensor | None = None, rows_dev: torch.Tensor | None = None) -> Grad:
+    """One entry of ember_clip_grads: the gradient src, written clipped to dst
+    (None: in place); rows_dev: a device int64 of one element that says how many
+    of its rows hold a gradient.  A 2-D tensor with unit column stride, or any
+    contiguous one.  The tensors must stay alive until the call has run."""
+    if dst is None:
+        dst = src
+    if dst.shape != src.shape:
+        raise ValueError(f"gradient {tuple(src.shape)} does not fit its destination {tuple(dst.shape)}")
+    if rows_dev is not None and (rows_dev.dtype != torch.int64 or src.dim() != 2):
+        raise TypeError("rows_dev must be int64 and its gradient 2-D")
+    if src.dim() == 2:
+        (rows, cols), lds, ldd = src.shape, src.stride(0), dst.stride(0)
+        for t in (src, dst):
+            if cols > 1 and t.stride(1) != 1 and t.numel():
+                raise TypeError("a 2-D gradient needs unit column stride")
+        if rows == 1:
+            lds = ldd = cols
+    else:
+        if not (src.is_contiguous() and dst.is_contiguous()):
+            raise TypeError("a gradient that is not 2-D must be contiguous")
+        rows, cols = 1, src.numel()
+        lds = ldd = cols
+    return Grad(_ptr(src), _dtype(src), lds, _ptr(dst), _dtype(dst), ldd, rows, cols, _ptr(rows_dev))
+
+
+def ember_clip_grads(grads, max_norm: float, out: torch.Tensor, ws: torch.Tensor) -> None:
+    """Clip gradients (a ctypes array of Grad entries, or a list of them) by
+    their global norm; out (device, two floats) receives the norm and the factor."""
+    arr = grads if isinstance(grads, ctypes.Array) else (Grad * len(grads))(*grads)
+    _shaped("out", out, (2,), torch.float32)
+    _check(LIB.ember_clip_grads(arr, len(arr), float(max_norm), _ptr(out), _ptr(ws),
+                                ws.numel() * ws.element_size(), _stream(out)), "ember_clip_grads")
+
+
+class HeadNorm:
+    """The final norm of a model: its gains (D values), eps and the workspace of
+    its gradient for up to max_tokens tokens.  Call it for the norm; ``grad`` is
+    its gradient."""
+
+    def __init__(self, gain: torch.Tensor, eps: float = 1e-6, max_tokens: int = 0):
+        self.gain, self.eps, self.max_tokens = gain, float(eps), int(max_tokens)
+        self.D = gain.numel()
+        nbytes = ember_rmsnorm_grad_workspace_bytes(self.max_tokens, self.D)
+        self.ws = torch.empty(nbytes, dtype=torch.uint8, device=gain.device)
+
+    def __call__(self, X, R=None, S=None, Y=None, Q=None, qscale=None, rstd=None) -> None:
+        ember_rmsnorm(X, self.gain, self.eps, R, S, Y, Q, qscale, rstd)
+
+    def grad(self, dY, S, rstd, dX, dgain, dS=None) -> None:
+        ember_rmsnorm_grad(dY, S, self.gain, rstd, dX, dgain, self.ws, dS)
+
+
+class HeadQ8:
+    """An LM head in 8 bits: codes Wq (V x D, rows on 16-byte boundaries), one
+    scale a row and, if the head has one, a bias."""
+
+    def __init__(self, Wq: torch.Tensor, wscale: torch.Tensor, bias: torch.Tensor | None = None):
+        self.Wq, self.wscale, self.bias = Wq, wscale, bias
+
+    @classmethod
+    def from_table(cls, W: torch.Tensor, bias: torch.Tensor | None = None) -> "HeadQ8":
+        """The head of a table (V x D, fp32 or bf16)."""
+        V, D = W.shape
+        Wq = torch.empty(V, (D + 15) // 16 * 16, dtype=torch.int8, device=W.device)[:, :D]
+        head = cls(Wq, torch.empty(V, dtype=torch.float32, device=W.device), bias)
+        head.load(W)
+        return head
+
+    def load(self, W: torch.Tensor) -> None:
+        """Take the table's present rows (after steps on it)."""
+        ember_quantize_rows(W, self.Wq, self.wscale)
+
+    def logits(self, Xq: torch.Tensor, xscale: torch.Tensor, Y: torch.Tensor) -> None:
+        ember_logits_q8(Xq, xscale, self.Wq, self.wscale, Y, self.bias)
+
+
+class GradClipper:
+    """Clips a fixed list of gradient tensors by their global norm.  out: where
+    each goes (None: in place), counts: for each None or its device row count.
+    Call it with the largest norm allowed; it returns the norm and the factor,
+    scalars on the device that the next call overwrites."""
+
+    def __init__(self, grads, out=None, counts=None):
+        grads = list(grads)
+        out = [None] * len(grads) if out is None else list(out)
+        counts = [None] * len(grads) if counts is None else list(counts)
+        if not grads or len(out) != len(grads) or len(counts) != len(grads):
+            raise ValueError("one gradient at least, and out and counts as long as the list")
+        self.tensors = (grads, out, counts)    # kept alive: the entries hold their addresses
+        self.entries = (Grad * len(grads))(*[grad_entry(*x) for x in zip(grads, out, counts)])
+        self.out = torch.zeros(2, dtype=torch.float32, device=grads[0].device)
+        self.norm, self.factor = self.out[0], self.out[1]
+        nbytes = ember_clip_workspace_bytes(len(grads))
+        self.ws = torch.empty(nbytes, dtype=torch.uint8, device=grads[0].device)
+
+    def __call__(self, max_norm: float):
+        ember_clip_grads(self.entries, max_norm, self.out, self.ws)
+        return self.norm, self.factor
 
 
 def table_step(W: torch.Tensor, G: torch.Tensor | None, r: torch.Tensor, c: torch.Tensor | None, t: int,

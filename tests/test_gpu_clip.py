@@ -1,0 +1,195 @@
+"""Global gradient norm and clipping (ember_clip_grads), through the C ABI.
+
+The norm is a float64 sum rounded once to fp32: within 2^-23 of float64's.  The
+clipped values are one fp32 product with the factor the call reports, rounded to
+the destination's type: the same bits as torch's."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+BF, F = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(scope="module")
+def em():
+    from paper_2607_01455_amd import ember
+    return ember
+
+
+def bits(t):
+    return t.contiguous().view({2: torch.int16, 4: torch.int32}[t.element_size()])
+
+
+def norm64(ts):
+    return math.sqrt(sum(float(t.double().square().sum()) for t in ts))
+
+
+def check(em, grads, max_norm, out=None, counts=None):
+    """One call against torch; returns the norm and the factor."""
+    before = [g.clone() for g in grads]
+    held = [g if c is None else g[:max(0, min(int(c), g.shape[0]))] for g, c in
+            zip(before, counts or [None] * len(grads))]
+    clip = em.GradClipper(grads, out=out, counts=counts)
+    old = [None if o is None else o.clone() for o in (out or [None] * len(grads))]
+    norm, factor = (x.item() for x in clip(max_norm))
+    want = norm64(held)
+    assert abs(norm - want) <= 2.0 ** -23 * want
+    if want > max_norm:
+        assert abs(factor - max_norm / want) <= 2.0 ** -23 * factor
+    else:
+        assert factor == 1.0
+    for g, b, h, o, was in zip(grads, before, held, out or [None] * len(grads), old):
+        to, was = (g, b) if o is None else (o, was)
+        n = h.shape[0] if h.dim() else 0
+        want = (h.float() * torch.tensor(factor, device=DEV)).to(to.dtype)
+        assert torch.equal(bits(to[:n]), bits(want))
+        assert torch.equal(bits(to[n:]), bits(was[n:]))
+        if o is not None:
+            assert torch.equal(bits(g), bits(b))
+    return norm, factor
+
+
+def randn(*shape, dtype=F, seed=0, std=1.0):
+    g = torch.Generator(device=DEV).manual_seed(seed + sum(shape))
+    return (torch.randn(*shape, generator=g, device=DEV) * std).to(dtype)
+
+
+@pytest.mark.parametrize("n", [1, 2, 7, 8, 63, 64, 255, 1000, 4095, 4096, 4097, 16384, 100003, 3000001])
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_one_tensor_in_place(em, n, dtype):
+    print(f"clip n={n} {dtype}", flush=True)
+    check(em, [randn(n, dtype=dtype)], 0.5)
+    check(em, [randn(n, dtype=dtype)], 1e9)
+
+
+@pytest.mark.parametrize("src,dst", [(F, BF), (BF, F), (F, F), (BF, BF)])
+def test_views_of_a_bucket_into_another(em, src, dst):
+    """Views at every offset from a 16-byte boundary, written to views at others."""
+    print(f"clip views {src} {dst}", flush=True)
+    sizes = [1, 2, 3, 5, 7, 8, 9, 15, 17, 100, 4096, 4099, 8191, 20000] * 3
+    a, b = randn(sum(sizes) + 5, dtype=src), torch.zeros(sum(sizes) + 9, dtype=dst, device=DEV)
+    for sa, sb in ((0, 0), (1, 0), (3, 5)):
+        grads, out = list(torch.split(a[sa:sa + sum(sizes)], sizes)), list(torch.split(b[sb:sb + sum(sizes)], sizes))
+        b.fill_(7.0)
+        check(em, grads, 3.0, out=out)
+        assert (b[:sb] == 7).all() and (b[sb + sum(sizes):] == 7).all()
+    check(em, list(torch.split(a[1:1 + sum(sizes)], sizes)), 3.0)
+
+
+@pytest.mark.parametrize("count", [1, 47, 48, 49, 97, 300])
+def test_many_tensors(em, count):
+    print(f"clip {count} tensors", flush=True)
+    grads = [randn(1 + 37 * i % 5000, dtype=BF if i % 3 else F, seed=i) for i in range(count)]
+    check(em, grads, 0.5)
+    check(em, grads, 1e6)
+    check(em, grads, math.inf)
+    check(em, grads, 1e6, out=[torch.zeros(g.shape, dtype=F if i % 2 else BF, device=DEV)
+                               for i, g in enumerate(grads)])
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_tables_with_strides_and_counts(em, dtype):
+    print(f"clip tables {dtype}", flush=True)
+    head = randn(1000, 72, dtype=dtype)[:, :65]
+    wide = randn(9, 10000, dtype=dtype)[:, 1:9000]
+    tall = randn(5000, 3, dtype=dtype)[:, :2]
+    rows = randn(300, 128, dtype=dtype)
+    more = randn(200, 4100, dtype=dtype)
+    out = [torch.full((1000, 65), 9.0, dtype=BF, device=DEV), torch.full((9, 9001), 9.0, dtype=F, device=DEV)[:, :8999],
+           torch.full((5000, 2), 9.0, dtype=BF, device=DEV), torch.full((300, 130), 9.0, dtype=dtype, device=DEV)[:, :128],
+           None]
+
+    def cnt(k):
+        return torch.tensor([k], dtype=torch.int64, device=DEV)
+    for a, b in ((100, 0), (300, 200), (0, 1), (-1, 1000)):
+        check(em, [head, wide, tall, rows, more], 5.0, out=out, counts=[None, None, None, cnt(a), cnt(b)])
+
+
+def test_rows_past_the_count_may_hold_anything(em):
+    rows = randn(64, 100)
+    rows[40:] = float("nan")
+    n, f = check(em, [rows], 1.0, counts=[torch.tensor([40], device=DEV)])
+    assert math.isfinite(n) and f < 1.0
+
+
+def test_range_of_fp32(em):
+    """Squares past the fp32 range, and below it, are summed."""
+    n, f = check(em, [torch.full((5000,), 1e30, device=DEV)], 1.0)
+    assert abs(n / (1e30 * math.sqrt(5000)) - 1) < 1e-6
+    n, f = check(em, [torch.full((5000,), 1e-30, device=DEV)], 1.0)
+    assert abs(n / (1e-30 * math.sqrt(5000)) - 1) < 1e-6 and f == 1.0
+
+
+def test_norms_that_are_not_finite(em):
+    for bad in (float("nan"), float("inf")):
+        g = randn(3000)
+        g[1234] = bad
+        was = g.clone()
+        norm, factor = em.GradClipper([g])(1.0)
+        assert not math.isfinite(norm.item()) and factor.item() == 1.0
+        assert torch.equal(bits(g), bits(was))
+
+
+def test_limits_and_empty_tensors(em):
+    g = randn(777)
+    check(em, [g, torch.empty(0, device=DEV), torch.empty(0, 8, device=DEV), torch.empty(4, 0, device=DEV)], 0.25)
+    n, f = check(em, [g], 0.0)
+    assert f == 0.0 and (g == 0).all()
+    n, f = check(em, [torch.empty(0, device=DEV)], 1.0)
+    assert n == 0.0 and f == 1.0
+    # at the limit exactly: norm 5, nothing changes
+    n, f = check(em, [torch.tensor([3.0, 4.0], device=DEV)], 5.0)
+    assert n == 5.0 and f == 1.0
+
+
+def test_same_bits_on_every_run(em):
+    grads = [randn(100000, seed=i) for i in range(5)]
+    clip = em.GradClipper(grads, out=[torch.empty_like(g) for g in grads])
+    got = {(clip(1.0)[0].item(), clip.factor.item()) for _ in range(5)}
+    assert len(got) == 1
+
+
+def test_a_gradient_past_32_bit_offsets(em):
+    print("clip 2^32 elements", flush=True)
+    g = torch.zeros((1 << 32) + 100, dtype=BF, device=DEV)
+    g[-3:] = 2.0
+    g[5] = 2.0
+    norm, factor = em.GradClipper([g])(2.0)
+    assert norm.item() == 4.0 and factor.item() == 0.5
+    assert (g[-3:] == 1.0).all() and g[5] == 1.0 and g[-4] == 0.0
+
+
+def test_on_another_stream_and_in_a_graph(em):
+    a, b = randn(5000), randn(300, 40, dtype=BF)
+    oa, ob = torch.zeros(5000, dtype=BF, device=DEV), torch.zeros(300, 40, dtype=BF, device=DEV)
+    cnt = torch.tensor([100], device=DEV)
+    clip = em.GradClipper([a, b], out=[oa, ob], counts=[None, cnt])
+    outs = (oa, ob, clip.out)
+    clip(1.0)
+    want = [t.clone() for t in outs]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        for t in outs:
+            t.zero_()
+        clip(1.0)
+    side.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(want, outs))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        clip(1.0)
+    for k in range(4):
+        a.mul_(0.3)
+        cnt.fill_(100 + 50 * k)
+        ob.zero_()
+        clip(1.0)
+        want = [t.clone() for t in outs]
+        for t in outs:
+            t.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(want, outs)), k
