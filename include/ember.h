@@ -398,6 +398,10 @@ int ember_lmhead_step(void* W, int w_dtype, int64_t ldw,
                       float lr, float beta2, float eps, int maximize,
                       void* ws, size_t ws_bytes, hipStream_t stream);
 
+/* Row strides of 8-bit codes below 2^22 bytes (the rows of one tile are then
+ * addressable with 32-bit offsets). */
+#define EMBER_Q8_MAX_LD ((int64_t)(1 << 22))
+
 /*
  * The final norm: a residual addition, a root-mean-square norm and, where the
  * rows go to an 8-bit head, their rounding to 8 bits, in one pass.  For each of
@@ -420,7 +424,7 @@ int ember_lmhead_step(void* W, int w_dtype, int64_t ldw,
  *                        NaN, which makes its logits NaN;
  *   rstd (T)             kept for the gradient.
  * X, R (x_dtype), S, Y: layout rules of W and G.  Q: 16-byte aligned, ldq a
- * multiple of 16; columns D..ldq-1 are not written.  gain: D values of
+ * multiple of 16 below EMBER_Q8_MAX_LD; columns D..ldq-1 are not written.  gain: D values of
  * gain_dtype, 16-byte aligned.  0 <= T <= EMBER_MAX_TOKENS (0: nothing to do, the
  * pointers may be NULL), 1 <= D <= EMBER_NORM_MAX_D, eps >= 0 and finite.
  */
@@ -468,10 +472,10 @@ int ember_quantize_rows(const void* X, int x_dtype, int64_t ldx, int64_t rows, i
  * Xq (T x D) and Wq (V x D) are int8 codes with one fp32 scale a row (xscale: T,
  * wscale: V), bias (V, fp32) may be NULL, Y is T x V of y_dtype.  The sum over D
  * is exact (int32), the scaling fp32, and the result is rounded once to y_dtype.
- * Layout: bases 16-byte aligned, ldx and ldw multiples of 16, Y as W and G.  The
- * padding of Xq and Wq (columns D..ld-1) is not used.  0 <= T <=
- * EMBER_MAX_TOKENS (0: nothing to do), 1 <= V <= EMBER_MAX_V,
- * 1 <= D <= EMBER_NORM_MAX_D.
+ * Layout: bases 16-byte aligned, ldx and ldw multiples of 16 below
+ * EMBER_Q8_MAX_LD, Y as W and G.  The padding of Xq and Wq (columns D..ld-1) may
+ * be read but never affects a stored value.  0 <= T <= EMBER_MAX_TOKENS (0:
+ * nothing to do), 1 <= V <= EMBER_MAX_V, 1 <= D <= EMBER_NORM_MAX_D.
  */
 int ember_logits_q8(const int8_t* Xq, int64_t ldx, const float* xscale,
                     const int8_t* Wq, int64_t ldw, const float* wscale, const float* bias,

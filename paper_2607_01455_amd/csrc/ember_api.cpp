@@ -292,7 +292,7 @@ int check_gain(const void* gain, int dtype) {
 int check_codes(const int8_t* q, int64_t ld, const float* scale, int64_t D, bool may_be_null) {
     if (q == nullptr && scale == nullptr && may_be_null) return EMBER_OK;
     if (q == nullptr || scale == nullptr) return EMBER_ERR_ARG;
-    if (ld < D) return EMBER_ERR_SHAPE;
+    if (ld < D || ld >= EMBER_Q8_MAX_LD) return EMBER_ERR_SHAPE;
     return aligned(q, 16) && ld % 16 == 0 && aligned(scale, 4) ? EMBER_OK : EMBER_ERR_ALIGN;
 }
 

@@ -1,11 +1,23 @@
 // Logits of an LM head held in 8 bits (gfx950):
 //   Y_tv = (sum_k Xq_tk Wq_vk) xscale_t wscale_v + bias_v,
 // with int8 matrix instructions.  The sum is exact in int32 (D is limited to
-// EMBER_Q8_MAX_D), so neither tiling nor order changes a bit of it; it is rounded
-// to fp32 once, scaled and rounded to the type of Y.
+// EMBER_NORM_MAX_D), so neither tiling nor order changes a bit of it; it is
+// rounded to fp32 once, scaled, and rounded to the type of Y.
+//
+// Tiling: a block computes BM tokens x BN channels; its wavefronts hold their
+// parts of the tile as 32 x 32 MFMA accumulators.  Both operands have the
+// contraction contiguous, so a step's slices (BM and BN rows of KS bytes) go from
+// global memory straight into LDS (16-byte buffer loads with an LDS destination)
+// and are read from there as MFMA operands, 16 consecutive columns a lane.  A ring
+// of LDS stages keeps the loads of the next steps in flight; the operands of
+// each 32-column sub-step are read behind the previous sub-step's MFMAs, across
+// the step barrier too.
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+
+#include <algorithm>
+#include <cmath>
 
 #include "ember_device.h"
 #include "ember_launch.h"
@@ -16,60 +28,652 @@ namespace {
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x16 __attribute__((ext_vector_type(16)));
 
-constexpr int kTile = 64;   // tokens and channels a block
-constexpr int kStep = 64;   // columns a step
+constexpr int kXcds = 8;
+constexpr uint32_t kRotate = 5;            // steps between the first steps of neighbouring tiles
+constexpr int kBufferWord3 = 0x00020000;   // raw 32-bit data format, gfx9 family
+constexpr int kBufferMax = 0x7FFFFFF0;     // bytes of a buffer at most; an offset past every buffer
 
-// 16 columns [k, k + 16) of a row: zeros past the row's D columns.
-__device__ __forceinline__ i32x4 load16(const int8_t* row, int k, int D, bool valid) {
-    i32x4 w = {0, 0, 0, 0};
-    if (!valid) return w;
-    if (k + 16 <= D) return *reinterpret_cast<const i32x4*>(row + k);
-    for (int e = 0; e < 16; ++e)
-        if (k + e < D) w[e >> 2] |= (int)(uint8_t)row[k + e] << (8 * (e & 3));
-    return w;
+struct Params {
+    LogitsArgs a;
+    int nk;              // steps of the contraction
+    int MT;              // tiles of tokens
+    int64_t NT;          // tiles of channels
+    int64_t tile0;       // this launch's tiles: [tile0, tile1) of the MT * NT
+    int64_t tile1;
+    int64_t per_xcd;     // tiles per XCD
+    int group_m;         // token tiles a group of the tile order
+};
+
+// Raw buffer resource of `bytes` bytes at a wave-uniform base.
+__device__ __forceinline__ i32x4 rsrc(const void* base, int64_t bytes) {
+    const uint64_t p = reinterpret_cast<uint64_t>(base);
+    i32x4 r;
+    r.x = __builtin_amdgcn_readfirstlane((int)p);
+    r.y = __builtin_amdgcn_readfirstlane((int)(p >> 32) & 0xFFFF);
+    r.z = __builtin_amdgcn_readfirstlane(bytes > kBufferMax ? kBufferMax : bytes < 0 ? 0 : (int)bytes);
+    r.w = kBufferWord3;
+    return r;
 }
 
-__global__ __launch_bounds__(kBlock) void ember_logits_tile(LogitsArgs a) {
-    __shared__ __attribute__((aligned(16))) int8_t lx[kTile][kStep + 16], lw[kTile][kStep + 16];
-    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    const int64_t t0 = (int64_t)blockIdx.y * kTile, v0 = (int64_t)blockIdx.x * kTile;
-    const int row = threadIdx.x / 4, chunk = threadIdx.x % 4;
-    const int wt = (wave & 1) * 32, wv = (wave >> 1) * 32;
-    i32x16 acc = {};
-    const int D = (int)a.D;
-    for (int k = 0; k < D; k += kStep) {
-        const i32x4 x = load16(a.Xq + (t0 + row) * a.ldx, k + 16 * chunk, D, t0 + row < a.T);
-        const i32x4 w = load16(a.Wq + (v0 + row) * a.ldw, k + 16 * chunk, D, v0 + row < a.V);
-        __syncthreads();
-        *reinterpret_cast<i32x4*>(&lx[row][16 * chunk]) = x;
-        *reinterpret_cast<i32x4*>(&lw[row][16 * chunk]) = w;
-        __syncthreads();
+// 16 bytes per lane from a buffer into LDS at lds_base + 16 lane; lanes outside
+// the buffer's range write zeros.  Inline assembly, so that the compiler does
+// not make every later LDS read wait for it; completion is awaited with
+// wait_step before a stage is read.  M0 holds the (wave-uniform) LDS base.
+__device__ __forceinline__ void load_to_lds(i32x4 rs, uint32_t lds_base, int voffset) {
+    const uint32_t base = __builtin_amdgcn_readfirstlane(lds_base);
+    uint32_t saved;
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\t"
+                 "buffer_load_dwordx4 %2, %3, 0 offen lds\n\ts_mov_b32 m0, %0"
+                 : "=&s"(saved)
+                 : "s"(base), "v"(voffset), "s"(rs)
+                 : "memory");
+}
+
+// The step barrier: at most N of this wave's vector-memory loads outstanding and
+// all of its LDS reads returned, then the block's waves meet.
+template <int N>
+__device__ __forceinline__ void wait_step() {
+    static_assert(N >= 0 && N < 64, "vmcnt range");
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4));
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// Orders a wave's LDS accesses before and after it (they execute in order, so
+// only the compiler has to be held).
+__device__ __forceinline__ void wave_lds_order() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// Logical tile -> (token tile, channel tile): groups of group_m token tiles,
+// token tile fastest inside a group.
+__device__ __forceinline__ void tile_of(const Params& p, int64_t l, int& tm, int64_t& tn) {
+    const int64_t per_group = (int64_t)p.group_m * p.NT;
+    const int64_t g = l / per_group;
+    const int first = (int)(g * p.group_m);
+    const int gm = min(p.MT - first, p.group_m);
+    const int64_t q = l - g * per_group;
+    tm = first + (int)(q % gm);
+    tn = q / gm;
+}
+
+template <int BM_, int BN_, int WM_, int WN_, int KS_, int STAGES_>
+struct Tile {
+    static constexpr int BM = BM_, BN = BN_;       // tokens, channels a block
+    static constexpr int WM = WM_, WN = WN_;       // wavefronts over them
+    static constexpr int KS = KS_;                 // columns (bytes) a step
+    static constexpr int kStages = STAGES_;
+    static constexpr int kWavesB = WM * WN;
+    static constexpr int kThreads = kWavesB * kWave;
+    static constexpr int MT = BM / WM / 32, NT = BN / WN / 32;   // MFMA tiles a wave
+    static constexpr int kSub = KS / 32;
+    static constexpr int kChunks = KS / 16;        // 16-byte chunks of a slice's row
+    static constexpr int kRowsPerLoad = kWave / kChunks;
+    static constexpr int kLoadsA = BM / kRowsPerLoad, kLoadsB = BN / kRowsPerLoad;
+    static constexpr int kLoads = (kLoadsA + kLoadsB) / kWavesB;   // a wave and step
+    static constexpr int kStageBytes = (BM + BN) * KS;
+    static constexpr int kLds = kStages * kStageBytes;
+    static_assert((kLoadsA + kLoadsB) % kWavesB == 0, "equal loads a wave");
+    static_assert(kSub >= 2 && kSub % 2 == 0, "a step ends on the register set it began with");
+    static_assert(kStages >= 2 && (kStages - 2) * kLoads < 64, "vmcnt range");
+    static_assert((int64_t)std::max(BM, BN) * EMBER_Q8_MAX_LD < (int64_t)1 << 31, "32-bit load offsets");
+    static_assert(kLds <= 160 * 1024, "LDS of one CU");
+};
+
+// Chunk c of a slice's row r sits at position c ^ swizzle(r): the reads of the
+// same chunk of 8 (or 16) consecutive rows then cover 32 (or all 64) LDS banks
+// once, and a wave-wide load still fills whole rows.
+template <int kChunks>
+__device__ __forceinline__ int swizzle(int r) {
+    return kChunks == 16 ? r & 15 : ((kChunks == 8 ? r & 7 : (r >> 1) & 3) ^ ((r >> 3) & 1));
+}
+
+// kMask: D is not a multiple of 16, so the last chunk of a row holds columns
+// that do not count; they are cleared in the tokens' operand.
+template <typename C, typename YT, bool kMask>
+__global__ __launch_bounds__(C::kThreads) void ember_logits_q8(Params p) {
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[C::kLds];
+    const LogitsArgs& a = p.a;
+    const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
+    const int lane = threadIdx.x & (kWave - 1);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int wm = wave % C::WM, wn = wave / C::WM;
+
+    // blocks of one XCD take consecutive tiles
+    const int64_t l = p.tile0 + (int64_t)(blockIdx.x % kXcds) * p.per_xcd + blockIdx.x / kXcds;
+    if (l >= p.tile1 || (int64_t)(blockIdx.x / kXcds) >= p.per_xcd) return;
+    int tm;
+    int64_t tn;
+    tile_of(p, l, tm, tn);
+    const int64_t t0 = (int64_t)tm * C::BM, v0 = tn * C::BN;
+    const int nk = p.nk, D = (int)a.D;
+
+    // load j of this wave fills rows [kRowsPerLoad q, ..) of the tokens' slice, then
+    // of the channels', q = wave + kWavesB j
+    int off[C::kLoads];
+    const int chunk_pos = lane % C::kChunks, load_row = lane / C::kChunks;
+    int load_k[C::kLoads];
 #pragma unroll
-        for (int kk = 0; kk < kStep; kk += 32) {
-            const i32x4 fa = *reinterpret_cast<const i32x4*>(&lx[wt + (lane & 31)][kk + 16 * (lane >> 5)]);
-            const i32x4 fb = *reinterpret_cast<const i32x4*>(&lw[wv + (lane & 31)][kk + 16 * (lane >> 5)]);
-            acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(fa, fb, acc, 0, 0, 0);
+    for (int j = 0; j < C::kLoads; ++j) {
+        const int q = wave + C::kWavesB * j;
+        const bool is_b = q >= C::kLoadsA;
+        const int row = (is_b ? q - C::kLoadsA : q) * C::kRowsPerLoad + load_row;
+        const int chunk = chunk_pos ^ swizzle<C::kChunks>(row);
+        load_k[j] = chunk * 16;
+        off[j] = row * (int)(is_b ? a.ldw : a.ldx) + chunk * 16;
+    }
+    struct StepLoads {
+        i32x4 ra, rb;
+        int left;      // columns from the step's first to D
+    };
+    // Blocks with other channels begin at other steps (the sum has no order): in
+    // step, all of them would read the same columns of rows that lie a power of
+    // two apart, and so a few of the memory's channels at a time (64 tokens x
+    // 128256 x 4096: 127 us in step, 105 like this; one token: 110 and 91).
+    const int rot = (int)((uint64_t)tn * kRotate % (uint32_t)nk);
+    auto loads_of = [&](int kt) {
+        const bool in = kt < nk;
+        const int ks = kt + rot < nk ? kt + rot : kt + rot - nk;
+        const int64_t k0 = in ? (int64_t)ks * C::KS : 0;
+        StepLoads sl;
+        sl.ra = rsrc(a.Xq + t0 * a.ldx + k0, in ? (a.T - t0) * a.ldx - k0 : 0);
+        sl.rb = rsrc(a.Wq + v0 * a.ldw + k0, in ? (a.V - v0) * a.ldw - k0 : 0);
+        sl.left = D - (int)k0;
+        return sl;
+    };
+    auto issue_one = [&](const StepLoads& sl, uint32_t st, int j) {
+        const int q = wave + C::kWavesB * j;
+        // chunks past column D are zeros
+        const int o = load_k[j] < sl.left ? off[j] : kBufferMax;
+        load_to_lds(q >= C::kLoadsA ? sl.rb : sl.ra, st + q * (C::kRowsPerLoad * C::KS), o);
+    };
+
+    // operand reads: lane l takes row l % 32 of an MFMA tile, columns
+    // 16 (l / 32) .. + 15 of the sub-step
+    auto frag = [&](uint32_t st, int row, int kk) {
+        const int c = 2 * kk + (lane >> 5);
+        const uint32_t at = st + row * C::KS + ((c ^ swizzle<C::kChunks>(row)) * 16);
+        return *(const __attribute__((address_space(3))) i32x4*)(uintptr_t)at;
+    };
+    const int row_a = wm * (C::MT * 32) + (lane & 31), row_b = C::BM + wn * (C::NT * 32) + (lane & 31);
+    static_assert(C::BM % 16 == 0, "the channels' rows have the swizzle of their number");
+    auto mask_a = [&](int kt, int kk, i32x4& x) {
+        const int n = D - kt * C::KS - 32 * kk - 16 * (lane >> 5);   // columns that count of these 16
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const int b = n - 4 * w;
+            x[w] &= b >= 4 ? -1 : b <= 0 ? 0 : (int)((1u << (8 * b)) - 1);
+        }
+    };
+
+    i32x16 acc[C::MT][C::NT];
+#pragma unroll
+    for (int mt = 0; mt < C::MT; ++mt)
+#pragma unroll
+        for (int nt = 0; nt < C::NT; ++nt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[mt][nt][i] = 0;
+
+#pragma unroll
+    for (int q = 0; q < C::kStages; ++q) {
+        const StepLoads sl = loads_of(q);
+#pragma unroll
+        for (int j = 0; j < C::kLoads; ++j) issue_one(sl, lds_base + q * C::kStageBytes, j);
+    }
+    wait_step<(C::kStages - 1) * C::kLoads>();
+    i32x4 af[2][C::MT], bf[2][C::NT];
+#pragma unroll
+    for (int m = 0; m < C::MT; ++m) af[0][m] = frag(lds_base, row_a + 32 * m, 0);
+#pragma unroll
+    for (int n = 0; n < C::NT; ++n) bf[0][n] = frag(lds_base, row_b + 32 * n, 0);
+
+    // Step kt multiplies its stage in kSub sub-steps; while the MFMAs of one run,
+    // the operands of the next are read into the other register set.  The step
+    // barrier sits before the last sub-step, whose operands are in registers by
+    // then: past it no wave reads this stage any more, so the loads of step
+    // kt + kStages may fill it; and at most (kStages - 2) kLoads loads of each
+    // wave are outstanding, which are those of steps kt + 2 and later, so step
+    // kt + 1 lies in its stage.
+    uint32_t st = lds_base;
+    for (int kt = 0; kt < nk; ++kt) {
+        const uint32_t next = st + C::kStageBytes == lds_base + C::kLds ? lds_base : st + C::kStageBytes;
+        const StepLoads sl = loads_of(kt + C::kStages);
+#pragma unroll
+        for (int kk = 0; kk < C::kSub; ++kk) {
+            const int cur = kk & 1;
+            const bool last = kk == C::kSub - 1;
+            if constexpr (kMask) {
+                const int ks = kt + rot < nk ? kt + rot : kt + rot - nk;
+                if (ks == nk - 1) {
+#pragma unroll
+                    for (int m = 0; m < C::MT; ++m) mask_a(ks, kk, af[cur][m]);
+                }
+            }
+            if (last) wait_step<(C::kStages - 2) * C::kLoads>();
+            __builtin_amdgcn_sched_barrier(0);
+            constexpr int kSlots = C::MT * C::NT > C::MT + C::NT ? C::MT * C::NT : C::MT + C::NT;
+            constexpr int kAll = kSlots > C::kLoads ? kSlots : C::kLoads;
+#pragma unroll
+            for (int i = 0; i < kAll; ++i) {
+                if (i < C::MT * C::NT) {
+                    const int m = i / C::NT, n = i % C::NT;
+                    acc[m][n] = __builtin_amdgcn_mfma_i32_32x32x32_i8(af[cur][m], bf[cur][n], acc[m][n], 0, 0, 0);
+                }
+                // operands in the order the MFMAs first use them: A 0, all of B, the rest of A
+                if (i < C::MT + C::NT) {
+                    const bool is_b = i >= 1 && i <= C::NT;
+                    const int f = i == 0 ? 0 : is_b ? i - 1 : i - C::NT;
+                    const i32x4 x = frag(last ? next : st, (is_b ? row_b : row_a) + 32 * f, last ? 0 : kk + 1);
+                    if (is_b) bf[cur ^ 1][f] = x;
+                    else af[cur ^ 1][f] = x;
+                }
+                if (last && i < C::kLoads) issue_one(sl, st, i);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        st = next;
+    }
+    // the zero-filling loads past the end have landed and every wave is done with the stages
+    wait_step<0>();
+
+    // Epilogue: each wave takes its part in strips of kRows tokens: the values
+    // go to a wave-private LDS strip in the MFMA layout and are stored from it row
+    // by row, 16 bytes a lane.
+    constexpr int kEs = (int)sizeof(YT);
+    constexpr int kRows = 16;
+    constexpr int kCols = C::NT * 32;
+    constexpr int kPitch = kCols * kEs + 16;
+    constexpr int kLanesPerRow = kCols * kEs / 16;
+    constexpr int kRowsPerPass = kWave / kLanesPerRow;
+    constexpr int kEpc = 16 / kEs;
+    static_assert(C::kWavesB * kRows * kPitch <= C::kLds && kRows % kRowsPerPass == 0, "strips fit the stages");
+    uint8_t* const strip = lds + wave * (kRows * kPitch);
+    const int half = lane >> 5, col = lane & 31;
+    const int64_t vw = v0 + wn * kCols;
+    float ws[C::NT], bias[C::NT];
+#pragma unroll
+    for (int n = 0; n < C::NT; ++n) {
+        const int64_t v = vw + n * 32 + col;
+        ws[n] = v < a.V ? a.wscale[v] : 0.0f;
+        bias[n] = a.bias && v < a.V ? a.bias[v] : 0.0f;
+    }
+#pragma unroll
+    for (int m = 0; m < C::MT; ++m) {
+#pragma unroll
+        for (int s = 0; s < 32 / kRows; ++s) {
+            // rows s kRows .. of the MFMA tile: registers i with 8 (i / 4) + 4 half + i % 4 in them
+            const int64_t ts = t0 + (wm * C::MT + m) * 32 + s * kRows;
+#pragma unroll
+            for (int ii = 0; ii < kRows / 2; ++ii) {
+                const int i = s * (kRows / 2) + ii;
+                const int r = 8 * (i >> 2) + 4 * half + (i & 3) - s * kRows;
+                const float xs = ts + r < a.T ? a.xscale[ts + r] : 0.0f;
+#pragma unroll
+                for (int n = 0; n < C::NT; ++n) {
+                    const float y = (float)acc[m][n][i] * (xs * ws[n]) + bias[n];
+                    uint8_t* e = strip + r * kPitch + (n * 32 + col) * kEs;
+                    if constexpr (kEs == 2) *reinterpret_cast<uint16_t*>(e) = (uint16_t)pack_bf16(y, 0.0f);
+                    else *reinterpret_cast<float*>(e) = y;
+                }
+            }
+            wave_lds_order();
+#pragma unroll
+            for (int ps = 0; ps < kRows / kRowsPerPass; ++ps) {
+                const int r = ps * kRowsPerPass + lane / kLanesPerRow;
+                const int c = lane % kLanesPerRow;
+                const int64_t t = ts + r, v = vw + c * kEpc;
+                const u32x4_t w = *reinterpret_cast<const u32x4_t*>(strip + r * kPitch + c * 16);
+                if (t < a.T) {
+                    YT* y = static_cast<YT*>(a.Y) + t * a.ldy + v;
+                    if (v + kEpc <= a.V) {
+                        *reinterpret_cast<u32x4_t*>(y) = w;
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < kEpc; ++e) {
+                            if (v + e < a.V) {
+                                if constexpr (kEs == 2)
+                                    reinterpret_cast<uint16_t*>(y)[e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
+                                else
+                                    reinterpret_cast<uint32_t*>(y)[e] = w[e];
+                            }
+                        }
+                    }
+                }
+            }
+            wave_lds_order();   // the strip is rewritten next
         }
     }
-    const int64_t v = v0 + wv + (lane & 31);
-    if (v >= a.V) return;
-    const float ws = a.wscale[v], bias = a.bias ? a.bias[v] : 0.0f;
+}
+
+// ---------------------------------------------------------------------------
+// few tokens
+// ---------------------------------------------------------------------------
+
+constexpr int kFewWaves = 8;                 // wavefronts that share the contraction, and one that adds up
+constexpr int kFewThreads = (kFewWaves + 1) * kWave;
+constexpr int kStrip = 16;                   // channels of a strip
+constexpr int kFewBlocks = 256;              // one a compute unit
+
+struct FewParams {
+    LogitsArgs a;
+    int64_t rounds;      // rounds of SB strips over the table
+    int per_xcd;         // rounds of one pass of the grid, per XCD
+};
+
+// Up to 16 NB tokens: bound by the table's bytes.  Eight waves share the columns
+// (KF blocks of 64 each) and hold their part of all the tokens as MFMA operands in
+// registers, loaded once; then they stream the table, SB strips of 16 channels a
+// round, straight from memory into the other operand, two rounds in flight.
+// They leave their sums of a round in LDS, where a ninth wave adds them up
+// scales and stores them while the others go on (the streaming waves have no
+// memory operations but their loads, which return in order).  Columns past D are
+// zeros in the tokens' operand, so what the table's operand holds there (some
+// column before D) does not matter.
+template <int KF, int KP, int SB, int NB, typename YT>
+__global__ __launch_bounds__(kFewThreads) void ember_logits_few(FewParams p) {
+    const LogitsArgs& a = p.a;
+    constexpr int N = kChunkElems<YT>;
+    constexpr int kPitch = SB * kStrip + N;
+    __shared__ __attribute__((aligned(16))) int part[2][SB][NB][kFewWaves][4 * kWave];
+    __shared__ __attribute__((aligned(16))) YT ybuf[16 * NB][kPitch];
+    const int lane = threadIdx.x & (kWave - 1);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int D = (int)a.D;
+    const int row = lane & 15, quarter = lane >> 4;
+
+    // rounds of one pass of the grid: consecutive ones within an XCD
+    const int64_t pass = (int64_t)p.per_xcd * kXcds;
+    const int64_t first = (int64_t)(blockIdx.x % kXcds) * p.per_xcd + blockIdx.x / kXcds;
+    if (first >= p.rounds) return;   // the whole block: no meeting is missed
+    // this block's rounds, made even: one past the table reads and stores nothing
+    const int rounds = (int)((p.rounds - first + pass - 1) / pass + 1) & ~1;
+    auto channel = [&](int i) { return (first + i * pass) * SB * kStrip; };   // first one of the block's round i
+
+    // The block's waves meet once a round, the streaming ones with their loads in
+    // flight.  Half `buf` of part is written before the round's meeting, read
+    // before the next one and written again after that.
+    auto meet = [&] {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0)
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    auto buffer = [&](const void* base, int64_t bytes) {
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0,
+                                                 (int)(bytes < kBufferMax ? bytes : kBufferMax), kBufferWord3);
+    };
+
+    if (wave == kFewWaves) {
+        float xs[NB];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const int64_t t = t0 + wt + 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3);
-        if (t >= a.T) continue;
-        const float y = (float)acc[i] * (a.xscale[t] * ws) + bias;
-        if (a.y_dtype == EMBER_F32) static_cast<float*>(a.Y)[t * a.ldy + v] = y;
-        else static_cast<uint16_t*>(a.Y)[t * a.ldy + v] = (uint16_t)pack_bf16(y, 0.0f);
+        for (int b = 0; b < NB; ++b) xs[b] = 16 * b + row < a.T ? a.xscale[16 * b + row] : 0.0f;
+        struct Scales {
+            float ws[SB][4], bias[SB][4];
+        };
+        // lane: token lane % 16, channels 4 (lane / 16) .. + 3 of a strip; zeros past the table
+        auto load = [&](int i, Scales& x) {
+            const int64_t v = channel(i);
+            const int64_t left = v < a.V ? a.V - v : 0;
+            const auto rw = buffer(a.wscale + (v < a.V ? v : 0), left * 4);
+            const auto rb = buffer(a.bias ? a.bias + (v < a.V ? v : 0) : a.wscale, a.bias ? left * 4 : 0);
+#pragma unroll
+            for (int s = 0; s < SB; ++s) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int at = (s * kStrip + 4 * quarter + e) * 4;
+                    x.ws[s][e] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rw, at, 0, 0));
+                    x.bias[s][e] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rb, at, 0, 0));
+                }
+            }
+        };
+        auto sum = [&](int i, int buf, const Scales& x, Scales& next) {
+            meet();
+            load(i + 1, next);   // a round ahead
+#pragma unroll
+            for (int s = 0; s < SB; ++s) {
+#pragma unroll
+                for (int b = 0; b < NB; ++b) {
+                    i32x4 acc = {0, 0, 0, 0};
+#pragma unroll
+                    for (int q = 0; q < kFewWaves; ++q)
+                        acc += *reinterpret_cast<const i32x4*>(&part[buf][s][b][q][4 * lane]);
+                    float y[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) y[e] = (float)acc[e] * (xs[b] * x.ws[s][e]) + x.bias[s][e];
+                    store_values<YT, 4>(&ybuf[16 * b + row][s * kStrip + 4 * quarter], 0, 4, y);
+                }
+            }
+            // 16 bytes a lane, row by row
+            wave_lds_order();
+            constexpr int kPerRow = SB * kStrip / N;
+            const int64_t v0 = channel(i);
+#pragma unroll
+            for (int q = lane; q < 16 * NB * kPerRow; q += kWave) {
+                const int t = q / kPerRow, c = q % kPerRow * N;
+                if (t >= a.T || v0 + c >= a.V) continue;
+                const u32x4_t w = *reinterpret_cast<const u32x4_t*>(&ybuf[t][c]);
+                YT* y = static_cast<YT*>(a.Y) + t * a.ldy + v0 + c;
+                if (v0 + c + N <= a.V) {
+                    *reinterpret_cast<u32x4_t*>(y) = w;
+                } else {
+                    for (int e = 0; e < N; ++e)
+                        if (v0 + c + e < a.V) y[e] = ybuf[t][c + e];
+                }
+            }
+            wave_lds_order();
+        };
+        Scales s0, s1;
+        load(0, s0);
+        for (int i = 0; i < rounds; i += 2) {
+            sum(i, 0, s0, s1);
+            sum(i + 1, 1, s1, s0);
+        }
+        return;
     }
+
+    // The loads of part h (of KP) of a round's columns: zeros for columns past D and
+    // rows past the table (a round past the last one reads nothing), so that
+    // every round has the same loads.
+    const int col0 = wave * (KF * 64) + 16 * quarter;
+    const int row_off = row * (int)a.ldw + col0;
+    const int64_t row_end = (a.D + 15) / 16 * 16;   // of the last row that is read
+    auto load = [&](int i, int h, i32x4 (&w)[SB][KF]) {
+        const int64_t v0 = channel(i);
+#pragma unroll
+        for (int s = 0; s < SB; ++s) {
+            const int64_t v = v0 + s * kStrip;
+            const auto rs = buffer(a.Wq + (v < a.V ? v * a.ldw : 0), v < a.V ? (a.V - 1 - v) * a.ldw + row_end : 0);
+#pragma unroll
+            for (int f = 0; f < KF; ++f) {
+                const int at = (h * kFewWaves * KF + f) * 64;
+                const int off = col0 + at < D ? row_off : kBufferMax;
+                w[s][f] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, off + f * 64, at - f * 64, 0));
+            }
+        }
+    };
+    i32x4 x[KP][NB][KF];
+    const int64_t xt = a.T - 1;
+#pragma unroll
+    for (int h = 0; h < KP; ++h) {
+#pragma unroll
+        for (int f = 0; f < KF; ++f) {
+            const int k = col0 + (h * kFewWaves * KF + f) * 64;
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                // lanes without a column or a token read others and are cleared below
+                const int64_t t = min((int64_t)(16 * b + row), xt);
+                x[h][b][f] = *reinterpret_cast<const i32x4*>(a.Xq + t * a.ldx + (k < D ? k : 0));
+            }
+        }
+    }
+    i32x4 w0[SB][KF], w1[SB][KF];
+    load(0, 0, w0);
+    if constexpr (KP == 2) load(0, 1, w1);
+    else load(1, 0, w1);
+#pragma unroll
+    for (int h = 0; h < KP; ++h) {
+#pragma unroll
+        for (int f = 0; f < KF; ++f) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int n = D - col0 - (h * kFewWaves * KF + f) * 64 - 4 * q;   // columns that count of these four
+                const int m = n >= 4 ? -1 : n <= 0 ? 0 : (int)((1u << (8 * n)) - 1);
+#pragma unroll
+                for (int b = 0; b < NB; ++b) x[h][b][f][q] &= 16 * b + row < a.T ? m : 0;
+            }
+        }
+    }
+    i32x4 acc[SB][NB];
+    auto multiply = [&](int h, const i32x4 (&w)[SB][KF]) {
+#pragma unroll
+        for (int s = 0; s < SB; ++s) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                if (h == 0) acc[s][b] = i32x4{0, 0, 0, 0};
+#pragma unroll
+                for (int f = 0; f < KF; ++f)
+                    acc[s][b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[s][f], x[h][b][f], acc[s][b], 0, 0, 0);
+            }
+        }
+    };
+    auto leave = [&](int buf) {
+#pragma unroll
+        for (int s = 0; s < SB; ++s)
+#pragma unroll
+            for (int b = 0; b < NB; ++b) *reinterpret_cast<i32x4*>(&part[buf][s][b][wave][4 * lane]) = acc[s][b];
+    };
+    // the next loads go out before the MFMAs behind them wait for theirs
+    auto refill = [&](int i, int h, i32x4 (&w)[SB][KF]) {
+        __builtin_amdgcn_sched_barrier(0);
+        load(i, h, w);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    for (int i = 0; i < rounds; i += 2) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            if constexpr (KP == 2) {
+                multiply(0, w0);
+                refill(i + u + 1, 0, w0);
+                multiply(1, w1);
+                leave(u);
+                refill(i + u + 1, 1, w1);
+            } else {
+                multiply(0, u == 0 ? w0 : w1);
+                leave(u);
+                refill(i + u + 2, 0, u == 0 ? w0 : w1);
+            }
+            meet();
+        }
+    }
+}
+
+template <int KF, int KP, int SB, int NB>
+hipError_t launch_few(const LogitsArgs& a, hipStream_t s) {
+    FewParams p;
+    p.a = a;
+    p.rounds = (a.V + SB * kStrip - 1) / (SB * kStrip);
+    p.per_xcd = (int)std::min<int64_t>((p.rounds + kXcds - 1) / kXcds, kFewBlocks / kXcds);
+    const dim3 grid((unsigned)(p.per_xcd * kXcds));
+    if (a.y_dtype == EMBER_F32) ember_logits_few<KF, KP, SB, NB, float><<<grid, kFewThreads, 0, s>>>(p);
+    else ember_logits_few<KF, KP, SB, NB, uint16_t><<<grid, kFewThreads, 0, s>>>(p);
+    return hipGetLastError();
+}
+
+template <typename C>
+hipError_t launch_tiles(const LogitsArgs& a, hipStream_t s) {
+    Params p;
+    p.a = a;
+    p.nk = (int)((a.D + C::KS - 1) / C::KS);
+    p.MT = (int)((a.T + C::BM - 1) / C::BM);
+    p.NT = (a.V + C::BN - 1) / C::BN;
+    p.group_m = 8;
+    const int64_t total = (int64_t)p.MT * p.NT;
+    const bool mask = a.D % 16 != 0;
+    for (int64_t t0 = 0; t0 < total; t0 += kMaxGridBlocks) {
+        p.tile0 = t0;
+        p.tile1 = std::min(t0 + kMaxGridBlocks, total);
+        p.per_xcd = (p.tile1 - t0 + kXcds - 1) / kXcds;
+        const dim3 grid((unsigned)(p.per_xcd * kXcds));
+        if (a.y_dtype == EMBER_F32) {
+            if (mask) ember_logits_q8<C, float, true><<<grid, C::kThreads, 0, s>>>(p);
+            else ember_logits_q8<C, float, false><<<grid, C::kThreads, 0, s>>>(p);
+        } else {
+            if (mask) ember_logits_q8<C, uint16_t, true><<<grid, C::kThreads, 0, s>>>(p);
+            else ember_logits_q8<C, uint16_t, false><<<grid, C::kThreads, 0, s>>>(p);
+        }
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 } // namespace
 
+namespace {
+
+using T256x256 = Tile<256, 256, 4, 2, 64, 4>;
+using T128x256 = Tile<128, 256, 2, 4, 64, 4>;
+using T128x128 = Tile<128, 128, 2, 2, 64, 4>;
+using T64x256 = Tile<64, 256, 1, 8, 128, 3>;
+using T64x128 = Tile<64, 128, 1, 4, 128, 3>;
+using T32x128 = Tile<32, 128, 1, 4, 128, 3>;
+
+// What a launch of a tiling takes, in us: passes over the 256 compute units, each
+// the tile's columns at a rate between that of a tile that has the chip to
+// itself and that of a full chip (us per 4096 columns, both measured), and
+// filling and draining the pipeline, which the passes overlap in part.
+struct TileCost {
+    int bm, bn;
+    double alone, full, fill;
+};
+constexpr TileCost kTiles[] = {
+    {256, 256, 40.5, 68.6, 8.0}, {128, 256, 32.0, 45.8, 6.5}, {128, 128, 25.5, 24.2, 5.0},
+    {64, 256, 21.0, 29.0, 5.0},  {64, 128, 16.5, 13.6, 4.0},  {32, 128, 13.0, 10.0, 3.0},
+};
+double tile_us(const TileCost& c, const LogitsArgs& a) {
+    const double tiles = (double)((a.T + c.bm - 1) / c.bm) * (double)((a.V + c.bn - 1) / c.bn);
+    const double passes = std::max(1.0, std::ceil(tiles / 256.0));
+    const double rate = c.alone + (c.full - c.alone) * std::min(1.0, tiles / 256.0);
+    return c.fill * (1.0 + passes) / 2.0 + passes * rate * (double)a.D / 4096.0;
+}
+
+} // namespace
+
+// Few tokens take the streaming form while their operands fit its registers (us,
+// streaming / best tiling: 1 token x 128256 x 4096 82 / 91, 16 tokens 90 / 94, 32
+// tokens 96 / 98, 20 x 50000 x 3000 32 / 37, 64 x 100000 x 1000 29 / 39, 64 x 30000 x
+// 2000 18 / 21; past those limits 10 x 32768 x 8192 62 / 47, 50 x 200000 x 500 50 /
+// 42).  Others the tiling that should take least: 333 x 8191 x 1000 15 us with
+// 64 x 256 tiles and 22 with 256 x 256, 128 x 128256 x 4096 129 with 128 x 256 and
+// 149, 4096 x 128256 x 4096 2870 and 2150.
 hipError_t launch_logits(const LogitsArgs& a, hipStream_t s) {
-    const dim3 grid((unsigned)((a.V + kTile - 1) / kTile), (unsigned)((a.T + kTile - 1) / kTile));
-    ember_logits_tile<<<grid, kBlock, 0, s>>>(a);
-    return hipGetLastError();
+    if (a.T <= 16) {
+        if (a.D <= 512) return launch_few<1, 1, 4, 1>(a, s);
+        if (a.D <= 1024) return launch_few<2, 1, 2, 1>(a, s);
+        if (a.D <= 2048) return launch_few<4, 1, 1, 1>(a, s);
+        if (a.D <= 4096) return launch_few<4, 2, 1, 1>(a, s);
+    } else if (a.T <= 32) {
+        if (a.D <= 512) return launch_few<1, 1, 2, 2>(a, s);
+        if (a.D <= 1024) return launch_few<2, 1, 2, 2>(a, s);
+        if (a.D <= 2048) return launch_few<4, 1, 1, 2>(a, s);
+        if (a.D <= 4096) return launch_few<4, 2, 1, 2>(a, s);
+    } else if (a.T <= 64 && a.D > 512) {
+        if (a.D <= 1024) return launch_few<2, 1, 1, 4>(a, s);
+        if (a.D <= 2048) return launch_few<2, 2, 1, 4>(a, s);
+    }
+    int best = 0;
+    for (int i = 1; i < (int)(sizeof kTiles / sizeof kTiles[0]); ++i)
+        if (tile_us(kTiles[i], a) < tile_us(kTiles[best], a)) best = i;
+    switch (best) {
+    case 0: return launch_tiles<T256x256>(a, s);
+    case 1: return launch_tiles<T128x256>(a, s);
+    case 2: return launch_tiles<T128x128>(a, s);
+    case 3: return launch_tiles<T64x256>(a, s);
+    case 4: return launch_tiles<T64x128>(a, s);
+    default: return launch_tiles<T32x128>(a, s);
+    }
 }
 
 } // namespace ember

@@ -42,7 +42,9 @@ def sums(Xq, Wq):
 SHAPES = [(1, 1, 1), (1, 5, 16), (1, 300, 64), (2, 1000, 200), (3, 64, 4096), (5, 257, 1023), (15, 2000, 130),
           (16, 513, 512), (17, 600, 96), (31, 100, 77), (32, 1024, 64), (33, 1025, 640), (64, 256, 128),
           (65, 700, 1000), (100, 4097, 48), (129, 515, 333), (255, 256, 256), (256, 1000, 896), (300, 3001, 520),
-          (513, 770, 100), (1, 40000, 256), (700, 2500, 72), (2, 37, 32768), (1, 3, 15), (4, 129, 17)]
+          (513, 770, 100), (1, 40000, 256), (700, 2500, 72), (2, 37, 32768), (1, 3, 15), (4, 129, 17),
+          (16, 130, 8192), (3, 500, 5000), (32, 200, 4096), (30, 333, 3001), (9, 5000, 1040), (16, 9000, 2047),
+          (31, 9000, 2048), (2, 70000, 40), (40, 300, 8200), (17, 90, 4097)]
 
 
 @pytest.mark.parametrize("T,V,D", SHAPES)
@@ -129,20 +131,21 @@ def test_offsets_past_32_bits(em):
 
 
 def test_wide_strides(em):
-    """Rows of a few codes at a stride of 40 MB: what counts is the row's own offset."""
-    ld = 40 << 20
-    buf = torch.zeros(100 * ld, dtype=torch.int8, device=DEV)
-    Wq = buf.as_strided((100, 48), (ld, 1))
-    Wq.copy_(codes(100, 48, 1))
-    for T in (1, 20, 70):
+    """Rows of a few codes at the largest stride: what counts is the row's own offset."""
+    ld = (1 << 22) - 16
+    n = 600      # 2.5 GB from the first row to the last
+    buf = torch.zeros(n * ld, dtype=torch.int8, device=DEV)
+    Wq = buf.as_strided((n, 48), (ld, 1))
+    Wq.copy_(codes(n, 48, 1))
+    for T in (1, 20, 70, 300):
         print(f"logits wide strides T={T}", flush=True)
         Xq = codes(T, 48, T)
-        Y = out(T, 100, F, 0)
-        em.ember_logits_q8(Xq, torch.ones(T, device=DEV), Wq, torch.ones(100, device=DEV), Y)
+        Y = out(T, n, F, 0)
+        em.ember_logits_q8(Xq, torch.ones(T, device=DEV), Wq, torch.ones(n, device=DEV), Y)
         assert torch.equal(Y, sums(Xq, Wq).float()), T
         # and the other way round: the tokens far apart
-        Z = out(100, T, F, 0)
-        em.ember_logits_q8(Wq, torch.ones(100, device=DEV), Xq, torch.ones(T, device=DEV), Z)
+        Z = out(n, T, F, 0)
+        em.ember_logits_q8(Wq, torch.ones(n, device=DEV), Xq, torch.ones(T, device=DEV), Z)
         assert torch.equal(Z, sums(Wq, Xq).float()), T
 
 

@@ -121,7 +121,7 @@ def _logits(em, **kw):
 
 @pytest.mark.parametrize("kw,status", [
     (dict(T=-1), "SHAPE"), (dict(V=0), "SHAPE"), (dict(V=2 ** 31), "SHAPE"), (dict(D=0), "SHAPE"),
-    (dict(D=32769, ldx=32784, ldw=32784), "SHAPE"), (dict(ldx=48), "SHAPE"), (dict(ldw=48), "SHAPE"),
+    (dict(D=32769, ldx=32784, ldw=32784), "SHAPE"), (dict(ldw=2 ** 22), "SHAPE"), (dict(ldx=48), "SHAPE"), (dict(ldw=48), "SHAPE"),
     (dict(ldy=96), "SHAPE"),
     (dict(Xq=None), "ARG"), (dict(xs=None), "ARG"), (dict(Wq=None), "ARG"), (dict(ws=None), "ARG"),
     (dict(Wq=None, ws=None), "ARG"), (dict(Xq=None, xs=None), "ARG"), (dict(Y=None), "ARG"),
