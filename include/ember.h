@@ -494,13 +494,14 @@ int ember_logits_q8(const int8_t* Xq, int64_t ldx, const float* xscale,
  * One ember_grad per tensor: rows x cols elements, row i at element i * ld;
  *   src, src_dtype, lds   the gradient, aligned to its element size (views at
  *                         any element of a bucket are fine);
- *   dst, dst_dtype, ldd   where it goes: src itself (same dtype and ld; in
- *                         place, and then nothing is written when factor is 1) or
- *                         other memory, of either dtype;
+ *   dst, dst_dtype, ldd   where it goes: src itself (same dtype and ld; then its
+ *                         rows are left alone when factor is 1) or other memory,
+ *                         of either dtype;
  *   rows_dev              NULL, or a device int64 (8-byte aligned) that says how
  *                         many of the rows hold a gradient (ember_coalesce_rows
- *                         writes it); the others are neither read nor written.
- *                         A value outside [0, rows] counts as the nearer end.
+ *                         writes it); the others are not read, and zeros are
+ *                         written in their place in dst.  A value outside
+ *                         [0, rows] counts as the nearer end.
  * Tensors must not overlap each other's memory.  rows, cols >= 0 (an empty
  * tensor's pointers may be NULL), rows * cols <= 2^42, 0 <= n_grads <=
  * EMBER_MAX_GRADS, max_norm >= 0 (infinite: only the norm, and copies).  The

@@ -332,7 +332,6 @@ struct LogitsArgs {
 hipError_t launch_logits(const LogitsArgs& a, hipStream_t s);
 
 // Global gradient norm and clipping (ember_clip.hip).
-constexpr int kClipPerLaunch = 48;    // tensors described in one launch's arguments
 size_t clip_ws_bytes(int64_t n);
 hipError_t launch_clip(const ember_grad* g, int64_t n, float max_norm, float* out, char* ws, hipStream_t s);
 

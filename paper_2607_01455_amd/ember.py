@@ -449,7 +449,7 @@ def ember_clip_workspace_bytes(n_grads: int) -> int:
 def grad_entry(src: torch.Tensor, dst: torch.Tensor | None = None, rows_dev: torch.Tensor | None = None) -> Grad:
     """One entry of ember_clip_grads: the gradient src, written clipped to dst
     (None: in place); rows_dev: a device int64 of one element that says how many
-    of its rows hold a gradient.  A 2-D tensor with unit column stride, or any
+    of its rows hold a gradient (the others become zeros).  A 2-D tensor with unit column stride, or any
     contiguous one.  The tensors must stay alive until the call has run."""
     if dst is None:
         dst = src

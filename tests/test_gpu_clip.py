@@ -33,7 +33,6 @@ def check(em, grads, max_norm, out=None, counts=None):
     held = [g if c is None else g[:max(0, min(int(c), g.shape[0]))] for g, c in
             zip(before, counts or [None] * len(grads))]
     clip = em.GradClipper(grads, out=out, counts=counts)
-    old = [None if o is None else o.clone() for o in (out or [None] * len(grads))]
     norm, factor = (x.item() for x in clip(max_norm))
     want = norm64(held)
     assert abs(norm - want) <= 2.0 ** -23 * want
@@ -41,12 +40,12 @@ def check(em, grads, max_norm, out=None, counts=None):
         assert abs(factor - max_norm / want) <= 2.0 ** -23 * factor
     else:
         assert factor == 1.0
-    for g, b, h, o, was in zip(grads, before, held, out or [None] * len(grads), old):
-        to, was = (g, b) if o is None else (o, was)
+    for g, b, h, o in zip(grads, before, held, out or [None] * len(grads)):
+        to = g if o is None else o
         n = h.shape[0] if h.dim() else 0
         want = (h.float() * torch.tensor(factor, device=DEV)).to(to.dtype)
         assert torch.equal(bits(to[:n]), bits(want))
-        assert torch.equal(bits(to[n:]), bits(was[n:]))
+        assert (to[n:] == 0).all()
         if o is not None:
             assert torch.equal(bits(g), bits(b))
     return norm, factor
@@ -79,7 +78,7 @@ def test_views_of_a_bucket_into_another(em, src, dst):
     check(em, list(torch.split(a[1:1 + sum(sizes)], sizes)), 3.0)
 
 
-@pytest.mark.parametrize("count", [1, 47, 48, 49, 97, 300])
+@pytest.mark.parametrize("count", [1, 47, 48, 49, 97, 151, 152, 153, 300, 700])
 def test_many_tensors(em, count):
     print(f"clip {count} tensors", flush=True)
     grads = [randn(1 + 37 * i % 5000, dtype=BF if i % 3 else F, seed=i) for i in range(count)]
@@ -109,10 +108,20 @@ def test_tables_with_strides_and_counts(em, dtype):
 
 
 def test_rows_past_the_count_may_hold_anything(em):
-    rows = randn(64, 100)
-    rows[40:] = float("nan")
-    n, f = check(em, [rows], 1.0, counts=[torch.tensor([40], device=DEV)])
-    assert math.isfinite(n) and f < 1.0
+    """They are not read, and become zeros, also where nothing else changes."""
+    for limit in (1.0, 1e6, math.inf):
+        rows = randn(64, 100)
+        rows[40:] = float("nan")
+        n, f = check(em, [rows], limit, counts=[torch.tensor([40], device=DEV)])
+        assert math.isfinite(n) and (f < 1.0) == (limit == 1.0)
+
+
+def test_many_tables(em):
+    """More strided tables than one launch describes, beside contiguous ones."""
+    grads = [randn(5 + i % 7, 40, dtype=BF if i % 2 else F, seed=i)[:, :33] for i in range(101)]
+    grads += [randn(10 + i, seed=i) for i in range(20)]
+    check(em, grads, 0.5)
+    check(em, grads, 1e6, out=[torch.zeros(g.shape, dtype=BF, device=DEV) for g in grads])
 
 
 def test_range_of_fp32(em):
