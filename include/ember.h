@@ -503,7 +503,7 @@ int ember_logits_q8(const int8_t* Xq, int64_t ldx, const float* xscale,
  *                         written in their place in dst.  A value outside
  *                         [0, rows] counts as the nearer end.
  * Tensors must not overlap each other's memory.  rows, cols >= 0 (an empty
- * tensor's pointers may be NULL), rows * cols <= 2^42, 0 <= n_grads <=
+ * tensor's pointers may be NULL), rows * cols <= 2^40, 0 <= n_grads <=
  * EMBER_MAX_GRADS, max_norm >= 0 (infinite: only the norm, and copies).  The
  * workspace (device, 256-byte aligned, ember_clip_workspace_bytes(n_grads))
  * needs no initialisation.  grads is read before the call returns.

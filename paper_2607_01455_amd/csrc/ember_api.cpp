@@ -329,7 +329,7 @@ int check_grad(const ember_grad& g) {
     if (g.rows < 0 || g.cols < 0) return EMBER_ERR_SHAPE;
     if (!dtype_ok(g.src_dtype) || !dtype_ok(g.dst_dtype)) return EMBER_ERR_DTYPE;
     if (g.rows == 0 || g.cols == 0) return EMBER_OK;
-    if (g.cols > ((int64_t)1 << 42) / g.rows) return EMBER_ERR_SHAPE;
+    if (g.cols > ((int64_t)1 << 40) / g.rows) return EMBER_ERR_SHAPE;
     if (g.rows > 1 && (g.lds < g.cols || g.ldd < g.cols)) return EMBER_ERR_SHAPE;
     if (g.src == nullptr || g.dst == nullptr) return EMBER_ERR_ARG;
     if (!aligned(g.src, dtype_size(g.src_dtype)) || !aligned(g.dst, dtype_size(g.dst_dtype)) ||

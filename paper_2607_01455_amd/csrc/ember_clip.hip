@@ -10,11 +10,15 @@
 // added in float64: fp32 squares leave the range at gradients of 2e19 and would
 // have to be scaled, and beside the memory the float64 arithmetic is free.
 //
-// The work is cut into runs: at most kRun elements of one row, or of a tensor
-// whose rows are contiguous and which is taken as one row.  A block takes
-// consecutive runs, one a wave at a time; the second pass takes them in the
-// opposite order, so that it begins with what the first one left in the
-// last-level cache.  Tensors are described in the kernel's arguments (nothing is
+// The work is cut into runs: at most 8 KB of one row, or of a tensor whose rows
+// are contiguous and which is taken as one row.  A wave takes one run at a
+// time, eight 16-byte loads a lane; the waves of the launch go through the runs
+// side by side.  (With a share of consecutive runs for each block, the blocks
+// read a power of two apart, which few of the memory's channels serve.)  The
+// second pass goes backwards, so that it begins with what the first one left in
+// the last-level cache, and its own loads and stores are non-temporal, which
+// leaves more of that there (128256 x 4096 and 16384 x 4096 bf16 written elsewhere:
+// 649 us with ordinary ones, 588 like this).  Tensors are described in the kernel's arguments (nothing is
 // uploaded, and a captured launch holds its own copy), contiguous ones in
 // 24 bytes each, 152 a launch.
 
@@ -30,11 +34,11 @@
 namespace ember {
 namespace {
 
-constexpr int kRun = 4096;            // elements a run at most
+constexpr int kLoads = 8;             // 16-byte loads a lane of a whole run
+constexpr int kRunBytes = kLoads * kWave * 16;
 constexpr int kMaxClipBlocks = 1024;  // blocks (and float64 sums) a launch at most
 constexpr int kMinClipBlocks = 64;    // and at least, where there is work for them
 constexpr int kMaxSums = 8192;        // sums of all launches, as far as kMinClipBlocks allows
-constexpr int kLoadsInFlight = 8;     // 16-byte loads a lane
 
 // A contiguous tensor of fewer than 2^30 elements.
 struct FlatTensor {
@@ -59,6 +63,8 @@ struct RowsTensor {
 };
 constexpr int kFlatPerLaunch = 152, kRowsPerLaunch = 48;
 
+template <typename T> constexpr int kRun = kRunBytes / (int)sizeof(T);   // elements of a whole run of T
+
 template <typename T> constexpr int kPerLaunch = 0;
 template <> constexpr int kPerLaunch<FlatTensor> = kFlatPerLaunch;
 template <> constexpr int kPerLaunch<RowsTensor> = kRowsPerLaunch;
@@ -81,68 +87,92 @@ __device__ __forceinline__ void add_squares(const u32x4_t& w, double (&s)[2]) {
     }
 }
 
+// A whole run that begins on a 16-byte boundary: its loads, all at once.
+template <typename T>
+__device__ __forceinline__ bool whole(const void* p, int n) {
+    return n == kRun<T> && (reinterpret_cast<uintptr_t>(p) & 15) == 0;
+}
+template <bool kNT>
+__device__ __forceinline__ void load_whole(const void* p, int lane, u32x4_t (&w)[kLoads]) {
+    const u32x4_t* q = static_cast<const u32x4_t*>(p);
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u) w[u] = kNT ? __builtin_nontemporal_load(q + lane + u * kWave) : q[lane + u * kWave];
+}
+
+// Any other run: the elements before its first 16-byte boundary, whole chunks, the rest.
+struct Parts {
+    int head, chunks, tail;
+};
+template <typename T>
+__device__ __forceinline__ Parts parts_of(const T* p, int n) {
+    Parts x;
+    x.head = min(n, (int)((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / (int)sizeof(T));
+    x.chunks = (n - x.head) / kChunkElems<T>;
+    x.tail = x.head + x.chunks * kChunkElems<T>;
+    return x;
+}
+
 template <typename T>
 __device__ __forceinline__ void square_run(const T* p, int n, int lane, double (&s)[2]) {
-    // elements before the first 16-byte boundary, whole chunks, the rest
-    const int head = min(n, (int)((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / (int)sizeof(T));
-    const int chunks = (n - head) / kChunkElems<T>;
-    const int tail = head + chunks * kChunkElems<T>;
-    const u32x4_t* q = reinterpret_cast<const u32x4_t*>(p + head);
-    int c = lane;
-    for (; c + (kLoadsInFlight - 1) * kWave < chunks; c += kLoadsInFlight * kWave) {
-        u32x4_t w[kLoadsInFlight];
+    const Parts x = parts_of(p, n);
+    const u32x4_t* q = reinterpret_cast<const u32x4_t*>(p + x.head);
+#pragma unroll 4
+    for (int c = lane; c < x.chunks; c += kWave) add_squares<T>(q[c], s);
+    if (lane < x.head) {
+        const double v = (double)load_elem(p, lane, sizeof(T) == 2);
+        s[0] += v * v;
+    }
+    if (lane < n - x.tail) {
+        const double v = (double)load_elem(p, x.tail + lane, sizeof(T) == 2);
+        s[1] += v * v;
+    }
+}
+
+// A chunk of T, scaled, to N elements of U; vec: they are aligned for vector stores.
+template <typename T, typename U>
+__device__ __forceinline__ void scale_chunk(const u32x4_t& w, U* out, bool vec, float f) {
+    constexpr int N = kChunkElems<T>;
+    float v[N];
 #pragma unroll
-        for (int u = 0; u < kLoadsInFlight; ++u) w[u] = q[c + u * kWave];
+    for (int e = 0; e < N; ++e) v[e] = elem<T>(w, e) * f;
+    if (vec) {
+        store_values<U, N, true>(out, 0, N, v);
+    } else {
 #pragma unroll
-        for (int u = 0; u < kLoadsInFlight; ++u) add_squares<T>(w[u], s);
+        for (int e = 0; e < N; ++e) {
+            if constexpr (sizeof(U) == 4) out[e] = v[e];
+            else out[e] = (U)pack_bf16(v[e], 0.0f);
+        }
     }
-    for (; c < chunks; c += kWave) add_squares<T>(q[c], s);
-    if (lane < head) {
-        const double x = (double)load_elem(p, lane, sizeof(T) == 2);
-        s[0] += x * x;
-    }
-    if (lane < n - tail) {
-        const double x = (double)load_elem(p, tail + lane, sizeof(T) == 2);
-        s[1] += x * x;
-    }
+}
+template <typename T, typename U>
+__device__ __forceinline__ bool stores_vectors(const U* out) {
+    constexpr int kOut = kChunkElems<T> * (int)sizeof(U) < 16 ? kChunkElems<T> * (int)sizeof(U) : 16;
+    return (reinterpret_cast<uintptr_t>(out) & (kOut - 1)) == 0;
 }
 
 template <typename T, typename U>
 __device__ __forceinline__ void scale_run(const T* p, U* out, int n, int lane, float f) {
-    const int head = min(n, (int)((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / (int)sizeof(T));
-    const int chunks = (n - head) / kChunkElems<T>;
-    const int tail = head + chunks * kChunkElems<T>;
-    const u32x4_t* q = reinterpret_cast<const u32x4_t*>(p + head);
-    constexpr int N = kChunkElems<T>;
-    // whole chunks are stored as vectors where the destination's are aligned too
-    constexpr int kOut = N * (int)sizeof(U) < 16 ? N * (int)sizeof(U) : 16;
-    const bool vec = (reinterpret_cast<uintptr_t>(out + head) & (kOut - 1)) == 0;
-    auto put = [&](int i, float v) {
+    if (whole<T>(p, n)) {
+        u32x4_t w[kLoads];
+        load_whole<true>(p, lane, w);
+        const bool vec = stores_vectors<T>(out);
+#pragma unroll
+        for (int u = 0; u < kLoads; ++u) scale_chunk<T>(w[u], out + (lane + u * kWave) * kChunkElems<T>, vec, f);
+        return;
+    }
+    const Parts x = parts_of(p, n);
+    const u32x4_t* q = reinterpret_cast<const u32x4_t*>(p + x.head);
+    const bool vec = stores_vectors<T>(out + x.head);
+#pragma unroll 4
+    for (int c = lane; c < x.chunks; c += kWave) scale_chunk<T>(q[c], out + x.head + c * kChunkElems<T>, vec, f);
+    auto one = [&](int i) {
+        const float v = load_elem(p, i, sizeof(T) == 2) * f;
         if constexpr (sizeof(U) == 4) out[i] = v;
         else out[i] = (U)pack_bf16(v, 0.0f);
     };
-    auto chunk = [&](int c, const u32x4_t& w) {
-        float v[N];
-#pragma unroll
-        for (int e = 0; e < N; ++e) v[e] = elem<T>(w, e) * f;
-        if (vec) {
-            store_values<U, N>(out + head + c * N, 0, N, v);
-        } else {
-#pragma unroll
-            for (int e = 0; e < N; ++e) put(head + c * N + e, v[e]);
-        }
-    };
-    int c = lane;
-    for (; c + (kLoadsInFlight - 1) * kWave < chunks; c += kLoadsInFlight * kWave) {
-        u32x4_t w[kLoadsInFlight];
-#pragma unroll
-        for (int u = 0; u < kLoadsInFlight; ++u) w[u] = q[c + u * kWave];
-#pragma unroll
-        for (int u = 0; u < kLoadsInFlight; ++u) chunk(c + u * kWave, w[u]);
-    }
-    for (; c < chunks; c += kWave) chunk(c, q[c]);
-    if (lane < head) put(lane, load_elem(p, lane, sizeof(T) == 2) * f);
-    if (lane < n - tail) put(tail + lane, load_elem(p, tail + lane, sizeof(T) == 2) * f);
+    if (lane < x.head) one(lane);
+    if (lane < n - x.tail) one(x.tail + lane);
 }
 
 // A run of a batch: n elements at src and dst; absent: its row holds no gradient.
@@ -165,15 +195,28 @@ __device__ __forceinline__ int tensor_of(const Batch<T>& b, int64_t r) {
     return lo;
 }
 
+// Run k of a row of n elements at p: whole runs begin on 16-byte boundaries of
+// the source, so the first one is short by the elements between the boundary
+// before p and p.
+struct Piece {
+    int64_t at;
+    int n;
+};
+__device__ __forceinline__ Piece piece_of(const void* p, bool bf16, int64_t n, int64_t k) {
+    const int64_t run = bf16 ? kRun<uint16_t> : kRun<float>;
+    const int64_t before = (int64_t)(reinterpret_cast<uintptr_t>(p) & 15) >> (bf16 ? 1 : 2);
+    const int64_t begin = max(k * run - before, (int64_t)0), end = min((k + 1) * run - before, n);
+    return Piece{begin, (int)(end - begin)};
+}
+
 __device__ __forceinline__ Run run_of(const FlatTensor& t, int64_t r) {
     Run x;
-    const uint32_t n = t.n & 0x3FFFFFFFu;
-    const uint32_t at = (uint32_t)(r - t.run0) * kRun;
     x.src_bf16 = t.n >> 31;
     x.dst_bf16 = (t.n >> 30) & 1;
-    x.src = static_cast<const char*>(t.src) + (size_t)at * (x.src_bf16 ? 2 : 4);
-    x.dst = static_cast<char*>(t.dst) + (size_t)at * (x.dst_bf16 ? 2 : 4);
-    x.n = (int)min(n - at, (uint32_t)kRun);
+    const Piece q = piece_of(t.src, x.src_bf16, t.n & 0x3FFFFFFFu, r - t.run0);
+    x.src = static_cast<const char*>(t.src) + q.at * (x.src_bf16 ? 2 : 4);
+    x.dst = static_cast<char*>(t.dst) + q.at * (x.dst_bf16 ? 2 : 4);
+    x.n = q.n;
     x.absent = false;
     x.in_place = t.src == t.dst;
     return x;
@@ -181,40 +224,54 @@ __device__ __forceinline__ Run run_of(const FlatTensor& t, int64_t r) {
 
 __device__ __forceinline__ Run run_of(const RowsTensor& t, int64_t r) {
     Run x;
-    const int64_t k = r - t.run0, row = t.segs == 1 ? k : k / t.segs, col = (k - row * t.segs) * kRun;
     x.src_bf16 = t.src_bf16;
     x.dst_bf16 = t.dst_bf16;
-    x.src = static_cast<const char*>(t.src) + (row * t.lds + col) * (x.src_bf16 ? 2 : 4);
-    x.dst = static_cast<char*>(t.dst) + (row * t.ldd + col) * (x.dst_bf16 ? 2 : 4);
-    x.n = (int)min(t.cols - col, (int64_t)kRun);
+    const int64_t k = r - t.run0, row = t.segs == 1 ? k : k / t.segs;
+    const char* src = static_cast<const char*>(t.src) + row * t.lds * (x.src_bf16 ? 2 : 4);
+    const Piece q = piece_of(src, x.src_bf16, t.cols, k - row * t.segs);   // a row's last one may be empty
+    x.src = src + q.at * (x.src_bf16 ? 2 : 4);
+    x.dst = static_cast<char*>(t.dst) + (row * t.ldd + q.at) * (x.dst_bf16 ? 2 : 4);
+    x.n = max(q.n, 0);
     x.absent = t.rows_dev && row >= *t.rows_dev;   // a count of less than 0: no row
     x.in_place = t.src == t.dst;
     return x;
 }
 
-// Calls f(run) for this wave's runs of the launch.  Block i has the i-th of
-// gridDim.x even shares; its waves take the runs of its share in turn.
-template <bool kBackwards, typename T, typename F>
-__device__ __forceinline__ void each_run(const Batch<T>& b, F f) {
-    const int64_t share = b.runs / gridDim.x, over = b.runs % gridDim.x, i = blockIdx.x;
-    const int64_t r0 = share * i + min(i, over), r1 = r0 + share + (i < over ? 1 : 0);
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    for (int64_t k = wave; k < r1 - r0; k += kWaves) {
-        const int64_t r = kBackwards ? r1 - 1 - k : r0 + k;
-        f(run_of(b.t[tensor_of(b, r)], r));
-    }
+// This wave's first run of the launch, and how far apart its runs are.
+__device__ __forceinline__ int64_t first_run() {
+    return (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
 }
+__device__ __forceinline__ int64_t run_step() { return (int64_t)gridDim.x * kWaves; }
 
 template <typename T>
 __global__ __launch_bounds__(kBlock) void ember_grad_squares(Batch<T> b, double* sums) {
     __shared__ double red[kWaves];
     const int lane = threadIdx.x & (kWave - 1);
     double s[2] = {0.0, 0.0};
-    each_run<false>(b, [&](const Run& x) {
-        if (x.absent) return;
-        if (x.src_bf16) square_run(reinterpret_cast<const uint16_t*>(x.src), x.n, lane, s);
-        else square_run(reinterpret_cast<const float*>(x.src), x.n, lane, s);
-    });
+    int64_t r = first_run();
+    Run x{};
+    if (r < b.runs) x = run_of(b.t[tensor_of(b, r)], r);
+    while (r < b.runs) {
+        const Run c = x;
+        u32x4_t w[kLoads];
+        const bool all = !c.absent && (c.src_bf16 ? whole<uint16_t>(c.src, c.n) : whole<float>(c.src, c.n));
+        if (all) load_whole<false>(c.src, lane, w);
+        // the next run is looked up while the loads are on their way
+        r += run_step();
+        if (r < b.runs) x = run_of(b.t[tensor_of(b, r)], r);
+        if (all) {
+            if (c.src_bf16) {
+#pragma unroll
+                for (int u = 0; u < kLoads; ++u) add_squares<uint16_t>(w[u], s);
+            } else {
+#pragma unroll
+                for (int u = 0; u < kLoads; ++u) add_squares<float>(w[u], s);
+            }
+        } else if (!c.absent) {
+            if (c.src_bf16) square_run(reinterpret_cast<const uint16_t*>(c.src), c.n, lane, s);
+            else square_run(reinterpret_cast<const float*>(c.src), c.n, lane, s);
+        }
+    }
     const double total = row_all<kBlock>(s[0] + s[1], [](double p, double q) { return p + q; }, red);
     if (threadIdx.x == 0) sums[blockIdx.x] = total;
 }
@@ -241,16 +298,18 @@ __global__ __launch_bounds__(kBlock) void ember_grad_scale(Batch<T> b, const dou
     }
     if (f == 1.0f && !b.always) return;
     const int lane = threadIdx.x & (kWave - 1);
-    each_run<true>(b, [&](const Run& x) {
+    for (int64_t r = first_run(); r < b.runs; r += run_step()) {
+        const int64_t back = b.runs - 1 - r;
+        const Run x = run_of(b.t[tensor_of(b, back)], back);
         if (x.absent) {
             if (x.dst_bf16) {
                 for (int i = lane; i < x.n; i += kWave) reinterpret_cast<uint16_t*>(x.dst)[i] = 0;
             } else {
                 for (int i = lane; i < x.n; i += kWave) reinterpret_cast<float*>(x.dst)[i] = 0.0f;
             }
-            return;
+            continue;
         }
-        if (x.in_place && f == 1.0f) return;   // it is what it would be
+        if (x.in_place && f == 1.0f) continue;   // it is what it would be
         if (x.src_bf16) {
             const uint16_t* p = reinterpret_cast<const uint16_t*>(x.src);
             if (x.dst_bf16) scale_run(p, reinterpret_cast<uint16_t*>(x.dst), x.n, lane, f);
@@ -260,7 +319,7 @@ __global__ __launch_bounds__(kBlock) void ember_grad_scale(Batch<T> b, const dou
             if (x.dst_bf16) scale_run(p, reinterpret_cast<uint16_t*>(x.dst), x.n, lane, f);
             else scale_run(p, reinterpret_cast<float*>(x.dst), x.n, lane, f);
         }
-    });
+    }
 }
 
 bool empty(const ember_grad& x) { return x.rows == 0 || x.cols == 0; }
@@ -269,13 +328,20 @@ bool contiguous(const ember_grad& x) {
 }
 bool is_flat(const ember_grad& x) { return contiguous(x) && x.rows * x.cols < ((int64_t)1 << 30); }
 
+// Runs of n elements that begin `at` bytes behind a 16-byte boundary (2^40 elements
+// at most: below 2^29).
+int64_t runs_of(const ember_grad& x, int64_t n, int64_t at) {
+    const int64_t es = x.src_dtype == EMBER_BF16 ? 2 : 4;
+    return (n * es + at + kRunBytes - 1) / kRunBytes;
+}
+
 int64_t fill(FlatTensor& t, const ember_grad& x, int64_t run0) {
     const int64_t n = x.rows * x.cols;
     t.src = x.src;
     t.dst = x.dst;
     t.n = (uint32_t)n | (x.src_dtype == EMBER_BF16 ? 1u << 31 : 0) | (x.dst_dtype == EMBER_BF16 ? 1u << 30 : 0);
-    t.run0 = (uint32_t)run0;   // below 152 * 2^18
-    return (n + kRun - 1) / kRun;
+    t.run0 = (uint32_t)run0;   // below 152 * 2^19
+    return runs_of(x, n, reinterpret_cast<uintptr_t>(x.src) & 15);
 }
 int64_t fill(RowsTensor& t, const ember_grad& x, int64_t run0) {
     const bool one = contiguous(x);
@@ -287,7 +353,10 @@ int64_t fill(RowsTensor& t, const ember_grad& x, int64_t run0) {
     t.lds = x.lds;
     t.ldd = x.ldd;
     t.run0 = run0;
-    t.segs = (int32_t)((t.cols + kRun - 1) / kRun);   // at most 2^30
+    // rows that begin on different boundaries: as many runs as the worst of them
+    const int64_t es = x.src_dtype == EMBER_BF16 ? 2 : 4;
+    const uintptr_t at = reinterpret_cast<uintptr_t>(x.src) & 15;
+    t.segs = (int32_t)runs_of(x, t.cols, t.rows == 1 || x.lds * es % 16 == 0 ? at : 16 - es);
     t.src_bf16 = x.src_dtype == EMBER_BF16;
     t.dst_bf16 = x.dst_dtype == EMBER_BF16;
     return t.rows * t.segs;

@@ -54,10 +54,17 @@ __device__ __forceinline__ u32x4_t load_chunk(const T* row, int col, int D) {
     return w;
 }
 
+template <bool kNT, typename V>
+__device__ __forceinline__ void store_vec(void* p, V v) {
+    if constexpr (kNT) __builtin_nontemporal_store(v, static_cast<V*>(p));
+    else *static_cast<V*>(p) = v;
+}
+
 // N fp32 values into columns [col, col + N) of a row of T, rounded to nearest
 // even for bf16: vector stores where they lie inside the row (col * sizeof(T) a
-// multiple of the vector's size), element stores in its last partial chunk.
-template <typename T, int N>
+// multiple of the vector's size; kNT: non-temporal), element stores in its last
+// partial chunk.
+template <typename T, int N, bool kNT = false>
 __device__ __forceinline__ void store_values(T* row, int col, int D, const float (&v)[N]) {
     constexpr int kWords = N * (int)sizeof(T) / 4;
     uint32_t w[kWords];
@@ -68,12 +75,11 @@ __device__ __forceinline__ void store_values(T* row, int col, int D, const float
     }
     if (col + N <= D) {
         if constexpr (kWords == 2) {
-            *reinterpret_cast<u32x2_t*>(row + col) = u32x2_t{w[0], w[1]};
+            store_vec<kNT>(row + col, u32x2_t{w[0], w[1]});
         } else {
 #pragma unroll
             for (int q = 0; q < kWords; q += 4)
-                *reinterpret_cast<u32x4_t*>(reinterpret_cast<uint32_t*>(row + col) + q) =
-                    u32x4_t{w[q], w[q + 1], w[q + 2], w[q + 3]};
+                store_vec<kNT>(reinterpret_cast<uint32_t*>(row + col) + q, u32x4_t{w[q], w[q + 1], w[q + 2], w[q + 3]});
         }
     } else {
 #pragma unroll
