@@ -9,9 +9,8 @@
 // Gradient, with u = dy gain and k = mean_j u_j s_j:
 //   dx_j = rstd u_j - rstd^3 k s_j + ds_j,   dgain_j = sum_t dy_tj s_tj rstd_t.
 //
-// One pass over the data each: TPR threads hold a row in registers, 16-byte
-// chunks dealt round robin, between the loads, the row's one or two reductions
-// and the stores.
+// One pass over the data each.  TPR threads hold a row between its loads, its one
+// or two reductions and its stores, 16-byte chunks dealt round robin.
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -48,6 +47,7 @@ struct FwdParams {
     int64_t ldq;
     float* qscale;
     float* rstd;          // or null
+    bool stream;          // S and Y are stored non-temporally
 };
 
 template <typename XT>
@@ -97,54 +97,93 @@ __device__ __forceinline__ void store_codes(int8_t* row, int col, int D, const f
     }
 }
 
-// kNorm: with the norm; otherwise the row itself goes to 8 bits.
-template <typename XT, int TPR, int NC, bool kNorm>
-__global__ __launch_bounds__(TPR < kBlock ? kBlock : TPR) void ember_rmsnorm_fwd(FwdParams a) {
-    constexpr int kThreads = TPR < kBlock ? kBlock : TPR;
-    constexpr int kRows = kThreads / TPR;
+// The chunk at column col: a full row (D a multiple of the chunk) has whole ones only.
+template <typename XT, bool kFull>
+__device__ __forceinline__ u32x4_t chunk_at(const XT* row, int col, int D) {
+    if constexpr (kFull) {
+        u32x4_t w = {0, 0, 0, 0};
+        if (col < D) w = *reinterpret_cast<const u32x4_t*>(row + col);
+        return w;
+    } else {
+        return load_chunk<XT>(row, col, D);
+    }
+}
+template <typename T, int N, bool kFull>
+__device__ __forceinline__ void store_at(T* row, int col, int D, const float (&v)[N], bool stream) {
+    if (kFull && col >= D) return;
+    const int end = kFull ? col + N : D;
+    if (stream) store_values<T, N, true>(row, col, end, v);
+    else store_values<T, N, false>(row, col, end, v);
+}
+template <int N, bool kFull>
+__device__ __forceinline__ void codes_at(int8_t* row, int col, int D, const float (&y)[N], float inv) {
+    if constexpr (kFull) {
+        if (col < D) store_codes<N>(row, col, col + N, y, inv);
+    } else {
+        store_codes<N>(row, col, D, y, inv);
+    }
+}
+
+constexpr int threads_of(int tpr) { return tpr < kBlock ? kBlock : tpr; }
+
+// kNorm: with the norm; otherwise the row itself goes to 8 bits.  The threads of a
+// row that spans several waves are the block's, so all of them meet at its
+// barriers; a block's rows have LDS slots by turns, which the barrier between
+// two rows' reductions keeps apart.
+template <typename XT, int TPR, int NC, bool kNorm, bool kFull>
+__global__ __launch_bounds__(threads_of(TPR)) void ember_rmsnorm_fwd(FwdParams a) {
+    constexpr int kRows = threads_of(TPR) / TPR;
     constexpr int N = kChunkElems<XT>;
-    __shared__ float red_sum[kThreads / kWave];
-    __shared__ uint32_t red_max[kThreads / kWave];
-    const int lane = threadIdx.x % TPR;
-    // the loop's bounds are the same for all threads of a row, and where a
-    // row's threads meet at barriers it is the block's only one
-    for (int64_t t = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR; t < a.T; t += (int64_t)gridDim.x * kRows) {
-        const XT* x = static_cast<const XT*>(a.X) + t * a.ldx;
-        const XT* r = static_cast<const XT*>(a.R) + (a.R ? t * a.ldr : 0);
+    __shared__ float red_sum[2][threads_of(TPR) / kWave];
+    __shared__ uint32_t red_max[2][threads_of(TPR) / kWave];
+    const int lane = threadIdx.x % TPR, D = a.D;
+    const int64_t step = (int64_t)gridDim.x * kRows;
+    int64_t t = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR;
+    float g[NC][N];
+    if constexpr (kNorm) {
+#pragma unroll
+        for (int c = 0; c < NC; ++c) load_gain<XT>(a.gain, a.gain_bf16, (lane + c * TPR) * N, D, g[c]);
+    }
+    for (int turn = 0; t < a.T; t += step, turn ^= 1) {
+        u32x4_t wx[NC], wr[NC];
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+            wx[c] = chunk_at<XT, kFull>(static_cast<const XT*>(a.X) + t * a.ldx, (lane + c * TPR) * N, D);
+        if (kNorm && a.R) {
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+                wr[c] = chunk_at<XT, kFull>(static_cast<const XT*>(a.R) + t * a.ldr, (lane + c * TPR) * N, D);
+        }
         float v[NC][N];
-        float sq = 0.0f;
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-            const int col = (lane + c * TPR) * N;
-            const u32x4_t w = load_chunk<XT>(x, col, a.D);
 #pragma unroll
-            for (int e = 0; e < N; ++e) v[c][e] = elem<XT>(w, e);
-            if (a.R) {
-                const u32x4_t z = load_chunk<XT>(r, col, a.D);
+            for (int e = 0; e < N; ++e) v[c][e] = elem<XT>(wx[c], e);
+        }
+        if (kNorm && a.R) {
 #pragma unroll
-                for (int e = 0; e < N; ++e) v[c][e] += elem<XT>(z, e);
-            }
+            for (int c = 0; c < NC; ++c)
+#pragma unroll
+                for (int e = 0; e < N; ++e) v[c][e] += elem<XT>(wr[c], e);
         }
         if constexpr (kNorm) {
+            float sq = 0.0f;
 #pragma unroll
-            for (int c = 0; c < NC; ++c) {
+            for (int c = 0; c < NC; ++c)
 #pragma unroll
                 for (int e = 0; e < N; ++e) sq += v[c][e] * v[c][e];
-                if (a.S) store_values<XT, N>(static_cast<XT*>(a.S) + t * a.lds, (lane + c * TPR) * N, a.D, v[c]);
-            }
-            sq = row_all<TPR>(sq, [](float p, float q) { return p + q; }, red_sum);
-            const float rstd = 1.0f / sqrtf(sq / (float)a.D + a.eps);
+            sq = row_all<TPR>(sq, [](float p, float q) { return p + q; }, red_sum[turn]);
+            const float rstd = 1.0f / sqrtf(sq / (float)D + a.eps);
             if (a.rstd && lane == 0) a.rstd[t] = rstd;
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
                 const int col = (lane + c * TPR) * N;
-                float g[N];
-                load_gain<XT>(a.gain, a.gain_bf16, col, a.D, g);
+                if (a.S) store_at<XT, N, kFull>(static_cast<XT*>(a.S) + t * a.lds, col, D, v[c], a.stream);
 #pragma unroll
-                for (int e = 0; e < N; ++e) v[c][e] = v[c][e] * rstd * g[e];
+                for (int e = 0; e < N; ++e) v[c][e] = v[c][e] * rstd * g[c][e];
                 if (a.Y) {
-                    if (a.y_bf16) store_values<uint16_t, N>(static_cast<uint16_t*>(a.Y) + t * a.ldy, col, a.D, v[c]);
-                    else store_values<float, N>(static_cast<float*>(a.Y) + t * a.ldy, col, a.D, v[c]);
+                    if (a.y_bf16) store_at<uint16_t, N, kFull>(static_cast<uint16_t*>(a.Y) + t * a.ldy, col, D, v[c], a.stream);
+                    else store_at<float, N, kFull>(static_cast<float*>(a.Y) + t * a.ldy, col, D, v[c], a.stream);
                 }
             }
         }
@@ -155,21 +194,21 @@ __global__ __launch_bounds__(TPR < kBlock ? kBlock : TPR) void ember_rmsnorm_fwd
             for (int c = 0; c < NC; ++c)
 #pragma unroll
                 for (int e = 0; e < N; ++e) m = max(m, __float_as_uint(v[c][e]) & 0x7FFFFFFFu);
-            m = row_all<TPR>(m, [](uint32_t p, uint32_t q) { return max(p, q); }, red_max);
+            m = row_all<TPR>(m, [](uint32_t p, uint32_t q) { return max(p, q); }, red_max[turn]);
             const float top = __uint_as_float(m);
             const bool finite = m < 0x7F800000u, some = finite && top >= kTinyRow;
             const float inv = some ? (float)kCodeMax / top : 0.0f;
+            if (!finite) {
 #pragma unroll
-            for (int c = 0; c < NC; ++c) {
-                if (!finite) {
+                for (int c = 0; c < NC; ++c)
 #pragma unroll
                     for (int e = 0; e < N; ++e) v[c][e] = 0.0f;
-                }
-                store_codes<N>(a.Q + t * a.ldq, (lane + c * TPR) * N, a.D, v[c], inv);
             }
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+                codes_at<N, kFull>(a.Q + t * a.ldq, (lane + c * TPR) * N, D, v[c], inv);
             if (lane == 0) a.qscale[t] = some ? top / (float)kCodeMax : finite ? 0.0f : __uint_as_float(0x7FC00000u);
         }
-        if constexpr (TPR > kWave) __syncthreads();   // the reductions' slots are used again
     }
 }
 
@@ -187,86 +226,136 @@ struct GradParams {
     int D;
     void* dX;
     int64_t lddx;
-    float* part;          // [gridDim.x * rows per block][D]: sums of dgain
+    float* part;          // [gridDim.x][D]: sums of dgain
+    bool stream;          // dX is stored non-temporally
 };
 
-template <typename XT, int TPR, int NC>
-__global__ __launch_bounds__(TPR < kBlock ? kBlock : TPR) void ember_rmsnorm_bwd(GradParams a) {
-    constexpr int kThreads = TPR < kBlock ? kBlock : TPR;
-    constexpr int kRows = kThreads / TPR;
+// kGroups rows at a time per block, TPR threads each; every thread keeps the
+// sums of dgain for its columns over all its rows, and the block adds up its
+// groups' at the end, in order.
+template <typename XT, int TPR, int NC, int kGroups, bool kFull>
+__global__ __launch_bounds__(TPR * kGroups) void ember_rmsnorm_bwd(GradParams a) {
     constexpr int N = kChunkElems<XT>;
-    __shared__ float red[kThreads / kWave];
-    const int lane = threadIdx.x % TPR;
-    const int64_t group = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR;
-    float acc[NC][N];
+    constexpr int kRowWaves = TPR / kWave;
+    __shared__ float red[2][kGroups][kRowWaves];
+    __shared__ float sums[kGroups > 1 ? kGroups - 1 : 1][TPR * N];
+    const int lane = threadIdx.x % TPR, group = threadIdx.x / TPR, D = a.D;
+    const int64_t step = (int64_t)gridDim.x * kGroups;
+    const int64_t rounds = (a.T - (int64_t)blockIdx.x * kGroups + step - 1) / step;   // of the block: all its threads take part
+    int64_t t = (int64_t)blockIdx.x * kGroups + group;
+    float g[NC][N], acc[NC][N];
 #pragma unroll
-    for (int c = 0; c < NC; ++c)
+    for (int c = 0; c < NC; ++c) {
+        load_gain<XT>(a.gain, a.gain_bf16, (lane + c * TPR) * N, D, g[c]);
 #pragma unroll
         for (int e = 0; e < N; ++e) acc[c][e] = 0.0f;
-    for (int64_t t = group; t < a.T; t += (int64_t)gridDim.x * kRows) {
-        const XT* dy = static_cast<const XT*>(a.dY) + t * a.lddy;
-        const XT* s = static_cast<const XT*>(a.S) + t * a.lds;
-        const float rstd = a.rstd[t];
-        u32x4_t wy[NC], ws[NC];
+    }
+    u32x4_t ny[NC], ns[NC], nd[NC];
+    float nrstd;
+    auto load = [&](int64_t row) {
+        row = min(row, a.T - 1);
+        nrstd = a.rstd[row];
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const int col = (lane + c * TPR) * N;
+            ny[c] = chunk_at<XT, kFull>(static_cast<const XT*>(a.dY) + row * a.lddy, col, D);
+            ns[c] = chunk_at<XT, kFull>(static_cast<const XT*>(a.S) + row * a.lds, col, D);
+            if (a.dS) nd[c] = chunk_at<XT, kFull>(static_cast<const XT*>(a.dS) + row * a.ldds, col, D);
+        }
+    };
+    // the next row's loads are in flight behind this one's reduction, where the
+    // registers hold both
+    constexpr bool kAhead = NC == 1;
+    if (kAhead) load(t);
+    for (int64_t i = 0; i < rounds; ++i, t += step) {
+        if (!kAhead) load(t);
+        u32x4_t wy[NC], ws[NC], wd[NC];
+        const float rstd = nrstd;
+        const bool there = t < a.T;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            wy[c] = ny[c];
+            ws[c] = ns[c];
+            if (a.dS) wd[c] = nd[c];
+        }
+        if (kAhead && i + 1 < rounds) load(t + step);
         float k = 0.0f;
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-            const int col = (lane + c * TPR) * N;
-            wy[c] = load_chunk<XT>(dy, col, a.D);
-            ws[c] = load_chunk<XT>(s, col, a.D);
-        }
-#pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            float g[N];
-            load_gain<XT>(a.gain, a.gain_bf16, (lane + c * TPR) * N, a.D, g);
 #pragma unroll
             for (int e = 0; e < N; ++e) {
                 const float p = elem<XT>(wy[c], e) * elem<XT>(ws[c], e);
-                k += p * g[e];
-                acc[c][e] += p * rstd;
+                k += p * g[c][e];
+                if (there) acc[c][e] += p * rstd;
             }
         }
-        k = row_all<TPR>(k, [](float p, float q) { return p + q; }, red);
-        const float ks = k / (float)a.D * rstd * rstd * rstd;
+        // by hand over the row's waves: the block's other rows have slots of their own
+        k = wave_all(k, [](float p, float q) { return p + q; });
+        if constexpr (TPR > kWave) {
+            float* slot = red[i & 1][group];
+            if ((threadIdx.x & (kWave - 1)) == 0) slot[lane / kWave] = k;
+            __syncthreads();
+            k = slot[0];
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            const int col = (lane + c * TPR) * N;
-            float g[N], d[N];
-            load_gain<XT>(a.gain, a.gain_bf16, col, a.D, g);
-#pragma unroll
-            for (int e = 0; e < N; ++e) d[e] = elem<XT>(wy[c], e) * g[e] * rstd - ks * elem<XT>(ws[c], e);
-            if (a.dS) {
-                const u32x4_t w = load_chunk<XT>(static_cast<const XT*>(a.dS) + t * a.ldds, col, a.D);
-#pragma unroll
-                for (int e = 0; e < N; ++e) d[e] += elem<XT>(w, e);
-            }
-            store_values<XT, N>(static_cast<XT*>(a.dX) + t * a.lddx, col, a.D, d);
+            for (int w = 1; w < kRowWaves; ++w) k += slot[w];
         }
-        if constexpr (TPR > kWave) __syncthreads();   // the reduction's slots are used again
+        const float ks = k / (float)D * rstd * rstd * rstd;
+        if (there) {
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                float d[N];
+#pragma unroll
+                for (int e = 0; e < N; ++e) d[e] = elem<XT>(wy[c], e) * g[c][e] * rstd - ks * elem<XT>(ws[c], e);
+                if (a.dS) {
+#pragma unroll
+                    for (int e = 0; e < N; ++e) d[e] += elem<XT>(wd[c], e);
+                }
+                store_at<XT, N, kFull>(static_cast<XT*>(a.dX) + t * a.lddx, (lane + c * TPR) * N, D, d, a.stream);
+            }
+        }
     }
-    float* part = a.part + group * a.D;
+    float* part = a.part + (int64_t)blockIdx.x * D;
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
+        if constexpr (kGroups > 1) {
+            __syncthreads();
+            if (group > 0) {
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-            const int col = (lane + c * TPR) * N + e;
-            if (col < a.D) part[col] = acc[c][e];
+                for (int e = 0; e < N; ++e) sums[group - 1][lane + e * TPR] = acc[c][e];
+            }
+            __syncthreads();
+            if (group == 0) {
+#pragma unroll
+                for (int q = 1; q < kGroups; ++q)
+#pragma unroll
+                    for (int e = 0; e < N; ++e) acc[c][e] += sums[q - 1][lane + e * TPR];
+            }
+        }
+        if (group == 0) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const int col = (lane + c * TPR) * N + e;
+                if (col < D) part[col] = acc[c][e];
+            }
         }
     }
 }
 
 constexpr int kSumCols = 64;      // columns per block of the partials' sum
-constexpr int kSumGroups = kBlock / kSumCols;
+constexpr int kSumThreads = 1024;
+constexpr int kSumGroups = kSumThreads / kSumCols;
 
 // dgain_j = the sum of the partial rows in a fixed order: kSumGroups
 // interleaved sums a column, then those in order.
-__global__ __launch_bounds__(kBlock) void ember_rmsnorm_dgain(const float* part, int n, int D, float* dgain) {
+__global__ __launch_bounds__(kSumThreads) void ember_rmsnorm_dgain(const float* part, int n, int D, float* dgain) {
     __shared__ float sums[kSumGroups][kSumCols];
     const int x = threadIdx.x % kSumCols, g = threadIdx.x / kSumCols;
     const int col = blockIdx.x * kSumCols + x;
     float s = 0.0f;
-    if (col < D)
+    if (col < D) {
+#pragma unroll 8
         for (int i = g; i < n; i += kSumGroups) s += part[(int64_t)i * D + col];
+    }
     sums[g][x] = s;
     __syncthreads();
     if (g == 0 && col < D) {
@@ -276,95 +365,116 @@ __global__ __launch_bounds__(kBlock) void ember_rmsnorm_dgain(const float* part,
     }
 }
 
-// Threads per row and chunks per thread for a row of `chunks` 16-byte chunks.
+// Threads per row and chunks per thread.
 struct RowPlan {
     int tpr, nc;
+    bool full;     // D a multiple of the chunk
 };
-RowPlan row_plan(int64_t T, int D, int dtype) {
-    const int epc = dtype == EMBER_F32 ? 4 : 8;
-    const int chunks = (D + epc - 1) / epc;
-    int tpr = chunks <= 64 ? 64 : chunks <= 2048 ? 256 : 1024;
-    int nc = 1;
-    while (tpr * nc < chunks) nc *= 2;
-    (void)T;
-    return RowPlan{tpr, nc};
+RowPlan row_plan(int D, int dtype, bool grad) {
+    const int epc = dtype == EMBER_F32 ? 4 : 8, chunks = (D + epc - 1) / epc;
+    RowPlan p;
+    if (grad) p.tpr = chunks <= 64 ? 64 : chunks <= 256 ? 256 : chunks <= 512 ? 512 : 1024;
+    else p.tpr = chunks <= 128 ? 64 : chunks <= 512 ? 256 : chunks <= 1024 ? 512 : 1024;
+    const int n = (chunks + p.tpr - 1) / p.tpr;
+    p.nc = n <= 1 ? 1 : n <= 2 ? 2 : n <= 4 ? 4 : 8;
+    p.full = D % epc == 0;
+    return p;
 }
 
-template <typename XT, bool kNorm>
+// Outputs up to this size are stored non-temporally.  With what reads y next
+// (us, ordinary / non-temporal): 2048 x 8192 bf16, 67 MB of s and y, 31.6 / 28.0,
+// 4096 x 4096 29.3 / 27.7 (the norm alone 25.3 / 21.3); 16384 x 4096, 268 MB,
+// 108.7 / 111.7.
+constexpr int64_t kStreamBytes = (int64_t)128 << 20;
+int64_t bytes_of(int64_t T, int64_t D, int dtype) { return T * D * (dtype == EMBER_F32 ? 4 : 2); }
+
+template <typename XT, bool kNorm, bool kFull>
 hipError_t launch_fwd(const FwdParams& p, const RowPlan& pl, hipStream_t s) {
-    const int rows = pl.tpr < kBlock ? kBlock / pl.tpr : 1;
+    const int threads = threads_of(pl.tpr), rows = threads / pl.tpr;
+    // one row a block (or four): fewer blocks that go through more rows each took
+    // 99 to 103 us instead of 94 at 16384 x 4096 bf16
     const dim3 grid((unsigned)capped_blocks((p.T + rows - 1) / rows));
 #define EMBER_FWD(TPR, NC) \
-    if (pl.tpr == TPR && pl.nc == NC) ember_rmsnorm_fwd<XT, TPR, NC, kNorm><<<grid, TPR < kBlock ? kBlock : TPR, 0, s>>>(p)
+    if (pl.tpr == TPR && pl.nc == NC) ember_rmsnorm_fwd<XT, TPR, NC, kNorm, kFull><<<grid, threads, 0, s>>>(p)
     EMBER_FWD(64, 1);
+    else EMBER_FWD(64, 2);
     else EMBER_FWD(256, 1);
     else EMBER_FWD(256, 2);
-    else EMBER_FWD(256, 4);
-    else EMBER_FWD(256, 8);
+    else EMBER_FWD(512, 2);
+    else EMBER_FWD(1024, 2);
     else EMBER_FWD(1024, 4);
-    else EMBER_FWD(1024, 8);
-    else return hipErrorInvalidValue;
+    else if constexpr (sizeof(XT) == 4) {
+        EMBER_FWD(1024, 8);
+        else return hipErrorInvalidValue;
+    } else return hipErrorInvalidValue;
 #undef EMBER_FWD
     return hipGetLastError();
 }
 
-template <typename XT>
+// Rows a block of the gradient takes at a time, and its blocks: one of 16 waves a
+// compute unit, so that few partial rows are left to add up (512 blocks: 106 us
+// instead of 102 at 16384 x 4096 bf16, 40 instead of 33 at 2048 x 8192).
+constexpr int kGradBlocks = 256;
+int grad_groups(const RowPlan& pl) { return 1024 / pl.tpr; }
+int grad_blocks(int64_t T, const RowPlan& pl) {
+    return (int)std::min<int64_t>((T + grad_groups(pl) - 1) / grad_groups(pl), kGradBlocks);
+}
+
+template <typename XT, bool kFull>
 hipError_t launch_bwd(const GradParams& p, const RowPlan& pl, int blocks, hipStream_t s) {
     const dim3 grid((unsigned)blocks);
-#define EMBER_BWD(TPR, NC) \
-    if (pl.tpr == TPR && pl.nc == NC) ember_rmsnorm_bwd<XT, TPR, NC><<<grid, TPR < kBlock ? kBlock : TPR, 0, s>>>(p)
-    EMBER_BWD(64, 1);
-    else EMBER_BWD(256, 1);
-    else EMBER_BWD(256, 2);
-    else EMBER_BWD(256, 4);
-    else EMBER_BWD(256, 8);
-    else EMBER_BWD(1024, 4);
-    else EMBER_BWD(1024, 8);
-    else return hipErrorInvalidValue;
+#define EMBER_BWD(TPR, NC, G) \
+    if (pl.tpr == TPR && pl.nc == NC) ember_rmsnorm_bwd<XT, TPR, NC, G, kFull><<<grid, TPR * G, 0, s>>>(p)
+    EMBER_BWD(64, 1, 16);
+    else EMBER_BWD(256, 1, 4);
+    else EMBER_BWD(512, 1, 2);
+    else EMBER_BWD(1024, 1, 1);
+    else EMBER_BWD(1024, 2, 1);
+    else EMBER_BWD(1024, 4, 1);
+    else if constexpr (sizeof(XT) == 4) {
+        EMBER_BWD(1024, 8, 1);
+        else return hipErrorInvalidValue;
+    } else return hipErrorInvalidValue;
 #undef EMBER_BWD
     return hipGetLastError();
 }
 
-constexpr int kGradBlocks = 1024;   // blocks of the gradient's pass at most
-
-int grad_blocks(int64_t T, const RowPlan& pl) {
-    const int rows = pl.tpr < kBlock ? kBlock / pl.tpr : 1;
-    return (int)std::min<int64_t>((T + rows - 1) / rows, kGradBlocks);
+template <typename XT>
+hipError_t launch_fwd_of(const FwdParams& p, bool norm, const RowPlan& pl, hipStream_t s) {
+    if (norm) return pl.full ? launch_fwd<XT, true, true>(p, pl, s) : launch_fwd<XT, true, false>(p, pl, s);
+    return pl.full ? launch_fwd<XT, false, true>(p, pl, s) : launch_fwd<XT, false, false>(p, pl, s);
 }
 
 } // namespace
 
 hipError_t launch_rmsnorm(const NormArgs& x, hipStream_t s) {
     FwdParams p{x.X, x.ldx, x.R, x.ldr, x.gain, x.gain_dtype == EMBER_BF16, x.eps, x.T, (int)x.D, x.S, x.lds,
-                x.Y, x.y_dtype == EMBER_BF16, x.ldy, x.Q, x.ldq, x.qscale, x.rstd};
-    const RowPlan pl = row_plan(x.T, (int)x.D, x.x_dtype);
-    if (x.x_dtype == EMBER_F32) return x.gain ? launch_fwd<float, true>(p, pl, s) : launch_fwd<float, false>(p, pl, s);
-    return x.gain ? launch_fwd<uint16_t, true>(p, pl, s) : launch_fwd<uint16_t, false>(p, pl, s);
+                x.Y, x.y_dtype == EMBER_BF16, x.ldy, x.Q, x.ldq, x.qscale, x.rstd,
+                (x.S ? bytes_of(x.T, x.D, x.x_dtype) : 0) + (x.Y ? bytes_of(x.T, x.D, x.y_dtype) : 0) <= kStreamBytes};
+    const RowPlan pl = row_plan((int)x.D, x.x_dtype, false);
+    return x.x_dtype == EMBER_F32 ? launch_fwd_of<float>(p, x.gain != nullptr, pl, s)
+                                  : launch_fwd_of<uint16_t>(p, x.gain != nullptr, pl, s);
 }
 
 size_t norm_grad_ws_bytes(int64_t T, int64_t D) {
-    size_t n = 1;
-    for (int dtype : {(int)EMBER_F32, (int)EMBER_BF16}) {
-        const RowPlan pl = row_plan(T, (int)D, dtype);
-        const size_t rows = pl.tpr < kBlock ? kBlock / pl.tpr : 1;
-        n = std::max(n, (size_t)grad_blocks(T, pl) * rows);
-    }
-    return (n * (size_t)D * sizeof(float) + 255) / 256 * 256;
+    int n = 1;
+    for (int dtype : {(int)EMBER_F32, (int)EMBER_BF16}) n = std::max(n, grad_blocks(T, row_plan((int)D, dtype, true)));
+    return ((size_t)n * (size_t)D * sizeof(float) + 255) / 256 * 256;
 }
 
 hipError_t launch_rmsnorm_grad(const NormGradArgs& x, hipStream_t s) {
     GradParams p{x.dY, x.lddy, x.S, x.lds, x.gain, x.gain_dtype == EMBER_BF16, x.rstd, x.dS, x.ldds, x.T, (int)x.D,
-                 x.dX, x.lddx, reinterpret_cast<float*>(x.ws)};
-    const RowPlan pl = row_plan(x.T, (int)x.D, x.x_dtype);
+                 x.dX, x.lddx, reinterpret_cast<float*>(x.ws), bytes_of(x.T, x.D, x.x_dtype) <= kStreamBytes};
+    const RowPlan pl = row_plan((int)x.D, x.x_dtype, true);
     const int blocks = grad_blocks(x.T, pl);
-    const int n = blocks * (pl.tpr < kBlock ? kBlock / pl.tpr : 1);
     if (blocks > 0) {
-        const hipError_t e = x.x_dtype == EMBER_F32 ? launch_bwd<float>(p, pl, blocks, s)
-                                                    : launch_bwd<uint16_t>(p, pl, blocks, s);
+        hipError_t e;
+        if (x.x_dtype == EMBER_F32) e = pl.full ? launch_bwd<float, true>(p, pl, blocks, s) : launch_bwd<float, false>(p, pl, blocks, s);
+        else e = pl.full ? launch_bwd<uint16_t, true>(p, pl, blocks, s) : launch_bwd<uint16_t, false>(p, pl, blocks, s);
         if (e != hipSuccess) return e;
     }
-    ember_rmsnorm_dgain<<<dim3((unsigned)((x.D + kSumCols - 1) / kSumCols)), kBlock, 0, s>>>(p.part, n, (int)x.D,
-                                                                                            x.dgain);
+    ember_rmsnorm_dgain<<<dim3((unsigned)((x.D + kSumCols - 1) / kSumCols)), kSumThreads, 0, s>>>(p.part, blocks,
+                                                                                                 (int)x.D, x.dgain);
     return hipGetLastError();
 }
 

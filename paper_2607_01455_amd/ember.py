@@ -355,17 +355,32 @@ def ember_lmhead_step(W: torch.Tensor, dY: torch.Tensor, H: torch.Tensor, G: tor
                                  ws.numel() * ws.element_size(), _stream(W)), "ember_lmhead_step")
 
 
-def _shaped(what: str, t: torch.Tensor | None, shape, dtype=None) -> None:
-    """Refuses a tensor the C entry point would index past its end: those know
-    pointers and the sizes they are given, not what memory lies behind them."""
-    if t is None:
-        return
+# The C entry points know pointers and the sizes they are given, not what memory
+# lies behind them: these refuse a tensor that would be indexed past its end.
+
+def _misfit(what, t, shape, dtype):
     if t.shape != shape:
         raise ValueError(f"{what}: shape {tuple(t.shape)}, expected {tuple(shape)}")
-    if dtype is not None and t.dtype != dtype:
-        raise TypeError(f"{what}: {t.dtype}, expected {dtype}")
-    if len(shape) == 1 and shape[0] > 1 and t.stride(0) != 1:
-        raise TypeError(f"{what}: a contiguous tensor is required")
+    raise TypeError(f"{what}: a contiguous {dtype or 'tensor'} is required" if len(shape) == 1 else
+                    f"{what}: {t.dtype}, expected {dtype}")
+
+
+def _matrix(what, t, shape, dtype=None):
+    """(address, row stride) of a 2-D tensor of this shape and type; None: no tensor."""
+    if t is None:
+        return None, 0
+    if t.shape != shape or (dtype is not None and t.dtype != dtype):
+        _misfit(what, t, shape, dtype)
+    return t.data_ptr(), _ld(t)
+
+
+def _vector(what, t, shape, dtype=torch.float32):
+    """Address of a contiguous 1-D tensor of this shape and type; None: no tensor."""
+    if t is None:
+        return None
+    if t.shape != shape or (dtype is not None and t.dtype != dtype) or not t.is_contiguous():
+        _misfit(what, t, shape, dtype)
+    return t.data_ptr()
 
 
 def ember_rmsnorm(X: torch.Tensor, gain: torch.Tensor, eps: float = 1e-6, R: torch.Tensor | None = None,
@@ -373,20 +388,18 @@ def ember_rmsnorm(X: torch.Tensor, gain: torch.Tensor, eps: float = 1e-6, R: tor
                   qscale: torch.Tensor | None = None, rstd: torch.Tensor | None = None) -> None:
     """S = X + R and its root-mean-square norm with gains, to Y and, in 8 bits
     with one scale a row, to (Q, qscale); rstd is kept for the gradient."""
-    shape = X.shape
+    shape, dtype = X.shape, X.dtype
+    x, ldx = _matrix("X", X, shape)
+    r, ldr = _matrix("R", R, shape, dtype)
+    sm, lds = _matrix("S", S, shape, dtype)
+    y, ldy = _matrix("Y", Y, shape)
+    q, ldq = _matrix("Q", Q, shape, torch.int8)
     T, D = shape
-    rows = (T,)
-    _shaped("gain", gain, (D,))
-    _shaped("R", R, shape, X.dtype)
-    _shaped("S", S, shape, X.dtype)
-    _shaped("Y", Y, shape)
-    _shaped("Q", Q, shape, torch.int8)
-    _shaped("qscale", qscale, rows, torch.float32)
-    _shaped("rstd", rstd, rows, torch.float32)
-    _check(LIB.ember_rmsnorm(_ptr(X), _dtype(X), _ld(X), _ptr(R), 0 if R is None else _ld(R), _ptr(gain),
-                             _dtype(gain), eps, T, D, _ptr(S), 0 if S is None else _ld(S), _ptr(Y),
-                             EMBER_F32 if Y is None else _dtype(Y), 0 if Y is None else _ld(Y), _ptr(Q),
-                             0 if Q is None else _ld(Q), _ptr(qscale), _ptr(rstd), _stream(X)), "ember_rmsnorm")
+    rows = shape[:1]
+    _check(LIB.ember_rmsnorm(x, _dtype(X), ldx, r, ldr, _vector("gain", gain, shape[1:], None), _dtype(gain), eps,
+                             T, D, sm, lds, y, EMBER_F32 if Y is None else _dtype(Y), ldy, q, ldq,
+                             _vector("qscale", qscale, rows), _vector("rstd", rstd, rows), _stream(X)),
+           "ember_rmsnorm")
 
 
 def ember_rmsnorm_grad_workspace_bytes(max_tokens: int, D: int) -> int:
@@ -401,26 +414,26 @@ def ember_rmsnorm_grad(dY: torch.Tensor, S: torch.Tensor, gain: torch.Tensor, rs
                        dS: torch.Tensor | None = None) -> None:
     """Gradient of ember_rmsnorm: dX (of X and of R) and dgain from dY, the sum S
     and rstd of the forward call, plus dS, the sum's gradient by other ways."""
-    shape = S.shape
+    shape, dtype = S.shape, S.dtype
+    s, lds = _matrix("S", S, shape)
+    dy, lddy = _matrix("dY", dY, shape, dtype)
+    dx, lddx = _matrix("dX", dX, shape, dtype)
+    ds, ldds = _matrix("dS", dS, shape, dtype)
     T, D = shape
-    _shaped("dY", dY, shape, S.dtype)
-    _shaped("dX", dX, shape, S.dtype)
-    _shaped("dS", dS, shape, S.dtype)
-    _shaped("gain", gain, (D,))
-    _shaped("rstd", rstd, (T,), torch.float32)
-    _shaped("dgain", dgain, (D,), torch.float32)
-    _check(LIB.ember_rmsnorm_grad(_ptr(dY), _ld(dY), _ptr(S), _dtype(S), _ld(S), _ptr(gain), _dtype(gain),
-                                  _ptr(rstd), _ptr(dS), 0 if dS is None else _ld(dS), T, D, _ptr(dX), _ld(dX),
-                                  _ptr(dgain), _ptr(ws), ws.numel() * ws.element_size(), _stream(dgain)),
-           "ember_rmsnorm_grad")
+    cols = shape[1:]
+    _check(LIB.ember_rmsnorm_grad(dy, lddy, s, _dtype(S), lds, _vector("gain", gain, cols, None), _dtype(gain),
+                                  _vector("rstd", rstd, shape[:1]), ds, ldds, T, D, dx, lddx,
+                                  _vector("dgain", dgain, cols), ws.data_ptr(), ws.numel() * ws.element_size(),
+                                  _stream(dgain)), "ember_rmsnorm_grad")
 
 
 def ember_quantize_rows(X: torch.Tensor, Q: torch.Tensor, qscale: torch.Tensor) -> None:
     """Rows of X in 8 bits: codes Q and one scale a row."""
-    rows, D = X.shape
-    _shaped("Q", Q, X.shape, torch.int8)
-    _shaped("qscale", qscale, (rows,), torch.float32)
-    _check(LIB.ember_quantize_rows(_ptr(X), _dtype(X), _ld(X), rows, D, _ptr(Q), _ld(Q), _ptr(qscale),
+    shape = X.shape
+    x, ldx = _matrix("X", X, shape)
+    q, ldq = _matrix("Q", Q, shape, torch.int8)
+    rows, D = shape
+    _check(LIB.ember_quantize_rows(x, _dtype(X), ldx, rows, D, q, ldq, _vector("qscale", qscale, shape[:1]),
                                    _stream(X)), "ember_quantize_rows")
 
 
@@ -428,16 +441,15 @@ def ember_logits_q8(Xq: torch.Tensor, xscale: torch.Tensor, Wq: torch.Tensor, ws
                     Y: torch.Tensor, bias: torch.Tensor | None = None) -> None:
     """Y = (Xq Wq^T) xscale wscale + bias: logits of T tokens from 8-bit hidden
     states and an 8-bit table, each with one scale a row."""
-    T, D = Xq.shape
-    V = Wq.shape[0]
-    _shaped("Xq", Xq, (T, D), torch.int8)
-    _shaped("Wq", Wq, (V, D), torch.int8)
-    _shaped("xscale", xscale, (T,), torch.float32)
-    _shaped("wscale", wscale, (V,), torch.float32)
-    _shaped("bias", bias, (V,), torch.float32)
-    _shaped("Y", Y, (T, V))
-    _check(LIB.ember_logits_q8(_ptr(Xq), _ld(Xq), _ptr(xscale), _ptr(Wq), _ld(Wq), _ptr(wscale), _ptr(bias),
-                               T, V, D, _ptr(Y), _dtype(Y), _ld(Y), _stream(Wq)), "ember_logits_q8")
+    xs, ws = Xq.shape, Wq.shape
+    T, D = xs
+    V = ws[0]
+    x, ldx = _matrix("Xq", Xq, xs, torch.int8)
+    w, ldw = _matrix("Wq", Wq, (V, D), torch.int8)
+    y, ldy = _matrix("Y", Y, (T, V))
+    _check(LIB.ember_logits_q8(x, ldx, _vector("xscale", xscale, xs[:1]), w, ldw, _vector("wscale", wscale, ws[:1]),
+                               _vector("bias", bias, ws[:1]), T, V, D, y, _dtype(Y), ldy, _stream(Wq)),
+           "ember_logits_q8")
 
 
 def ember_clip_workspace_bytes(n_grads: int) -> int:
@@ -476,8 +488,7 @@ def ember_clip_grads(grads, max_norm: float, out: torch.Tensor, ws: torch.Tensor
     """Clip gradients (a ctypes array of Grad entries, or a list of them) by
     their global norm; out (device, two floats) receives the norm and the factor."""
     arr = grads if isinstance(grads, ctypes.Array) else (Grad * len(grads))(*grads)
-    _shaped("out", out, (2,), torch.float32)
-    _check(LIB.ember_clip_grads(arr, len(arr), float(max_norm), _ptr(out), _ptr(ws),
+    _check(LIB.ember_clip_grads(arr, len(arr), float(max_norm), _vector("out", out, (2,)), _ptr(ws),
                                 ws.numel() * ws.element_size(), _stream(out)), "ember_clip_grads")
 
 
