@@ -613,11 +613,11 @@ hipError_t launch_tiles(const LogitsArgs& a, hipStream_t s) {
 
 namespace {
 
-using T256x256 = Tile<256, 256, 4, 2, 64, 4>;
-using T128x256 = Tile<128, 256, 2, 4, 64, 4>;
-using T128x128 = Tile<128, 128, 2, 2, 64, 4>;
-using T64x256 = Tile<64, 256, 1, 8, 128, 3>;
-using T64x128 = Tile<64, 128, 1, 4, 128, 3>;
+using T256x256 = Tile<256, 256, 4, 2, 128, 2>;
+using T128x256 = Tile<128, 256, 4, 2, 128, 3>;
+using T128x128 = Tile<128, 128, 4, 2, 128, 2>;
+using T64x256 = Tile<64, 256, 2, 4, 128, 3>;
+using T64x128 = Tile<64, 128, 2, 2, 128, 3>;
 using T32x128 = Tile<32, 128, 1, 4, 128, 3>;
 
 // What a launch of a tiling takes, in us: passes over the 256 compute units, each
@@ -629,8 +629,8 @@ struct TileCost {
     double alone, full, fill;
 };
 constexpr TileCost kTiles[] = {
-    {256, 256, 40.5, 68.6, 8.0}, {128, 256, 32.0, 45.8, 6.5}, {128, 128, 25.5, 24.2, 5.0},
-    {64, 256, 21.0, 29.0, 5.0},  {64, 128, 16.5, 13.6, 4.0},  {32, 128, 13.0, 10.0, 3.0},
+    {256, 256, 41.0, 65.0, 9.2}, {128, 256, 26.5, 38.3, 7.1}, {128, 128, 20.0, 20.6, 5.5},
+    {64, 256, 20.0, 25.6, 5.2},  {64, 128, 15.3, 12.9, 3.5},  {32, 128, 13.0, 9.5, 2.6},
 };
 double tile_us(const TileCost& c, const LogitsArgs& a) {
     const double tiles = (double)((a.T + c.bm - 1) / c.bm) * (double)((a.V + c.bn - 1) / c.bn);
@@ -645,9 +645,9 @@ double tile_us(const TileCost& c, const LogitsArgs& a) {
 // streaming / best tiling: 1 token x 128256 x 4096 82 / 91, 16 tokens 90 / 94, 32
 // tokens 96 / 98, 20 x 50000 x 3000 32 / 37, 64 x 100000 x 1000 29 / 39, 64 x 30000 x
 // 2000 18 / 21; past those limits 10 x 32768 x 8192 62 / 47, 50 x 200000 x 500 50 /
-// 42).  Others the tiling that should take least: 333 x 8191 x 1000 15 us with
-// 64 x 256 tiles and 22 with 256 x 256, 128 x 128256 x 4096 129 with 128 x 256 and
-// 149, 4096 x 128256 x 4096 2870 and 2150.
+// 42).  Others the tiling that should take least: 333 x 8191 x 1000 13 us with
+// 128 x 128 tiles and 25 with 256 x 256, 128 x 128256 x 4096 117 with 128 x 256
+// and 144, 2000 x 32000 x 8192 508 with 256 x 256 and 643 with 128 x 128.
 hipError_t launch_logits(const LogitsArgs& a, hipStream_t s) {
     if (a.T <= 16) {
         if (a.D <= 512) return launch_few<1, 1, 4, 1>(a, s);
