@@ -44,7 +44,11 @@ SHAPES = [(1, 1, 1), (1, 5, 16), (1, 300, 64), (2, 1000, 200), (3, 64, 4096), (5
           (65, 700, 1000), (100, 4097, 48), (129, 515, 333), (255, 256, 256), (256, 1000, 896), (300, 3001, 520),
           (513, 770, 100), (1, 40000, 256), (700, 2500, 72), (2, 37, 32768), (1, 3, 15), (4, 129, 17),
           (16, 130, 8192), (3, 500, 5000), (32, 200, 4096), (30, 333, 3001), (9, 5000, 1040), (16, 9000, 2047),
-          (31, 9000, 2048), (2, 70000, 40), (40, 300, 8200), (17, 90, 4097)]
+          (31, 9000, 2048), (2, 70000, 40), (40, 300, 8200), (17, 90, 4097),
+          # each tiling, with whole and with ragged 16-column chunks
+          (300, 30000, 512), (300, 30001, 500), (257, 40000, 130), (1000, 6000, 256), (600, 9003, 333),
+          (333, 8200, 1024), (333, 8191, 1000), (64, 40000, 512), (60, 40003, 300), (64, 30000, 128),
+          (129, 9001, 300), (12, 3000, 768), (32, 4097, 1024), (20, 5000, 1001), (64, 3000, 2048), (50, 2001, 1100)]
 
 
 @pytest.mark.parametrize("T,V,D", SHAPES)

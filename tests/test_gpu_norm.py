@@ -79,7 +79,7 @@ def check_codes(Q, qscale, y):
     assert (Q.int().abs().amax(dim=1) == 127).all()
 
 
-SHAPES = [(1, 1), (3, 7), (5, 8), (2, 64), (130, 200), (4, 512), (9, 513), (33, 1023), (6, 2049), (17, 4096), (3, 8192),
+SHAPES = [(1, 1), (3, 7), (5, 8), (2, 64), (130, 200), (4, 512), (9, 513), (33, 1023), (5, 2000), (4, 2048), (6, 2049), (17, 4096), (3, 8192),
           (2, 8200), (2, 16385), (3, 32768)]
 
 
@@ -123,6 +123,29 @@ def test_forward_over_token_counts(em, T, D, dtype):
     assert ((rstd.double() - rs).abs() <= 64 * U * rs).all()
     assert ((Y.double() - y).abs() <= 68 * U * y.abs() + store_err(y, dtype)).all()
     check_codes(Q, qscale, y)
+
+
+def test_outputs_past_what_is_streamed(em):
+    """147 MB of Y and as much of dX: these are not stored non-temporally."""
+    T, D = 9000, 8192
+    print("rmsnorm 9000 x 8192", flush=True)
+    X, R, g = make(T, D, BF, 3, True, extra=0)
+    gain = 0.5 + torch.rand(D, generator=g, device=DEV)
+    norm = em.HeadNorm(gain, EPS, max_tokens=T)
+    S, Y, dX, rstd, dgain = padded(T, D, BF), padded(T, D, BF), padded(T, D, BF), torch.zeros(T, device=DEV), torch.zeros(D, device=DEV)
+    norm(X, R, S, Y, rstd=rstd)
+    norm.grad(R, S, rstd, dX, dgain)
+    total = torch.zeros(D, dtype=torch.float64, device=DEV)
+    mag = torch.zeros(D, dtype=torch.float64, device=DEV)
+    for t0 in range(0, T, 3000):
+        at = slice(t0, t0 + 3000)
+        s, rs, y = forward64(X[at], R[at], gain)
+        assert torch.equal(bits(S[at]), bits((X[at].float() + R[at].float()).to(BF)))
+        assert ((Y[at].double() - y).abs() <= 68 * U * y.abs() + store_err(y, BF)).all()
+        dx, A, dg, m = grad64(R[at], S[at], gain, rstd[at], None)
+        assert ((dX[at].double() - dx).abs() <= 100 * U * A + store_err(dx, BF)).all()
+        total, mag = total + dg, mag + m
+    assert ((dgain.double() - total).abs() <= (T + 3) * U * mag).all()
 
 
 def test_outputs_in_place(em):
