@@ -122,6 +122,16 @@ struct Tile {
     static_assert(kLds <= 160 * 1024, "LDS of one CU");
 };
 
+// The epilogue's use of the LDS: a strip a wave, then the channels' scales and biases.
+template <typename C, typename YT>
+struct Epilogue {
+    static constexpr int kGroup = std::min(C::NT, 256 / (32 * (int)sizeof(YT)));   // MFMA tiles side by side in a strip
+    static constexpr int kCols = kGroup * 32;
+    static constexpr int kPitch = kCols * (int)sizeof(YT) + 16;   // bytes a token
+    static constexpr int kStrips = C::kWavesB * 32 * kPitch;
+    static constexpr int kBytes = kStrips + 2 * C::BN * 4;
+};
+
 // Chunk c of a slice's row r sits at position c ^ swizzle(r): the reads of the
 // same chunk of 8 (or 16) consecutive rows then cover 32 (or all 64) LDS banks
 // once, and a wave-wide load still fills whole rows.
@@ -134,7 +144,7 @@ __device__ __forceinline__ int swizzle(int r) {
 // that do not count; they are cleared in the tokens' operand.
 template <typename C, typename YT, bool kMask>
 __global__ __launch_bounds__(C::kThreads) void ember_logits_q8(Params p) {
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[C::kLds];
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[std::max(C::kLds, Epilogue<C, YT>::kBytes)];
     const LogitsArgs& a = p.a;
     const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
     const int lane = threadIdx.x & (kWave - 1);
@@ -216,6 +226,17 @@ __global__ __launch_bounds__(C::kThreads) void ember_logits_q8(Params p) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[mt][nt][i] = 0;
 
+    // the scales the epilogue needs, ahead of the operands
+    float xs[C::MT];
+#pragma unroll
+    for (int m = 0; m < C::MT; ++m) {
+        const int64_t t = t0 + (wm * C::MT + m) * 32 + (lane & 31);
+        xs[m] = t < a.T ? a.xscale[t] : 0.0f;
+    }
+    const int64_t my_v = v0 + threadIdx.x;
+    const bool has_v = (int)threadIdx.x < C::BN && my_v < a.V;
+    const float my_wscale = has_v ? a.wscale[my_v] : 0.0f, my_bias = has_v && a.bias ? a.bias[my_v] : 0.0f;
+
 #pragma unroll
     for (int q = 0; q < C::kStages; ++q) {
         const StepLoads sl = loads_of(q);
@@ -259,7 +280,7 @@ __global__ __launch_bounds__(C::kThreads) void ember_logits_q8(Params p) {
             for (int i = 0; i < kAll; ++i) {
                 if (i < C::MT * C::NT) {
                     const int m = i / C::NT, n = i % C::NT;
-                    acc[m][n] = __builtin_amdgcn_mfma_i32_32x32x32_i8(af[cur][m], bf[cur][n], acc[m][n], 0, 0, 0);
+                    acc[m][n] = __builtin_amdgcn_mfma_i32_32x32x32_i8(bf[cur][n], af[cur][m], acc[m][n], 0, 0, 0);
                 }
                 // operands in the order the MFMAs first use them: A 0, all of B, the rest of A
                 if (i < C::MT + C::NT) {
@@ -278,52 +299,51 @@ __global__ __launch_bounds__(C::kThreads) void ember_logits_q8(Params p) {
     // the zero-filling loads past the end have landed and every wave is done with the stages
     wait_step<0>();
 
-    // Epilogue: each wave takes its part in strips of kRows tokens: the values
-    // go to a wave-private LDS strip in the MFMA layout and are stored from it row
-    // by row, 16 bytes a lane.
-    constexpr int kEs = (int)sizeof(YT);
-    constexpr int kRows = 16;
-    constexpr int kCols = C::NT * 32;
-    constexpr int kPitch = kCols * kEs + 16;
+    // Epilogue: the channels are the rows of the MFMA tiles, so a lane holds four
+    // consecutive ones of a token.  Each wave takes its part in strips of 32 tokens
+    // x up to 256 bytes of channels: the values go to a wave-private LDS strip
+    // and are stored from it row by row, 16 bytes a lane.
+    using E = Epilogue<C, YT>;
+    constexpr int kEs = (int)sizeof(YT), kGroup = E::kGroup, kCols = E::kCols, kPitch = E::kPitch;
     constexpr int kLanesPerRow = kCols * kEs / 16;
     constexpr int kRowsPerPass = kWave / kLanesPerRow;
     constexpr int kEpc = 16 / kEs;
-    static_assert(C::kWavesB * kRows * kPitch <= C::kLds && kRows % kRowsPerPass == 0, "strips fit the stages");
-    uint8_t* const strip = lds + wave * (kRows * kPitch);
-    const int half = lane >> 5, col = lane & 31;
-    const int64_t vw = v0 + wn * kCols;
-    float ws[C::NT], bias[C::NT];
-#pragma unroll
-    for (int n = 0; n < C::NT; ++n) {
-        const int64_t v = vw + n * 32 + col;
-        ws[n] = v < a.V ? a.wscale[v] : 0.0f;
-        bias[n] = a.bias && v < a.V ? a.bias[v] : 0.0f;
+    static_assert(C::NT % kGroup == 0 && 32 % kRowsPerPass == 0 && C::kThreads >= C::BN, "whole strips");
+    uint8_t* const strip = lds + wave * (32 * kPitch);
+    float* const sw = reinterpret_cast<float*>(lds + E::kStrips);
+    float* const sb = sw + C::BN;
+    if ((int)threadIdx.x < C::BN) {
+        sw[threadIdx.x] = my_wscale;
+        sb[threadIdx.x] = my_bias;
     }
+    __syncthreads();
+    const int half = lane >> 5, tok = lane & 31;
+    typedef float f32x4 __attribute__((ext_vector_type(4)));
 #pragma unroll
     for (int m = 0; m < C::MT; ++m) {
+        const int64_t ts = t0 + (wm * C::MT + m) * 32;
 #pragma unroll
-        for (int s = 0; s < 32 / kRows; ++s) {
-            // rows s kRows .. of the MFMA tile: registers i with 8 (i / 4) + 4 half + i % 4 in them
-            const int64_t ts = t0 + (wm * C::MT + m) * 32 + s * kRows;
+        for (int g = 0; g < C::NT / kGroup; ++g) {
+            const int c0 = wn * (C::NT * 32) + g * kCols;   // the strip's first channel in the tile
 #pragma unroll
-            for (int ii = 0; ii < kRows / 2; ++ii) {
-                const int i = s * (kRows / 2) + ii;
-                const int r = 8 * (i >> 2) + 4 * half + (i & 3) - s * kRows;
-                const float xs = ts + r < a.T ? a.xscale[ts + r] : 0.0f;
+            for (int n = 0; n < kGroup; ++n) {
 #pragma unroll
-                for (int n = 0; n < C::NT; ++n) {
-                    const float y = (float)acc[m][n][i] * (xs * ws[n]) + bias[n];
-                    uint8_t* e = strip + r * kPitch + (n * 32 + col) * kEs;
-                    if constexpr (kEs == 2) *reinterpret_cast<uint16_t*>(e) = (uint16_t)pack_bf16(y, 0.0f);
-                    else *reinterpret_cast<float*>(e) = y;
+                for (int q = 0; q < 4; ++q) {
+                    const int at = n * 32 + 8 * q + 4 * half;   // registers 4 q .. 4 q + 3
+                    const f32x4 w = *reinterpret_cast<const f32x4*>(sw + c0 + at);
+                    const f32x4 b = *reinterpret_cast<const f32x4*>(sb + c0 + at);
+                    float y[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) y[e] = (float)acc[m][g * kGroup + n][4 * q + e] * (xs[m] * w[e]) + b[e];
+                    store_values<YT, 4>(reinterpret_cast<YT*>(strip + tok * kPitch) + at, 0, 4, y);
                 }
             }
             wave_lds_order();
 #pragma unroll
-            for (int ps = 0; ps < kRows / kRowsPerPass; ++ps) {
+            for (int ps = 0; ps < 32 / kRowsPerPass; ++ps) {
                 const int r = ps * kRowsPerPass + lane / kLanesPerRow;
                 const int c = lane % kLanesPerRow;
-                const int64_t t = ts + r, v = vw + c * kEpc;
+                const int64_t t = ts + r, v = v0 + c0 + c * kEpc;
                 const u32x4_t w = *reinterpret_cast<const u32x4_t*>(strip + r * kPitch + c * 16);
                 if (t < a.T) {
                     YT* y = static_cast<YT*>(a.Y) + t * a.ldy + v;
@@ -616,27 +636,29 @@ namespace {
 using T256x256 = Tile<256, 256, 4, 2, 128, 2>;
 using T128x256 = Tile<128, 256, 4, 2, 128, 3>;
 using T128x128 = Tile<128, 128, 4, 2, 128, 2>;
-using T64x256 = Tile<64, 256, 2, 4, 128, 3>;
+using T128x128s = Tile<128, 128, 2, 2, 64, 3>;   // 48 KB of shared memory: three a compute unit
 using T64x128 = Tile<64, 128, 2, 2, 128, 3>;
 using T32x128 = Tile<32, 128, 1, 4, 128, 3>;
 
-// What a launch of a tiling takes, in us: passes over the 256 compute units, each
-// the tile's columns at a rate between that of a tile that has the chip to
-// itself and that of a full chip (us per 4096 columns, both measured), and
-// filling and draining the pipeline, which the passes overlap in part.
+// What a launch of a tiling takes, in us, fitted to 26 shapes of 100 to 4096 tokens,
+// 2000 to 128256 channels and 128 to 4096 columns (rms error 10 to 16%): one
+// fill of the pipeline, then the tiles of a compute unit one after the other, each
+// its columns at the rate of a full chip (us per 4096) and its epilogue, which
+// is twice as long for fp32 logits.  Where one tile has a compute unit to itself
+// the last ones are a whole round; where several share it they are about half of one.
 struct TileCost {
     int bm, bn;
-    double alone, full, fill;
+    bool alone;
+    double fill, columns, epilogue;
 };
 constexpr TileCost kTiles[] = {
-    {256, 256, 41.0, 65.0, 9.2}, {128, 256, 26.5, 38.3, 7.1}, {128, 128, 20.0, 20.6, 5.5},
-    {64, 256, 20.0, 25.6, 5.2},  {64, 128, 15.3, 12.9, 3.5},  {32, 128, 13.0, 9.5, 2.6},
+    {256, 256, true, 2.5, 49.7, 7.1},  {128, 256, true, 2.5, 33.2, 4.3},  {128, 128, false, 3.6, 20.4, 1.6},
+    {128, 128, false, 5.1, 21.5, 1.1}, {64, 128, false, 4.2, 12.0, 1.5},  {32, 128, false, 4.3, 8.8, 1.2},
 };
 double tile_us(const TileCost& c, const LogitsArgs& a) {
-    const double tiles = (double)((a.T + c.bm - 1) / c.bm) * (double)((a.V + c.bn - 1) / c.bn);
-    const double passes = std::max(1.0, std::ceil(tiles / 256.0));
-    const double rate = c.alone + (c.full - c.alone) * std::min(1.0, tiles / 256.0);
-    return c.fill * (1.0 + passes) / 2.0 + passes * rate * (double)a.D / 4096.0;
+    const double tiles = (double)((a.T + c.bm - 1) / c.bm) * (double)((a.V + c.bn - 1) / c.bn) / 256.0;
+    const double rounds = c.alone ? std::ceil(tiles) : std::max(1.0, tiles + 0.5);
+    return c.fill + rounds * (c.columns * (double)a.D / 4096.0 + c.epilogue * (a.y_dtype == EMBER_F32 ? 2 : 1));
 }
 
 } // namespace
@@ -645,9 +667,11 @@ double tile_us(const TileCost& c, const LogitsArgs& a) {
 // streaming / best tiling: 1 token x 128256 x 4096 82 / 91, 16 tokens 90 / 94, 32
 // tokens 96 / 98, 20 x 50000 x 3000 32 / 37, 64 x 100000 x 1000 29 / 39, 64 x 30000 x
 // 2000 18 / 21; past those limits 10 x 32768 x 8192 62 / 47, 50 x 200000 x 500 50 /
-// 42).  Others the tiling that should take least: 333 x 8191 x 1000 13 us with
-// 128 x 128 tiles and 25 with 256 x 256, 128 x 128256 x 4096 117 with 128 x 256
-// and 144, 2000 x 32000 x 8192 508 with 256 x 256 and 643 with 128 x 128.
+// 42).  Others the tiling that should take least (us): 333 x 8191 x 1000 12 with
+// 128 x 128 tiles and 22 with 256 x 256, 330 x 110820 x 128 26 with 128 x 128 three a
+// compute unit, 29 with two and 36 with 256 x 256, 128 x 128256 x 4096 112 with 128 x 256
+// and 134 with 256 x 256, 211 x 36770 x 2896 50 with 256 x 256 and 76 with 128 x 128,
+// 128 x 4000 x 2000 10 with 32 x 128 and 16 with 128 x 128.
 hipError_t launch_logits(const LogitsArgs& a, hipStream_t s) {
     if (a.T <= 16) {
         if (a.D <= 512) return launch_few<1, 1, 4, 1>(a, s);
@@ -670,7 +694,7 @@ hipError_t launch_logits(const LogitsArgs& a, hipStream_t s) {
     case 0: return launch_tiles<T256x256>(a, s);
     case 1: return launch_tiles<T128x256>(a, s);
     case 2: return launch_tiles<T128x128>(a, s);
-    case 3: return launch_tiles<T64x256>(a, s);
+    case 3: return launch_tiles<T128x128s>(a, s);
     case 4: return launch_tiles<T64x128>(a, s);
     default: return launch_tiles<T32x128>(a, s);
     }

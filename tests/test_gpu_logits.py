@@ -48,7 +48,8 @@ SHAPES = [(1, 1, 1), (1, 5, 16), (1, 300, 64), (2, 1000, 200), (3, 64, 4096), (5
           # each tiling, with whole and with ragged 16-column chunks
           (300, 30000, 512), (300, 30001, 500), (257, 40000, 130), (1000, 6000, 256), (600, 9003, 333),
           (333, 8200, 1024), (333, 8191, 1000), (64, 40000, 512), (60, 40003, 300), (64, 30000, 128),
-          (129, 9001, 300), (12, 3000, 768), (32, 4097, 1024), (20, 5000, 1001), (64, 3000, 2048), (50, 2001, 1100)]
+          (129, 9001, 300), (12, 3000, 768), (32, 4097, 1024), (20, 5000, 1001), (64, 3000, 2048), (50, 2001, 1100),
+          (257, 40000, 128), (400, 30003, 144), (900, 12345, 64)]
 
 
 @pytest.mark.parametrize("T,V,D", SHAPES)
