@@ -18,15 +18,24 @@
 // second pass goes backwards, so that it begins with what the first one left in
 // the last-level cache, and its own loads and stores are non-temporal, which
 // leaves more of that there (128256 x 4096 and 16384 x 4096 bf16 written elsewhere:
-// 649 us with ordinary ones, 588 like this).  Tensors are described in the kernel's arguments (nothing is
-// uploaded, and a captured launch holds its own copy), contiguous ones in
-// 24 bytes each, 152 a launch.
+// 649 us with ordinary ones, 588 like this).
+//
+// Narrow rows at a stride share runs: a run is then 512 pieces of 16 bytes, or of
+// one element where rows do not begin on 16-byte boundaries, and a lane has eight
+// loads in flight there too (copied and clipped, bf16, us: 156294 rows of 108 a wave
+// each 100, sharing runs 32; 100000 of 130 at a stride of 131 96 and 40).  Rows of
+// more than 256 pieces have waves of their own.
+//
+// Tensors are described in the kernel's arguments (nothing is uploaded, and a
+// captured launch holds its own copy), contiguous ones in 24 bytes each, others in
+// 80, as many a launch as fit.
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "ember_device.h"
 #include "ember_launch.h"
@@ -57,26 +66,34 @@ struct RowsTensor {
     int64_t lds;
     int64_t ldd;
     int64_t run0;
-    int32_t segs;              // runs a row
-    int16_t src_bf16;
-    int16_t dst_bf16;
+    int32_t segs;              // runs a row; 0: rows share runs
+    int32_t pieces;            // if they do: whole pieces a row,
+    uint32_t inverse;          // 2^20 / pieces, rounded up,
+    int8_t vec;                // pieces of 16 bytes, else of an element
+    int8_t vec_dst;            // and their results can be stored as vectors
+    int8_t src_bf16;
+    int8_t dst_bf16;
 };
-constexpr int kFlatPerLaunch = 152, kRowsPerLaunch = 48;
+constexpr int kPerRun = 512;          // pieces of a shared run
+constexpr int kMaxPieces = 256;       // of a row that shares runs: below 256 + 512 pieces, x / pieces = (x inverse) >> 20
 
 template <typename T> constexpr int kRun = kRunBytes / (int)sizeof(T);   // elements of a whole run of T
 
-template <typename T> constexpr int kPerLaunch = 0;
-template <> constexpr int kPerLaunch<FlatTensor> = kFlatPerLaunch;
-template <> constexpr int kPerLaunch<RowsTensor> = kRowsPerLaunch;
-
-template <typename T>
+// The tensors of a launch: contiguous ones from the front of the space, others from its back.
+constexpr int kSpace = 3808;
+constexpr int kLeastPerLaunch = kSpace / (int)sizeof(RowsTensor);
+constexpr int kMaxLaunches = (EMBER_MAX_GRADS + kLeastPerLaunch - 1) / kLeastPerLaunch;
 struct Batch {
-    T t[kPerLaunch<T>];
-    int64_t runs;
-    int n;
-    bool always;      // the second pass has work at f = 1 too
+    alignas(8) char space[kSpace];
+    int64_t flat_runs, runs;   // of the contiguous tensors, and in all
+    int16_t flats, others;
+    bool always;               // the second pass has work at f = 1 too
+    __host__ __device__ const FlatTensor& flat(int i) const { return reinterpret_cast<const FlatTensor*>(space)[i]; }
+    __host__ __device__ const RowsTensor& other(int i) const {
+        return reinterpret_cast<const RowsTensor*>(space + kSpace)[-1 - i];
+    }
 };
-static_assert(sizeof(Batch<FlatTensor>) <= 3840 && sizeof(Batch<RowsTensor>) <= 3840, "kernel arguments");
+static_assert(sizeof(Batch) <= 3840 && kSpace % 16 == 0 && sizeof(RowsTensor) == 80, "kernel arguments");
 
 template <typename T>
 __device__ __forceinline__ void add_squares(const u32x4_t& w, double (&s)[2]) {
@@ -175,21 +192,151 @@ __device__ __forceinline__ void scale_run(const T* p, U* out, int n, int lane, f
     if (lane < n - x.tail) one(x.tail + lane);
 }
 
+// A run of rows that share runs, from its first piece on.
+template <typename T, bool kVec>
+struct Shared {
+    static constexpr int N = kVec ? kChunkElems<T> : 1;   // elements a piece
+    int64_t row;       // the run's first row
+    int x0;            // pieces of it that belong to earlier runs
+    int64_t there;     // rows from it on, and
+    int64_t held;      // those that hold gradients (may be negative)
+    int tail;          // elements of a row behind its whole pieces
+    int tails;         // rows whose last whole piece is in this run
+    __device__ __forceinline__ Shared(const RowsTensor& t, int64_t k) {
+        const int64_t base = k * kPerRun;
+        row = base / t.pieces;
+        x0 = (int)(base - row * t.pieces);
+        there = t.rows - row;
+        held = t.rows_dev ? min(*t.rows_dev - row, there) : there;
+        tail = (int)t.cols - t.pieces * N;
+        tails = (int)min((int64_t)(((uint32_t)(x0 + kPerRun) * t.inverse) >> 20), there);
+    }
+    // piece x0 + i: its row behind the first and its first element there
+    __device__ __forceinline__ void at(const RowsTensor& t, int i, int& q, int& e) const {
+        const uint32_t x = (uint32_t)(x0 + i);
+        q = (int)((x * t.inverse) >> 20);
+        e = ((int)x - q * t.pieces) * N;
+    }
+    // element i of the rows' tails, i < tails * tail
+    __device__ __forceinline__ void at_tail(const RowsTensor& t, int i, int& q, int& e) const {
+        q = i / tail;
+        e = t.pieces * N + i - q * tail;
+    }
+};
+
+// The pieces of a run, all of their loads at once; those of rows without a gradient are zeros.
+template <typename T, bool kVec, bool kNT>
+__device__ __forceinline__ void load_shared(const RowsTensor& t, const Shared<T, kVec>& h, int lane,
+                                            u32x4_t (&w)[kLoads]) {
+    const T* p = static_cast<const T*>(t.src) + h.row * t.lds;
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u) {
+        int q, e;
+        h.at(t, lane + u * kWave, q, e);
+        // the others load the run's first row, which has one
+        const T* from = q < h.held ? p + (int64_t)q * t.lds + e : p;
+        if constexpr (kVec) {
+            const u32x4_t* v = reinterpret_cast<const u32x4_t*>(from);
+            w[u] = kNT ? __builtin_nontemporal_load(v) : *v;
+        } else {
+            using Bits = std::conditional_t<sizeof(T) == 2, uint16_t, uint32_t>;
+            const Bits* v = reinterpret_cast<const Bits*>(from);
+            w[u][0] = kNT ? __builtin_nontemporal_load(v) : *v;
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u) {
+        int q, e;
+        h.at(t, lane + u * kWave, q, e);
+        if (q >= h.held) w[u] = u32x4_t{0, 0, 0, 0};
+    }
+}
+
+template <typename T, bool kVec>
+__device__ __forceinline__ void square_shared(const RowsTensor& t, int64_t k, int lane, double (&s)[2]) {
+    const Shared<T, kVec> h(t, k);
+    if (h.held <= 0) return;
+    u32x4_t w[kLoads];
+    load_shared<T, kVec, false>(t, h, lane, w);
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u) {
+        if constexpr (kVec) {
+            add_squares<T>(w[u], s);
+        } else {
+            const double x = (double)elem<T>(w[u], 0);
+            s[u & 1] += x * x;
+        }
+    }
+    if (!kVec || h.tail == 0) return;
+    const T* p = static_cast<const T*>(t.src) + h.row * t.lds;
+    const int n = (int)min((int64_t)h.tails, h.held) * h.tail;
+    for (int i = lane; i < n; i += kWave) {
+        int q, e;
+        h.at_tail(t, i, q, e);
+        const double x = (double)load_elem(p + (int64_t)q * t.lds, e, sizeof(T) == 2);
+        s[0] += x * x;
+    }
+}
+
+template <typename U>
+__device__ __forceinline__ void store_elem(U* out, float v) {
+    if constexpr (sizeof(U) == 4) *out = v;
+    else *out = (U)pack_bf16(v, 0.0f);
+}
+
+template <typename T, typename U, bool kVec>
+__device__ __forceinline__ void scale_shared(const RowsTensor& t, int64_t k, int lane, float f) {
+    const Shared<T, kVec> h(t, k);
+    // in place and unscaled, the rows with a gradient are what they would be
+    const int64_t from = t.src == t.dst && f == 1.0f ? h.held : 0;
+    if (from >= h.there) return;
+    u32x4_t w[kLoads];
+    if (h.held > 0) {
+        load_shared<T, kVec, true>(t, h, lane, w);
+    } else {
+#pragma unroll
+        for (int u = 0; u < kLoads; ++u) w[u] = u32x4_t{0, 0, 0, 0};
+    }
+    U* out = static_cast<U*>(t.dst) + h.row * t.ldd;
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u) {
+        int q, e;
+        h.at(t, lane + u * kWave, q, e);
+        if (q >= h.there || q < from) continue;
+        U* to = out + (int64_t)q * t.ldd + e;
+        if constexpr (kVec) scale_chunk<T>(w[u], to, t.vec_dst, f);
+        else store_elem(to, elem<T>(w[u], 0) * f);
+    }
+    if (!kVec || h.tail == 0) return;
+    const T* p = static_cast<const T*>(t.src) + h.row * t.lds;
+    const int n = h.tails * h.tail;
+    for (int i = lane; i < n; i += kWave) {
+        int q, e;
+        h.at_tail(t, i, q, e);
+        if (q < from) continue;
+        const float v = q < h.held ? load_elem(p + (int64_t)q * t.lds, e, sizeof(T) == 2) * f : 0.0f;
+        store_elem(out + (int64_t)q * t.ldd + e, v);
+    }
+}
+
 // A run of a batch: n elements at src and dst; absent: its row holds no gradient.
+// Or run k of tensor `shared`, whose rows share runs.
 struct Run {
     const char* src;
     char* dst;
     int n;
+    int shared;        // or -1
+    int64_t k;
     bool src_bf16, dst_bf16, absent, in_place;
 };
 
-// The tensor of run r: its runs begin at or before r, the next one's after it.
-template <typename T>
-__device__ __forceinline__ int tensor_of(const Batch<T>& b, int64_t r) {
-    int lo = 0, hi = b.n;   // in [lo, hi)
+// The one of n tensors that has run r: its runs begin at or before r, the next one's after it.
+template <typename F>
+__device__ __forceinline__ int tensor_of(int n, int64_t r, F run0) {
+    int lo = 0, hi = n;   // in [lo, hi)
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
-        if ((int64_t)b.t[mid].run0 <= r) lo = mid;
+        if ((int64_t)run0(mid) <= r) lo = mid;
         else hi = mid;
     }
     return lo;
@@ -219,14 +366,18 @@ __device__ __forceinline__ Run run_of(const FlatTensor& t, int64_t r) {
     x.n = q.n;
     x.absent = false;
     x.in_place = t.src == t.dst;
+    x.shared = -1;
     return x;
 }
 
-__device__ __forceinline__ Run run_of(const RowsTensor& t, int64_t r) {
+__device__ __forceinline__ Run run_of(const RowsTensor& t, int i, int64_t r) {
     Run x;
     x.src_bf16 = t.src_bf16;
     x.dst_bf16 = t.dst_bf16;
-    const int64_t k = r - t.run0, row = t.segs == 1 ? k : k / t.segs;
+    x.shared = t.segs == 0 ? i : -1;
+    x.k = r - t.run0;
+    if (t.segs == 0) return x;
+    const int64_t k = x.k, row = t.segs == 1 ? k : k / t.segs;
     const char* src = static_cast<const char*>(t.src) + row * t.lds * (x.src_bf16 ? 2 : 4);
     const Piece q = piece_of(src, x.src_bf16, t.cols, k - row * t.segs);   // a row's last one may be empty
     x.src = src + q.at * (x.src_bf16 ? 2 : 4);
@@ -237,28 +388,34 @@ __device__ __forceinline__ Run run_of(const RowsTensor& t, int64_t r) {
     return x;
 }
 
+__device__ __forceinline__ Run run_of(const Batch& b, int64_t r) {
+    if (r < b.flat_runs) return run_of(b.flat(tensor_of(b.flats, r, [&](int i) { return b.flat(i).run0; })), r);
+    const int i = tensor_of(b.others, r, [&](int j) { return b.other(j).run0; });
+    return run_of(b.other(i), i, r);
+}
+
 // This wave's first run of the launch, and how far apart its runs are.
 __device__ __forceinline__ int64_t first_run() {
     return (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
 }
 __device__ __forceinline__ int64_t run_step() { return (int64_t)gridDim.x * kWaves; }
 
-template <typename T>
-__global__ __launch_bounds__(kBlock) void ember_grad_squares(Batch<T> b, double* sums) {
+__global__ __launch_bounds__(kBlock) void ember_grad_squares(Batch b, double* sums) {
     __shared__ double red[kWaves];
     const int lane = threadIdx.x & (kWave - 1);
     double s[2] = {0.0, 0.0};
     int64_t r = first_run();
     Run x{};
-    if (r < b.runs) x = run_of(b.t[tensor_of(b, r)], r);
+    if (r < b.runs) x = run_of(b, r);
     while (r < b.runs) {
         const Run c = x;
         u32x4_t w[kLoads];
-        const bool all = !c.absent && (c.src_bf16 ? whole<uint16_t>(c.src, c.n) : whole<float>(c.src, c.n));
+        const bool all = c.shared < 0 && !c.absent &&
+                         (c.src_bf16 ? whole<uint16_t>(c.src, c.n) : whole<float>(c.src, c.n));
         if (all) load_whole<false>(c.src, lane, w);
         // the next run is looked up while the loads are on their way
         r += run_step();
-        if (r < b.runs) x = run_of(b.t[tensor_of(b, r)], r);
+        if (r < b.runs) x = run_of(b, r);
         if (all) {
             if (c.src_bf16) {
 #pragma unroll
@@ -266,6 +423,15 @@ __global__ __launch_bounds__(kBlock) void ember_grad_squares(Batch<T> b, double*
             } else {
 #pragma unroll
                 for (int u = 0; u < kLoads; ++u) add_squares<float>(w[u], s);
+            }
+        } else if (c.shared >= 0) {
+            const RowsTensor& t = b.other(c.shared);
+            if (c.src_bf16) {
+                if (t.vec) square_shared<uint16_t, true>(t, c.k, lane, s);
+                else square_shared<uint16_t, false>(t, c.k, lane, s);
+            } else {
+                if (t.vec) square_shared<float, true>(t, c.k, lane, s);
+                else square_shared<float, false>(t, c.k, lane, s);
             }
         } else if (!c.absent) {
             if (c.src_bf16) square_run(reinterpret_cast<const uint16_t*>(c.src), c.n, lane, s);
@@ -286,8 +452,13 @@ __device__ __forceinline__ float clip_factor(const double* sums, int n, float ma
     return clip ? (float)((double)max_norm / norm) : 1.0f;
 }
 
-template <typename T>
-__global__ __launch_bounds__(kBlock) void ember_grad_scale(Batch<T> b, const double* sums, int n, float max_norm,
+template <typename T, typename U>
+__device__ __forceinline__ void scale_shared(const RowsTensor& t, int64_t k, int lane, float f) {
+    if (t.vec) scale_shared<T, U, true>(t, k, lane, f);
+    else scale_shared<T, U, false>(t, k, lane, f);
+}
+
+__global__ __launch_bounds__(kBlock) void ember_grad_scale(Batch b, const double* sums, int n, float max_norm,
                                                            float* out) {
     __shared__ double red[kWaves];
     double norm;
@@ -300,7 +471,18 @@ __global__ __launch_bounds__(kBlock) void ember_grad_scale(Batch<T> b, const dou
     const int lane = threadIdx.x & (kWave - 1);
     for (int64_t r = first_run(); r < b.runs; r += run_step()) {
         const int64_t back = b.runs - 1 - r;
-        const Run x = run_of(b.t[tensor_of(b, back)], back);
+        const Run x = run_of(b, back);
+        if (x.shared >= 0) {
+            const RowsTensor& t = b.other(x.shared);
+            if (x.src_bf16) {
+                if (x.dst_bf16) scale_shared<uint16_t, uint16_t>(t, x.k, lane, f);
+                else scale_shared<uint16_t, float>(t, x.k, lane, f);
+            } else {
+                if (x.dst_bf16) scale_shared<float, uint16_t>(t, x.k, lane, f);
+                else scale_shared<float, float>(t, x.k, lane, f);
+            }
+            continue;
+        }
         if (x.absent) {
             if (x.dst_bf16) {
                 for (int i = lane; i < x.n; i += kWave) reinterpret_cast<uint16_t*>(x.dst)[i] = 0;
@@ -340,7 +522,7 @@ int64_t fill(FlatTensor& t, const ember_grad& x, int64_t run0) {
     t.src = x.src;
     t.dst = x.dst;
     t.n = (uint32_t)n | (x.src_dtype == EMBER_BF16 ? 1u << 31 : 0) | (x.dst_dtype == EMBER_BF16 ? 1u << 30 : 0);
-    t.run0 = (uint32_t)run0;   // below 152 * 2^19
+    t.run0 = (uint32_t)run0;   // below 158 * 2^19
     return runs_of(x, n, reinterpret_cast<uintptr_t>(x.src) & 15);
 }
 int64_t fill(RowsTensor& t, const ember_grad& x, int64_t run0) {
@@ -353,104 +535,89 @@ int64_t fill(RowsTensor& t, const ember_grad& x, int64_t run0) {
     t.lds = x.lds;
     t.ldd = x.ldd;
     t.run0 = run0;
-    // rows that begin on different boundaries: as many runs as the worst of them
-    const int64_t es = x.src_dtype == EMBER_BF16 ? 2 : 4;
-    const uintptr_t at = reinterpret_cast<uintptr_t>(x.src) & 15;
-    t.segs = (int32_t)runs_of(x, t.cols, t.rows == 1 || x.lds * es % 16 == 0 ? at : 16 - es);
     t.src_bf16 = x.src_dtype == EMBER_BF16;
     t.dst_bf16 = x.dst_dtype == EMBER_BF16;
+    const int64_t es = t.src_bf16 ? 2 : 4, esd = t.dst_bf16 ? 2 : 4;
+    const uintptr_t at = reinterpret_cast<uintptr_t>(x.src) & 15;
+    const int64_t chunk = 16 / es, out = std::min<int64_t>(16, chunk * esd);   // elements; bytes a chunk is stored in at once
+    t.vec = at == 0 && x.lds * es % 16 == 0 && t.cols >= chunk;
+    t.vec_dst = (reinterpret_cast<uintptr_t>(x.dst) | (uintptr_t)(x.ldd * esd)) % (uintptr_t)out == 0;
+    if (t.rows > 1 && (t.vec ? t.cols / chunk : t.cols) <= kMaxPieces) {
+        t.pieces = (int32_t)(t.vec ? t.cols / chunk : t.cols);
+        t.inverse = ((1u << 20) + (uint32_t)t.pieces - 1) / (uint32_t)t.pieces;
+        t.segs = 0;
+        return (t.rows * t.pieces + kPerRun - 1) / kPerRun;
+    }
+    t.pieces = 0;
+    t.inverse = 0;
+    // rows that begin on different boundaries: as many runs as the worst of them
+    t.segs = (int32_t)runs_of(x, t.cols, t.rows == 1 || x.lds * es % 16 == 0 ? at : 16 - es);
     return t.rows * t.segs;
 }
 
-// The k-th launch's tensors of one kind.
-template <typename T>
-void batch_of(const ember_grad* g, int64_t n, int64_t k, Batch<T>& b) {
-    constexpr bool kFlat = sizeof(T) == sizeof(FlatTensor);
-    b.n = 0;
-    b.runs = 0;
+// The tensors from g[i] on that one launch describes, empty ones aside; returns the next one's index.
+int64_t batch_of(const ember_grad* g, int64_t n, int64_t i, Batch& b) {
+    b.flats = b.others = 0;
+    b.flat_runs = b.runs = 0;
     b.always = false;
-    int64_t seen = 0;
-    for (int64_t i = 0; i < n && b.n < kPerLaunch<T>; ++i) {
-        if (empty(g[i]) || is_flat(g[i]) != kFlat) continue;
-        if (seen++ < k * kPerLaunch<T>) continue;
+    for (; i < n; ++i) {
+        if (empty(g[i])) continue;
+        const bool flat = is_flat(g[i]);
+        const size_t used = b.flats * sizeof(FlatTensor) + b.others * sizeof(RowsTensor);
+        if (used + (flat ? sizeof(FlatTensor) : sizeof(RowsTensor)) > (size_t)kSpace) break;
         b.always = b.always || g[i].src != g[i].dst || g[i].rows_dev != nullptr;
-        b.runs += fill(b.t[b.n++], g[i], b.runs);
+        if (flat) b.flat_runs += fill(const_cast<FlatTensor&>(b.flat(b.flats++)), g[i], b.flat_runs);
+        else b.runs += fill(const_cast<RowsTensor&>(b.other(b.others++)), g[i], b.runs);
     }
+    for (int k = 0; k < b.others; ++k) const_cast<RowsTensor&>(b.other(k)).run0 += b.flat_runs;
+    b.runs += b.flat_runs;
+    return i;
 }
 
-struct ClipCall {
-    const ember_grad* g;
-    int64_t n;
-    float max_norm;
-    float* out;
-    double* sums;
-    int most;        // blocks a launch
-    hipStream_t s;
-};
-template <typename T>
-int blocks_of(const Batch<T>& b, const ClipCall& c) {
-    return (int)std::max<int64_t>(1, std::min<int64_t>((b.runs + kWaves - 1) / kWaves, c.most));
-}
-
-// The first pass over the launches of one kind; total: sums so far.
-template <typename T>
-hipError_t squares(const ClipCall& c, int64_t launches, int& total) {
-    Batch<T> b;
-    for (int64_t k = 0; k < launches; ++k) {
-        batch_of(c.g, c.n, k, b);
-        const int nb = blocks_of(b, c);
-        ember_grad_squares<T><<<dim3((unsigned)nb), kBlock, 0, c.s>>>(b, c.sums + total);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-        total += nb;
-    }
-    return hipSuccess;
-}
-
-// The second pass, last launch first; the norm and the factor are written by
-// the first one made.
-template <typename T>
-hipError_t scales(const ClipCall& c, int64_t launches, int total, float*& out) {
-    Batch<T> b;
-    for (int64_t k = launches - 1; k >= 0; --k) {
-        batch_of(c.g, c.n, k, b);
-        const bool work = b.always || !std::isinf(c.max_norm);
-        if (!work && out == nullptr) continue;
-        const int nb = work ? blocks_of(b, c) : 1;
-        ember_grad_scale<T><<<dim3((unsigned)nb), kBlock, 0, c.s>>>(b, c.sums, total, c.max_norm, out);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-        out = nullptr;
-    }
-    return hipSuccess;
+int blocks_of(const Batch& b, int most) {
+    return (int)std::max<int64_t>(1, std::min<int64_t>((b.runs + kWaves - 1) / kWaves, most));
 }
 
 } // namespace
 
 size_t clip_ws_bytes(int64_t n) {
-    // the most sums that n tensors can have: launches of either kind, each at
-    // its most blocks
-    const int64_t launches = (n + kRowsPerLaunch - 1) / kRowsPerLaunch + 1;
+    // the most sums that n tensors can have
+    const int64_t launches = std::max<int64_t>(1, (n + kLeastPerLaunch - 1) / kLeastPerLaunch);
     const int64_t sums = std::max<int64_t>(launches * kMinClipBlocks, std::min<int64_t>(launches * kMaxClipBlocks,
                                                                                       kMaxSums));
     return ((size_t)sums * sizeof(double) + 255) / 256 * 256;
 }
 
 hipError_t launch_clip(const ember_grad* g, int64_t n, float max_norm, float* out, char* ws, hipStream_t s) {
-    int64_t flats = 0, others = 0;
-    for (int64_t i = 0; i < n; ++i)
-        if (!empty(g[i])) ++(is_flat(g[i]) ? flats : others);
-    int64_t lf = (flats + kFlatPerLaunch - 1) / kFlatPerLaunch;
-    const int64_t lr = (others + kRowsPerLaunch - 1) / kRowsPerLaunch;
-    if (lf + lr == 0) lf = 1;   // no element at all: an empty launch writes the norm
-    ClipCall c{g, n, max_norm, out, reinterpret_cast<double*>(ws), 0, s};
-    c.most = (int)std::max<int64_t>(kMinClipBlocks, std::min<int64_t>(kMaxClipBlocks, kMaxSums / (lf + lr)));
+    Batch b;
+    int32_t first[kMaxLaunches];   // tensor of each launch
+    int launches = 0;
+    for (int64_t i = 0; i < n || launches == 0;) {   // no tensor that is not empty: one launch that writes the norm
+        first[launches++] = (int32_t)i;
+        i = batch_of(g, n, i, b);
+    }
+    const int most = std::max(kMinClipBlocks, std::min(kMaxClipBlocks, kMaxSums / launches));
+    double* const sums = reinterpret_cast<double*>(ws);
     int total = 0;
-    hipError_t e = squares<RowsTensor>(c, lr, total);
-    if (e == hipSuccess) e = squares<FlatTensor>(c, lf, total);
-    if (e == hipSuccess) e = scales<FlatTensor>(c, lf, total, out);
-    if (e == hipSuccess) e = scales<RowsTensor>(c, lr, total, out);
-    return e;
+    for (int k = 0; k < launches; ++k) {
+        if (launches > 1) batch_of(g, n, first[k], b);
+        const int blocks = blocks_of(b, most);
+        ember_grad_squares<<<dim3((unsigned)blocks), kBlock, 0, s>>>(b, sums + total);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        total += blocks;
+    }
+    // the second pass, last launch first; the first one made writes the norm and the factor
+    for (int k = launches - 1; k >= 0; --k) {
+        if (k < launches - 1) batch_of(g, n, first[k], b);
+        const bool work = b.always || !std::isinf(max_norm);
+        if (!work && out == nullptr) continue;
+        ember_grad_scale<<<dim3((unsigned)(work ? blocks_of(b, most) : 1)), kBlock, 0, s>>>(b, sums, total, max_norm, out);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        out = nullptr;
+    }
+    return hipSuccess;
 }
 
 } // namespace ember

@@ -107,6 +107,44 @@ def test_tables_with_strides_and_counts(em, dtype):
         check(em, [head, wide, tall, rows, more], 5.0, out=out, counts=[None, None, None, cnt(a), cnt(b)])
 
 
+@pytest.mark.parametrize("src,dst", [(F, F), (F, BF), (BF, F), (BF, BF)])
+@pytest.mark.parametrize("rows,cols,pad", [(2, 8, 8), (700, 8, 8), (3, 4, 12), (1500, 108, 4), (1500, 107, 5), (900, 5, 11),
+                                           (333, 129, 7), (200, 1000, 24), (150, 1023, 1), (90, 1030, 10), (64, 2047, 17),
+                                           (40, 2056, 8), (700, 3, 1), (500, 127, 2), (500, 128, 3), (500, 130, 1), (4000, 1, 2)])
+def test_narrow_rows(em, rows, cols, pad, src, dst):
+    """Rows at a stride that share runs or nearly do; what lies between them is neither read nor written."""
+    print(f"clip narrow {rows} x {cols} + {pad} {src} {dst}", flush=True)
+    for off in (0, 1):
+        buf = randn(rows * (cols + pad) + 16, dtype=src)
+        g = buf[off:off + rows * (cols + pad)].view(rows, cols + pad)[:, :cols]
+        held = g.clone()
+        buf.fill_(float("nan"))
+        g.copy_(held)
+        to = torch.full((rows, cols + pad + off), 9.0, dtype=dst, device=DEV)
+        for count in (None, 0, 1, rows // 2, rows - 1, rows):
+            c = None if count is None else torch.tensor([count], device=DEV)
+            for limit in (1e9, 0.5):
+                to.fill_(9.0)
+                check(em, [g], limit, out=[to[:, :cols]], counts=[c])
+                assert (to[:, cols:] == 9).all()
+        if src == dst:
+            for count in (rows, rows // 2):
+                check(em, [g], 0.5, counts=[torch.tensor([count], device=DEV)])
+                check(em, [g], 1e9, counts=[torch.tensor([count // 2], device=DEV)])
+            assert torch.isnan(buf[off:off + rows * (cols + pad)].view(rows, cols + pad)[:, cols:]).all()
+
+
+def test_tables_and_tensors_in_turn(em):
+    """Kinds that alternate, over several launches."""
+    grads = []
+    for i in range(160):
+        grads.append(randn(1 + 300 * i % 9001, dtype=BF if i % 3 else F, seed=i))
+        grads.append(randn(20 + i, 40, dtype=BF if i % 2 else F, seed=i)[:, :5 + i % 30])
+    for k in (2, 60, 61, 74, 75, 320):
+        check(em, grads[:k], 0.5)
+        check(em, grads[:k], 1e6, out=[torch.zeros(g.shape, dtype=BF, device=DEV) for g in grads[:k]])
+
+
 def test_rows_past_the_count_may_hold_anything(em):
     """They are not read, and become zeros, also where nothing else changes."""
     for limit in (1.0, 1e6, math.inf):
