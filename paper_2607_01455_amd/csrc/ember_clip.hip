@@ -27,8 +27,8 @@
 // more than 256 pieces have waves of their own.
 //
 // Tensors are described in the kernel's arguments (nothing is uploaded, and a
-// captured launch holds its own copy), contiguous ones in 24 bytes each, others in
-// 80, as many a launch as fit.
+// captured launch holds its own copy), contiguous ones in 12 bytes each, others in
+// 80, as many a launch as fit: 304 and 45.
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -49,12 +49,10 @@ constexpr int kMaxClipBlocks = 1024;  // blocks (and float64 sums) a launch at m
 constexpr int kMinClipBlocks = 64;    // and at least, where there is work for them
 constexpr int kMaxSums = 8192;        // sums of all launches, as far as kMinClipBlocks allows
 
-// A contiguous tensor of fewer than 2^30 elements.
+// A contiguous tensor of fewer than 2^29 elements.
 struct FlatTensor {
-    const void* src;
-    void* dst;
-    uint32_t n;       // elements; bit 31: src is bf16, bit 30: dst is
-    uint32_t run0;    // runs of this launch before this tensor's
+    int32_t src, dst;   // in 2 bytes, from the launch's bases
+    uint32_t n;         // elements; bit 31: src is bf16, bit 30: dst is
 };
 // Any other: rows at a stride, a device row count, or more elements.
 struct RowsTensor {
@@ -80,20 +78,26 @@ constexpr int kMaxPieces = 256;       // of a row that shares runs: below 256 + 
 template <typename T> constexpr int kRun = kRunBytes / (int)sizeof(T);   // elements of a whole run of T
 
 // The tensors of a launch: contiguous ones from the front of the space, others from its back.
-constexpr int kSpace = 3808;
+constexpr int kSpace = 3648;
+constexpr int kGroup = 8;              // contiguous tensors whose first run is found by adding up
+constexpr int kGroups = kSpace / (kGroup * (int)sizeof(FlatTensor));
 constexpr int kLeastPerLaunch = kSpace / (int)sizeof(RowsTensor);
 constexpr int kMaxLaunches = (EMBER_MAX_GRADS + kLeastPerLaunch - 1) / kLeastPerLaunch;
 struct Batch {
     alignas(8) char space[kSpace];
-    int64_t flat_runs, runs;   // of the contiguous tensors, and in all
+    uint32_t group_run0[kGroups];      // runs before each group
+    const char* src;                   // bases of the contiguous ones
+    char* dst;
+    int64_t flat_runs, runs;           // of the contiguous tensors, and in all
     int16_t flats, others;
-    bool always;               // the second pass has work at f = 1 too
+    bool always;                       // the second pass has work at f = 1 too
     __host__ __device__ const FlatTensor& flat(int i) const { return reinterpret_cast<const FlatTensor*>(space)[i]; }
     __host__ __device__ const RowsTensor& other(int i) const {
         return reinterpret_cast<const RowsTensor*>(space + kSpace)[-1 - i];
     }
 };
-static_assert(sizeof(Batch) <= 3840 && kSpace % 16 == 0 && sizeof(RowsTensor) == 80, "kernel arguments");
+static_assert(sizeof(Batch) <= 3840 && kSpace % 16 == 0 && kSpace % (kGroup * sizeof(FlatTensor)) == 0 &&
+                  sizeof(RowsTensor) == 80, "kernel arguments");
 
 template <typename T>
 __device__ __forceinline__ void add_squares(const u32x4_t& w, double (&s)[2]) {
@@ -169,15 +173,15 @@ __device__ __forceinline__ bool stores_vectors(const U* out) {
 }
 
 template <typename T, typename U>
-__device__ __forceinline__ void scale_run(const T* p, U* out, int n, int lane, float f) {
-    if (whole<T>(p, n)) {
-        u32x4_t w[kLoads];
-        load_whole<true>(p, lane, w);
-        const bool vec = stores_vectors<T>(out);
+__device__ __forceinline__ void scale_whole(const u32x4_t (&w)[kLoads], U* out, int lane, float f) {
+    const bool vec = stores_vectors<T>(out);
 #pragma unroll
-        for (int u = 0; u < kLoads; ++u) scale_chunk<T>(w[u], out + (lane + u * kWave) * kChunkElems<T>, vec, f);
-        return;
-    }
+    for (int u = 0; u < kLoads; ++u) scale_chunk<T>(w[u], out + (lane + u * kWave) * kChunkElems<T>, vec, f);
+}
+
+// Any other run.
+template <typename T, typename U>
+__device__ __forceinline__ void scale_run(const T* p, U* out, int n, int lane, float f) {
     const Parts x = parts_of(p, n);
     const u32x4_t* q = reinterpret_cast<const u32x4_t*>(p + x.head);
     const bool vec = stores_vectors<T>(out + x.head);
@@ -330,9 +334,9 @@ struct Run {
     bool src_bf16, dst_bf16, absent, in_place;
 };
 
-// The one of n tensors that has run r: its runs begin at or before r, the next one's after it.
+// The last of n whose first run, run0(i), is not behind run r.
 template <typename F>
-__device__ __forceinline__ int tensor_of(int n, int64_t r, F run0) {
+__device__ __forceinline__ int last_before(int n, int64_t r, F run0) {
     int lo = 0, hi = n;   // in [lo, hi)
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
@@ -356,16 +360,35 @@ __device__ __forceinline__ Piece piece_of(const void* p, bool bf16, int64_t n, i
     return Piece{begin, (int)(end - begin)};
 }
 
-__device__ __forceinline__ Run run_of(const FlatTensor& t, int64_t r) {
+// Runs of n < 2^29 contiguous elements at p.
+__host__ __device__ __forceinline__ uint32_t flat_runs_of(const void* p, uint32_t n, bool bf16) {
+    return ((n << (bf16 ? 1 : 2)) + (uint32_t)(reinterpret_cast<uintptr_t>(p) & 15) + kRunBytes - 1) / kRunBytes;
+}
+__device__ __forceinline__ Run flat_run_of(const Batch& b, int64_t r) {
+    const int group = last_before((b.flats + kGroup - 1) / kGroup, r, [&](int i) { return b.group_run0[i]; });
+    uint32_t k = (uint32_t)r - b.group_run0[group];
+    int i = 0;
+#pragma unroll
+    for (int j = 0; j < kGroup - 1; ++j) {   // the tensor with run r is not behind the last one
+        const FlatTensor& t = b.flat(group * kGroup + j);
+        const uint32_t runs = flat_runs_of(b.src + (int64_t)t.src * 2, t.n & 0x1FFFFFFFu, t.n >> 31);
+        if (i == j && k >= runs) {
+            k -= runs;
+            ++i;
+        }
+    }
+    const FlatTensor& t = b.flat(group * kGroup + i);
+    const char* const src = b.src + (int64_t)t.src * 2;
+    char* const dst = b.dst + (int64_t)t.dst * 2;
     Run x;
     x.src_bf16 = t.n >> 31;
     x.dst_bf16 = (t.n >> 30) & 1;
-    const Piece q = piece_of(t.src, x.src_bf16, t.n & 0x3FFFFFFFu, r - t.run0);
-    x.src = static_cast<const char*>(t.src) + q.at * (x.src_bf16 ? 2 : 4);
-    x.dst = static_cast<char*>(t.dst) + q.at * (x.dst_bf16 ? 2 : 4);
+    const Piece q = piece_of(src, x.src_bf16, t.n & 0x1FFFFFFFu, k);
+    x.src = src + q.at * (x.src_bf16 ? 2 : 4);
+    x.dst = dst + q.at * (x.dst_bf16 ? 2 : 4);
     x.n = q.n;
+    x.in_place = src == dst;
     x.absent = false;
-    x.in_place = t.src == t.dst;
     x.shared = -1;
     return x;
 }
@@ -389,8 +412,8 @@ __device__ __forceinline__ Run run_of(const RowsTensor& t, int i, int64_t r) {
 }
 
 __device__ __forceinline__ Run run_of(const Batch& b, int64_t r) {
-    if (r < b.flat_runs) return run_of(b.flat(tensor_of(b.flats, r, [&](int i) { return b.flat(i).run0; })), r);
-    const int i = tensor_of(b.others, r, [&](int j) { return b.other(j).run0; });
+    if (r < b.flat_runs) return flat_run_of(b, r);
+    const int i = last_before(b.others, r, [&](int j) { return b.other(j).run0; });
     return run_of(b.other(i), i, r);
 }
 
@@ -469,10 +492,36 @@ __global__ __launch_bounds__(kBlock) void ember_grad_scale(Batch b, const double
     }
     if (f == 1.0f && !b.always) return;
     const int lane = threadIdx.x & (kWave - 1);
-    for (int64_t r = first_run(); r < b.runs; r += run_step()) {
-        const int64_t back = b.runs - 1 - r;
-        const Run x = run_of(b, back);
-        if (x.shared >= 0) {
+    int64_t r = first_run();
+    Run next{};
+    if (r < b.runs) next = run_of(b, b.runs - 1 - r);
+    while (r < b.runs) {
+        const Run x = next;
+        const bool work = x.shared < 0 && !x.absent && !(x.in_place && f == 1.0f);   // else it is what it would be
+        const bool all = work && (x.src_bf16 ? whole<uint16_t>(x.src, x.n) : whole<float>(x.src, x.n));
+        u32x4_t w[kLoads];
+        if (all) load_whole<true>(x.src, lane, w);
+        r += run_step();
+        if (r < b.runs) next = run_of(b, b.runs - 1 - r);
+        if (all) {
+            if (x.src_bf16) {
+                if (x.dst_bf16) scale_whole<uint16_t>(w, reinterpret_cast<uint16_t*>(x.dst), lane, f);
+                else scale_whole<uint16_t>(w, reinterpret_cast<float*>(x.dst), lane, f);
+            } else {
+                if (x.dst_bf16) scale_whole<float>(w, reinterpret_cast<uint16_t*>(x.dst), lane, f);
+                else scale_whole<float>(w, reinterpret_cast<float*>(x.dst), lane, f);
+            }
+        } else if (work) {
+            if (x.src_bf16) {
+                const uint16_t* p = reinterpret_cast<const uint16_t*>(x.src);
+                if (x.dst_bf16) scale_run(p, reinterpret_cast<uint16_t*>(x.dst), x.n, lane, f);
+                else scale_run(p, reinterpret_cast<float*>(x.dst), x.n, lane, f);
+            } else {
+                const float* p = reinterpret_cast<const float*>(x.src);
+                if (x.dst_bf16) scale_run(p, reinterpret_cast<uint16_t*>(x.dst), x.n, lane, f);
+                else scale_run(p, reinterpret_cast<float*>(x.dst), x.n, lane, f);
+            }
+        } else if (x.shared >= 0) {
             const RowsTensor& t = b.other(x.shared);
             if (x.src_bf16) {
                 if (x.dst_bf16) scale_shared<uint16_t, uint16_t>(t, x.k, lane, f);
@@ -481,25 +530,12 @@ __global__ __launch_bounds__(kBlock) void ember_grad_scale(Batch b, const double
                 if (x.dst_bf16) scale_shared<float, uint16_t>(t, x.k, lane, f);
                 else scale_shared<float, float>(t, x.k, lane, f);
             }
-            continue;
-        }
-        if (x.absent) {
+        } else if (x.absent) {
             if (x.dst_bf16) {
                 for (int i = lane; i < x.n; i += kWave) reinterpret_cast<uint16_t*>(x.dst)[i] = 0;
             } else {
                 for (int i = lane; i < x.n; i += kWave) reinterpret_cast<float*>(x.dst)[i] = 0.0f;
             }
-            continue;
-        }
-        if (x.in_place && f == 1.0f) continue;   // it is what it would be
-        if (x.src_bf16) {
-            const uint16_t* p = reinterpret_cast<const uint16_t*>(x.src);
-            if (x.dst_bf16) scale_run(p, reinterpret_cast<uint16_t*>(x.dst), x.n, lane, f);
-            else scale_run(p, reinterpret_cast<float*>(x.dst), x.n, lane, f);
-        } else {
-            const float* p = reinterpret_cast<const float*>(x.src);
-            if (x.dst_bf16) scale_run(p, reinterpret_cast<uint16_t*>(x.dst), x.n, lane, f);
-            else scale_run(p, reinterpret_cast<float*>(x.dst), x.n, lane, f);
         }
     }
 }
@@ -508,7 +544,7 @@ bool empty(const ember_grad& x) { return x.rows == 0 || x.cols == 0; }
 bool contiguous(const ember_grad& x) {
     return x.rows_dev == nullptr && (x.rows == 1 || (x.lds == x.cols && x.ldd == x.cols));
 }
-bool is_flat(const ember_grad& x) { return contiguous(x) && x.rows * x.cols < ((int64_t)1 << 30); }
+bool is_flat(const ember_grad& x) { return contiguous(x) && x.rows * x.cols < ((int64_t)1 << 29); }
 
 // Runs of n elements that begin `at` bytes behind a 16-byte boundary (2^40 elements
 // at most: below 2^29).
@@ -517,14 +553,6 @@ int64_t runs_of(const ember_grad& x, int64_t n, int64_t at) {
     return (n * es + at + kRunBytes - 1) / kRunBytes;
 }
 
-int64_t fill(FlatTensor& t, const ember_grad& x, int64_t run0) {
-    const int64_t n = x.rows * x.cols;
-    t.src = x.src;
-    t.dst = x.dst;
-    t.n = (uint32_t)n | (x.src_dtype == EMBER_BF16 ? 1u << 31 : 0) | (x.dst_dtype == EMBER_BF16 ? 1u << 30 : 0);
-    t.run0 = (uint32_t)run0;   // below 158 * 2^19
-    return runs_of(x, n, reinterpret_cast<uintptr_t>(x.src) & 15);
-}
 int64_t fill(RowsTensor& t, const ember_grad& x, int64_t run0) {
     const bool one = contiguous(x);
     t.src = x.src;
@@ -561,13 +589,32 @@ int64_t batch_of(const ember_grad* g, int64_t n, int64_t i, Batch& b) {
     b.flat_runs = b.runs = 0;
     b.always = false;
     for (; i < n; ++i) {
-        if (empty(g[i])) continue;
-        const bool flat = is_flat(g[i]);
+        const ember_grad& x = g[i];
+        if (empty(x)) continue;
+        bool flat = is_flat(x);
+        int64_t src = 0, dst = 0;
+        if (flat) {
+            if (b.flats == 0) {
+                b.src = static_cast<const char*>(x.src);
+                b.dst = static_cast<char*>(x.dst);
+            }
+            src = ((int64_t)reinterpret_cast<uintptr_t>(x.src) - (int64_t)reinterpret_cast<uintptr_t>(b.src)) / 2;
+            dst = ((int64_t)reinterpret_cast<uintptr_t>(x.dst) - (int64_t)reinterpret_cast<uintptr_t>(b.dst)) / 2;
+            flat = src == (int32_t)src && dst == (int32_t)dst;   // else too far from the first: described in full
+        }
         const size_t used = b.flats * sizeof(FlatTensor) + b.others * sizeof(RowsTensor);
         if (used + (flat ? sizeof(FlatTensor) : sizeof(RowsTensor)) > (size_t)kSpace) break;
-        b.always = b.always || g[i].src != g[i].dst || g[i].rows_dev != nullptr;
-        if (flat) b.flat_runs += fill(const_cast<FlatTensor&>(b.flat(b.flats++)), g[i], b.flat_runs);
-        else b.runs += fill(const_cast<RowsTensor&>(b.other(b.others++)), g[i], b.runs);
+        b.always = b.always || x.src != x.dst || x.rows_dev != nullptr;
+        if (flat) {
+            const uint32_t count = (uint32_t)(x.rows * x.cols);
+            const bool bf16 = x.src_dtype == EMBER_BF16;
+            if (b.flats % kGroup == 0) b.group_run0[b.flats / kGroup] = (uint32_t)b.flat_runs;   // below 304 * 2^18
+            const_cast<FlatTensor&>(b.flat(b.flats++)) = FlatTensor{
+                (int32_t)src, (int32_t)dst, count | (bf16 ? 1u << 31 : 0) | (x.dst_dtype == EMBER_BF16 ? 1u << 30 : 0)};
+            b.flat_runs += flat_runs_of(x.src, count, bf16);
+        } else {
+            b.runs += fill(const_cast<RowsTensor&>(b.other(b.others++)), x, b.runs);
+        }
     }
     for (int k = 0; k < b.others; ++k) const_cast<RowsTensor&>(b.other(k)).run0 += b.flat_runs;
     b.runs += b.flat_runs;

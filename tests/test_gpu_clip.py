@@ -78,7 +78,7 @@ def test_views_of_a_bucket_into_another(em, src, dst):
     check(em, list(torch.split(a[1:1 + sum(sizes)], sizes)), 3.0)
 
 
-@pytest.mark.parametrize("count", [1, 47, 48, 49, 97, 151, 152, 153, 300, 700])
+@pytest.mark.parametrize("count", [1, 7, 8, 9, 47, 48, 49, 97, 151, 152, 153, 300, 303, 304, 305, 700])
 def test_many_tensors(em, count):
     print(f"clip {count} tensors", flush=True)
     grads = [randn(1 + 37 * i % 5000, dtype=BF if i % 3 else F, seed=i) for i in range(count)]
@@ -143,6 +143,20 @@ def test_tables_and_tensors_in_turn(em):
     for k in (2, 60, 61, 74, 75, 320):
         check(em, grads[:k], 0.5)
         check(em, grads[:k], 1e6, out=[torch.zeros(g.shape, dtype=BF, device=DEV) for g in grads[:k]])
+
+
+def test_tensors_far_apart(em):
+    """Contiguous gradients gigabytes from each other, forwards and backwards."""
+    print("clip far apart", flush=True)
+    buf = torch.zeros(6 << 30, dtype=BF, device=DEV)
+    at = [0, 5000, (1 << 31) + 11, (1 << 32) - 77, (5 << 30) + 3, (6 << 30) - 9000]
+    for order in (at, at[::-1], at[2:] + at[:2]):
+        grads = [buf[a:a + 3001] for a in order]
+        for i, g in enumerate(grads):
+            g.copy_(randn(3001, dtype=BF, seed=i))
+        check(em, grads, 0.5)
+        check(em, grads, 1e6, out=[torch.zeros(3001, device=DEV) for _ in grads])
+        check(em, [randn(500 + i) for i in range(6)], 0.5, out=[buf[a:a + 500 + i] for i, a in enumerate(order)])
 
 
 def test_rows_past_the_count_may_hold_anything(em):
