@@ -416,7 +416,12 @@ hipError_t launch_fwd(const FwdParams& p, const RowPlan& pl, hipStream_t s) {
 // instead of 102 at 16384 x 4096 bf16, 40 instead of 33 at 2048 x 8192).
 constexpr int kGradBlocks = 256;
 int grad_groups(const RowPlan& pl) { return 1024 / pl.tpr; }
+// A block alone has the sums of dgain, and there is no second launch: as long as
+// that makes up for its rounds (us, alone / with the second launch: 4 rounds, 4 x
+// 8192 bf16 10.2 / 11.0, 16 x 2048 8.3 / 11.0; 8 rounds, 8 x 8192 15.3 / 10.9).
+constexpr int kAloneRounds = 4;
 int grad_blocks(int64_t T, const RowPlan& pl) {
+    if (T <= kAloneRounds * grad_groups(pl)) return T > 0;
     return (int)std::min<int64_t>((T + grad_groups(pl) - 1) / grad_groups(pl), kGradBlocks);
 }
 
@@ -467,11 +472,12 @@ hipError_t launch_rmsnorm_grad(const NormGradArgs& x, hipStream_t s) {
                  x.dX, x.lddx, reinterpret_cast<float*>(x.ws), bytes_of(x.T, x.D, x.x_dtype) <= kStreamBytes};
     const RowPlan pl = row_plan((int)x.D, x.x_dtype, true);
     const int blocks = grad_blocks(x.T, pl);
+    if (blocks == 1) p.part = x.dgain;   // a single block's sums are the result
     if (blocks > 0) {
         hipError_t e;
         if (x.x_dtype == EMBER_F32) e = pl.full ? launch_bwd<float, true>(p, pl, blocks, s) : launch_bwd<float, false>(p, pl, blocks, s);
         else e = pl.full ? launch_bwd<uint16_t, true>(p, pl, blocks, s) : launch_bwd<uint16_t, false>(p, pl, blocks, s);
-        if (e != hipSuccess) return e;
+        if (e != hipSuccess || blocks == 1) return e;
     }
     ember_rmsnorm_dgain<<<dim3((unsigned)((x.D + kSumCols - 1) / kSumCols)), kSumThreads, 0, s>>>(p.part, blocks,
                                                                                                  (int)x.D, x.dgain);

@@ -369,8 +369,12 @@ def _matrix(what, t, shape, dtype=None):
     """(address, row stride) of a 2-D tensor of this shape and type; None: no tensor."""
     if t is None:
         return None, 0
-    if t.shape != shape or (dtype is not None and t.dtype != dtype):
+    if t.shape != shape or (dtype is not None and t.dtype is not dtype):
         _misfit(what, t, shape, dtype)
+    if len(shape) == 2:
+        ld, unit = t.stride()
+        if unit == 1 and shape[0] > 1:
+            return t.data_ptr(), ld
     return t.data_ptr(), _ld(t)
 
 
@@ -378,7 +382,7 @@ def _vector(what, t, shape, dtype=torch.float32):
     """Address of a contiguous 1-D tensor of this shape and type; None: no tensor."""
     if t is None:
         return None
-    if t.shape != shape or (dtype is not None and t.dtype != dtype) or not t.is_contiguous():
+    if t.shape != shape or (dtype is not None and t.dtype is not dtype) or not t.is_contiguous():
         _misfit(what, t, shape, dtype)
     return t.data_ptr()
 

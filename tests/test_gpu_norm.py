@@ -220,7 +220,10 @@ def grad64(dY, S, gain, rstd, dS):
     return dx, A, terms.sum(dim=0), terms.abs().sum(dim=0)
 
 
-@pytest.mark.parametrize("T,D", SHAPES + [(300, 896), (1500, 72), (2500, 1000), (1100, 4096)])
+@pytest.mark.parametrize("T,D", SHAPES + [(300, 896), (1500, 72), (2500, 1000), (1100, 4096),
+                                          # one block alone, and the first count with two launches
+                                          (64, 512), (65, 512), (16, 2048), (17, 2048), (8, 4096), (9, 4096), (4, 8192),
+                                          (5, 8192), (4, 32768), (5, 32768)])
 @pytest.mark.parametrize("dtype,gdtype,other", [(BF, F, True), (F, BF, False)])
 def test_gradient(em, T, D, dtype, gdtype, other):
     print(f"rmsnorm grad T={T} D={D} {dtype} gain {gdtype} dS={other}", flush=True)
