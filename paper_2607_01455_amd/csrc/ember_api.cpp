@@ -10,6 +10,7 @@
 #include <string>
 #include <vector>
 
+#include "ember_interface_launch.h"
 #include "ember_launch.h"
 
 namespace {

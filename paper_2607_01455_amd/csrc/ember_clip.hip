@@ -38,7 +38,7 @@
 #include <type_traits>
 
 #include "ember_device.h"
-#include "ember_launch.h"
+#include "ember_interface_launch.h"
 
 namespace ember {
 namespace {

@@ -18,7 +18,7 @@
 #include <algorithm>
 
 #include "ember_device.h"
-#include "ember_launch.h"
+#include "ember_interface_launch.h"
 
 namespace ember {
 namespace {

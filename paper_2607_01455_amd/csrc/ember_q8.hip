@@ -20,7 +20,7 @@
 #include <cmath>
 
 #include "ember_device.h"
-#include "ember_launch.h"
+#include "ember_interface_launch.h"
 
 namespace ember {
 namespace {
