@@ -29,6 +29,7 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int kXcds = 8;
+constexpr int kCus = 256;
 constexpr uint32_t kRotate = 5;            // steps between the first steps of neighbouring tiles
 constexpr int kBufferWord3 = 0x00020000;   // raw 32-bit data format, gfx9 family
 constexpr int kBufferMax = 0x7FFFFFF0;     // bytes of a buffer at most; an offset past every buffer
@@ -41,6 +42,7 @@ struct Params {
     int64_t tile0;       // this launch's tiles: [tile0, tile1) of the MT * NT
     int64_t tile1;
     int64_t per_xcd;     // tiles per XCD
+    int64_t blocks;      // blocks per XCD: each takes every blocks-th of its tiles
     int group_m;         // token tiles a group of the tile order
 };
 
@@ -132,6 +134,17 @@ struct Epilogue {
     static constexpr int kBytes = kStrips + 2 * C::BN * 4;
 };
 
+// Where a compute unit holds one block, the block goes through several tiles, and the
+// next one's first stage is loaded while an epilogue works behind it (us, a tile a
+// block / like this, 256 x 256 tiles: 4096 x 128256 x 4096 2115 / 2001, 955 x 33990 x
+// 3381 fp32 165 / 161, 1500 x 50000 x 1024 106 / 103).
+template <typename C>
+constexpr bool kGoesOn = C::kLds > 80 * 1024;
+template <typename C, typename YT>
+constexpr int epilogue_at() { return kGoesOn<C> ? C::kStageBytes : 0; }
+template <typename C, typename YT>
+constexpr int lds_of() { return std::max(C::kLds, epilogue_at<C, YT>() + Epilogue<C, YT>::kBytes); }
+
 // Chunk c of a slice's row r sits at position c ^ swizzle(r): the reads of the
 // same chunk of 8 (or 16) consecutive rows then cover 32 (or all 64) LDS banks
 // once, and a wave-wide load still fills whole rows.
@@ -144,7 +157,7 @@ __device__ __forceinline__ int swizzle(int r) {
 // that do not count; they are cleared in the tokens' operand.
 template <typename C, typename YT, bool kMask>
 __global__ __launch_bounds__(C::kThreads) void ember_logits_q8(Params p) {
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[std::max(C::kLds, Epilogue<C, YT>::kBytes)];
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[lds_of<C, YT>()];
     const LogitsArgs& a = p.a;
     const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
     const int lane = threadIdx.x & (kWave - 1);
@@ -152,52 +165,57 @@ __global__ __launch_bounds__(C::kThreads) void ember_logits_q8(Params p) {
     const int wm = wave % C::WM, wn = wave / C::WM;
 
     // blocks of one XCD take consecutive tiles
-    const int64_t l = p.tile0 + (int64_t)(blockIdx.x % kXcds) * p.per_xcd + blockIdx.x / kXcds;
-    if (l >= p.tile1 || (int64_t)(blockIdx.x / kXcds) >= p.per_xcd) return;
-    int tm;
-    int64_t tn;
-    tile_of(p, l, tm, tn);
-    const int64_t t0 = (int64_t)tm * C::BM, v0 = tn * C::BN;
+    const int64_t first = p.tile0 + (int64_t)(blockIdx.x % kXcds) * p.per_xcd;
+    const int64_t end = min(first + p.per_xcd, p.tile1);
+    int64_t l = first + blockIdx.x / kXcds;
+    if (l >= end) return;
     const int nk = p.nk, D = (int)a.D;
-
-    // load j of this wave fills rows [kRowsPerLoad q, ..) of the tokens' slice, then
-    // of the channels', q = wave + kWavesB j
-    int off[C::kLoads];
-    const int chunk_pos = lane % C::kChunks, load_row = lane / C::kChunks;
-    int load_k[C::kLoads];
-#pragma unroll
-    for (int j = 0; j < C::kLoads; ++j) {
-        const int q = wave + C::kWavesB * j;
-        const bool is_b = q >= C::kLoadsA;
-        const int row = (is_b ? q - C::kLoadsA : q) * C::kRowsPerLoad + load_row;
-        const int chunk = chunk_pos ^ swizzle<C::kChunks>(row);
-        load_k[j] = chunk * 16;
-        off[j] = row * (int)(is_b ? a.ldw : a.ldx) + chunk * 16;
-    }
-    struct StepLoads {
-        i32x4 ra, rb;
-        int left;      // columns from the step's first to D
+    struct At {
+        int64_t t0, v0;
+        int rot;
     };
     // Blocks with other channels begin at other steps (the sum has no order): in
     // step, all of them would read the same columns of rows that lie a power of
     // two apart, and so a few of the memory's channels at a time (64 tokens x
     // 128256 x 4096: 127 us in step, 105 like this; one token: 110 and 91).
-    const int rot = (int)((uint64_t)tn * kRotate % (uint32_t)nk);
+    auto tile_at = [&](int64_t i) {
+        int tm;
+        int64_t tn;
+        tile_of(p, i, tm, tn);
+        return At{(int64_t)tm * C::BM, tn * C::BN, (int)((uint64_t)tn * kRotate % (uint32_t)nk)};
+    };
+    At at = tile_at(l);
+
+    // load j of this wave fills rows [kRowsPerLoad q, ..) of the tokens' slice, q =
+    // wave + kWavesB j, then of the channels'; a lane's chunk is the same in all of them
+    static_assert(C::kWavesB % 2 == 0 && C::kLoadsA % C::kWavesB == 0, "one load_k for all loads, each of one operand");
+    const int load_row = wave * C::kRowsPerLoad + lane / C::kChunks;
+    const int load_k = ((lane % C::kChunks) ^ swizzle<C::kChunks>(load_row)) * 16;
+    const int load_a = load_row * (int)a.ldx + load_k, load_b = load_row * (int)a.ldw + load_k;
+    struct StepLoads {
+        i32x4 ra, rb;
+        int oa, ob;
+    };
     auto loads_of = [&](int kt) {
         const bool in = kt < nk;
-        const int ks = kt + rot < nk ? kt + rot : kt + rot - nk;
+        const int ks = kt + at.rot < nk ? kt + at.rot : kt + at.rot - nk;
         const int64_t k0 = in ? (int64_t)ks * C::KS : 0;
         StepLoads sl;
-        sl.ra = rsrc(a.Xq + t0 * a.ldx + k0, in ? (a.T - t0) * a.ldx - k0 : 0);
-        sl.rb = rsrc(a.Wq + v0 * a.ldw + k0, in ? (a.V - v0) * a.ldw - k0 : 0);
-        sl.left = D - (int)k0;
+        sl.ra = rsrc(a.Xq + at.t0 * a.ldx + k0, in ? (a.T - at.t0) * a.ldx - k0 : 0);
+        sl.rb = rsrc(a.Wq + at.v0 * a.ldw + k0, in ? (a.V - at.v0) * a.ldw - k0 : 0);
+        // Chunks past column D are zeros (no row's offset brings kBufferMax back).
+        // The offsets of a step's loads are formed anew in each, hidden from the
+        // compiler, which would keep all of them in registers.
+        const bool whole = load_k < D - (int)k0;
+        sl.oa = whole ? load_a : kBufferMax;
+        sl.ob = whole ? load_b : kBufferMax;
+        asm volatile("" : "+v"(sl.oa), "+v"(sl.ob));
         return sl;
     };
     auto issue_one = [&](const StepLoads& sl, uint32_t st, int j) {
-        const int q = wave + C::kWavesB * j;
-        // chunks past column D are zeros
-        const int o = load_k[j] < sl.left ? off[j] : kBufferMax;
-        load_to_lds(q >= C::kLoadsA ? sl.rb : sl.ra, st + q * (C::kRowsPerLoad * C::KS), o);
+        constexpr int kA = C::kLoadsA / C::kWavesB, kRows = C::kWavesB * C::kRowsPerLoad;
+        const int o = j < kA ? sl.oa + j * (kRows * (int)a.ldx) : sl.ob + (j - kA) * (kRows * (int)a.ldw);
+        load_to_lds(j < kA ? sl.ra : sl.rb, st + (wave + C::kWavesB * j) * (C::kRowsPerLoad * C::KS), o);
     };
 
     // operand reads: lane l takes row l % 32 of an MFMA tile, columns
@@ -218,152 +236,174 @@ __global__ __launch_bounds__(C::kThreads) void ember_logits_q8(Params p) {
         }
     };
 
-    i32x16 acc[C::MT][C::NT];
-#pragma unroll
-    for (int mt = 0; mt < C::MT; ++mt)
-#pragma unroll
-        for (int nt = 0; nt < C::NT; ++nt)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) acc[mt][nt][i] = 0;
-
-    // the scales the epilogue needs, ahead of the operands
-    float xs[C::MT];
-#pragma unroll
-    for (int m = 0; m < C::MT; ++m) {
-        const int64_t t = t0 + (wm * C::MT + m) * 32 + (lane & 31);
-        xs[m] = t < a.T ? a.xscale[t] : 0.0f;
-    }
-    const int64_t my_v = v0 + threadIdx.x;
-    const bool has_v = (int)threadIdx.x < C::BN && my_v < a.V;
-    const float my_wscale = has_v ? a.wscale[my_v] : 0.0f, my_bias = has_v && a.bias ? a.bias[my_v] : 0.0f;
-
-#pragma unroll
-    for (int q = 0; q < C::kStages; ++q) {
+    auto issue = [&](int q) {
         const StepLoads sl = loads_of(q);
 #pragma unroll
         for (int j = 0; j < C::kLoads; ++j) issue_one(sl, lds_base + q * C::kStageBytes, j);
-    }
-    wait_step<(C::kStages - 1) * C::kLoads>();
-    i32x4 af[2][C::MT], bf[2][C::NT];
+    };
+    issue(0);
+    for (bool fresh = true;; fresh = false) {
+        i32x16 acc[C::MT][C::NT];
 #pragma unroll
-    for (int m = 0; m < C::MT; ++m) af[0][m] = frag(lds_base, row_a + 32 * m, 0);
+        for (int mt = 0; mt < C::MT; ++mt)
 #pragma unroll
-    for (int n = 0; n < C::NT; ++n) bf[0][n] = frag(lds_base, row_b + 32 * n, 0);
+            for (int nt = 0; nt < C::NT; ++nt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[mt][nt][i] = 0;
 
-    // Step kt multiplies its stage in kSub sub-steps; while the MFMAs of one run,
-    // the operands of the next are read into the other register set.  The step
-    // barrier sits before the last sub-step, whose operands are in registers by
-    // then: past it no wave reads this stage any more, so the loads of step
-    // kt + kStages may fill it; and at most (kStages - 2) kLoads loads of each
-    // wave are outstanding, which are those of steps kt + 2 and later, so step
-    // kt + 1 lies in its stage.
-    uint32_t st = lds_base;
-    for (int kt = 0; kt < nk; ++kt) {
-        const uint32_t next = st + C::kStageBytes == lds_base + C::kLds ? lds_base : st + C::kStageBytes;
-        const StepLoads sl = loads_of(kt + C::kStages);
+        // the scales the epilogue needs, ahead of the operands
+        const int64_t t0 = at.t0, v0 = at.v0;
+        float xs[C::MT];
 #pragma unroll
-        for (int kk = 0; kk < C::kSub; ++kk) {
-            const int cur = kk & 1;
-            const bool last = kk == C::kSub - 1;
-            if constexpr (kMask) {
-                const int ks = kt + rot < nk ? kt + rot : kt + rot - nk;
-                if (ks == nk - 1) {
-#pragma unroll
-                    for (int m = 0; m < C::MT; ++m) mask_a(ks, kk, af[cur][m]);
-                }
-            }
-            if (last) wait_step<(C::kStages - 2) * C::kLoads>();
-            __builtin_amdgcn_sched_barrier(0);
-            constexpr int kSlots = C::MT * C::NT > C::MT + C::NT ? C::MT * C::NT : C::MT + C::NT;
-            constexpr int kAll = kSlots > C::kLoads ? kSlots : C::kLoads;
-#pragma unroll
-            for (int i = 0; i < kAll; ++i) {
-                if (i < C::MT * C::NT) {
-                    const int m = i / C::NT, n = i % C::NT;
-                    acc[m][n] = __builtin_amdgcn_mfma_i32_32x32x32_i8(bf[cur][n], af[cur][m], acc[m][n], 0, 0, 0);
-                }
-                // operands in the order the MFMAs first use them: A 0, all of B, the rest of A
-                if (i < C::MT + C::NT) {
-                    const bool is_b = i >= 1 && i <= C::NT;
-                    const int f = i == 0 ? 0 : is_b ? i - 1 : i - C::NT;
-                    const i32x4 x = frag(last ? next : st, (is_b ? row_b : row_a) + 32 * f, last ? 0 : kk + 1);
-                    if (is_b) bf[cur ^ 1][f] = x;
-                    else af[cur ^ 1][f] = x;
-                }
-                if (last && i < C::kLoads) issue_one(sl, st, i);
-                __builtin_amdgcn_sched_barrier(0);
-            }
+        for (int m = 0; m < C::MT; ++m) {
+            const int64_t t = t0 + (wm * C::MT + m) * 32 + (lane & 31);
+            xs[m] = t < a.T ? a.xscale[t] : 0.0f;
         }
-        st = next;
-    }
-    // the zero-filling loads past the end have landed and every wave is done with the stages
-    wait_step<0>();
+        const int64_t my_v = v0 + threadIdx.x;
+        const bool has_v = (int)threadIdx.x < C::BN && my_v < a.V;
+        const float my_wscale = has_v ? a.wscale[my_v] : 0.0f, my_bias = has_v && a.bias ? a.bias[my_v] : 0.0f;
 
-    // Epilogue: the channels are the rows of the MFMA tiles, so a lane holds four
-    // consecutive ones of a token.  Each wave takes its part in strips of 32 tokens
-    // x up to 256 bytes of channels: the values go to a wave-private LDS strip
-    // and are stored from it row by row, 16 bytes a lane.
-    using E = Epilogue<C, YT>;
-    constexpr int kEs = (int)sizeof(YT), kGroup = E::kGroup, kCols = E::kCols, kPitch = E::kPitch;
-    constexpr int kLanesPerRow = kCols * kEs / 16;
-    constexpr int kRowsPerPass = kWave / kLanesPerRow;
-    constexpr int kEpc = 16 / kEs;
-    static_assert(C::NT % kGroup == 0 && 32 % kRowsPerPass == 0 && C::kThreads >= C::BN, "whole strips");
-    uint8_t* const strip = lds + wave * (32 * kPitch);
-    float* const sw = reinterpret_cast<float*>(lds + E::kStrips);
-    float* const sb = sw + C::BN;
-    if ((int)threadIdx.x < C::BN) {
-        sw[threadIdx.x] = my_wscale;
-        sb[threadIdx.x] = my_bias;
-    }
-    __syncthreads();
-    const int half = lane >> 5, tok = lane & 31;
-    typedef float f32x4 __attribute__((ext_vector_type(4)));
 #pragma unroll
-    for (int m = 0; m < C::MT; ++m) {
-        const int64_t ts = t0 + (wm * C::MT + m) * 32;
+        for (int q = 1; q < C::kStages; ++q) issue(q);
+        l += p.blocks;
+        const bool more = kGoesOn<C> && l < end;
+        At then = at;
+        if (more) then = tile_at(l);
+        if (fresh) wait_step<(C::kStages - 1) * C::kLoads>();
+        i32x4 af[2][C::MT], bf[2][C::NT];
 #pragma unroll
-        for (int g = 0; g < C::NT / kGroup; ++g) {
-            const int c0 = wn * (C::NT * 32) + g * kCols;   // the strip's first channel in the tile
+        for (int m = 0; m < C::MT; ++m) af[0][m] = frag(lds_base, row_a + 32 * m, 0);
 #pragma unroll
-            for (int n = 0; n < kGroup; ++n) {
+        for (int n = 0; n < C::NT; ++n) bf[0][n] = frag(lds_base, row_b + 32 * n, 0);
+
+        // Step kt multiplies its stage in kSub sub-steps; while the MFMAs of one run,
+        // the operands of the next are read into the other register set.  The step
+        // barrier sits before the last sub-step, whose operands are in registers by
+        // then: past it no wave reads this stage any more, so the loads of step
+        // kt + kStages may fill it; and at most (kStages - 2) kLoads loads of each
+        // wave are outstanding, which are those of steps kt + 2 and later, so step
+        // kt + 1 lies in its stage.
+        uint32_t st = lds_base;
+        for (int kt = 0; kt < nk; ++kt) {
+            const uint32_t next = st + C::kStageBytes == lds_base + C::kLds ? lds_base : st + C::kStageBytes;
+            const StepLoads sl = loads_of(kt + C::kStages);
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int at = n * 32 + 8 * q + 4 * half;   // registers 4 q .. 4 q + 3
-                    const f32x4 w = *reinterpret_cast<const f32x4*>(sw + c0 + at);
-                    const f32x4 b = *reinterpret_cast<const f32x4*>(sb + c0 + at);
-                    float y[4];
+            for (int kk = 0; kk < C::kSub; ++kk) {
+                const int cur = kk & 1;
+                const bool last = kk == C::kSub - 1;
+                if constexpr (kMask) {
+                    const int ks = kt + at.rot < nk ? kt + at.rot : kt + at.rot - nk;
+                    if (ks == nk - 1) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) y[e] = (float)acc[m][g * kGroup + n][4 * q + e] * (xs[m] * w[e]) + b[e];
-                    store_values<YT, 4>(reinterpret_cast<YT*>(strip + tok * kPitch) + at, 0, 4, y);
+                        for (int m = 0; m < C::MT; ++m) mask_a(ks, kk, af[cur][m]);
+                    }
+                }
+                if (last) wait_step<(C::kStages - 2) * C::kLoads>();
+                __builtin_amdgcn_sched_barrier(0);
+                constexpr int kSlots = C::MT * C::NT > C::MT + C::NT ? C::MT * C::NT : C::MT + C::NT;
+                constexpr int kAll = kSlots > C::kLoads ? kSlots : C::kLoads;
+#pragma unroll
+                for (int i = 0; i < kAll; ++i) {
+                    if (i < C::MT * C::NT) {
+                        const int m = i / C::NT, n = i % C::NT;
+                        acc[m][n] = __builtin_amdgcn_mfma_i32_32x32x32_i8(bf[cur][n], af[cur][m], acc[m][n], 0, 0, 0);
+                    }
+                    // operands in the order the MFMAs first use them: A 0, all of B, the rest of A
+                    if (i < C::MT + C::NT) {
+                        const bool is_b = i >= 1 && i <= C::NT;
+                        const int f = i == 0 ? 0 : is_b ? i - 1 : i - C::NT;
+                        const i32x4 x = frag(last ? next : st, (is_b ? row_b : row_a) + 32 * f, last ? 0 : kk + 1);
+                        if (is_b) bf[cur ^ 1][f] = x;
+                        else af[cur ^ 1][f] = x;
+                    }
+                    if (last && i < C::kLoads) issue_one(sl, st, i);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
             }
-            wave_lds_order();
+            st = next;
+        }
+        // the zero-filling loads past the end have landed and every wave is done with the stages
+        wait_step<0>();
+        if (more) {
+            at = then;
+            issue(0);
+        }
+
+        // Epilogue: the channels are the rows of the MFMA tiles, so a lane holds four
+        // consecutive ones of a token.  Each wave takes its part in strips of 32 tokens
+        // x up to 256 bytes of channels: the values go to a wave-private LDS strip
+        // and are stored from it row by row, 16 bytes a lane.
+        using E = Epilogue<C, YT>;
+        constexpr int kEs = (int)sizeof(YT), kGroup = E::kGroup, kCols = E::kCols, kPitch = E::kPitch;
+        constexpr int kLanesPerRow = kCols * kEs / 16;
+        constexpr int kRowsPerPass = kWave / kLanesPerRow;
+        constexpr int kEpc = 16 / kEs;
+        static_assert(C::NT % kGroup == 0 && 32 % kRowsPerPass == 0 && C::kThreads >= C::BN, "whole strips");
+        uint8_t* const strip = lds + epilogue_at<C, YT>() + wave * (32 * kPitch);
+        float* const sw = reinterpret_cast<float*>(lds + epilogue_at<C, YT>() + E::kStrips);
+        float* const sb = sw + C::BN;
+        if ((int)threadIdx.x < C::BN) {
+            sw[threadIdx.x] = my_wscale;
+            sb[threadIdx.x] = my_bias;
+        }
+        wait_step<63>();
+        int el = lane;
+        asm volatile("" : "+v"(el));   // what follows from it is not kept in registers over the loop above
+        const int half = el >> 5, tok = el & 31;
+        typedef float f32x4 __attribute__((ext_vector_type(4)));
 #pragma unroll
-            for (int ps = 0; ps < 32 / kRowsPerPass; ++ps) {
-                const int r = ps * kRowsPerPass + lane / kLanesPerRow;
-                const int c = lane % kLanesPerRow;
-                const int64_t t = ts + r, v = v0 + c0 + c * kEpc;
-                const u32x4_t w = *reinterpret_cast<const u32x4_t*>(strip + r * kPitch + c * 16);
-                if (t < a.T) {
-                    YT* y = static_cast<YT*>(a.Y) + t * a.ldy + v;
-                    if (v + kEpc <= a.V) {
-                        *reinterpret_cast<u32x4_t*>(y) = w;
-                    } else {
+        for (int m = 0; m < C::MT; ++m) {
+            const int64_t ts = t0 + (wm * C::MT + m) * 32;
 #pragma unroll
-                        for (int e = 0; e < kEpc; ++e) {
-                            if (v + e < a.V) {
-                                if constexpr (kEs == 2)
-                                    reinterpret_cast<uint16_t*>(y)[e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
-                                else
-                                    reinterpret_cast<uint32_t*>(y)[e] = w[e];
+            for (int g = 0; g < C::NT / kGroup; ++g) {
+                const int c0 = wn * (C::NT * 32) + g * kCols;   // the strip's first channel in the tile
+#pragma unroll
+                for (int n = 0; n < kGroup; ++n) {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const int at = n * 32 + 8 * q + 4 * half;   // registers 4 q .. 4 q + 3
+                        const f32x4 w = *reinterpret_cast<const f32x4*>(sw + c0 + at);
+                        const f32x4 b = *reinterpret_cast<const f32x4*>(sb + c0 + at);
+                        float y[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            y[e] = (float)acc[m][g * kGroup + n][4 * q + e] * (xs[m] * w[e]) + b[e];
+                        store_values<YT, 4>(reinterpret_cast<YT*>(strip + tok * kPitch) + at, 0, 4, y);
+                    }
+                }
+                wave_lds_order();
+                // this wave's share of the next tile's first stage has landed before its
+                // stores are on their way, so that no one waits for these
+                if (kGoesOn<C> && m == 0 && g == 0) __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
+#pragma unroll
+                for (int ps = 0; ps < 32 / kRowsPerPass; ++ps) {
+                    const int r = ps * kRowsPerPass + el / kLanesPerRow;
+                    const int c = el % kLanesPerRow;
+                    const int64_t t = ts + r, v = v0 + c0 + c * kEpc;
+                    const u32x4_t w = *reinterpret_cast<const u32x4_t*>(strip + r * kPitch + c * 16);
+                    if (t < a.T) {
+                        YT* y = static_cast<YT*>(a.Y) + t * a.ldy + v;
+                        if (v + kEpc <= a.V) {
+                            *reinterpret_cast<u32x4_t*>(y) = w;
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < kEpc; ++e) {
+                                if (v + e < a.V) {
+                                    if constexpr (kEs == 2)
+                                        reinterpret_cast<uint16_t*>(y)[e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
+                                    else
+                                        reinterpret_cast<uint32_t*>(y)[e] = w[e];
+                                }
                             }
                         }
                     }
                 }
+                wave_lds_order();   // the strip is rewritten next
             }
-            wave_lds_order();   // the strip is rewritten next
         }
+        if (!more) break;
+        // every wave is done with its strip and has its share of the stage
+        wait_step<63>();
     }
 }
 
@@ -615,7 +655,8 @@ hipError_t launch_tiles(const LogitsArgs& a, hipStream_t s) {
         p.tile0 = t0;
         p.tile1 = std::min(t0 + kMaxGridBlocks, total);
         p.per_xcd = (p.tile1 - t0 + kXcds - 1) / kXcds;
-        const dim3 grid((unsigned)(p.per_xcd * kXcds));
+        p.blocks = kGoesOn<C> ? std::min<int64_t>(p.per_xcd, kCus / kXcds) : p.per_xcd;
+        const dim3 grid((unsigned)(p.blocks * kXcds));
         if (a.y_dtype == EMBER_F32) {
             if (mask) ember_logits_q8<C, float, true><<<grid, C::kThreads, 0, s>>>(p);
             else ember_logits_q8<C, float, false><<<grid, C::kThreads, 0, s>>>(p);
@@ -652,7 +693,7 @@ struct TileCost {
     double fill, columns, epilogue;
 };
 constexpr TileCost kTiles[] = {
-    {256, 256, true, 2.5, 49.7, 7.1},  {128, 256, true, 2.5, 33.2, 4.3},  {128, 128, false, 3.6, 20.4, 1.6},
+    {256, 256, true, 2.5, 52.0, 6.2},  {128, 256, true, 2.5, 33.0, 4.0},  {128, 128, false, 3.6, 20.4, 1.6},
     {128, 128, false, 5.1, 21.5, 1.1}, {64, 128, false, 4.2, 12.0, 1.5},  {32, 128, false, 4.3, 8.8, 1.2},
 };
 double tile_us(const TileCost& c, const LogitsArgs& a) {
@@ -668,9 +709,9 @@ double tile_us(const TileCost& c, const LogitsArgs& a) {
 // tokens 96 / 98, 20 x 50000 x 3000 32 / 37, 64 x 100000 x 1000 29 / 39, 64 x 30000 x
 // 2000 18 / 21; past those limits 10 x 32768 x 8192 62 / 47, 50 x 200000 x 500 50 /
 // 42).  Others the tiling that should take least (us): 333 x 8191 x 1000 12 with
-// 128 x 128 tiles and 22 with 256 x 256, 330 x 110820 x 128 26 with 128 x 128 three a
-// compute unit, 29 with two and 36 with 256 x 256, 128 x 128256 x 4096 112 with 128 x 256
-// and 134 with 256 x 256, 211 x 36770 x 2896 50 with 256 x 256 and 76 with 128 x 128,
+// 128 x 128 tiles and 21 with 256 x 256, 330 x 110820 x 128 26 with 128 x 128 three a
+// compute unit, 28 with two and 33 with 256 x 256, 128 x 128256 x 4096 112 with 128 x 256
+// and 133 with 256 x 256, 211 x 36770 x 2896 49 with 256 x 256 and 76 with 128 x 128,
 // 128 x 4000 x 2000 10 with 32 x 128 and 16 with 128 x 128.
 hipError_t launch_logits(const LogitsArgs& a, hipStream_t s) {
     if (a.T <= 16) {
