@@ -49,7 +49,9 @@ SHAPES = [(1, 1, 1), (1, 5, 16), (1, 300, 64), (2, 1000, 200), (3, 64, 4096), (5
           (300, 30000, 512), (300, 30001, 500), (257, 40000, 130), (1000, 6000, 256), (600, 9003, 333),
           (333, 8200, 1024), (333, 8191, 1000), (64, 40000, 512), (60, 40003, 300), (64, 30000, 128),
           (129, 9001, 300), (12, 3000, 768), (32, 4097, 1024), (20, 5000, 1001), (64, 3000, 2048), (50, 2001, 1100),
-          (257, 40000, 128), (400, 30003, 144), (900, 12345, 64)]
+          (257, 40000, 128), (400, 30003, 144), (900, 12345, 64),
+          # blocks that go on to other tiles
+          (262, 43046, 500), (261, 42975, 512), (386, 56313, 500), (391, 55480, 512), (520, 100003, 500)]
 
 
 @pytest.mark.parametrize("T,V,D", SHAPES)
