@@ -44,6 +44,7 @@ struct Params {
     int64_t per_xcd;     // tiles per XCD
     int64_t blocks;      // blocks per XCD: each takes every blocks-th of its tiles
     int group_m;         // token tiles a group of the tile order
+    int in_step;         // log2 of the channel tiles that begin at the same step
 };
 
 // Raw buffer resource of `bytes` bytes at a wave-uniform base.
@@ -177,12 +178,16 @@ __global__ __launch_bounds__(C::kThreads) void ember_logits_q8(Params p) {
     // Blocks with other channels begin at other steps (the sum has no order): in
     // step, all of them would read the same columns of rows that lie a power of
     // two apart, and so a few of the memory's channels at a time (64 tokens x
-    // 128256 x 4096: 127 us in step, 105 like this; one token: 110 and 91).
+    // 128256 x 4096: 127 us in step, 105 like this; one token: 110 and 91).  With
+    // several token tiles, eight channel tiles are in step: an XCD's blocks then
+    // read the tokens' slices together, not each from beyond its L2, which costs
+    // power and so clock (4096 x 128256 x 4096: 1997 us with one in step, groups of
+    // eight token tiles; 1885 with eight in step; 1867 with groups of four too).
     auto tile_at = [&](int64_t i) {
         int tm;
         int64_t tn;
         tile_of(p, i, tm, tn);
-        return At{(int64_t)tm * C::BM, tn * C::BN, (int)((uint64_t)tn * kRotate % (uint32_t)nk)};
+        return At{(int64_t)tm * C::BM, tn * C::BN, (int)((uint64_t)(tn >> p.in_step) * kRotate % (uint32_t)nk)};
     };
     At at = tile_at(l);
 
@@ -648,7 +653,8 @@ hipError_t launch_tiles(const LogitsArgs& a, hipStream_t s) {
     p.nk = (int)((a.D + C::KS - 1) / C::KS);
     p.MT = (int)((a.T + C::BM - 1) / C::BM);
     p.NT = (a.V + C::BN - 1) / C::BN;
-    p.group_m = 8;
+    p.group_m = 4;
+    p.in_step = p.MT > 1 ? 3 : 0;
     const int64_t total = (int64_t)p.MT * p.NT;
     const bool mask = a.D % 16 != 0;
     for (int64_t t0 = 0; t0 < total; t0 += kMaxGridBlocks) {
