@@ -11,7 +11,8 @@
 // and are read from there as MFMA operands, 16 consecutive columns a lane.  A ring
 // of LDS stages keeps the loads of the next steps in flight; the operands of
 // each 32-column sub-step are read behind the previous sub-step's MFMAs, across
-// the step barrier too.
+// the step barrier too.  In the small tilings several groups of wavefronts share a
+// tile's steps, each with a ring of its own, and their sums are added at the end.
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -102,14 +103,15 @@ __device__ __forceinline__ void tile_of(const Params& p, int64_t l, int& tm, int
     tn = q / gm;
 }
 
-template <int BM_, int BN_, int WM_, int WN_, int KS_, int STAGES_>
+template <int BM_, int BN_, int WM_, int WN_, int KS_, int STAGES_, int KG_ = 1>
 struct Tile {
     static constexpr int BM = BM_, BN = BN_;       // tokens, channels a block
     static constexpr int WM = WM_, WN = WN_;       // wavefronts over them
     static constexpr int KS = KS_;                 // columns (bytes) a step
     static constexpr int kStages = STAGES_;
-    static constexpr int kWavesB = WM * WN;
-    static constexpr int kThreads = kWavesB * kWave;
+    static constexpr int KG = KG_;                 // groups of wavefronts that share the steps, each with a ring
+    static constexpr int kWavesB = WM * WN;        // of a group
+    static constexpr int kThreads = KG * kWavesB * kWave;
     static constexpr int MT = BM / WM / 32, NT = BN / WN / 32;   // MFMA tiles a wave
     static constexpr int kSub = KS / 32;
     static constexpr int kChunks = KS / 16;        // 16-byte chunks of a slice's row
@@ -117,7 +119,8 @@ struct Tile {
     static constexpr int kLoadsA = BM / kRowsPerLoad, kLoadsB = BN / kRowsPerLoad;
     static constexpr int kLoads = (kLoadsA + kLoadsB) / kWavesB;   // a wave and step
     static constexpr int kStageBytes = (BM + BN) * KS;
-    static constexpr int kLds = kStages * kStageBytes;
+    static constexpr int kRing = kStages * kStageBytes;
+    static constexpr int kLds = KG * kRing;
     static_assert((kLoadsA + kLoadsB) % kWavesB == 0, "equal loads a wave");
     static_assert(kSub >= 2 && kSub % 2 == 0, "a step ends on the register set it began with");
     static_assert(kStages >= 2 && (kStages - 2) * kLoads < 64, "vmcnt range");
@@ -140,7 +143,7 @@ struct Epilogue {
 // block / like this, 256 x 256 tiles: 4096 x 128256 x 4096 2115 / 2001, 955 x 33990 x
 // 3381 fp32 165 / 161, 1500 x 50000 x 1024 106 / 103).
 template <typename C>
-constexpr bool kGoesOn = C::kLds > 80 * 1024;
+constexpr bool kGoesOn = C::KG == 1 && C::kLds > 80 * 1024;
 template <typename C, typename YT>
 constexpr int epilogue_at() { return kGoesOn<C> ? C::kStageBytes : 0; }
 template <typename C, typename YT>
@@ -160,10 +163,11 @@ template <typename C, typename YT, bool kMask>
 __global__ __launch_bounds__(C::kThreads) void ember_logits_q8(Params p) {
     __shared__ __attribute__((aligned(1024))) uint8_t lds[lds_of<C, YT>()];
     const LogitsArgs& a = p.a;
-    const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
     const int lane = threadIdx.x & (kWave - 1);
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int wave_all = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int group = wave_all / C::kWavesB, wave = wave_all % C::kWavesB;
     const int wm = wave % C::WM, wn = wave / C::WM;
+    const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds + group * C::kRing;
 
     // blocks of one XCD take consecutive tiles
     const int64_t first = p.tile0 + (int64_t)(blockIdx.x % kXcds) * p.per_xcd;
@@ -171,6 +175,7 @@ __global__ __launch_bounds__(C::kThreads) void ember_logits_q8(Params p) {
     int64_t l = first + blockIdx.x / kXcds;
     if (l >= end) return;
     const int nk = p.nk, D = (int)a.D;
+    const int steps = (nk + C::KG - 1) / C::KG;   // of each group; past the last they are zeros
     struct At {
         int64_t t0, v0;
         int rot;
@@ -201,7 +206,9 @@ __global__ __launch_bounds__(C::kThreads) void ember_logits_q8(Params p) {
         i32x4 ra, rb;
         int oa, ob;
     };
-    auto loads_of = [&](int kt) {
+    // step i of this wave's group
+    auto loads_of = [&](int i) {
+        const int kt = i * C::KG + group;
         const bool in = kt < nk;
         const int ks = kt + at.rot < nk ? kt + at.rot : kt + at.rot - nk;
         const int64_t k0 = in ? (int64_t)ks * C::KS : 0;
@@ -289,15 +296,15 @@ __global__ __launch_bounds__(C::kThreads) void ember_logits_q8(Params p) {
         // wave are outstanding, which are those of steps kt + 2 and later, so step
         // kt + 1 lies in its stage.
         uint32_t st = lds_base;
-        for (int kt = 0; kt < nk; ++kt) {
-            const uint32_t next = st + C::kStageBytes == lds_base + C::kLds ? lds_base : st + C::kStageBytes;
-            const StepLoads sl = loads_of(kt + C::kStages);
+        for (int i = 0; i < steps; ++i) {
+            const uint32_t next = st + C::kStageBytes == lds_base + C::kRing ? lds_base : st + C::kStageBytes;
+            const StepLoads sl = loads_of(i + C::kStages);
 #pragma unroll
             for (int kk = 0; kk < C::kSub; ++kk) {
                 const int cur = kk & 1;
                 const bool last = kk == C::kSub - 1;
                 if constexpr (kMask) {
-                    const int ks = kt + at.rot < nk ? kt + at.rot : kt + at.rot - nk;
+                    const int kt = i * C::KG + group, ks = kt + at.rot < nk ? kt + at.rot : kt + at.rot - nk;
                     if (ks == nk - 1) {
 #pragma unroll
                         for (int m = 0; m < C::MT; ++m) mask_a(ks, kk, af[cur][m]);
@@ -308,20 +315,20 @@ __global__ __launch_bounds__(C::kThreads) void ember_logits_q8(Params p) {
                 constexpr int kSlots = C::MT * C::NT > C::MT + C::NT ? C::MT * C::NT : C::MT + C::NT;
                 constexpr int kAll = kSlots > C::kLoads ? kSlots : C::kLoads;
 #pragma unroll
-                for (int i = 0; i < kAll; ++i) {
-                    if (i < C::MT * C::NT) {
-                        const int m = i / C::NT, n = i % C::NT;
+                for (int x = 0; x < kAll; ++x) {
+                    if (x < C::MT * C::NT) {
+                        const int m = x / C::NT, n = x % C::NT;
                         acc[m][n] = __builtin_amdgcn_mfma_i32_32x32x32_i8(bf[cur][n], af[cur][m], acc[m][n], 0, 0, 0);
                     }
                     // operands in the order the MFMAs first use them: A 0, all of B, the rest of A
-                    if (i < C::MT + C::NT) {
-                        const bool is_b = i >= 1 && i <= C::NT;
-                        const int f = i == 0 ? 0 : is_b ? i - 1 : i - C::NT;
-                        const i32x4 x = frag(last ? next : st, (is_b ? row_b : row_a) + 32 * f, last ? 0 : kk + 1);
-                        if (is_b) bf[cur ^ 1][f] = x;
-                        else af[cur ^ 1][f] = x;
+                    if (x < C::MT + C::NT) {
+                        const bool is_b = x >= 1 && x <= C::NT;
+                        const int f = x == 0 ? 0 : is_b ? x - 1 : x - C::NT;
+                        const i32x4 w = frag(last ? next : st, (is_b ? row_b : row_a) + 32 * f, last ? 0 : kk + 1);
+                        if (is_b) bf[cur ^ 1][f] = w;
+                        else af[cur ^ 1][f] = w;
                     }
-                    if (last && i < C::kLoads) issue_one(sl, st, i);
+                    if (last && x < C::kLoads) issue_one(sl, st, x);
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
@@ -332,6 +339,33 @@ __global__ __launch_bounds__(C::kThreads) void ember_logits_q8(Params p) {
         if (more) {
             at = then;
             issue(0);
+        }
+
+        if constexpr (C::KG > 1) {
+            // the other groups' sums join the first one's
+            constexpr int kSums = C::kWavesB * C::MT * C::NT * 16 * kWave;
+            static_assert((C::KG - 1) * kSums * 4 <= C::kLds, "the sums of the groups");
+            int* const sums = reinterpret_cast<int*>(lds) + (wave * C::MT * C::NT * 16) * kWave + lane;
+#pragma unroll
+            for (int m = 0; m < C::MT; ++m)
+#pragma unroll
+                for (int n = 0; n < C::NT; ++n)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (group > 0) sums[(group - 1) * kSums + ((m * C::NT + n) * 16 + i) * kWave] = acc[m][n][i];
+            wait_step<63>();
+            if (group == 0) {
+#pragma unroll
+                for (int q = 0; q < C::KG - 1; ++q)
+#pragma unroll
+                    for (int m = 0; m < C::MT; ++m)
+#pragma unroll
+                        for (int n = 0; n < C::NT; ++n)
+#pragma unroll
+                            for (int i = 0; i < 16; ++i)
+                                acc[m][n][i] += sums[q * kSums + ((m * C::NT + n) * 16 + i) * kWave];
+            }
+            wait_step<63>();
         }
 
         // Epilogue: the channels are the rows of the MFMA tiles, so a lane holds four
@@ -352,6 +386,7 @@ __global__ __launch_bounds__(C::kThreads) void ember_logits_q8(Params p) {
             sb[threadIdx.x] = my_bias;
         }
         wait_step<63>();
+        if (C::KG > 1 && group > 0) break;
         int el = lane;
         asm volatile("" : "+v"(el));   // what follows from it is not kept in registers over the loop above
         const int half = el >> 5, tok = el & 31;
@@ -680,15 +715,16 @@ hipError_t launch_tiles(const LogitsArgs& a, hipStream_t s) {
 
 namespace {
 
-using T256x256 = Tile<256, 256, 4, 2, 128, 2>;
-using T128x256 = Tile<128, 256, 4, 2, 128, 3>;
+using T64x128 = Tile<64, 128, 2, 2, 128, 3>;
+using T32x64 = Tile<32, 64, 1, 2, 128, 3, 4>;    // four and three groups of wavefronts share the steps
+using T64x64 = Tile<64, 64, 2, 2, 128, 3, 3>;
 using T128x128 = Tile<128, 128, 4, 2, 128, 2>;
 using T128x128s = Tile<128, 128, 2, 2, 64, 3>;   // 48 KB of shared memory: three a compute unit
-using T64x128 = Tile<64, 128, 2, 2, 128, 3>;
-using T32x128 = Tile<32, 128, 1, 4, 128, 3>;
+using T128x256 = Tile<128, 256, 4, 2, 128, 3>;
+using T256x256 = Tile<256, 256, 4, 2, 128, 2>;
 
-// What a launch of a tiling takes, in us, fitted to 26 shapes of 100 to 4096 tokens,
-// 2000 to 128256 channels and 128 to 4096 columns (rms error 10 to 16%): one
+// What a launch of a tiling takes, in us, fitted to 50 shapes of 10 to 4096 tokens,
+// 1000 to 128256 channels and 128 to 8192 columns (rms error 10 to 20%): one
 // fill of the pipeline, then the tiles of a compute unit one after the other, each
 // its columns at the rate of a full chip (us per 4096) and its epilogue, which
 // is twice as long for fp32 logits.  Where one tile has a compute unit to itself
@@ -699,13 +735,16 @@ struct TileCost {
     double fill, columns, epilogue;
 };
 constexpr TileCost kTiles[] = {
-    {256, 256, true, 2.5, 52.0, 6.2},  {128, 256, true, 2.5, 33.0, 4.0},  {128, 128, false, 3.6, 20.4, 1.6},
-    {128, 128, false, 5.1, 21.5, 1.1}, {64, 128, false, 4.2, 12.0, 1.5},  {32, 128, false, 4.3, 8.8, 1.2},
+    {64, 128, false, 3.6, 12.0, 1.5},  {32, 64, true, 2.0, 5.0, 2.6},     {64, 64, true, 3.5, 9.0, 1.9},
+    {128, 128, false, 3.6, 20.4, 1.6}, {128, 128, false, 5.1, 21.5, 1.1}, {128, 256, true, 2.5, 33.0, 4.0},
+    {256, 256, true, 2.5, 52.0, 6.2},
 };
+constexpr double kTableBytesPerUs = 5.8e6;   // no tiling reads the table faster
 double tile_us(const TileCost& c, const LogitsArgs& a) {
     const double tiles = (double)((a.T + c.bm - 1) / c.bm) * (double)((a.V + c.bn - 1) / c.bn) / 256.0;
     const double rounds = c.alone ? std::ceil(tiles) : std::max(1.0, tiles + 0.5);
-    return c.fill + rounds * (c.columns * (double)a.D / 4096.0 + c.epilogue * (a.y_dtype == EMBER_F32 ? 2 : 1));
+    const double tile = c.columns * (double)a.D / 4096.0 + c.epilogue * (a.y_dtype == EMBER_F32 ? 2 : 1);
+    return std::max(c.fill + rounds * tile, (double)a.V * (double)a.D / kTableBytesPerUs);
 }
 
 } // namespace
@@ -718,7 +757,11 @@ double tile_us(const TileCost& c, const LogitsArgs& a) {
 // 128 x 128 tiles and 21 with 256 x 256, 330 x 110820 x 128 26 with 128 x 128 three a
 // compute unit, 28 with two and 33 with 256 x 256, 128 x 128256 x 4096 112 with 128 x 256
 // and 133 with 256 x 256, 211 x 36770 x 2896 49 with 256 x 256 and 76 with 128 x 128,
-// 128 x 4000 x 2000 10 with 32 x 128 and 16 with 128 x 128.
+// 40 x 128256 x 4096 98 with 64 x 128 and 126 with 256 x 256.  Where few tiles are
+// there and D is long, one tile's chain of steps is what counts, and groups of
+// wavefronts that share it help (64 x 1500 x 4096 9 with 32 x 64 tiles and four groups,
+// 15 with 32 x 128 and none; 500 x 2000 x 4096 12 with 64 x 64 and three, 16; more
+// stages instead of groups 16 and 16).
 hipError_t launch_logits(const LogitsArgs& a, hipStream_t s) {
     if (a.T <= 16) {
         if (a.D <= 512) return launch_few<1, 1, 4, 1>(a, s);
@@ -738,12 +781,13 @@ hipError_t launch_logits(const LogitsArgs& a, hipStream_t s) {
     for (int i = 1; i < (int)(sizeof kTiles / sizeof kTiles[0]); ++i)
         if (tile_us(kTiles[i], a) < tile_us(kTiles[best], a)) best = i;
     switch (best) {
-    case 0: return launch_tiles<T256x256>(a, s);
-    case 1: return launch_tiles<T128x256>(a, s);
-    case 2: return launch_tiles<T128x128>(a, s);
-    case 3: return launch_tiles<T128x128s>(a, s);
-    case 4: return launch_tiles<T64x128>(a, s);
-    default: return launch_tiles<T32x128>(a, s);
+    case 0: return launch_tiles<T64x128>(a, s);
+    case 1: return launch_tiles<T32x64>(a, s);
+    case 2: return launch_tiles<T64x64>(a, s);
+    case 3: return launch_tiles<T128x128>(a, s);
+    case 4: return launch_tiles<T128x128s>(a, s);
+    case 5: return launch_tiles<T128x256>(a, s);
+    default: return launch_tiles<T256x256>(a, s);
     }
 }
 

@@ -51,7 +51,10 @@ SHAPES = [(1, 1, 1), (1, 5, 16), (1, 300, 64), (2, 1000, 200), (3, 64, 4096), (5
           (129, 9001, 300), (12, 3000, 768), (32, 4097, 1024), (20, 5000, 1001), (64, 3000, 2048), (50, 2001, 1100),
           (257, 40000, 128), (400, 30003, 144), (900, 12345, 64),
           # blocks that go on to other tiles
-          (262, 43046, 500), (261, 42975, 512), (386, 56313, 500), (391, 55480, 512), (520, 100003, 500)]
+          (262, 43046, 500), (261, 42975, 512), (386, 56313, 500), (391, 55480, 512), (520, 100003, 500),
+          # groups of wavefronts that share the steps
+          (500, 2000, 1008), (500, 2000, 1001), (64, 12000, 2064), (60, 12001, 2050), (64, 1500, 4096), (28, 3743, 6096),
+          (40, 1000, 8175)]
 
 
 @pytest.mark.parametrize("T,V,D", SHAPES)
