@@ -124,12 +124,11 @@ def _load(path: str = _LIB_PATH) -> ctypes.CDLL:
 LIB = _load()
 
 
+_DTYPES = {torch.float32: EMBER_F32, torch.bfloat16: EMBER_BF16}
+
+
 def _dtype(t: torch.Tensor) -> int:
-    if t.dtype == torch.float32:
-        return EMBER_F32
-    if t.dtype == torch.bfloat16:
-        return EMBER_BF16
-    return 99  # rejected by the library with EMBER_ERR_DTYPE
+    return _DTYPES.get(t.dtype, 99)  # 99: rejected by the library with EMBER_ERR_DTYPE
 
 
 def _ld(t: torch.Tensor) -> int:
@@ -399,9 +398,9 @@ def ember_rmsnorm(X: torch.Tensor, gain: torch.Tensor, eps: float = 1e-6, R: tor
     y, ldy = _matrix("Y", Y, shape)
     q, ldq = _matrix("Q", Q, shape, torch.int8)
     T, D = shape
-    rows = shape[:1]
-    _check(LIB.ember_rmsnorm(x, _dtype(X), ldx, r, ldr, _vector("gain", gain, shape[1:], None), _dtype(gain), eps,
-                             T, D, sm, lds, y, EMBER_F32 if Y is None else _dtype(Y), ldy, q, ldq,
+    rows = (T,)
+    _check(LIB.ember_rmsnorm(x, _DTYPES.get(dtype, 99), ldx, r, ldr, _vector("gain", gain, (D,), None),
+                             _dtype(gain), eps, T, D, sm, lds, y, EMBER_F32 if Y is None else _dtype(Y), ldy, q, ldq,
                              _vector("qscale", qscale, rows), _vector("rstd", rstd, rows), _stream(X)),
            "ember_rmsnorm")
 
@@ -424,9 +423,9 @@ def ember_rmsnorm_grad(dY: torch.Tensor, S: torch.Tensor, gain: torch.Tensor, rs
     dx, lddx = _matrix("dX", dX, shape, dtype)
     ds, ldds = _matrix("dS", dS, shape, dtype)
     T, D = shape
-    cols = shape[1:]
-    _check(LIB.ember_rmsnorm_grad(dy, lddy, s, _dtype(S), lds, _vector("gain", gain, cols, None), _dtype(gain),
-                                  _vector("rstd", rstd, shape[:1]), ds, ldds, T, D, dx, lddx,
+    cols = (D,)
+    _check(LIB.ember_rmsnorm_grad(dy, lddy, s, _DTYPES.get(dtype, 99), lds, _vector("gain", gain, cols, None),
+                                  _dtype(gain), _vector("rstd", rstd, (T,)), ds, ldds, T, D, dx, lddx,
                                   _vector("dgain", dgain, cols), ws.data_ptr(), ws.numel() * ws.element_size(),
                                   _stream(dgain)), "ember_rmsnorm_grad")
 
@@ -437,7 +436,7 @@ def ember_quantize_rows(X: torch.Tensor, Q: torch.Tensor, qscale: torch.Tensor) 
     x, ldx = _matrix("X", X, shape)
     q, ldq = _matrix("Q", Q, shape, torch.int8)
     rows, D = shape
-    _check(LIB.ember_quantize_rows(x, _dtype(X), ldx, rows, D, q, ldq, _vector("qscale", qscale, shape[:1]),
+    _check(LIB.ember_quantize_rows(x, _dtype(X), ldx, rows, D, q, ldq, _vector("qscale", qscale, (rows,)),
                                    _stream(X)), "ember_quantize_rows")
 
 
@@ -445,14 +444,13 @@ def ember_logits_q8(Xq: torch.Tensor, xscale: torch.Tensor, Wq: torch.Tensor, ws
                     Y: torch.Tensor, bias: torch.Tensor | None = None) -> None:
     """Y = (Xq Wq^T) xscale wscale + bias: logits of T tokens from 8-bit hidden
     states and an 8-bit table, each with one scale a row."""
-    xs, ws = Xq.shape, Wq.shape
-    T, D = xs
-    V = ws[0]
-    x, ldx = _matrix("Xq", Xq, xs, torch.int8)
+    T, D = Xq.shape
+    V = wscale.numel()
+    x, ldx = _matrix("Xq", Xq, (T, D), torch.int8)
     w, ldw = _matrix("Wq", Wq, (V, D), torch.int8)
     y, ldy = _matrix("Y", Y, (T, V))
-    _check(LIB.ember_logits_q8(x, ldx, _vector("xscale", xscale, xs[:1]), w, ldw, _vector("wscale", wscale, ws[:1]),
-                               _vector("bias", bias, ws[:1]), T, V, D, y, _dtype(Y), ldy, _stream(Wq)),
+    _check(LIB.ember_logits_q8(x, ldx, _vector("xscale", xscale, (T,)), w, ldw, _vector("wscale", wscale, (V,)),
+                               _vector("bias", bias, (V,)), T, V, D, y, _dtype(Y), ldy, _stream(Wq)),
            "ember_logits_q8")
 
 
