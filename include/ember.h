@@ -423,7 +423,8 @@ int ember_lmhead_step(void* W, int w_dtype, int64_t ldw,
  *                        that holds an infinity or a NaN has codes 0 and scale
  *                        NaN, which makes its logits NaN;
  *   rstd (T)             kept for the gradient.
- * X, R (x_dtype), S, Y: layout rules of W and G.  Q: 16-byte aligned, ldq a
+ * X, R (x_dtype), S, Y: layout rules of W and G; between two rows the padding up to
+ * the next 16-byte boundary may be read, its values do not matter.  Q: 16-byte aligned, ldq a
  * multiple of 16 below EMBER_Q8_MAX_LD; columns D..ldq-1 are not written.  gain: D values of
  * gain_dtype, 16-byte aligned.  0 <= T <= EMBER_MAX_TOKENS (0: nothing to do, the
  * pointers may be NULL), 1 <= D <= EMBER_NORM_MAX_D, eps >= 0 and finite.

@@ -35,12 +35,13 @@ __device__ __forceinline__ float load_elem(const void* p, int64_t i, bool bf16) 
 }
 
 // The chunk at columns [col, col + chunk) of a row of D elements: one 16-byte
-// load where it lies inside the row, element loads in the row's last partial
-// chunk, zeros past it.
+// load where it lies inside the row, and in the row's last partial chunk too if
+// another row follows (what is loaded past the row is then its padding, see
+// kept_words); element loads there in the last row; zeros past it.
 template <typename T>
-__device__ __forceinline__ u32x4_t load_chunk(const T* row, int col, int D) {
+__device__ __forceinline__ u32x4_t load_chunk(const T* row, int col, int D, bool follows) {
     u32x4_t w = {0, 0, 0, 0};
-    if (col + kChunkElems<T> <= D) {
+    if (col + kChunkElems<T> <= D || (follows && col < D)) {
         w = *reinterpret_cast<const u32x4_t*>(row + col);
     } else {
 #pragma unroll
@@ -50,6 +51,19 @@ __device__ __forceinline__ u32x4_t load_chunk(const T* row, int col, int D) {
                 else w[e >> 1] |= (uint32_t)reinterpret_cast<const uint16_t*>(row)[col + e] << (16 * (e & 1));
             }
         }
+    }
+    return w;
+}
+
+// The bits of a chunk from load_chunk that belong to its row.
+template <typename T>
+__device__ __forceinline__ u32x4_t kept_words(int col, int D) {
+    constexpr int kPer = 4 / (int)sizeof(T);   // elements a word
+    u32x4_t w;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const int n = D - col - q * kPer;
+        w[q] = n >= kPer ? 0xFFFFFFFFu : kPer == 2 && n == 1 ? 0xFFFFu : 0u;
     }
     return w;
 }

@@ -47,7 +47,7 @@ struct FwdParams {
     int64_t ldq;
     float* qscale;
     float* rstd;          // or null
-    bool stream;          // S and Y are stored non-temporally
+    bool stream;          // Y is stored non-temporally (S is in any case)
 };
 
 template <typename XT>
@@ -99,21 +99,35 @@ __device__ __forceinline__ void store_codes(int8_t* row, int col, int D, const f
 
 // The chunk at column col: a full row (D a multiple of the chunk) has whole ones only.
 template <typename XT, bool kFull>
-__device__ __forceinline__ u32x4_t chunk_at(const XT* row, int col, int D) {
+__device__ __forceinline__ u32x4_t chunk_at(const XT* row, int col, int D, bool follows) {
     if constexpr (kFull) {
         u32x4_t w = {0, 0, 0, 0};
         if (col < D) w = *reinterpret_cast<const u32x4_t*>(row + col);
         return w;
     } else {
-        return load_chunk<XT>(row, col, D);
+        return load_chunk<XT>(row, col, D, follows);
     }
+}
+// Element e of it; keep: what counts of it (kept_words), applied where the chunk is
+// used, so that the loads of a row are in flight together (the gradient of 16384 x
+// 2047 bf16: 101 us with element loads at the end of every row, 53 like this).
+template <typename XT, bool kFull>
+__device__ __forceinline__ float elem_at(const u32x4_t& w, int e, const u32x4_t& keep) {
+    if constexpr (kFull) return elem<XT>(w, e);
+    else return elem<XT>(w & keep, e);
 }
 template <typename T, int N, bool kFull>
 __device__ __forceinline__ void store_at(T* row, int col, int D, const float (&v)[N], bool stream) {
     if (kFull && col >= D) return;
     const int end = kFull ? col + N : D;
-    if (stream) store_values<T, N, true>(row, col, end, v);
-    else store_values<T, N, false>(row, col, end, v);
+    if (stream) {
+        // the empty statements keep the compiler from making one ordinary store of the two
+        asm volatile("");
+        store_values<T, N, true>(row, col, end, v);
+        asm volatile("");
+    } else {
+        store_values<T, N, false>(row, col, end, v);
+    }
 }
 template <int N, bool kFull>
 __device__ __forceinline__ void codes_at(int8_t* row, int col, int D, const float (&y)[N], float inv) {
@@ -145,26 +159,30 @@ __global__ __launch_bounds__(threads_of(TPR)) void ember_rmsnorm_fwd(FwdParams a
         for (int c = 0; c < NC; ++c) load_gain<XT>(a.gain, a.gain_bf16, (lane + c * TPR) * N, D, g[c]);
     }
     for (int turn = 0; t < a.T; t += step, turn ^= 1) {
+        const bool follows = t + 1 < a.T;
         u32x4_t wx[NC], wr[NC];
 #pragma unroll
         for (int c = 0; c < NC; ++c)
-            wx[c] = chunk_at<XT, kFull>(static_cast<const XT*>(a.X) + t * a.ldx, (lane + c * TPR) * N, D);
+            wx[c] = chunk_at<XT, kFull>(static_cast<const XT*>(a.X) + t * a.ldx, (lane + c * TPR) * N, D, follows);
         if (kNorm && a.R) {
 #pragma unroll
             for (int c = 0; c < NC; ++c)
-                wr[c] = chunk_at<XT, kFull>(static_cast<const XT*>(a.R) + t * a.ldr, (lane + c * TPR) * N, D);
+                wr[c] = chunk_at<XT, kFull>(static_cast<const XT*>(a.R) + t * a.ldr, (lane + c * TPR) * N, D, follows);
         }
         float v[NC][N];
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
+            const u32x4_t keep = kept_words<XT>((lane + c * TPR) * N, D);
 #pragma unroll
-            for (int e = 0; e < N; ++e) v[c][e] = elem<XT>(wx[c], e);
+            for (int e = 0; e < N; ++e) v[c][e] = elem_at<XT, kFull>(wx[c], e, keep);
         }
         if (kNorm && a.R) {
 #pragma unroll
-            for (int c = 0; c < NC; ++c)
+            for (int c = 0; c < NC; ++c) {
+                const u32x4_t keep = kept_words<XT>((lane + c * TPR) * N, D);
 #pragma unroll
-                for (int e = 0; e < N; ++e) v[c][e] += elem<XT>(wr[c], e);
+                for (int e = 0; e < N; ++e) v[c][e] += elem_at<XT, kFull>(wr[c], e, keep);
+            }
         }
         if constexpr (kNorm) {
             float sq = 0.0f;
@@ -178,7 +196,7 @@ __global__ __launch_bounds__(threads_of(TPR)) void ember_rmsnorm_fwd(FwdParams a
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
                 const int col = (lane + c * TPR) * N;
-                if (a.S) store_at<XT, N, kFull>(static_cast<XT*>(a.S) + t * a.lds, col, D, v[c], a.stream);
+                if (a.S) store_at<XT, N, kFull>(static_cast<XT*>(a.S) + t * a.lds, col, D, v[c], true);
 #pragma unroll
                 for (int e = 0; e < N; ++e) v[c][e] = v[c][e] * rstd * g[c][e];
                 if (a.Y) {
@@ -254,13 +272,14 @@ __global__ __launch_bounds__(TPR * kGroups) void ember_rmsnorm_bwd(GradParams a)
     float nrstd;
     auto load = [&](int64_t row) {
         row = min(row, a.T - 1);
+        const bool follows = row + 1 < a.T;
         nrstd = a.rstd[row];
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
             const int col = (lane + c * TPR) * N;
-            ny[c] = chunk_at<XT, kFull>(static_cast<const XT*>(a.dY) + row * a.lddy, col, D);
-            ns[c] = chunk_at<XT, kFull>(static_cast<const XT*>(a.S) + row * a.lds, col, D);
-            if (a.dS) nd[c] = chunk_at<XT, kFull>(static_cast<const XT*>(a.dS) + row * a.ldds, col, D);
+            ny[c] = chunk_at<XT, kFull>(static_cast<const XT*>(a.dY) + row * a.lddy, col, D, follows);
+            ns[c] = chunk_at<XT, kFull>(static_cast<const XT*>(a.S) + row * a.lds, col, D, follows);
+            if (a.dS) nd[c] = chunk_at<XT, kFull>(static_cast<const XT*>(a.dS) + row * a.ldds, col, D, follows);
         }
     };
     // the next row's loads are in flight behind this one's reduction, where the
@@ -277,6 +296,11 @@ __global__ __launch_bounds__(TPR * kGroups) void ember_rmsnorm_bwd(GradParams a)
             wy[c] = ny[c];
             ws[c] = ns[c];
             if (a.dS) wd[c] = nd[c];
+            if constexpr (!kFull) {   // dS past the row only reaches dX past it, which is not stored
+                const u32x4_t keep = kept_words<XT>((lane + c * TPR) * N, D);
+                wy[c] &= keep;
+                ws[c] &= keep;
+            }
         }
         if (kAhead && i + 1 < rounds) load(t + step);
         float k = 0.0f;
@@ -368,7 +392,10 @@ __global__ __launch_bounds__(kSumThreads) void ember_rmsnorm_dgain(const float* 
 // Threads per row and chunks per thread.  The norm has a row in one wave up to 256
 // chunks (us, y / 8 bits: 16384 x 2048 bf16 47.3 / 43.5, in four waves 49.0 / 44.5) and in
 // four up to 1024 (2000 x 5000 bf16 19.2 / 16.8, in eight 20.2 / 19.4; 8192 x 4096 fp32
-// 92.3 / 75.5 and 94.2 / 76.9; 10000 x 8192 bf16 118 / 102 and 115 / 106).
+// 92.3 / 75.5 and 94.2 / 76.9; 10000 x 8192 bf16 118 / 102 and 115 / 106).  Its
+// gradient, whose registers hold one chunk a thread best, in as few waves as have
+// one for each (16384 x 1024 bf16 in two waves 28.9, in four 34.4, in one with two
+// chunks a thread 31.7).
 struct RowPlan {
     int tpr, nc;
     bool full;     // D a multiple of the chunk
@@ -376,7 +403,7 @@ struct RowPlan {
 RowPlan row_plan(int D, int dtype, bool grad) {
     const int epc = dtype == EMBER_F32 ? 4 : 8, chunks = (D + epc - 1) / epc;
     RowPlan p;
-    if (grad) p.tpr = chunks <= 64 ? 64 : chunks <= 256 ? 256 : chunks <= 512 ? 512 : 1024;
+    if (grad) p.tpr = chunks <= 64 ? 64 : chunks <= 128 ? 128 : chunks <= 256 ? 256 : chunks <= 512 ? 512 : 1024;
     else p.tpr = chunks <= 256 ? 64 : chunks <= 1024 ? 256 : 1024;
     const int n = (chunks + p.tpr - 1) / p.tpr;
     p.nc = n <= 1 ? 1 : n <= 2 ? 2 : n <= 4 ? 4 : 8;
@@ -384,11 +411,16 @@ RowPlan row_plan(int D, int dtype, bool grad) {
     return p;
 }
 
-// Outputs up to this size are stored non-temporally.  With what reads y next
-// (us, ordinary / non-temporal): 2048 x 8192 bf16, 67 MB of s and y, 31.6 / 28.0,
-// 4096 x 4096 29.3 / 27.7 (the norm alone 25.3 / 21.3); 16384 x 4096, 268 MB,
-// 108.7 / 111.7.
-constexpr int64_t kStreamBytes = (int64_t)128 << 20;
+// What is read next is stored ordinarily while the caches can keep it, the rest
+// non-temporally.  S is not: it waits for the gradient (us, alone and with a
+// kernel that reads Y next, S ordinary / non-temporal: 16384 x 4096 bf16 94.8 / 93.5
+// and 132 / 128, 4096 x 4096 26.0 / 26.1 and 36.2 / 33.8).  Y is, and stays longer than
+// dX, which the norm's gradient writes beside more reading (Y ordinary / non-temporal,
+// S non-temporal: 4096 x 4096 26.1 / 21.0 and 33.8 / 37.1, 16384 x 4096 93.5 / 91.7 and
+// 128.1 / 129.4, 32768 x 4096 184 / 181 and 254 / 252; dX: 4096 x 4096 31.0 / 29.9 and
+// 41.7 / 42.8, 8192 x 4096 53.5 / 52.4 and 73.2 / 72.5, 16384 x 4096 102.5 / 98.6 and
+// 138 / 139).
+constexpr int64_t kKeptY = (int64_t)256 << 20, kKeptDX = (int64_t)48 << 20;
 int64_t bytes_of(int64_t T, int64_t D, int dtype) { return T * D * (dtype == EMBER_F32 ? 4 : 2); }
 
 template <typename XT, bool kNorm, bool kFull>
@@ -434,6 +466,7 @@ hipError_t launch_bwd(const GradParams& p, const RowPlan& pl, int blocks, hipStr
 #define EMBER_BWD(TPR, NC, G) \
     if (pl.tpr == TPR && pl.nc == NC) ember_rmsnorm_bwd<XT, TPR, NC, G, kFull><<<grid, TPR * G, 0, s>>>(p)
     EMBER_BWD(64, 1, 16);
+    else EMBER_BWD(128, 1, 8);
     else EMBER_BWD(256, 1, 4);
     else EMBER_BWD(512, 1, 2);
     else EMBER_BWD(1024, 1, 1);
@@ -458,7 +491,7 @@ hipError_t launch_fwd_of(const FwdParams& p, bool norm, const RowPlan& pl, hipSt
 hipError_t launch_rmsnorm(const NormArgs& x, hipStream_t s) {
     FwdParams p{x.X, x.ldx, x.R, x.ldr, x.gain, x.gain_dtype == EMBER_BF16, x.eps, x.T, (int)x.D, x.S, x.lds,
                 x.Y, x.y_dtype == EMBER_BF16, x.ldy, x.Q, x.ldq, x.qscale, x.rstd,
-                (x.S ? bytes_of(x.T, x.D, x.x_dtype) : 0) + (x.Y ? bytes_of(x.T, x.D, x.y_dtype) : 0) <= kStreamBytes};
+                x.Y && bytes_of(x.T, x.D, x.y_dtype) >= kKeptY};
     const RowPlan pl = row_plan((int)x.D, x.x_dtype, false);
     return x.x_dtype == EMBER_F32 ? launch_fwd_of<float>(p, x.gain != nullptr, pl, s)
                                   : launch_fwd_of<uint16_t>(p, x.gain != nullptr, pl, s);
@@ -472,7 +505,7 @@ size_t norm_grad_ws_bytes(int64_t T, int64_t D) {
 
 hipError_t launch_rmsnorm_grad(const NormGradArgs& x, hipStream_t s) {
     GradParams p{x.dY, x.lddy, x.S, x.lds, x.gain, x.gain_dtype == EMBER_BF16, x.rstd, x.dS, x.ldds, x.T, (int)x.D,
-                 x.dX, x.lddx, reinterpret_cast<float*>(x.ws), bytes_of(x.T, x.D, x.x_dtype) <= kStreamBytes};
+                 x.dX, x.lddx, reinterpret_cast<float*>(x.ws), bytes_of(x.T, x.D, x.x_dtype) >= kKeptDX};
     const RowPlan pl = row_plan((int)x.D, x.x_dtype, true);
     const int blocks = grad_blocks(x.T, pl);
     if (blocks == 1) p.part = x.dgain;   // a single block's sums are the result

@@ -110,7 +110,7 @@ def test_forward(em, T, D, dtype, ydtype, gdtype, residual):
 
 
 @pytest.mark.parametrize("T", [1, 63, 300, 2000, 5000])
-@pytest.mark.parametrize("D,dtype", [(96, BF), (896, F), (1000, BF), (4096, BF)])
+@pytest.mark.parametrize("D,dtype", [(96, BF), (896, F), (1000, BF), (4096, BF), (699, BF), (1001, F), (2047, BF), (3001, F)])
 def test_forward_over_token_counts(em, T, D, dtype):
     print(f"rmsnorm T={T} D={D} {dtype}", flush=True)
     X, R, g = make(T, D, dtype, T + D, True, extra=0)
@@ -223,7 +223,9 @@ def grad64(dY, S, gain, rstd, dS):
 @pytest.mark.parametrize("T,D", SHAPES + [(300, 896), (1500, 72), (2500, 1000), (1100, 4096),
                                           # one block alone, and the first count with two launches
                                           (64, 512), (65, 512), (16, 2048), (17, 2048), (8, 4096), (9, 4096), (4, 8192),
-                                          (5, 8192), (4, 32768), (5, 32768)])
+                                          (5, 8192), (4, 32768), (5, 32768),
+                                          # rows that end inside a chunk, many
+                                          (5000, 700), (2000, 2047), (700, 3001), (1500, 300), (5000, 513)])
 @pytest.mark.parametrize("dtype,gdtype,other", [(BF, F, True), (F, BF, False)])
 def test_gradient(em, T, D, dtype, gdtype, other):
     print(f"rmsnorm grad T={T} D={D} {dtype} gain {gdtype} dS={other}", flush=True)
