@@ -92,6 +92,22 @@ def test_scales_and_bias(em, T, V, D, dtype):
         assert ((Y.double() - E).abs() <= bar + 1e-37).all()
 
 
+@pytest.mark.parametrize("V,D,dtype", [(300, 1100, BF), (77, 1024, F), (500, 65, F), (40, 1023, BF)])
+def test_head_of_a_table(em, V, D, dtype):
+    """from_table: the codes of ember_quantize_rows, wide rows on 128-byte boundaries."""
+    g = torch.Generator(device=DEV).manual_seed(V)
+    W = out(V, D, dtype, 0).copy_(torch.randn(V, D, generator=g, device=DEV))
+    head = em.HeadQ8.from_table(W)
+    q, scale = codes(V, D, 1), torch.empty(V, device=DEV)
+    em.ember_quantize_rows(W, q, scale)
+    assert torch.equal(head.Wq, q) and torch.equal(head.wscale, scale)
+    assert head.Wq.stride(0) % (128 if D >= 1024 else 16) == 0 and head.Wq.data_ptr() % 16 == 0
+    Xq, Y = codes(9, D, 2), out(9, V, F, 0)
+    head.logits(Xq, torch.ones(9, device=DEV), Y)
+    want = sums(Xq, head.Wq) * scale.double()
+    assert ((Y.double() - want).abs() <= 4 * U * want.abs() + 1e-37).all()
+
+
 def test_largest_sums_do_not_overflow(em):
     D = 32768
     Xq = torch.full((20, D), -128, dtype=torch.int8, device=DEV)
