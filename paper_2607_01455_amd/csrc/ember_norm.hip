@@ -9,8 +9,9 @@
 // Gradient, with u = dy gain and k = mean_j u_j s_j:
 //   dx_j = rstd u_j - rstd^3 k s_j + ds_j,   dgain_j = sum_t dy_tj s_tj rstd_t.
 //
-// One pass over the data each.  TPR threads hold a row between its loads, its one
-// or two reductions and its stores, 16-byte chunks dealt round robin.
+// One pass over the data each (but the gradient of few tokens, see kSumAtOnceT).  TPR
+// threads hold a row between its loads, its one or two reductions and its stores,
+// 16-byte chunks dealt round robin.
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -244,9 +245,88 @@ struct GradParams {
     int D;
     void* dX;
     int64_t lddx;
-    float* part;          // [gridDim.x][D]: sums of dgain
+    int blocks;           // blocks of rows; the others sum dgain themselves
+    float* part;          // [blocks][D]: sums of dgain, or null
+    float* dgain;
     bool stream;          // dX is stored non-temporally
 };
+
+constexpr int kSumGroups = 16;    // interleaved sums of the partial rows
+
+// dgain of 8 chunks of columns, from dY and S themselves, in the order in which the
+// partial rows of `blocks` blocks of kGroups rows would give it: what block b's group g
+// has over its rounds, those over the groups, those of every 16th block, and
+// those sixteen.  Wave w takes the blocks b = w (mod 16), eight at a time, a lane
+// the rows of one of them.
+template <typename XT, int kGroups, bool kFull>
+__device__ __forceinline__ void sum_dgain(const GradParams& a, int first_chunk, float* lds) {
+    constexpr int N = kChunkElems<XT>, kAtOnce = kGroups >= 4 ? 4 : 2;   // rows in flight
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, x = lane % 8;
+    const int col = (first_chunk + x) * N, step = a.blocks * kGroups;
+    const int rounds = (int)((a.T + step - 1) / step);
+    float sum[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) sum[e] = 0.0f;
+    for (int b0 = wave; b0 < a.blocks; b0 += kSumGroups * 8) {
+        const int b = b0 + kSumGroups * (lane / 8);
+        float acc[N], p[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) acc[e] = p[e] = 0.0f;
+        int g = 0, i = 0;     // group and round of the next row to load,
+        int ug = 0, ui = 0;   // and to add
+        for (int j = 0; j < kGroups * rounds; j += kAtOnce) {
+            u32x4_t wy[kAtOnce], ws[kAtOnce];
+            float r[kAtOnce];
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u) {
+                const int64_t t = min((int64_t)b * kGroups + g + (int64_t)i * step, a.T - 1);
+                wy[u] = chunk_at<XT, kFull>(static_cast<const XT*>(a.dY) + t * a.lddy, col, a.D, t + 1 < a.T);
+                ws[u] = chunk_at<XT, kFull>(static_cast<const XT*>(a.S) + t * a.lds, col, a.D, t + 1 < a.T);
+                r[u] = a.rstd[t];
+                if (++i == rounds) { i = 0; ++g; }
+            }
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u) {
+                if (ug < kGroups) {
+                    const bool there = (int64_t)b * kGroups + ug + (int64_t)ui * step < a.T;
+#pragma unroll
+                    for (int e = 0; e < N; ++e) {
+                        const float term = __builtin_fmaf(elem<XT>(wy[u], e) * elem<XT>(ws[u], e), r[u], acc[e]);
+                        acc[e] = there ? term : acc[e];
+                    }
+                    if (++ui == rounds) {
+                        ui = 0;
+#pragma unroll
+                        for (int e = 0; e < N; ++e) {
+                            p[e] = ug == 0 ? acc[e] : p[e] + acc[e];
+                            acc[e] = 0.0f;
+                        }
+                        ++ug;
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            if (b0 + kSumGroups * k < a.blocks) {
+#pragma unroll
+                for (int e = 0; e < N; ++e) sum[e] += __shfl(p[e], k * 8 + x);
+            }
+        }
+    }
+    if (lane < 8) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) lds[wave * 8 * N + lane * N + e] = sum[e];
+    }
+    __syncthreads();
+    const int y = threadIdx.x, to = first_chunk * N + y;
+    if (y < 8 * N && to < a.D) {
+        float total = lds[y];
+#pragma unroll
+        for (int q = 1; q < kSumGroups; ++q) total += lds[q * 8 * N + y];
+        a.dgain[to] = total;
+    }
+}
 
 // kGroups rows at a time per block, TPR threads each; every thread keeps the
 // sums of dgain for its columns over all its rows, and the block adds up its
@@ -257,8 +337,13 @@ __global__ __launch_bounds__(TPR * kGroups) void ember_rmsnorm_bwd(GradParams a)
     constexpr int kRowWaves = TPR / kWave;
     __shared__ float red[2][kGroups][kRowWaves];
     __shared__ float sums[kGroups > 1 ? kGroups - 1 : 1][TPR * N];
+    static_assert(TPR * kGroups == kSumGroups * kWave, "a wave for each of the interleaved sums");
+    if ((int)blockIdx.x >= a.blocks) {
+        sum_dgain<XT, kGroups, kFull>(a, ((int)blockIdx.x - a.blocks) * 8, &sums[0][0]);
+        return;
+    }
     const int lane = threadIdx.x % TPR, group = threadIdx.x / TPR, D = a.D;
-    const int64_t step = (int64_t)gridDim.x * kGroups;
+    const int64_t step = (int64_t)a.blocks * kGroups;
     const int64_t rounds = (a.T - (int64_t)blockIdx.x * kGroups + step - 1) / step;   // of the block: all its threads take part
     int64_t t = (int64_t)blockIdx.x * kGroups + group;
     float g[NC][N], acc[NC][N];
@@ -310,7 +395,7 @@ __global__ __launch_bounds__(TPR * kGroups) void ember_rmsnorm_bwd(GradParams a)
             for (int e = 0; e < N; ++e) {
                 const float p = elem<XT>(wy[c], e) * elem<XT>(ws[c], e);
                 k += p * g[c][e];
-                if (there) acc[c][e] += p * rstd;
+                if (there) acc[c][e] = __builtin_fmaf(p, rstd, acc[c][e]);
             }
         }
         // by hand over the row's waves: the block's other rows have slots of their own
@@ -338,6 +423,7 @@ __global__ __launch_bounds__(TPR * kGroups) void ember_rmsnorm_bwd(GradParams a)
             }
         }
     }
+    if (a.part == nullptr) return;
     float* part = a.part + (int64_t)blockIdx.x * D;
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
@@ -366,8 +452,7 @@ __global__ __launch_bounds__(TPR * kGroups) void ember_rmsnorm_bwd(GradParams a)
 }
 
 constexpr int kSumCols = 64;      // columns per block of the partials' sum
-constexpr int kSumThreads = 1024;
-constexpr int kSumGroups = kSumThreads / kSumCols;
+constexpr int kSumThreads = kSumGroups * kSumCols;
 
 // dgain_j = the sum of the partial rows in a fixed order: kSumGroups
 // interleaved sums a column, then those in order.
@@ -451,18 +536,19 @@ hipError_t launch_fwd(const FwdParams& p, const RowPlan& pl, hipStream_t s) {
 // instead of 102 at 16384 x 4096 bf16, 40 instead of 33 at 2048 x 8192).
 constexpr int kGradBlocks = 256;
 int grad_groups(const RowPlan& pl) { return 1024 / pl.tpr; }
-// A block alone has the sums of dgain, and there is no second launch: as long as
-// that makes up for its rounds (us, alone / with the second launch: 4 rounds, 4 x
-// 8192 bf16 10.2 / 11.0, 16 x 2048 8.3 / 11.0; 8 rounds, 8 x 8192 15.3 / 10.9).
-constexpr int kAloneRounds = 4;
 int grad_blocks(int64_t T, const RowPlan& pl) {
-    if (T <= kAloneRounds * grad_groups(pl)) return T > 0;
     return (int)std::min<int64_t>((T + grad_groups(pl) - 1) / grad_groups(pl), kGradBlocks);
 }
 
+// Up to this many tokens dgain is summed in the same launch, from dY and S read
+// again, unless dX takes the place of one of them (us, so / in a second launch: 128 x
+// 4096 bf16 7.3 / 10.4, 500 x 2048 7.4 / 10.8, 500 x 4096 11.2 / 12.8, 1000 x 4096 14.4 /
+// 13.3, 2000 x 2048 17.1 / 11.3).
+constexpr int64_t kSumAtOnceT = 512;
+
 template <typename XT, bool kFull>
-hipError_t launch_bwd(const GradParams& p, const RowPlan& pl, int blocks, hipStream_t s) {
-    const dim3 grid((unsigned)blocks);
+hipError_t launch_bwd(const GradParams& p, const RowPlan& pl, int sum_blocks, hipStream_t s) {
+    const dim3 grid((unsigned)(p.blocks + sum_blocks));
 #define EMBER_BWD(TPR, NC, G) \
     if (pl.tpr == TPR && pl.nc == NC) ember_rmsnorm_bwd<XT, TPR, NC, G, kFull><<<grid, TPR * G, 0, s>>>(p)
     EMBER_BWD(64, 1, 16);
@@ -478,6 +564,11 @@ hipError_t launch_bwd(const GradParams& p, const RowPlan& pl, int blocks, hipStr
     } else return hipErrorInvalidValue;
 #undef EMBER_BWD
     return hipGetLastError();
+}
+
+template <typename XT>
+hipError_t launch_bwd_of(const GradParams& p, const RowPlan& pl, int sum_blocks, hipStream_t s) {
+    return pl.full ? launch_bwd<XT, true>(p, pl, sum_blocks, s) : launch_bwd<XT, false>(p, pl, sum_blocks, s);
 }
 
 template <typename XT>
@@ -505,17 +596,24 @@ size_t norm_grad_ws_bytes(int64_t T, int64_t D) {
 
 hipError_t launch_rmsnorm_grad(const NormGradArgs& x, hipStream_t s) {
     GradParams p{x.dY, x.lddy, x.S, x.lds, x.gain, x.gain_dtype == EMBER_BF16, x.rstd, x.dS, x.ldds, x.T, (int)x.D,
-                 x.dX, x.lddx, reinterpret_cast<float*>(x.ws), bytes_of(x.T, x.D, x.x_dtype) >= kKeptDX};
+                 x.dX, x.lddx, 0, reinterpret_cast<float*>(x.ws), x.dgain, bytes_of(x.T, x.D, x.x_dtype) >= kKeptDX};
     const RowPlan pl = row_plan((int)x.D, x.x_dtype, true);
-    const int blocks = grad_blocks(x.T, pl);
-    if (blocks == 1) p.part = x.dgain;   // a single block's sums are the result
-    if (blocks > 0) {
+    p.blocks = grad_blocks(x.T, pl);
+    if (p.blocks > 0) {
+        int sum_blocks = 0;
+        if (p.blocks == 1) {
+            p.part = x.dgain;   // a single block's sums are the result
+        } else if (x.T <= kSumAtOnceT && x.dX != x.dY && x.dX != x.S) {
+            p.part = nullptr;   // dY and S stay as they are: other blocks sum dgain meanwhile
+            const int chunk = x.x_dtype == EMBER_F32 ? 4 : 8;
+            sum_blocks = ((int)x.D + 8 * chunk - 1) / (8 * chunk);
+        }
         hipError_t e;
-        if (x.x_dtype == EMBER_F32) e = pl.full ? launch_bwd<float, true>(p, pl, blocks, s) : launch_bwd<float, false>(p, pl, blocks, s);
-        else e = pl.full ? launch_bwd<uint16_t, true>(p, pl, blocks, s) : launch_bwd<uint16_t, false>(p, pl, blocks, s);
-        if (e != hipSuccess || blocks == 1) return e;
+        if (x.x_dtype == EMBER_F32) e = launch_bwd_of<float>(p, pl, sum_blocks, s);
+        else e = launch_bwd_of<uint16_t>(p, pl, sum_blocks, s);
+        if (e != hipSuccess || p.blocks == 1 || sum_blocks > 0) return e;
     }
-    ember_rmsnorm_dgain<<<dim3((unsigned)((x.D + kSumCols - 1) / kSumCols)), kSumThreads, 0, s>>>(p.part, blocks,
+    ember_rmsnorm_dgain<<<dim3((unsigned)((x.D + kSumCols - 1) / kSumCols)), kSumThreads, 0, s>>>(p.part, p.blocks,
                                                                                                  (int)x.D, x.dgain);
     return hipGetLastError();
 }

@@ -125,6 +125,7 @@ LIB = _load()
 
 
 _DTYPES = {torch.float32: EMBER_F32, torch.bfloat16: EMBER_BF16}
+_CHUNK = {torch.float32: 4, torch.bfloat16: 8, torch.int8: 16}   # elements of 16 bytes
 
 
 def _dtype(t: torch.Tensor) -> int:
@@ -372,8 +373,12 @@ def _matrix(what, t, shape, dtype=None):
         _misfit(what, t, shape, dtype)
     if len(shape) == 2:
         ld, unit = t.stride()
-        if unit == 1 and shape[0] > 1:
-            return t.data_ptr(), ld
+        if unit == 1:
+            if shape[0] > 1:
+                return t.data_ptr(), ld
+            q = _CHUNK.get(t.dtype)
+            if q is not None:   # one row, as _ld has it
+                return t.data_ptr(), (shape[1] + q - 1) // q * q
     return t.data_ptr(), _ld(t)
 
 

@@ -221,11 +221,14 @@ def grad64(dY, S, gain, rstd, dS):
 
 
 @pytest.mark.parametrize("T,D", SHAPES + [(300, 896), (1500, 72), (2500, 1000), (1100, 4096),
-                                          # one block alone, and the first count with two launches
+                                          # one block, and a few
                                           (64, 512), (65, 512), (16, 2048), (17, 2048), (8, 4096), (9, 4096), (4, 8192),
                                           (5, 8192), (4, 32768), (5, 32768),
                                           # rows that end inside a chunk, many
-                                          (5000, 700), (2000, 2047), (700, 3001), (1500, 300), (5000, 513)])
+                                          (5000, 700), (2000, 2047), (700, 3001), (1500, 300), (5000, 513),
+                                          # dgain in the same launch, and the first counts without
+                                          (512, 300), (513, 300), (100, 96), (512, 1000), (300, 2047), (512, 4096), (513, 4096),
+                                          (200, 8192), (512, 9000), (70, 20000)])
 @pytest.mark.parametrize("dtype,gdtype,other", [(BF, F, True), (F, BF, False)])
 def test_gradient(em, T, D, dtype, gdtype, other):
     print(f"rmsnorm grad T={T} D={D} {dtype} gain {gdtype} dS={other}", flush=True)
