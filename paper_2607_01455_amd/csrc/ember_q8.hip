@@ -144,10 +144,10 @@ struct Epilogue {
 // 3381 fp32 165 / 161, 1500 x 50000 x 1024 106 / 103).
 template <typename C>
 constexpr bool kGoesOn = C::KG == 1 && C::kLds > 80 * 1024;
+template <typename C>
+constexpr int kEpilogueAt = kGoesOn<C> ? C::kStageBytes : 0;   // in the LDS
 template <typename C, typename YT>
-constexpr int epilogue_at() { return kGoesOn<C> ? C::kStageBytes : 0; }
-template <typename C, typename YT>
-constexpr int lds_of() { return std::max(C::kLds, epilogue_at<C, YT>() + Epilogue<C, YT>::kBytes); }
+constexpr int kLdsBytes = std::max(C::kLds, kEpilogueAt<C> + Epilogue<C, YT>::kBytes);
 
 // Chunk c of a slice's row r sits at position c ^ swizzle(r): the reads of the
 // same chunk of 8 (or 16) consecutive rows then cover 32 (or all 64) LDS banks
@@ -161,7 +161,7 @@ __device__ __forceinline__ int swizzle(int r) {
 // that do not count; they are cleared in the tokens' operand.
 template <typename C, typename YT, bool kMask>
 __global__ __launch_bounds__(C::kThreads) void ember_logits_q8(Params p) {
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[lds_of<C, YT>()];
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[kLdsBytes<C, YT>];
     const LogitsArgs& a = p.a;
     const int lane = threadIdx.x & (kWave - 1);
     const int wave_all = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -378,8 +378,8 @@ __global__ __launch_bounds__(C::kThreads) void ember_logits_q8(Params p) {
         constexpr int kRowsPerPass = kWave / kLanesPerRow;
         constexpr int kEpc = 16 / kEs;
         static_assert(C::NT % kGroup == 0 && 32 % kRowsPerPass == 0 && C::kThreads >= C::BN, "whole strips");
-        uint8_t* const strip = lds + epilogue_at<C, YT>() + wave * (32 * kPitch);
-        float* const sw = reinterpret_cast<float*>(lds + epilogue_at<C, YT>() + E::kStrips);
+        uint8_t* const strip = lds + kEpilogueAt<C> + wave * (32 * kPitch);
+        float* const sw = reinterpret_cast<float*>(lds + kEpilogueAt<C> + E::kStrips);
         float* const sb = sw + C::BN;
         if ((int)threadIdx.x < C::BN) {
             sw[threadIdx.x] = my_wscale;
@@ -466,7 +466,7 @@ struct FewParams {
 // (KF blocks of 64 each) and hold their part of all the tokens as MFMA operands in
 // registers, loaded once; then they stream the table, SB strips of 16 channels a
 // round, straight from memory into the other operand, two rounds in flight.
-// They leave their sums of a round in LDS, where a ninth wave adds them up
+// They leave their sums of a round in LDS, where a ninth wave adds them up,
 // scales and stores them while the others go on (the streaming waves have no
 // memory operations but their loads, which return in order).  Columns past D are
 // zeros in the tokens' operand, so what the table's operand holds there (some
@@ -710,10 +710,6 @@ hipError_t launch_tiles(const LogitsArgs& a, hipStream_t s) {
     }
     return hipSuccess;
 }
-
-} // namespace
-
-namespace {
 
 using T64x128 = Tile<64, 128, 2, 2, 128, 3>;
 using T32x64 = Tile<32, 64, 1, 2, 128, 3, 4>;    // four and three groups of wavefronts share the steps
