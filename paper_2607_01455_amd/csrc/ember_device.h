@@ -42,7 +42,7 @@ template <typename T>
 __device__ __forceinline__ u32x4_t load_chunk(const T* row, int col, int D, bool follows) {
     u32x4_t w = {0, 0, 0, 0};
     if (col + kChunkElems<T> <= D || (follows && col < D)) {
-        w = *reinterpret_cast<const u32x4_t*>(row + col);
+        w = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(row + col));
     } else {
 #pragma unroll
         for (int e = 0; e < kChunkElems<T>; ++e) {

@@ -48,7 +48,6 @@ struct FwdParams {
     int64_t ldq;
     float* qscale;
     float* rstd;          // or null
-    bool stream;          // Y is stored non-temporally (S is in any case)
 };
 
 template <typename XT>
@@ -103,7 +102,7 @@ template <typename XT, bool kFull>
 __device__ __forceinline__ u32x4_t chunk_at(const XT* row, int col, int D, bool follows) {
     if constexpr (kFull) {
         u32x4_t w = {0, 0, 0, 0};
-        if (col < D) w = *reinterpret_cast<const u32x4_t*>(row + col);
+        if (col < D) w = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(row + col));
         return w;
     } else {
         return load_chunk<XT>(row, col, D, follows);
@@ -201,8 +200,10 @@ __global__ __launch_bounds__(threads_of(TPR)) void ember_rmsnorm_fwd(FwdParams a
 #pragma unroll
                 for (int e = 0; e < N; ++e) v[c][e] = v[c][e] * rstd * g[c][e];
                 if (a.Y) {
-                    if (a.y_bf16) store_at<uint16_t, N, kFull>(static_cast<uint16_t*>(a.Y) + t * a.ldy, col, D, v[c], a.stream);
-                    else store_at<float, N, kFull>(static_cast<float*>(a.Y) + t * a.ldy, col, D, v[c], a.stream);
+                    if (a.y_bf16)
+                        store_at<uint16_t, N, kFull>(static_cast<uint16_t*>(a.Y) + t * a.ldy, col, D, v[c], false);
+                    else
+                        store_at<float, N, kFull>(static_cast<float*>(a.Y) + t * a.ldy, col, D, v[c], false);
                 }
             }
         }
@@ -496,16 +497,15 @@ RowPlan row_plan(int D, int dtype, bool grad) {
     return p;
 }
 
-// What is read next is stored ordinarily while the caches can keep it, the rest
-// non-temporally.  S is not: it waits for the gradient (us, alone and with a
-// kernel that reads Y next, S ordinary / non-temporal: 16384 x 4096 bf16 94.8 / 93.5
-// and 132 / 128, 4096 x 4096 26.0 / 26.1 and 36.2 / 33.8).  Y is, and stays longer than
-// dX, which the norm's gradient writes beside more reading (Y ordinary / non-temporal,
-// S non-temporal: 4096 x 4096 26.1 / 21.0 and 33.8 / 37.1, 16384 x 4096 93.5 / 91.7 and
-// 128.1 / 129.4, 32768 x 4096 184 / 181 and 254 / 252; dX: 4096 x 4096 31.0 / 29.9 and
-// 41.7 / 42.8, 8192 x 4096 53.5 / 52.4 and 73.2 / 72.5, 16384 x 4096 102.5 / 98.6 and
-// 138 / 139).
-constexpr int64_t kKeptY = (int64_t)256 << 20, kKeptDX = (int64_t)48 << 20;
+// The caches are left to what is read next.  The inputs are read once, with
+// non-temporal loads, and S, which waits for the gradient, is stored so; Y ordinarily,
+// dX too while the caches can keep it (us, alone and with a kernel that reads Y or dX
+// next; 16384 x 4096 bf16: all ordinary 94.8 and 132, S non-temporal 93.5 and 128, the
+// loads too 93.6 and 116, Y too 91.0 and 126; 8192 x 4096 48.0 and 66.6, 48.3 and 65.3,
+// 43.1 and 60.3, 46.3 and 65.5; the gradient, ordinary loads / non-temporal / dX too:
+// 16384 x 4096 102 and 138, 95.5 and 123.5, 90.3 and 124.2, 12000 x 4096 76.7 and 104, 72.0
+// and 90.1, 68.8 and 94.2, 32768 x 4096 196 and 266, 185 and 243, 175 and 241).
+constexpr int64_t kKeptDX = (int64_t)128 << 20;
 int64_t bytes_of(int64_t T, int64_t D, int dtype) { return T * D * (dtype == EMBER_F32 ? 4 : 2); }
 
 template <typename XT, bool kNorm, bool kFull>
@@ -581,8 +581,7 @@ hipError_t launch_fwd_of(const FwdParams& p, bool norm, const RowPlan& pl, hipSt
 
 hipError_t launch_rmsnorm(const NormArgs& x, hipStream_t s) {
     FwdParams p{x.X, x.ldx, x.R, x.ldr, x.gain, x.gain_dtype == EMBER_BF16, x.eps, x.T, (int)x.D, x.S, x.lds,
-                x.Y, x.y_dtype == EMBER_BF16, x.ldy, x.Q, x.ldq, x.qscale, x.rstd,
-                x.Y && bytes_of(x.T, x.D, x.y_dtype) >= kKeptY};
+                x.Y, x.y_dtype == EMBER_BF16, x.ldy, x.Q, x.ldq, x.qscale, x.rstd};
     const RowPlan pl = row_plan((int)x.D, x.x_dtype, false);
     return x.x_dtype == EMBER_F32 ? launch_fwd_of<float>(p, x.gain != nullptr, pl, s)
                                   : launch_fwd_of<uint16_t>(p, x.gain != nullptr, pl, s);
