@@ -154,7 +154,8 @@ __global__ __launch_bounds__(threads_of(TPR)) void ember_rmsnorm_fwd(FwdParams a
     const int64_t step = (int64_t)gridDim.x * kRows;
     int64_t t = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR;
     float g[NC][N];
-    if constexpr (kNorm) {
+    constexpr bool kHoldGain = TPR < 1024 || NC <= 2;   // else there are no registers for it
+    if constexpr (kNorm && kHoldGain) {
 #pragma unroll
         for (int c = 0; c < NC; ++c) load_gain<XT>(a.gain, a.gain_bf16, (lane + c * TPR) * N, D, g[c]);
     }
@@ -170,16 +171,19 @@ __global__ __launch_bounds__(threads_of(TPR)) void ember_rmsnorm_fwd(FwdParams a
                 wr[c] = chunk_at<XT, kFull>(static_cast<const XT*>(a.R) + t * a.ldr, (lane + c * TPR) * N, D, follows);
         }
         float v[NC][N];
+        int kl = lane;
+        // what counts (and a gain that is not held) is formed anew for each row, not kept in registers
+        if constexpr (!kFull || !kHoldGain) asm volatile("" : "+v"(kl));
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-            const u32x4_t keep = kept_words<XT>((lane + c * TPR) * N, D);
+            const u32x4_t keep = kept_words<XT>((kl + c * TPR) * N, D);
 #pragma unroll
             for (int e = 0; e < N; ++e) v[c][e] = elem_at<XT, kFull>(wx[c], e, keep);
         }
         if (kNorm && a.R) {
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
-                const u32x4_t keep = kept_words<XT>((lane + c * TPR) * N, D);
+                const u32x4_t keep = kept_words<XT>((kl + c * TPR) * N, D);
 #pragma unroll
                 for (int e = 0; e < N; ++e) v[c][e] += elem_at<XT, kFull>(wr[c], e, keep);
             }
@@ -197,6 +201,7 @@ __global__ __launch_bounds__(threads_of(TPR)) void ember_rmsnorm_fwd(FwdParams a
             for (int c = 0; c < NC; ++c) {
                 const int col = (lane + c * TPR) * N;
                 if (a.S) store_at<XT, N, kFull>(static_cast<XT*>(a.S) + t * a.lds, col, D, v[c], true);
+                if constexpr (!kHoldGain) load_gain<XT>(a.gain, a.gain_bf16, (kl + c * TPR) * N, D, g[c]);
 #pragma unroll
                 for (int e = 0; e < N; ++e) v[c][e] = v[c][e] * rstd * g[c][e];
                 if (a.Y) {
@@ -347,10 +352,11 @@ __global__ __launch_bounds__(TPR * kGroups) void ember_rmsnorm_bwd(GradParams a)
     const int64_t step = (int64_t)a.blocks * kGroups;
     const int64_t rounds = (a.T - (int64_t)blockIdx.x * kGroups + step - 1) / step;   // of the block: all its threads take part
     int64_t t = (int64_t)blockIdx.x * kGroups + group;
+    constexpr bool kHoldGain = NC <= 2;   // else there are no registers for it
     float g[NC][N], acc[NC][N];
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-        load_gain<XT>(a.gain, a.gain_bf16, (lane + c * TPR) * N, D, g[c]);
+        if constexpr (kHoldGain) load_gain<XT>(a.gain, a.gain_bf16, (lane + c * TPR) * N, D, g[c]);
 #pragma unroll
         for (int e = 0; e < N; ++e) acc[c][e] = 0.0f;
     }
@@ -390,8 +396,11 @@ __global__ __launch_bounds__(TPR * kGroups) void ember_rmsnorm_bwd(GradParams a)
         }
         if (kAhead && i + 1 < rounds) load(t + step);
         float k = 0.0f;
+        int kl = lane;
+        if constexpr (!kHoldGain) asm volatile("" : "+v"(kl));
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
+            if constexpr (!kHoldGain) load_gain<XT>(a.gain, a.gain_bf16, (kl + c * TPR) * N, D, g[c]);
 #pragma unroll
             for (int e = 0; e < N; ++e) {
                 const float p = elem<XT>(wy[c], e) * elem<XT>(ws[c], e);
@@ -411,8 +420,10 @@ __global__ __launch_bounds__(TPR * kGroups) void ember_rmsnorm_bwd(GradParams a)
         }
         const float ks = k / (float)D * rstd * rstd * rstd;
         if (there) {
+            if constexpr (!kHoldGain) asm volatile("" : "+v"(kl));
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
+                if constexpr (!kHoldGain) load_gain<XT>(a.gain, a.gain_bf16, (kl + c * TPR) * N, D, g[c]);
                 float d[N];
 #pragma unroll
                 for (int e = 0; e < N; ++e) d[e] = elem<XT>(wy[c], e) * g[c][e] * rstd - ks * elem<XT>(ws[c], e);
