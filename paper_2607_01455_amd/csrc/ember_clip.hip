@@ -211,7 +211,8 @@ struct Shared {
         row = base / t.pieces;
         x0 = (int)(base - row * t.pieces);
         there = t.rows - row;
-        held = t.rows_dev ? min(*t.rows_dev - row, there) : there;
+        // the count before the difference: it may be any int64
+        held = t.rows_dev ? min(max(*t.rows_dev, (int64_t)0) - row, there) : there;
         tail = (int)t.cols - t.pieces * N;
         tails = (int)min((int64_t)(((uint32_t)(x0 + kPerRun) * t.inverse) >> 20), there);
     }

@@ -254,3 +254,19 @@ def test_on_another_stream_and_in_a_graph(em):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(x, y) for x, y in zip(want, outs)), k
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("rows,cols,pad", [(700, 8, 8), (1500, 107, 5), (64, 5000, 0)])
+def test_counts_at_the_ends_of_int64(em, rows, cols, pad, dtype):
+    """A count outside [0, rows] counts as the nearer end, however far outside it is."""
+    print(f"clip counts {rows} x {cols} {dtype}", flush=True)
+    least = -(1 << 63)
+    for count in (least, least + 1, least + rows - 1, least + 10 * rows, -1, (1 << 63) - 1):
+        for limit in (1e9, 0.5):
+            g = randn(rows, cols + pad, dtype=dtype)[:, :cols]
+            c = torch.tensor([count], dtype=torch.int64, device=DEV)
+            check(em, [g, randn(100)], limit, counts=[c, None])
+            g = randn(rows, cols + pad, dtype=dtype)[:, :cols]
+            check(em, [g, randn(100)], limit, out=[torch.full((rows, cols), 9.0, device=DEV), torch.zeros(100, device=DEV)],
+                  counts=[c, None])
