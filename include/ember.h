@@ -423,6 +423,9 @@ int ember_lmhead_step(void* W, int w_dtype, int64_t ldw,
  *                        that holds an infinity or a NaN has codes 0 and scale
  *                        NaN, which makes its logits NaN;
  *   rstd (T)             kept for the gradient.
+ * The mean square of a finite row is right over the whole range of x_dtype, also where
+ * squares leave that of fp32.  With an eps that does not bound it, rstd itself is infinite
+ * for rows whose root mean square is below 3e-39 (y is then not finite).
  * X, R (x_dtype), S, Y: layout rules of W and G; between two rows the padding up to
  * the next 16-byte boundary may be read, its values do not matter.  Q: 16-byte aligned, ldq a
  * multiple of 16 below EMBER_Q8_MAX_LD; columns D..ldq-1 are not written.  gain: D values of

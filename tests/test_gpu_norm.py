@@ -336,3 +336,57 @@ def test_on_another_stream_and_in_a_graph(em):
         graph.replay()
         torch.cuda.synchronize()
         assert same(want), k
+
+
+def rows_of_range(T, D, dtype, tiny, g):
+    """Rows of magnitudes whose squares, or their sums, leave the fp32 range: above it
+    (among them single large values, and numbers next to the largest), or below it."""
+    X = padded(T, D, dtype, 1)
+    x = torch.randn(T, D, generator=g, device=DEV)
+    sizes = [1.0, 1e-20, 1e-24, 1e-30, 1e-36] if tiny else [1.0, 1e18, 2e19, 1e30, 1e37]
+    for t in range(T):
+        k = t % 7
+        if k < 5:
+            x[t] *= sizes[k]
+        elif k == 5:     # one value apart from the others
+            x[t, t % D] = 1e-24 if tiny else 3e19
+            if tiny:
+                x[t, torch.arange(D, device=DEV) != t % D] = 0.0
+        elif not tiny:
+            x[t] = (2 * torch.rand(D, generator=g, device=DEV) - 1) * 3e38
+        else:
+            x[t] *= 1e-15
+    return X.copy_(x)
+
+
+def range_forward(em, T, D, dtype, tiny, eps):
+    g = torch.Generator(device=DEV).manual_seed(T + D)
+    X = rows_of_range(T, D, dtype, tiny, g)
+    gain = 0.5 + torch.rand(D, generator=g, device=DEV)
+    norm = em.HeadNorm(gain, eps, max_tokens=T)
+    Y, Q, qs, rstd = padded(T, D, F), padded(T, D, torch.int8), torch.zeros(T, device=DEV), torch.zeros(T, device=DEV)
+    norm(X, Y=Y, Q=Q, qscale=qs, rstd=rstd)
+    return norm, g, X, gain, Y, Q, qs, rstd
+
+
+RANGES = [(False, EPS), (False, 0.0), (False, 1e38), (True, 0.0), (True, 1e-44)]
+RANGE_SHAPES = [(14, 40), (7, 1023), (9, 2048), (600, 300), (21, 5000), (7, 8192), (8, 20000), (7, 32768)]
+
+
+@pytest.mark.parametrize("tiny,eps", RANGES)
+@pytest.mark.parametrize("T,D", RANGE_SHAPES)
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_squares_past_the_range_of_fp32(em, T, D, dtype, tiny, eps):
+    """A row's mean square, and so everything made of it, is right wherever rstd itself
+    is an fp32 number (below 2^-126 it is held to 2^-150)."""
+    print(f"rmsnorm range T={T} D={D} {dtype} tiny={tiny} eps={eps}", flush=True)
+    _, _, X, gain, Y, Q, qs, rstd = range_forward(em, T, D, dtype, tiny, eps)
+    s = X.double()
+    rs = (s.square().mean(dim=1) + torch.tensor(eps, dtype=F).double().item()).rsqrt()
+    y = s * rs[:, None] * gain.double()
+    assert ((rstd.double() - rs).abs() <= 64 * U * rs + 2.0 ** -150).all()
+    # (2^-150 is at most 4 u of an rstd above 2.9e-39)
+    assert ((Y.double() - y).abs() <= 72 * U * y.abs() + 1e-37).all()
+    normal = y.abs().amax(dim=1) > 1e-30
+    assert normal.any()
+    check_codes(Q[normal], qs[normal], y[normal])
