@@ -6,8 +6,9 @@
 // and scale a / 127.  The sum stays in fp32 from the addition to y: the rounded
 // s that is stored is an output, not what y is made of.
 //
-// Gradient, with u = dy gain and k = mean_j u_j s_j:
-//   dx_j = rstd u_j - rstd^3 k s_j + ds_j,   dgain_j = sum_t dy_tj s_tj rstd_t.
+// Gradient, with u = dy gain, h = s rstd and k = mean_j u_j h_j:
+//   dx_j = rstd (u_j - k h_j) + ds_j,   dgain_j = sum_t dy_tj h_tj.
+// h is formed first, so that no product leaves the fp32 range where s is far from 1.
 //
 // One pass over the data each (but the gradient of few tokens, see kSumAtOnceT).  TPR
 // threads hold a row between its loads, its one or two reductions and its stores,
@@ -318,7 +319,7 @@ __device__ __forceinline__ void sum_dgain(const GradParams& a, int first_chunk, 
                     const bool there = (int64_t)b * kGroups + ug + (int64_t)ui * step < a.T;
 #pragma unroll
                     for (int e = 0; e < N; ++e) {
-                        const float term = __builtin_fmaf(elem<XT>(wy[u], e) * elem<XT>(ws[u], e), r[u], acc[e]);
+                        const float term = __builtin_fmaf(elem<XT>(wy[u], e), elem<XT>(ws[u], e) * r[u], acc[e]);
                         acc[e] = there ? term : acc[e];
                     }
                     if (++ui == rounds) {
@@ -424,9 +425,9 @@ __global__ __launch_bounds__(TPR * kGroups) void ember_rmsnorm_bwd(GradParams a)
             if constexpr (!kHoldGain) load_gain<XT>(a.gain, a.gain_bf16, (kl + c * TPR) * N, D, g[c]);
 #pragma unroll
             for (int e = 0; e < N; ++e) {
-                const float p = elem<XT>(wy[c], e) * elem<XT>(ws[c], e);
-                k += p * g[c][e];
-                if (there) acc[c][e] = __builtin_fmaf(p, rstd, acc[c][e]);
+                const float dy = elem<XT>(wy[c], e), h = elem<XT>(ws[c], e) * rstd;
+                k += dy * g[c][e] * h;
+                if (there) acc[c][e] = __builtin_fmaf(dy, h, acc[c][e]);
             }
         }
         // by hand over the row's waves: the block's other rows have slots of their own
@@ -439,7 +440,7 @@ __global__ __launch_bounds__(TPR * kGroups) void ember_rmsnorm_bwd(GradParams a)
 #pragma unroll
             for (int w = 1; w < kRowWaves; ++w) k += slot[w];
         }
-        const float ks = k / (float)D * rstd * rstd * rstd;
+        k /= (float)D;
         if (there) {
             if constexpr (!kHoldGain) asm volatile("" : "+v"(kl));
 #pragma unroll
@@ -447,7 +448,7 @@ __global__ __launch_bounds__(TPR * kGroups) void ember_rmsnorm_bwd(GradParams a)
                 if constexpr (!kHoldGain) load_gain<XT>(a.gain, a.gain_bf16, (kl + c * TPR) * N, D, g[c]);
                 float d[N];
 #pragma unroll
-                for (int e = 0; e < N; ++e) d[e] = elem<XT>(wy[c], e) * g[c][e] * rstd - ks * elem<XT>(ws[c], e);
+                for (int e = 0; e < N; ++e) d[e] = (elem<XT>(wy[c], e) * g[c][e] - k * (elem<XT>(ws[c], e) * rstd)) * rstd;
                 if (a.dS) {
 #pragma unroll
                     for (int e = 0; e < N; ++e) d[e] += elem<XT>(wd[c], e);

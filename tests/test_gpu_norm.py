@@ -390,3 +390,25 @@ def test_squares_past_the_range_of_fp32(em, T, D, dtype, tiny, eps):
     normal = y.abs().amax(dim=1) > 1e-30
     assert normal.any()
     check_codes(Q[normal], qs[normal], y[normal])
+
+
+@pytest.mark.parametrize("tiny,eps", RANGES)
+@pytest.mark.parametrize("T,D", RANGE_SHAPES)
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_gradient_past_the_range_of_fp32(em, T, D, dtype, tiny, eps):
+    """Rows whose squares leave the fp32 range have a gradient like others."""
+    print(f"rmsnorm grad range T={T} D={D} {dtype} tiny={tiny} eps={eps}", flush=True)
+    norm, g, X, gain, _, _, _, rstd = range_forward(em, T, D, dtype, tiny, eps)
+    dY, dX = padded(T, D, dtype, 2), padded(T, D, dtype)
+    dY.copy_(torch.randn(T, D, generator=g, device=DEV))
+    dgain, dgain2 = torch.zeros(D, device=DEV), torch.zeros(D, device=DEV)
+    norm.grad(dY, X, rstd, dX, dgain)
+    dx, A, dg, mag = grad64(dY, X, gain, rstd, None)
+    inside = dx.abs() < 1e37      # of tiny rows; beyond lies the end of the range
+    assert inside.any()
+    # what is below 2^-126 is held to 2^-149 (bf16: 2^-134, after a rounding of 2^-150)
+    bar = 100 * U * A + (2.0 ** -8 * dx.abs() + 2.0 ** -133 if dtype == BF else 2.0 ** -148)
+    assert ((dX.double() - dx).abs() <= bar)[inside].all()
+    assert ((dgain.double() - dg).abs() <= (T + 3) * U * mag + 1e-37).all()
+    norm.grad(dY, X, rstd, dY, dgain2)
+    assert torch.equal(bits(dY), bits(dX)) and torch.equal(bits(dgain2), bits(dgain))
