@@ -33,7 +33,9 @@ constexpr int kXcds = 8;
 constexpr int kCus = 256;
 constexpr uint32_t kRotate = 5;            // steps between the first steps of neighbouring tiles
 constexpr int kBufferWord3 = 0x00020000;   // raw 32-bit data format, gfx9 family
-constexpr int kBufferMax = 0x7FFFFFF0;     // bytes of a buffer at most; an offset past every buffer
+// Bytes of a buffer at most; an offset past every buffer, also with what is added to it
+// (unsigned: below 2^30 + 2^12).
+constexpr uint32_t kBufferMax = 0x7FFFFFF0;
 
 struct Params {
     LogitsArgs a;
@@ -54,7 +56,7 @@ __device__ __forceinline__ i32x4 rsrc(const void* base, int64_t bytes) {
     i32x4 r;
     r.x = __builtin_amdgcn_readfirstlane((int)p);
     r.y = __builtin_amdgcn_readfirstlane((int)(p >> 32) & 0xFFFF);
-    r.z = __builtin_amdgcn_readfirstlane(bytes > kBufferMax ? kBufferMax : bytes < 0 ? 0 : (int)bytes);
+    r.z = __builtin_amdgcn_readfirstlane(bytes > kBufferMax ? (int)kBufferMax : bytes < 0 ? 0 : (int)bytes);
     r.w = kBufferWord3;
     return r;
 }
@@ -63,7 +65,7 @@ __device__ __forceinline__ i32x4 rsrc(const void* base, int64_t bytes) {
 // the buffer's range write zeros.  Inline assembly, so that the compiler does
 // not make every later LDS read wait for it; completion is awaited with
 // wait_step before a stage is read.  M0 holds the (wave-uniform) LDS base.
-__device__ __forceinline__ void load_to_lds(i32x4 rs, uint32_t lds_base, int voffset) {
+__device__ __forceinline__ void load_to_lds(i32x4 rs, uint32_t lds_base, uint32_t voffset) {
     const uint32_t base = __builtin_amdgcn_readfirstlane(lds_base);
     uint32_t saved;
     asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\t"
@@ -201,10 +203,10 @@ __global__ __launch_bounds__(C::kThreads) void ember_logits_q8(Params p) {
     static_assert(C::kWavesB % 2 == 0 && C::kLoadsA % C::kWavesB == 0, "one load_k for all loads, each of one operand");
     const int load_row = wave * C::kRowsPerLoad + lane / C::kChunks;
     const int load_k = ((lane % C::kChunks) ^ swizzle<C::kChunks>(load_row)) * 16;
-    const int load_a = load_row * (int)a.ldx + load_k, load_b = load_row * (int)a.ldw + load_k;
+    const uint32_t load_a = load_row * (uint32_t)a.ldx + load_k, load_b = load_row * (uint32_t)a.ldw + load_k;
     struct StepLoads {
         i32x4 ra, rb;
-        int oa, ob;
+        uint32_t oa, ob;
     };
     // step i of this wave's group
     auto loads_of = [&](int i) {
@@ -226,7 +228,7 @@ __global__ __launch_bounds__(C::kThreads) void ember_logits_q8(Params p) {
     };
     auto issue_one = [&](const StepLoads& sl, uint32_t st, int j) {
         constexpr int kA = C::kLoadsA / C::kWavesB, kRows = C::kWavesB * C::kRowsPerLoad;
-        const int o = j < kA ? sl.oa + j * (kRows * (int)a.ldx) : sl.ob + (j - kA) * (kRows * (int)a.ldw);
+        const uint32_t o = j < kA ? sl.oa + j * (kRows * (uint32_t)a.ldx) : sl.ob + (j - kA) * (kRows * (uint32_t)a.ldw);
         load_to_lds(j < kA ? sl.ra : sl.rb, st + (wave + C::kWavesB * j) * (C::kRowsPerLoad * C::KS), o);
     };
 
@@ -577,7 +579,7 @@ __global__ __launch_bounds__(kFewThreads) void ember_logits_few(FewParams p) {
     // rows past the table (a round past the last one reads nothing), so that
     // every round has the same loads.
     const int col0 = wave * (KF * 64) + 16 * quarter;
-    const int row_off = row * (int)a.ldw + col0;
+    const uint32_t row_off = row * (uint32_t)a.ldw + col0;
     const int64_t row_end = (a.D + 15) / 16 * 16;   // of the last row that is read
     auto load = [&](int i, int h, i32x4 (&w)[SB][KF]) {
         const int64_t v0 = channel(i);
@@ -587,9 +589,10 @@ __global__ __launch_bounds__(kFewThreads) void ember_logits_few(FewParams p) {
             const auto rs = buffer(a.Wq + (v < a.V ? v * a.ldw : 0), v < a.V ? (a.V - 1 - v) * a.ldw + row_end : 0);
 #pragma unroll
             for (int f = 0; f < KF; ++f) {
+                // all of the column in the offset that the buffer's range is checked against
                 const int at = (h * kFewWaves * KF + f) * 64;
-                const int off = col0 + at < D ? row_off : kBufferMax;
-                w[s][f] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, off + f * 64, at - f * 64, 0));
+                const uint32_t off = (col0 + at < D ? row_off : kBufferMax) + at;
+                w[s][f] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, off, 0, 0));
             }
         }
     };

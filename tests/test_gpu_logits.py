@@ -206,3 +206,16 @@ def test_on_another_stream_and_in_a_graph(em):
             graph.replay()
             torch.cuda.synchronize()
             assert torch.equal(Y, want), (T, k)
+
+
+@pytest.mark.parametrize("V", [1, 2, 5, 15, 16, 17])
+@pytest.mark.parametrize("T,D", [(1, 2500), (16, 4096), (17, 2064), (32, 4000), (33, 1100), (64, 2048), (3, 100)])
+def test_tables_shorter_than_a_strip(em, T, V, D):
+    """Fewer channels than a streaming round takes, with rounds past the table: columns in
+    two parts, of which the second one's loads end with the table too."""
+    print(f"logits T={T} V={V} D={D}", flush=True)
+    Xq, Wq = codes(T, D, T + D, 0, -128), codes(V, D, V + D, 0, -128)
+    Y = out(T, V, F)
+    em.ember_logits_q8(Xq, torch.ones(T, device=DEV), Wq, torch.ones(V, device=DEV), Y)
+    assert torch.equal(Y, sums(Xq, Wq).float())
+    assert torch.isnan(Y._base[:, V:]).all()
