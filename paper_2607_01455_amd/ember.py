@@ -631,9 +631,9 @@ def ember_profile_enable(enable: bool) -> None:
 
 def ember_profile_collect() -> dict:
     """{kernel name: (launches, total milliseconds)} since the last collect."""
-    buf = (_KernelStat * 16)()
+    buf = (_KernelStat * 64)()    # more than the library has names
     n = ctypes.c_int(0)
-    _check(LIB.ember_profile_collect(buf, 16, ctypes.byref(n)), "ember_profile_collect")
+    _check(LIB.ember_profile_collect(buf, len(buf), ctypes.byref(n)), "ember_profile_collect")
     return {buf[k].name.decode(): (buf[k].launches, buf[k].total_ms) for k in range(n.value)}
 
 

@@ -3,6 +3,7 @@ rejected on the host with the documented status codes before the device is
 touched (no GPU is needed), and the binding refuses tensors that do not fit."""
 import ctypes
 import os
+import re
 
 import pytest
 import torch
@@ -208,3 +209,25 @@ def test_binding_refuses_tensors_that_do_not_fit(em):
         em.GradClipper([])
     with pytest.raises(ValueError):
         em.GradClipper([X, X], out=[X])
+
+
+def test_profile_takes_every_kernel_the_library_names(em, monkeypatch):
+    """ember_profile_collect of the binding has room for all the names that the library times."""
+    names = set()
+    csrc = os.path.join(ROOT, "paper_2607_01455_amd", "csrc")
+    for f in os.listdir(csrc):
+        if f.endswith((".cpp", ".hip", ".h")):
+            names |= set(re.findall(r'timed\("(\w+)"', open(os.path.join(csrc, f)).read()))
+    assert "ember_clip_grads" in names and "ember_stats" in names
+
+    class Lib:
+        @staticmethod
+        def ember_profile_collect(buf, room, n):
+            k = min(room, len(names))
+            for i, name in zip(range(k), sorted(names)):
+                buf[i].name, buf[i].launches, buf[i].total_ms = name.encode(), 1, 0.5
+            n._obj.value = k
+            return em.EMBER_OK
+
+    monkeypatch.setattr(em, "LIB", Lib)
+    assert set(em.ember_profile_collect()) == names
