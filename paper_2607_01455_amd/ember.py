@@ -356,21 +356,26 @@ def ember_lmhead_step(W: torch.Tensor, dY: torch.Tensor, H: torch.Tensor, G: tor
 
 
 # The C entry points know pointers and the sizes they are given, not what memory
-# lies behind them: these refuse a tensor that would be indexed past its end.
+# lies behind them: these refuse a tensor that would be indexed past its end, and one
+# that is not on the call's GPU.
 
-def _misfit(what, t, shape, dtype):
+def _misfit(what, t, shape, device, dtype):
+    if t.get_device() != device:
+        raise ValueError(f"{what}: on {t.device}, the call's tensors are on " +
+                         (f"cuda:{device}" if device >= 0 else "the host"))
     if t.shape != shape:
         raise ValueError(f"{what}: shape {tuple(t.shape)}, expected {tuple(shape)}")
     raise TypeError(f"{what}: a contiguous {dtype or 'tensor'} is required" if len(shape) == 1 else
                     f"{what}: {t.dtype}, expected {dtype}")
 
 
-def _matrix(what, t, shape, dtype=None):
-    """(address, row stride) of a 2-D tensor of this shape and type; None: no tensor."""
+def _matrix(what, t, shape, device, dtype=None):
+    """(address, row stride) of a 2-D tensor of this shape and type on this GPU (its
+    index); None: no tensor."""
     if t is None:
         return None, 0
-    if t.shape != shape or (dtype is not None and t.dtype is not dtype):
-        _misfit(what, t, shape, dtype)
+    if t.shape != shape or t.get_device() != device or (dtype is not None and t.dtype is not dtype):
+        _misfit(what, t, shape, device, dtype)
     if len(shape) == 2:
         ld, unit = t.stride()
         if unit == 1:
@@ -382,13 +387,21 @@ def _matrix(what, t, shape, dtype=None):
     return t.data_ptr(), _ld(t)
 
 
-def _vector(what, t, shape, dtype=torch.float32):
-    """Address of a contiguous 1-D tensor of this shape and type; None: no tensor."""
+def _vector(what, t, shape, device, dtype=torch.float32):
+    """Address of a contiguous 1-D tensor of this shape and type on this GPU; None: no tensor."""
     if t is None:
         return None
-    if t.shape != shape or (dtype is not None and t.dtype is not dtype) or not t.is_contiguous():
-        _misfit(what, t, shape, dtype)
+    if t.shape != shape or t.get_device() != device or (dtype is not None and t.dtype is not dtype) or \
+            not t.is_contiguous():
+        _misfit(what, t, shape, device, dtype)
     return t.data_ptr()
+
+
+def _workspace(ws, device):
+    """Address and bytes of a workspace on this GPU."""
+    if ws.get_device() != device:
+        _misfit("ws", ws, ws.shape, device, None)
+    return ws.data_ptr(), ws.numel() * ws.element_size()
 
 
 def ember_rmsnorm(X: torch.Tensor, gain: torch.Tensor, eps: float = 1e-6, R: torch.Tensor | None = None,
@@ -396,17 +409,17 @@ def ember_rmsnorm(X: torch.Tensor, gain: torch.Tensor, eps: float = 1e-6, R: tor
                   qscale: torch.Tensor | None = None, rstd: torch.Tensor | None = None) -> None:
     """S = X + R and its root-mean-square norm with gains, to Y and, in 8 bits
     with one scale a row, to (Q, qscale); rstd is kept for the gradient."""
-    shape, dtype = X.shape, X.dtype
-    x, ldx = _matrix("X", X, shape)
-    r, ldr = _matrix("R", R, shape, dtype)
-    sm, lds = _matrix("S", S, shape, dtype)
-    y, ldy = _matrix("Y", Y, shape)
-    q, ldq = _matrix("Q", Q, shape, torch.int8)
+    shape, dtype, dev = X.shape, X.dtype, X.get_device()
+    x, ldx = _matrix("X", X, shape, dev)
+    r, ldr = _matrix("R", R, shape, dev, dtype)
+    sm, lds = _matrix("S", S, shape, dev, dtype)
+    y, ldy = _matrix("Y", Y, shape, dev)
+    q, ldq = _matrix("Q", Q, shape, dev, torch.int8)
     T, D = shape
     rows = (T,)
-    _check(LIB.ember_rmsnorm(x, _DTYPES.get(dtype, 99), ldx, r, ldr, _vector("gain", gain, (D,), None),
+    _check(LIB.ember_rmsnorm(x, _DTYPES.get(dtype, 99), ldx, r, ldr, _vector("gain", gain, (D,), dev, None),
                              _dtype(gain), eps, T, D, sm, lds, y, EMBER_F32 if Y is None else _dtype(Y), ldy, q, ldq,
-                             _vector("qscale", qscale, rows), _vector("rstd", rstd, rows), _stream(X)),
+                             _vector("qscale", qscale, rows, dev), _vector("rstd", rstd, rows, dev), _stream(X)),
            "ember_rmsnorm")
 
 
@@ -422,26 +435,27 @@ def ember_rmsnorm_grad(dY: torch.Tensor, S: torch.Tensor, gain: torch.Tensor, rs
                        dS: torch.Tensor | None = None) -> None:
     """Gradient of ember_rmsnorm: dX (of X and of R) and dgain from dY, the sum S
     and rstd of the forward call, plus dS, the sum's gradient by other ways."""
-    shape, dtype = S.shape, S.dtype
-    s, lds = _matrix("S", S, shape)
-    dy, lddy = _matrix("dY", dY, shape, dtype)
-    dx, lddx = _matrix("dX", dX, shape, dtype)
-    ds, ldds = _matrix("dS", dS, shape, dtype)
+    shape, dtype, dev = S.shape, S.dtype, S.get_device()
+    s, lds = _matrix("S", S, shape, dev)
+    dy, lddy = _matrix("dY", dY, shape, dev, dtype)
+    dx, lddx = _matrix("dX", dX, shape, dev, dtype)
+    ds, ldds = _matrix("dS", dS, shape, dev, dtype)
     T, D = shape
     cols = (D,)
-    _check(LIB.ember_rmsnorm_grad(dy, lddy, s, _DTYPES.get(dtype, 99), lds, _vector("gain", gain, cols, None),
-                                  _dtype(gain), _vector("rstd", rstd, (T,)), ds, ldds, T, D, dx, lddx,
-                                  _vector("dgain", dgain, cols), ws.data_ptr(), ws.numel() * ws.element_size(),
-                                  _stream(dgain)), "ember_rmsnorm_grad")
+    w, w_bytes = _workspace(ws, dev)
+    _check(LIB.ember_rmsnorm_grad(dy, lddy, s, _DTYPES.get(dtype, 99), lds, _vector("gain", gain, cols, dev, None),
+                                  _dtype(gain), _vector("rstd", rstd, (T,), dev), ds, ldds, T, D, dx, lddx,
+                                  _vector("dgain", dgain, cols, dev), w, w_bytes, _stream(dgain)),
+           "ember_rmsnorm_grad")
 
 
 def ember_quantize_rows(X: torch.Tensor, Q: torch.Tensor, qscale: torch.Tensor) -> None:
     """Rows of X in 8 bits: codes Q and one scale a row."""
-    shape = X.shape
-    x, ldx = _matrix("X", X, shape)
-    q, ldq = _matrix("Q", Q, shape, torch.int8)
+    shape, dev = X.shape, X.get_device()
+    x, ldx = _matrix("X", X, shape, dev)
+    q, ldq = _matrix("Q", Q, shape, dev, torch.int8)
     rows, D = shape
-    _check(LIB.ember_quantize_rows(x, _dtype(X), ldx, rows, D, q, ldq, _vector("qscale", qscale, (rows,)),
+    _check(LIB.ember_quantize_rows(x, _dtype(X), ldx, rows, D, q, ldq, _vector("qscale", qscale, (rows,), dev),
                                    _stream(X)), "ember_quantize_rows")
 
 
@@ -450,12 +464,13 @@ def ember_logits_q8(Xq: torch.Tensor, xscale: torch.Tensor, Wq: torch.Tensor, ws
     """Y = (Xq Wq^T) xscale wscale + bias: logits of T tokens from 8-bit hidden
     states and an 8-bit table, each with one scale a row."""
     T, D = Xq.shape
-    V = wscale.numel()
-    x, ldx = _matrix("Xq", Xq, (T, D), torch.int8)
-    w, ldw = _matrix("Wq", Wq, (V, D), torch.int8)
-    y, ldy = _matrix("Y", Y, (T, V))
-    _check(LIB.ember_logits_q8(x, ldx, _vector("xscale", xscale, (T,)), w, ldw, _vector("wscale", wscale, (V,)),
-                               _vector("bias", bias, (V,)), T, V, D, y, _dtype(Y), ldy, _stream(Wq)),
+    V, dev = wscale.numel(), Wq.get_device()
+    x, ldx = _matrix("Xq", Xq, (T, D), dev, torch.int8)
+    w, ldw = _matrix("Wq", Wq, (V, D), dev, torch.int8)
+    y, ldy = _matrix("Y", Y, (T, V), dev)
+    _check(LIB.ember_logits_q8(x, ldx, _vector("xscale", xscale, (T,), dev), w, ldw,
+                               _vector("wscale", wscale, (V,), dev), _vector("bias", bias, (V,), dev), T, V, D, y,
+                               _dtype(Y), ldy, _stream(Wq)),
            "ember_logits_q8")
 
 
@@ -468,10 +483,14 @@ def ember_clip_workspace_bytes(n_grads: int) -> int:
 def grad_entry(src: torch.Tensor, dst: torch.Tensor | None = None, rows_dev: torch.Tensor | None = None) -> Grad:
     """One entry of ember_clip_grads: the gradient src, written clipped to dst
     (None: in place); rows_dev: a device int64 of one element that says how many
-    of its rows hold a gradient (the others become zeros).  A 2-D tensor with unit column stride, or any
-    contiguous one.  The tensors must stay alive until the call has run."""
+    of its rows hold a gradient (the others become zeros), all of them on one GPU.  A 2-D tensor with
+    unit column stride, or any contiguous one.  The tensors must stay alive until the call has run."""
     if dst is None:
         dst = src
+    dev = src.get_device()
+    for what, t in (("gradient", src), ("destination", dst), ("rows_dev", rows_dev)):
+        if t is not None and (dev < 0 or t.get_device() != dev):
+            raise ValueError(f"{what}: on {t.device}; a gradient, its destination and its count are on one GPU")
     if dst.shape != src.shape:
         raise ValueError(f"gradient {tuple(src.shape)} does not fit its destination {tuple(dst.shape)}")
     if rows_dev is not None and (rows_dev.dtype != torch.int64 or src.dim() != 2):
@@ -488,15 +507,27 @@ def grad_entry(src: torch.Tensor, dst: torch.Tensor | None = None, rows_dev: tor
             raise TypeError("a gradient that is not 2-D must be contiguous")
         rows, cols = 1, src.numel()
         lds = ldd = cols
-    return Grad(_ptr(src), _dtype(src), lds, _ptr(dst), _dtype(dst), ldd, rows, cols, _ptr(rows_dev))
+    entry = Grad(_ptr(src), _dtype(src), lds, _ptr(dst), _dtype(dst), ldd, rows, cols, _ptr(rows_dev))
+    entry.device = dev
+    return entry
+
+
+def _grad_array(entries, device):
+    """The ctypes array of grad_entry's entries, all of them on this GPU."""
+    for i, e in enumerate(entries):
+        if getattr(e, "device", device) != device:
+            raise ValueError(f"gradient {i}: on cuda:{e.device}, the call's tensors are on cuda:{device}")
+    return (Grad * len(entries))(*entries)
 
 
 def ember_clip_grads(grads, max_norm: float, out: torch.Tensor, ws: torch.Tensor) -> None:
     """Clip gradients (a ctypes array of Grad entries, or a list of them) by
     their global norm; out (device, two floats) receives the norm and the factor."""
-    arr = grads if isinstance(grads, ctypes.Array) else (Grad * len(grads))(*grads)
-    _check(LIB.ember_clip_grads(arr, len(arr), float(max_norm), _vector("out", out, (2,)), _ptr(ws),
-                                ws.numel() * ws.element_size(), _stream(out)), "ember_clip_grads")
+    dev = out.get_device()
+    arr = grads if isinstance(grads, ctypes.Array) else _grad_array(grads, dev)
+    w, w_bytes = _workspace(ws, dev)
+    _check(LIB.ember_clip_grads(arr, len(arr), float(max_norm), _vector("out", out, (2,), dev), w, w_bytes,
+                                _stream(out)), "ember_clip_grads")
 
 
 class HeadNorm:
@@ -556,7 +587,7 @@ class GradClipper:
         if not grads or len(out) != len(grads) or len(counts) != len(grads):
             raise ValueError("one gradient at least, and out and counts as long as the list")
         self.tensors = (grads, out, counts)    # kept alive: the entries hold their addresses
-        self.entries = (Grad * len(grads))(*[grad_entry(*x) for x in zip(grads, out, counts)])
+        self.entries = _grad_array([grad_entry(*x) for x in zip(grads, out, counts)], grads[0].get_device())
         self.out = torch.zeros(2, dtype=torch.float32, device=grads[0].device)
         self.norm, self.factor = self.out[0], self.out[1]
         nbytes = ember_clip_workspace_bytes(len(grads))

@@ -231,3 +231,48 @@ def test_profile_takes_every_kernel_the_library_names(em, monkeypatch):
 
     monkeypatch.setattr(em, "LIB", Lib)
     assert set(em.ember_profile_collect()) == names
+
+
+class OnGpu(torch.Tensor):
+    """A host tensor that says it is on a GPU: the others of a call are then the ones to refuse."""
+    index, is_cuda = 0, True
+
+    def get_device(self):
+        return self.index
+
+
+class OnSecondGpu(OnGpu):
+    index = 1
+
+
+def test_binding_refuses_tensors_of_another_device(em):
+    """An operand on the host, or on another GPU than the call's, is refused: its address
+    would be read by the kernel (refused before the stream is asked for or any call is made)."""
+    def z(*shape, dtype=torch.float32, cls=OnGpu):
+        return torch.zeros(*shape, dtype=dtype).as_subclass(cls)
+
+    def check(f, args, only=None):
+        for name in args if only is None else only:
+            for cls in (torch.Tensor, OnSecondGpu):
+                with pytest.raises(ValueError, match=" on cpu"):
+                    f(**{**args, name: args[name].as_subclass(cls)})
+
+    i8 = torch.int8
+    args = dict(X=z(4, 64), gain=z(64), R=z(4, 64), S=z(4, 64), Y=z(4, 64), Q=z(4, 64, dtype=i8), qscale=z(4), rstd=z(4))
+    check(em.ember_rmsnorm, args)
+    args = dict(dY=z(4, 64), S=z(4, 64), gain=z(64), rstd=z(4), dX=z(4, 64), dgain=z(64), ws=z(4096), dS=z(4, 64))
+    check(em.ember_rmsnorm_grad, args)
+    check(em.ember_quantize_rows, dict(X=z(4, 64), Q=z(4, 64, dtype=i8), qscale=z(4)))
+    args = dict(Xq=z(4, 64, dtype=i8), xscale=z(4), Wq=z(9, 64, dtype=i8), wscale=z(9), Y=z(4, 9), bias=z(9))
+    check(em.ember_logits_q8, args)
+    one = z(1, dtype=torch.int64)
+    check(em.grad_entry, dict(src=z(4, 64), dst=z(4, 64), rows_dev=one))
+    with pytest.raises(ValueError):
+        em.grad_entry(torch.zeros(5))
+    entries = [em.grad_entry(z(5)), em.grad_entry(z(4, 8), rows_dev=one)]
+    check(lambda **kw: em.ember_clip_grads(entries, 1.0, **kw), dict(out=z(2), ws=z(4096)), only=["ws"])
+    for grads in ([z(5), torch.zeros(5)], [z(5), z(5, cls=OnSecondGpu)]):
+        with pytest.raises(ValueError):
+            em.GradClipper(grads)
+    with pytest.raises(ValueError):
+        em.ember_clip_grads([em.grad_entry(z(5)), em.grad_entry(z(5, cls=OnSecondGpu))], 1.0, z(2), z(4096))
