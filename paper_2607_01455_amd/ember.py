@@ -493,8 +493,8 @@ def grad_entry(src: torch.Tensor, dst: torch.Tensor | None = None, rows_dev: tor
             raise ValueError(f"{what}: on {t.device}; a gradient, its destination and its count are on one GPU")
     if dst.shape != src.shape:
         raise ValueError(f"gradient {tuple(src.shape)} does not fit its destination {tuple(dst.shape)}")
-    if rows_dev is not None and (rows_dev.dtype != torch.int64 or src.dim() != 2):
-        raise TypeError("rows_dev must be int64 and its gradient 2-D")
+    if rows_dev is not None and (rows_dev.dtype != torch.int64 or rows_dev.numel() != 1 or src.dim() != 2):
+        raise TypeError("rows_dev must be one int64 and its gradient 2-D")
     if src.dim() == 2:
         (rows, cols), lds, ldd = src.shape, src.stride(0), dst.stride(0)
         for t in (src, dst):

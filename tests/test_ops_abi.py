@@ -276,3 +276,12 @@ def test_binding_refuses_tensors_of_another_device(em):
             em.GradClipper(grads)
     with pytest.raises(ValueError):
         em.ember_clip_grads([em.grad_entry(z(5)), em.grad_entry(z(5, cls=OnSecondGpu))], 1.0, z(2), z(4096))
+
+
+def test_a_count_is_one_value(em):
+    """No value would mean that all rows hold a gradient, more than one is not a count of them."""
+    src = torch.zeros(4, 64).as_subclass(OnGpu)
+    for n in (0, 2, 4):
+        with pytest.raises(TypeError, match="one int64"):
+            em.grad_entry(src, rows_dev=torch.zeros(n, dtype=torch.int64).as_subclass(OnGpu))
+    assert em.grad_entry(src, rows_dev=torch.zeros((), dtype=torch.int64).as_subclass(OnGpu)).rows_dev
