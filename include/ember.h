@@ -463,7 +463,8 @@ int ember_rmsnorm_grad(const void* dY, int64_t lddy, const void* S, int x_dtype,
 /*
  * Rows of a table in 8 bits, as the norm writes Q and qscale, from the rows
  * themselves: what ember_logits_q8 reads as Wq and wscale.  1 <= D <=
- * EMBER_NORM_MAX_D, 0 <= rows <= EMBER_MAX_V.
+ * EMBER_NORM_MAX_D, 0 <= rows <= EMBER_MAX_V (0: nothing to do, the pointers may
+ * be NULL).
  */
 int ember_quantize_rows(const void* X, int x_dtype, int64_t ldx, int64_t rows, int64_t D,
                         int8_t* Q, int64_t ldq, float* qscale, hipStream_t stream);
@@ -479,7 +480,8 @@ int ember_quantize_rows(const void* X, int x_dtype, int64_t ldx, int64_t rows, i
  * Layout: bases 16-byte aligned, ldx and ldw multiples of 16 below
  * EMBER_Q8_MAX_LD, Y as W and G.  The padding of Xq and Wq (columns D..ld-1) may
  * be read but never affects a stored value.  0 <= T <= EMBER_MAX_TOKENS (0:
- * nothing to do), 1 <= V <= EMBER_MAX_V, 1 <= D <= EMBER_NORM_MAX_D.
+ * nothing to do, the pointers may be NULL), 1 <= V <= EMBER_MAX_V, 1 <= D <=
+ * EMBER_NORM_MAX_D.
  */
 int ember_logits_q8(const int8_t* Xq, int64_t ldx, const float* xscale,
                     const int8_t* Wq, int64_t ldw, const float* wscale, const float* bias,

@@ -283,15 +283,16 @@ int check_tokens(int64_t T, int64_t D) {
     return T < 0 || T > EMBER_MAX_TOKENS || D < 1 || D > EMBER_NORM_MAX_D ? EMBER_ERR_SHAPE : EMBER_OK;
 }
 
-int check_gain(const void* gain, int dtype) {
+int check_gain(const void* gain, int dtype, bool may_be_null) {
     if (!dtype_ok(dtype)) return EMBER_ERR_DTYPE;
-    if (gain == nullptr) return EMBER_ERR_ARG;
+    if (gain == nullptr) return may_be_null ? EMBER_OK : EMBER_ERR_ARG;
     return aligned(gain, 16) ? EMBER_OK : EMBER_ERR_ALIGN;
 }
 
-// Rows of codes and their scales; both NULL where that is allowed.
-int check_codes(const int8_t* q, int64_t ld, const float* scale, int64_t D, bool may_be_null) {
+// Rows of codes and their scales; both NULL where that is allowed, either where there are no rows.
+int check_codes(const int8_t* q, int64_t ld, const float* scale, int64_t D, bool may_be_null, bool no_rows) {
     if (q == nullptr && scale == nullptr && may_be_null) return EMBER_OK;
+    if (no_rows && (q == nullptr || scale == nullptr)) return EMBER_OK;
     if (q == nullptr || scale == nullptr) return EMBER_ERR_ARG;
     if (ld < D || ld >= EMBER_Q8_MAX_LD) return EMBER_ERR_SHAPE;
     return aligned(q, 16) && ld % 16 == 0 && aligned(scale, 4) ? EMBER_OK : EMBER_ERR_ALIGN;
@@ -794,11 +795,11 @@ int ember_rmsnorm(const void* X, int x_dtype, int64_t ldx, const void* R, int64_
     if (st == EMBER_OK && R != nullptr) st = check_matrix(R, x_dtype, ldr, D, false);
     if (st == EMBER_OK && S != nullptr) st = check_matrix(S, x_dtype, lds, D, false);
     if (st == EMBER_OK && Y != nullptr) st = check_matrix(Y, y_dtype, ldy, D, false);
-    if (st == EMBER_OK) st = check_codes(Q, ldq, qscale, D, true);
-    if (st == EMBER_OK) st = check_gain(gain, gain_dtype);
+    if (st == EMBER_OK) st = check_codes(Q, ldq, qscale, D, true, T == 0);
+    if (st == EMBER_OK) st = check_gain(gain, gain_dtype, T == 0);
     if (st == EMBER_OK && (!(eps >= 0.0f) || !std::isfinite(eps))) st = EMBER_ERR_ARG;
     if (st == EMBER_OK && T > 0 && Y == nullptr && Q == nullptr) st = EMBER_ERR_ARG;
-    if (st == EMBER_OK && S != nullptr && R == nullptr) st = EMBER_ERR_ARG;
+    if (st == EMBER_OK && T > 0 && S != nullptr && R == nullptr) st = EMBER_ERR_ARG;
     if (st == EMBER_OK && rstd != nullptr && !aligned(rstd, 4)) st = EMBER_ERR_ALIGN;
     if (st != EMBER_OK || T == 0) return st;
     const size_t es = dtype_size(x_dtype);
@@ -838,7 +839,7 @@ int ember_rmsnorm_grad(const void* dY, int64_t lddy, const void* S, int x_dtype,
     if (st == EMBER_OK) st = check_matrix(S, x_dtype, lds, D, T == 0);
     if (st == EMBER_OK) st = check_matrix(dX, x_dtype, lddx, D, T == 0);
     if (st == EMBER_OK && dS != nullptr) st = check_matrix(dS, x_dtype, ldds, D, false);
-    if (st == EMBER_OK) st = check_gain(gain, gain_dtype);
+    if (st == EMBER_OK) st = check_gain(gain, gain_dtype, false);
     if (st == EMBER_OK && ((T > 0 && rstd == nullptr) || dgain == nullptr || ws == nullptr)) st = EMBER_ERR_ARG;
     if (st == EMBER_OK && (!aligned(rstd, 4) || !aligned(dgain, 4) || !aligned(ws, 256))) st = EMBER_ERR_ALIGN;
     if (st == EMBER_OK && ws_bytes < ember::norm_grad_ws_bytes(T, D)) st = EMBER_ERR_WORKSPACE;
@@ -867,8 +868,7 @@ int ember_quantize_rows(const void* X, int x_dtype, int64_t ldx, int64_t rows, i
                         float* qscale, hipStream_t stream) {
     if (rows < 0 || rows > EMBER_MAX_V || D < 1 || D > EMBER_NORM_MAX_D) return EMBER_ERR_SHAPE;
     int st = check_matrix(X, x_dtype, ldx, D, rows == 0);
-    if (st == EMBER_OK) st = check_codes(Q, ldq, qscale, D, rows == 0);
-    if (st == EMBER_OK && rows > 0 && Q == nullptr) st = EMBER_ERR_ARG;
+    if (st == EMBER_OK) st = check_codes(Q, ldq, qscale, D, false, rows == 0);
     if (st != EMBER_OK || rows == 0) return st;
     const Output outs[] = {{Q, (size_t)(rows - 1) * (size_t)ldq + (size_t)D, 1, ldq},
                            {qscale, (size_t)rows * 4, 0, 0}};
@@ -892,10 +892,8 @@ int ember_logits_q8(const int8_t* Xq, int64_t ldx, const float* xscale, const in
                     int64_t ldy, hipStream_t stream) {
     int st = check_tokens(T, D);
     if (st == EMBER_OK && (V < 1 || V > EMBER_MAX_V)) st = EMBER_ERR_SHAPE;
-    if (st == EMBER_OK) st = check_codes(Xq, ldx, xscale, D, T == 0);
-    if (st == EMBER_OK && T > 0 && Xq == nullptr) st = EMBER_ERR_ARG;
-    if (st == EMBER_OK) st = check_codes(Wq, ldw, wscale, D, false);
-    if (st == EMBER_OK && Wq == nullptr) st = EMBER_ERR_ARG;
+    if (st == EMBER_OK) st = check_codes(Xq, ldx, xscale, D, false, T == 0);
+    if (st == EMBER_OK) st = check_codes(Wq, ldw, wscale, D, false, T == 0);
     if (st == EMBER_OK) st = check_matrix(Y, y_dtype, ldy, V, T == 0);
     if (st == EMBER_OK && bias != nullptr && !aligned(bias, 4)) st = EMBER_ERR_ALIGN;
     if (st != EMBER_OK || T == 0) return st;

@@ -285,3 +285,26 @@ def test_a_count_is_one_value(em):
         with pytest.raises(TypeError, match="one int64"):
             em.grad_entry(src, rows_dev=torch.zeros(n, dtype=torch.int64).as_subclass(OnGpu))
     assert em.grad_entry(src, rows_dev=torch.zeros((), dtype=torch.int64).as_subclass(OnGpu)).rows_dev
+
+
+def test_no_rows_need_no_pointers(em):
+    """With no tokens (no rows) there is nothing to do: any of the pointers may be NULL, and what
+    is given is checked as ever."""
+    none = dict(X=None, R=None, gain=None, S=None, Y=None, Q=None, qs=None, rstd=None)
+    given = dict(X=X_, R=R_, gain=GAIN_, S=S_, Y=Y_, Q=Q_, qs=QS_, rstd=RSTD_)
+    assert _norm(em, T=0, **none) == em.EMBER_OK
+    for name in none:
+        assert _norm(em, T=0, **{**none, name: given[name]}) == em.EMBER_OK
+        assert _norm(em, T=0, **{name: None}) == em.EMBER_OK
+    assert _norm(em, T=0, **{**none, "gd": 4}) == em.EMBER_ERR_DTYPE
+    assert _norm(em, T=0, **{**none, "gain": GAIN_ + 4}) == em.EMBER_ERR_ALIGN
+    assert _norm(em, T=0, **{**none, "D": 0}) == em.EMBER_ERR_SHAPE
+    none = dict(X=None, Q=None, qs=None)
+    assert _quant(em, rows=0, **none) == em.EMBER_OK
+    for name in none:
+        assert _quant(em, rows=0, **{name: None}) == em.EMBER_OK
+    none = dict(Xq=None, xs=None, Wq=None, ws=None, bias=None, Y=None)
+    assert _logits(em, T=0, **none) == em.EMBER_OK
+    for name in none:
+        assert _logits(em, T=0, **{name: None}) == em.EMBER_OK
+    assert _logits(em, T=0, V=0, **none) == em.EMBER_ERR_SHAPE
