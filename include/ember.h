@@ -429,8 +429,9 @@ int ember_lmhead_step(void* W, int w_dtype, int64_t ldw,
  * X, R (x_dtype), S, Y: layout rules of W and G; between two rows the padding up to
  * the next 16-byte boundary may be read, its values do not matter.  Q: 16-byte aligned, ldq a
  * multiple of 16 below EMBER_Q8_MAX_LD; columns D..ldq-1 are not written.  gain: D values of
- * gain_dtype, 16-byte aligned.  0 <= T <= EMBER_MAX_TOKENS (0: nothing to do, the
- * pointers may be NULL), 1 <= D <= EMBER_NORM_MAX_D, eps >= 0 and finite.
+ * gain_dtype, 16-byte aligned.  An output shares no memory with another argument other
+ * than as said (EMBER_ERR_ARG; columns of one buffer at one stride are fine).
+ * 0 <= T <= EMBER_MAX_TOKENS (0: nothing to do, the pointers may be NULL), 1 <= D <= EMBER_NORM_MAX_D, eps >= 0 and finite.
  */
 #define EMBER_NORM_MAX_D ((int64_t)32768)
 
@@ -448,8 +449,8 @@ int ember_rmsnorm(const void* X, int x_dtype, int64_t ldx, const void* R, int64_
  *   dx_j = rstd u_j - rstd^3 mean_k(u_k s_k) s_j + ds_j    -> dX (T x D, x_dtype)
  *   dgain_j = sum_t dy_tj s_tj rstd_t                      -> dgain (D, fp32)
  *
- * dX is the gradient of X and of R; it may be dY, dS or S itself (same ld).  dgain is
- * overwritten (zeros for T = 0); its sum has an order fixed by T and D.  The
+ * dX is the gradient of X and of R; it may be dY, dS or S itself (same ld) and shares no
+ * other memory with an argument.  dgain is overwritten (zeros for T = 0); its sum has an order fixed by T and D.  The
  * workspace (device, 256-byte aligned, ember_rmsnorm_grad_workspace_bytes of at
  * least T tokens and this D) needs no initialisation.
  */

@@ -4,6 +4,7 @@
 
 #include "ember.h"
 
+#include <algorithm>
 #include <atomic>
 #include <cmath>
 #include <mutex>
@@ -298,30 +299,46 @@ int check_codes(const int8_t* q, int64_t ld, const float* scale, int64_t D, bool
     return aligned(q, 16) && ld % 16 == 0 && aligned(scale, 4) ? EMBER_OK : EMBER_ERR_ALIGN;
 }
 
-// Memory a call writes, and memory it reads.  An output with the base, the
-// stride and the element size of an input takes its place element for element,
-// which the kernels allow where elem is set on both.
-struct Output {
+// Memory of an argument: rows of `width` bytes, `ld` bytes apart (no rows: no argument).
+struct Region {
     const void* p;
-    size_t bytes, elem;
-    int64_t ld;
+    int64_t rows;
+    size_t ld, width;
 };
-struct Input {
-    Span span;
-    const void* p;
+Region matrix_of(const void* p, int64_t rows, int64_t ld, int64_t cols, size_t elem) {
+    const size_t width = (size_t)cols * elem;
+    return Region{p, p == nullptr ? 0 : rows, rows > 1 ? (size_t)ld * elem : width, width};
+}
+Region array_of(const void* p, size_t bytes) { return Region{p, p == nullptr || bytes == 0 ? 0 : 1, bytes, bytes}; }
+
+// Whether two regions share a byte.  Rows at one stride do not where their columns
+// lie side by side (views of one buffer), nor does a single row that lies between rows.
+bool overlap(const Region& a, const Region& b) {
+    if (a.rows == 0 || b.rows == 0) return false;
+    const auto span = [](const Region& x) { return span_of(x.p, (size_t)(x.rows - 1) * x.ld + x.width); };
+    if (!overlap(span(a), span(b))) return false;
+    const size_t ld = a.rows > 1 ? a.ld : b.ld;
+    if ((a.rows == 1 && b.rows == 1) || (b.rows > 1 && b.ld != ld) || std::max(a.width, b.width) > ld) return true;
+    const uintptr_t pa = reinterpret_cast<uintptr_t>(a.p), pb = reinterpret_cast<uintptr_t>(b.p);
+    const size_t from = pb >= pa ? (pb - pa) % ld : (ld - (pa - pb) % ld) % ld;   // b's columns behind a's first
+    return from < a.width || from + b.width > ld;
+}
+
+// An argument a call writes, or reads.  An output with the base, the stride and the
+// element size of an input takes its place element for element, which the kernels
+// allow where elem is set on both.
+struct Operand {
+    Region at;
     size_t elem;
-    int64_t ld;
 };
-bool bad_overlap(const Output* outs, int n_out, const Input* ins, int n_in) {
+bool bad_overlap(const Operand* outs, int n_out, const Operand* ins, int n_in) {
     for (int i = 0; i < n_out; ++i) {
-        if (outs[i].p == nullptr) continue;
-        const Span o = span_of(outs[i].p, outs[i].bytes);
+        const Operand& o = outs[i];
         for (int j = 0; j < i; ++j)
-            if (outs[j].p != nullptr && overlap(o, span_of(outs[j].p, outs[j].bytes))) return true;
+            if (overlap(o.at, outs[j].at)) return true;
         for (int j = 0; j < n_in; ++j) {
-            const bool same = outs[i].elem != 0 && ins[j].p == outs[i].p && ins[j].elem == outs[i].elem &&
-                              ins[j].ld == outs[i].ld;
-            if (!same && overlap(o, ins[j].span)) return true;
+            const bool same = o.elem != 0 && ins[j].elem == o.elem && ins[j].at.p == o.at.p && ins[j].at.ld == o.at.ld;
+            if (!same && overlap(o.at, ins[j].at)) return true;
         }
     }
     return false;
@@ -339,10 +356,8 @@ int check_grad(const ember_grad& g) {
         return EMBER_ERR_ALIGN;
     if (g.src == g.dst)
         return g.src_dtype == g.dst_dtype && (g.rows == 1 || g.lds == g.ldd) ? EMBER_OK : EMBER_ERR_ARG;
-    const auto span = [&](const void* p, int dtype, int64_t ld) {
-        return span_of(p, matrix_bytes(g.rows, g.rows == 1 ? g.cols : ld, g.cols, dtype));
-    };
-    return overlap(span(g.src, g.src_dtype, g.lds), span(g.dst, g.dst_dtype, g.ldd)) ? EMBER_ERR_ARG : EMBER_OK;
+    const Region src = matrix_of(g.src, g.rows, g.lds, g.cols, dtype_size(g.src_dtype));
+    return overlap(src, matrix_of(g.dst, g.rows, g.ldd, g.cols, dtype_size(g.dst_dtype))) ? EMBER_ERR_ARG : EMBER_OK;
 }
 
 } // namespace
@@ -803,19 +818,17 @@ int ember_rmsnorm(const void* X, int x_dtype, int64_t ldx, const void* R, int64_
     if (st == EMBER_OK && rstd != nullptr && !aligned(rstd, 4)) st = EMBER_ERR_ALIGN;
     if (st != EMBER_OK || T == 0) return st;
     const size_t es = dtype_size(x_dtype);
-    const Span x = span_of(X, matrix_bytes(T, ldx, D, x_dtype));
-    const Span r = R ? span_of(R, matrix_bytes(T, ldr, D, x_dtype)) : span_of(nullptr, 0);
     // a row's outputs may take the place of its inputs, element for element;
     // any other overlap of an output would be read or written by another row
-    const Output outs[] = {
-        {S, S ? matrix_bytes(T, lds, D, x_dtype) : 0, es, lds},
-        {Y, Y ? matrix_bytes(T, ldy, D, y_dtype) : 0, Y ? dtype_size(y_dtype) : 0, ldy},
-        {Q, Q ? (size_t)(T - 1) * (size_t)ldq + (size_t)D : 0, 1, ldq},
-        {qscale, Q ? (size_t)T * 4 : 0, 0, 0},
-        {rstd, rstd ? (size_t)T * 4 : 0, 0, 0},
-    };
-    const Input ins[] = {{x, X, es, ldx}, {r, R, es, ldr},
-                         {span_of(gain, (size_t)D * dtype_size(gain_dtype)), nullptr, 0, 0}};
+    const size_t ys = Y ? dtype_size(y_dtype) : 0;
+    const Operand outs[] = {{matrix_of(S, T, lds, D, es), es},
+                            {matrix_of(Y, T, ldy, D, ys), ys},
+                            {matrix_of(Q, T, ldq, D, 1), 1},
+                            {array_of(qscale, (size_t)T * 4), 0},
+                            {array_of(rstd, (size_t)T * 4), 0}};
+    const Operand ins[] = {{matrix_of(X, T, ldx, D, es), es},
+                           {matrix_of(R, T, ldr, D, es), es},
+                           {array_of(gain, (size_t)D * dtype_size(gain_dtype)), 0}};
     if (bad_overlap(outs, 5, ins, 3)) return EMBER_ERR_ARG;
     const ember::NormArgs a{X, x_dtype, ldx, R, ldr, gain, gain_dtype, eps, T, D, S, lds, Y, y_dtype, ldy,
                             Q, ldq, qscale, rstd};
@@ -845,18 +858,14 @@ int ember_rmsnorm_grad(const void* dY, int64_t lddy, const void* S, int x_dtype,
     if (st == EMBER_OK && ws_bytes < ember::norm_grad_ws_bytes(T, D)) st = EMBER_ERR_WORKSPACE;
     if (st != EMBER_OK) return st;
     const size_t es = dtype_size(x_dtype);
-    const Output outs[] = {
-        {T ? dX : nullptr, T ? matrix_bytes(T, lddx, D, x_dtype) : 0, es, lddx},
-        {dgain, (size_t)D * 4, 0, 0},
-        {ws, ember::norm_grad_ws_bytes(T, D), 0, 0},
-    };
-    const Input ins[] = {
-        {span_of(dY, matrix_bytes(T, lddy, D, x_dtype)), dY, es, lddy},
-        {span_of(S, matrix_bytes(T, lds, D, x_dtype)), S, es, lds},
-        {span_of(dS, dS ? matrix_bytes(T, ldds, D, x_dtype) : 0), dS, es, ldds},
-        {span_of(gain, (size_t)D * dtype_size(gain_dtype)), nullptr, 0, 0},
-        {span_of(rstd, (size_t)T * 4), nullptr, 0, 0},
-    };
+    const Operand outs[] = {{matrix_of(dX, T, lddx, D, es), es},
+                            {array_of(dgain, (size_t)D * 4), 0},
+                            {array_of(ws, ember::norm_grad_ws_bytes(T, D)), 0}};
+    const Operand ins[] = {{matrix_of(dY, T, lddy, D, es), es},
+                           {matrix_of(S, T, lds, D, es), es},
+                           {matrix_of(dS, T, ldds, D, es), es},
+                           {array_of(gain, (size_t)D * dtype_size(gain_dtype)), 0},
+                           {array_of(rstd, (size_t)T * 4), 0}};
     if (bad_overlap(outs, 3, ins, 5)) return EMBER_ERR_ARG;
     const ember::NormGradArgs a{dY, lddy, S, x_dtype, lds, gain, gain_dtype, rstd, dS, ldds, T, D, dX, lddx, dgain,
                                 static_cast<char*>(ws)};
@@ -870,9 +879,8 @@ int ember_quantize_rows(const void* X, int x_dtype, int64_t ldx, int64_t rows, i
     int st = check_matrix(X, x_dtype, ldx, D, rows == 0);
     if (st == EMBER_OK) st = check_codes(Q, ldq, qscale, D, false, rows == 0);
     if (st != EMBER_OK || rows == 0) return st;
-    const Output outs[] = {{Q, (size_t)(rows - 1) * (size_t)ldq + (size_t)D, 1, ldq},
-                           {qscale, (size_t)rows * 4, 0, 0}};
-    const Input ins[] = {{span_of(X, matrix_bytes(rows, ldx, D, x_dtype)), nullptr, 0, 0}};
+    const Operand outs[] = {{matrix_of(Q, rows, ldq, D, 1), 0}, {array_of(qscale, (size_t)rows * 4), 0}};
+    const Operand ins[] = {{matrix_of(X, rows, ldx, D, dtype_size(x_dtype)), 0}};
     if (bad_overlap(outs, 2, ins, 1)) return EMBER_ERR_ARG;
     ember::NormArgs a{};
     a.X = X;
@@ -897,14 +905,12 @@ int ember_logits_q8(const int8_t* Xq, int64_t ldx, const float* xscale, const in
     if (st == EMBER_OK) st = check_matrix(Y, y_dtype, ldy, V, T == 0);
     if (st == EMBER_OK && bias != nullptr && !aligned(bias, 4)) st = EMBER_ERR_ALIGN;
     if (st != EMBER_OK || T == 0) return st;
-    const Output outs[] = {{Y, matrix_bytes(T, ldy, V, y_dtype), 0, 0}};
-    const Input ins[] = {
-        {span_of(Xq, (size_t)(T - 1) * (size_t)ldx + (size_t)D), nullptr, 0, 0},
-        {span_of(Wq, (size_t)(V - 1) * (size_t)ldw + (size_t)D), nullptr, 0, 0},
-        {span_of(xscale, (size_t)T * 4), nullptr, 0, 0},
-        {span_of(wscale, (size_t)V * 4), nullptr, 0, 0},
-        {span_of(bias, bias ? (size_t)V * 4 : 0), nullptr, 0, 0},
-    };
+    const Operand outs[] = {{matrix_of(Y, T, ldy, V, dtype_size(y_dtype)), 0}};
+    const Operand ins[] = {{matrix_of(Xq, T, ldx, D, 1), 0},
+                           {matrix_of(Wq, V, ldw, D, 1), 0},
+                           {array_of(xscale, (size_t)T * 4), 0},
+                           {array_of(wscale, (size_t)V * 4), 0},
+                           {array_of(bias, (size_t)V * 4), 0}};
     if (bad_overlap(outs, 1, ins, 5)) return EMBER_ERR_ARG;
     const ember::LogitsArgs a{Xq, ldx, xscale, Wq, ldw, wscale, bias, T, V, D, Y, y_dtype, ldy};
     const hipError_t e = timed("ember_logits_q8", stream, [&] { return ember::launch_logits(a, stream); });

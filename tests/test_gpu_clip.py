@@ -270,3 +270,19 @@ def test_counts_at_the_ends_of_int64(em, rows, cols, pad, dtype):
             g = randn(rows, cols + pad, dtype=dtype)[:, :cols]
             check(em, [g, randn(100)], limit, out=[torch.full((rows, cols), 9.0, device=DEV), torch.zeros(100, device=DEV)],
                   counts=[c, None])
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_columns_of_one_buffer(em, dtype):
+    """Gradients and their destinations side by side in one buffer's rows; what lies between keeps."""
+    for rows, cols, W in ((500, 37, 48), (60, 1000, 1007), (300, 64, 64)):
+        print(f"clip columns of one buffer {rows} x {cols} {dtype}", flush=True)
+        big = torch.full((rows, 3 * W), 9.0, dtype=dtype, device=DEV)
+        a, b = big[:, :cols], big[:, 2 * W:2 * W + cols]
+        a.copy_(randn(rows, cols, dtype=dtype))
+        check(em, [a, randn(100)], 0.5, out=[b, torch.zeros(100, device=DEV)])
+        check(em, [a], 0.25)
+        assert (big[:, cols:2 * W] == 9).all() and (big[:, 2 * W + cols:] == 9).all()
+        with pytest.raises(em.EmberError) as e:
+            em.GradClipper([a], out=[big[:, cols - 1:2 * cols - 1]])(1.0)
+        assert e.value.status == em.EMBER_ERR_ARG

@@ -412,3 +412,34 @@ def test_gradient_past_the_range_of_fp32(em, T, D, dtype, tiny, eps):
     assert ((dgain.double() - dg).abs() <= (T + 3) * U * mag + 1e-37).all()
     norm.grad(dY, X, rstd, dY, dgain2)
     assert torch.equal(bits(dY), bits(dX)) and torch.equal(bits(dgain2), bits(dgain))
+
+
+@pytest.mark.parametrize("T,D", [(1, 96), (40, 96), (40, 100), (600, 101), (9, 5000)])
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_columns_of_one_buffer(em, T, D, dtype):
+    """Inputs and outputs side by side in one buffer's rows: the bits of separate tensors, and
+    nothing between them is written."""
+    print(f"rmsnorm columns of one buffer T={T} D={D} {dtype}", flush=True)
+    W = (D + 7) // 8 * 8 + 8
+    big = torch.full((T, 6 * W), float("nan"), dtype=dtype, device=DEV)
+    x, r, s, y, dx, ds = (big[:, k * W:k * W + D] for k in (3, 0, 5, 1, 4, 2))
+    X, R, g = make(T, D, dtype, T + D, True)
+    gain = 0.5 + torch.rand(D, generator=g, device=DEV)
+    x.copy_(X), r.copy_(R), ds.copy_(R)
+    norm = em.HeadNorm(gain, EPS, max_tokens=T)
+    S, Y, dX = padded(T, D, dtype), padded(T, D, dtype), padded(T, D, dtype)
+    rstd, dgain = torch.zeros(T, device=DEV), torch.zeros(D, device=DEV)
+    rstd2, dgain2 = torch.zeros(T, device=DEV), torch.zeros(D, device=DEV)
+    norm(X, R, S, Y, rstd=rstd)
+    norm.grad(Y, S, rstd, dX, dgain, dS=R)
+    norm(x, r, s, y, rstd=rstd2)
+    norm.grad(y, s, rstd2, dx, dgain2, dS=ds)
+    for a, b in ((s, S), (y, Y), (dx, dX), (rstd2, rstd), (dgain2, dgain), (x, X), (r, R)):
+        assert torch.equal(bits(a), bits(b))
+    for k in range(6):
+        assert torch.isnan(big[:, k * W + D:(k + 1) * W].float()).all()
+    if T > 1:    # S over the last columns of Y, and over X but its first chunk
+        for start in (W + (D - 1) // 8 * 8, 3 * W + 8):
+            with pytest.raises(em.EmberError) as e:
+                norm(x, r, S=big[:, start:start + D], Y=y)
+            assert e.value.status == em.EMBER_ERR_ARG
