@@ -509,7 +509,8 @@ int ember_logits_q8(const int8_t* Xq, int64_t ldx, const float* xscale,
  *                         writes it); the others are not read, and zeros are
  *                         written in their place in dst.  A value outside
  *                         [0, rows] counts as the nearer end.
- * Tensors must not overlap each other's memory.  rows, cols >= 0 (an empty
+ * Tensors must not overlap each other's memory (not checked), nor out, the workspace
+ * or a row count (EMBER_ERR_ARG).  rows, cols >= 0 (an empty
  * tensor's pointers may be NULL), rows * cols <= 2^40, 0 <= n_grads <=
  * EMBER_MAX_GRADS, max_norm >= 0 (infinite: only the norm, and copies).  The
  * workspace (device, 256-byte aligned, ember_clip_workspace_bytes(n_grads))

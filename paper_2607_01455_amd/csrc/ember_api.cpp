@@ -344,7 +344,8 @@ bool bad_overlap(const Operand* outs, int n_out, const Operand* ins, int n_in) {
     return false;
 }
 
-int check_grad(const ember_grad& g) {
+// out, ws: what the call writes beside the gradients' destinations.
+int check_grad(const ember_grad& g, const Region& out, const Region& ws) {
     if (g.rows < 0 || g.cols < 0) return EMBER_ERR_SHAPE;
     if (!dtype_ok(g.src_dtype) || !dtype_ok(g.dst_dtype)) return EMBER_ERR_DTYPE;
     if (g.rows == 0 || g.cols == 0) return EMBER_OK;
@@ -354,10 +355,15 @@ int check_grad(const ember_grad& g) {
     if (!aligned(g.src, dtype_size(g.src_dtype)) || !aligned(g.dst, dtype_size(g.dst_dtype)) ||
         (g.rows_dev != nullptr && !aligned(g.rows_dev, 8)))
         return EMBER_ERR_ALIGN;
+    const Region src = matrix_of(g.src, g.rows, g.lds, g.cols, dtype_size(g.src_dtype));
+    const Region dst = matrix_of(g.dst, g.rows, g.ldd, g.cols, dtype_size(g.dst_dtype));
+    const Region count = array_of(g.rows_dev, 8);
+    for (const Region& own : {out, ws})
+        if (overlap(src, own) || overlap(dst, own) || overlap(count, own)) return EMBER_ERR_ARG;
+    if (overlap(dst, count)) return EMBER_ERR_ARG;
     if (g.src == g.dst)
         return g.src_dtype == g.dst_dtype && (g.rows == 1 || g.lds == g.ldd) ? EMBER_OK : EMBER_ERR_ARG;
-    const Region src = matrix_of(g.src, g.rows, g.lds, g.cols, dtype_size(g.src_dtype));
-    return overlap(src, matrix_of(g.dst, g.rows, g.ldd, g.cols, dtype_size(g.dst_dtype))) ? EMBER_ERR_ARG : EMBER_OK;
+    return overlap(src, dst) ? EMBER_ERR_ARG : EMBER_OK;
 }
 
 } // namespace
@@ -929,10 +935,12 @@ int ember_clip_grads(const ember_grad* grads, int64_t n_grads, float max_norm, f
     if (n_grads < 0 || n_grads > EMBER_MAX_GRADS) return EMBER_ERR_SHAPE;
     if ((n_grads > 0 && grads == nullptr) || out == nullptr || ws == nullptr || !(max_norm >= 0.0f))
         return EMBER_ERR_ARG;
+    const Region own_out = array_of(out, 8), own_ws = array_of(ws, ember::clip_ws_bytes(n_grads));
     for (int64_t i = 0; i < n_grads; ++i) {
-        const int st = check_grad(grads[i]);
+        const int st = check_grad(grads[i], own_out, own_ws);
         if (st != EMBER_OK) return st;
     }
+    if (overlap(own_out, own_ws)) return EMBER_ERR_ARG;
     if (!aligned(out, 4) || !aligned(ws, 256)) return EMBER_ERR_ALIGN;
     if (ws_bytes < ember::clip_ws_bytes(n_grads)) return EMBER_ERR_WORKSPACE;
     const hipError_t e = timed("ember_clip_grads", stream, [&] {

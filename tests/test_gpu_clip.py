@@ -286,3 +286,21 @@ def test_columns_of_one_buffer(em, dtype):
         with pytest.raises(em.EmberError) as e:
             em.GradClipper([a], out=[big[:, cols - 1:2 * cols - 1]])(1.0)
         assert e.value.status == em.EMBER_ERR_ARG
+
+
+def test_result_between_the_rows_of_a_gradient(em):
+    """out may lie in a buffer's columns beside the gradient, and not over it."""
+    big = torch.zeros(50, 72, device=DEV)
+    big[:, :64] = randn(50, 64)
+    ws = torch.empty(em.ember_clip_workspace_bytes(1), dtype=torch.uint8, device=DEV)
+    was = big[:, :64].clone()
+    em.ember_clip_grads([em.grad_entry(big[:, :64])], 0.5, big[3, 66:68], ws)
+    norm, factor = big[3, 66].item(), big[3, 67].item()
+    assert abs(norm - norm64([was])) <= 2.0 ** -23 * norm and factor < 1.0
+    assert torch.equal(big[:, :64], was * factor)
+    big[3, 66:68] = 0.0
+    assert (big[:, 64:] == 0).all()
+    for at in (big[3, 63:65], big[4, 0:2]):
+        with pytest.raises(em.EmberError) as e:
+            em.ember_clip_grads([em.grad_entry(big[:, :64])], 0.5, at, ws)
+        assert e.value.status == em.EMBER_ERR_ARG

@@ -308,3 +308,12 @@ def test_no_rows_need_no_pointers(em):
     for name in none:
         assert _logits(em, T=0, **{name: None}) == em.EMBER_OK
     assert _logits(em, T=0, V=0, **none) == em.EMBER_ERR_SHAPE
+
+
+def test_clip_refuses_gradients_over_what_it_writes(em):
+    """out, the workspace and a row count share no memory with a gradient, its destination or each other."""
+    n = 10 * 64
+    for kw in (dict(out=X_), dict(out=X_ + 2 * n - 4), dict(out=Y_ + 8), dict(out=Y_ + 4 * n - 4), dict(ws=X_), dict(ws=Y_ + 256),
+               dict(ws=Y_ - 256), dict(out=WS_ + 8), dict(out=R_), dict(ws=R_), dict(rows_dev=Y_ + 16),
+               dict(lds=128, out=X_ + 256 + 120), dict(out=X_ + (1 << 20) + 16)):
+        assert _clip(em, **kw) == em.EMBER_ERR_ARG, kw
