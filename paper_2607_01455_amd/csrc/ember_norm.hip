@@ -532,12 +532,13 @@ RowPlan row_plan(int D, int dtype, bool grad) {
 
 // The caches are left to what is read next.  The inputs are read once, with
 // non-temporal loads, and S, which waits for the gradient, is stored so; Y ordinarily,
-// dX too while the caches can keep it (us, alone and with a kernel that reads Y or dX
-// next; 16384 x 4096 bf16: all ordinary 94.8 and 132, S non-temporal 93.5 and 128, the
-// loads too 93.6 and 116, Y too 91.0 and 126; 8192 x 4096 48.0 and 66.6, 48.3 and 65.3,
-// 43.1 and 60.3, 46.3 and 65.5; the gradient, ordinary loads / non-temporal / dX too:
-// 16384 x 4096 102 and 138, 95.5 and 123.5, 90.3 and 124.2, 12000 x 4096 76.7 and 104, 72.0
-// and 90.1, 68.8 and 94.2, 32768 x 4096 196 and 266, 185 and 243, 175 and 241).
+// dX too while the caches can keep it.  us, alone and with a kernel that reads Y next, 16384 x
+// 4096 bf16: all ordinary 94.8 and 132, S non-temporal 93.5 and 128, the loads too 93.6
+// and 116, Y too 91.0 and 126; 8192 x 4096 48.0 and 66.6, 48.3 and 65.3, 43.1 and 60.3,
+// 46.3 and 65.5.  dX ordinary / non-temporal, x 4096 bf16, alone, with a kernel that reads it
+// next and with one that adds it to another tensor: 14000 85 / 79, 103 / 109, 138 / 140;
+// 16384 (128 MiB) 97 / 91, 123 / 125, 154 / 160; 18000 106 / 99, 136 / 136, 180 / 176; 24576 137 / 131,
+// 181 / 182, 252 / 237; 49152 278 / 264, 369 / 363, 494 / 467.
 constexpr int64_t kKeptDX = (int64_t)128 << 20;
 int64_t bytes_of(int64_t T, int64_t D, int dtype) { return T * D * (dtype == EMBER_F32 ? 4 : 2); }
 
@@ -628,7 +629,7 @@ size_t norm_grad_ws_bytes(int64_t T, int64_t D) {
 
 hipError_t launch_rmsnorm_grad(const NormGradArgs& x, hipStream_t s) {
     GradParams p{x.dY, x.lddy, x.S, x.lds, x.gain, x.gain_dtype == EMBER_BF16, x.rstd, x.dS, x.ldds, x.T, (int)x.D,
-                 x.dX, x.lddx, 0, reinterpret_cast<float*>(x.ws), x.dgain, bytes_of(x.T, x.D, x.x_dtype) >= kKeptDX};
+                 x.dX, x.lddx, 0, reinterpret_cast<float*>(x.ws), x.dgain, bytes_of(x.T, x.D, x.x_dtype) > kKeptDX};
     const RowPlan pl = row_plan((int)x.D, x.x_dtype, true);
     p.blocks = grad_blocks(x.T, pl);
     if (p.blocks > 0) {

@@ -443,3 +443,24 @@ def test_columns_of_one_buffer(em, T, D, dtype):
             with pytest.raises(em.EmberError) as e:
                 norm(x, r, S=big[:, start:start + D], Y=y)
             assert e.value.status == em.EMBER_ERR_ARG
+
+
+@pytest.mark.parametrize("T,D,dtype", [(16384, 4096, BF), (16385, 4096, BF), (16392, 2047, F), (16393, 2047, F)])
+def test_gradient_where_its_stores_change(em, T, D, dtype):
+    """dX of 128 MiB, the most that is stored ordinarily, and of a row more, stored non-temporally."""
+    print(f"rmsnorm grad T={T} D={D} {dtype}", flush=True)
+    X, _, g = make(T, D, dtype, T, False, extra=0)
+    gain = 0.5 + torch.rand(D, generator=g, device=DEV)
+    dY, dX = padded(T, D, dtype), padded(T, D, dtype)
+    dY.copy_(torch.randn(T, D, generator=g, device=DEV))
+    norm = em.HeadNorm(gain, EPS, max_tokens=T)
+    rstd, dgain = (X.float().square().mean(dim=1) + EPS).rsqrt(), torch.zeros(D, device=DEV)
+    norm.grad(dY, X, rstd, dX, dgain, dS=X)
+    total, mag = torch.zeros(D, dtype=torch.float64, device=DEV), torch.zeros(D, dtype=torch.float64, device=DEV)
+    for t0 in range(0, T, 5000):
+        at = slice(t0, t0 + 5000)
+        dx, A, dg, m = grad64(dY[at], X[at], gain, rstd[at], X[at])
+        assert ((dX[at].double() - dx).abs() <= 100 * U * A + store_err(dx, dtype)).all()
+        total, mag = total + dg, mag + m
+    assert ((dgain.double() - total).abs() <= (T + 3) * U * mag).all()
+    assert padding_kept(dX)
