@@ -13,7 +13,8 @@ would:
   steps                 EmberTable, the embedding's with its row count on the device
 
 with no value read back to the host.  Answering takes the norm's 8-bit output and
-the head rounded to 8 bits (HeadQ8).
+the head in 8 bits (HeadQ8), which takes the table's present rows once after the steps
+on it.
 
     python examples/token_interface.py [--steps N]
 """
@@ -44,6 +45,8 @@ class TokenInterface:
         self.norm = ember.HeadNorm(self.gain, max_tokens=tokens)
         self.head = ember.EmberTable(V, D, device=device, lr=lr)
         self.embedding = ember.EmberTable(V, D, device=device, lr=lr)
+        self.head8 = ember.HeadQ8.from_table(self.W)
+        self.head8_step = 0      # of the head's steps, that it was rounded after
         self.coalescer = ember.Coalescer(2 * tokens, V, D, device=device)
         self.G = torch.empty(V, D, **bf)
         self.S, self.H, self.dX = (torch.empty(tokens, D, **bf) for _ in range(3))
@@ -97,8 +100,11 @@ class TokenInterface:
         Q = torch.empty(n, (self.D + 15) // 16 * 16, dtype=torch.int8, device=X.device)[:, :self.D]   # 16-byte rows
         scale = torch.empty(n, device=X.device)
         logits = torch.empty(n, self.V, dtype=torch.bfloat16, device=X.device)
+        if self.head8_step != self.head.t:
+            self.head8.load(self.W)
+            self.head8_step = self.head.t
         self.norm(X, R, S=S, Q=Q, qscale=scale)
-        ember.HeadQ8.from_table(self.W).logits(Q, scale, logits)
+        self.head8.logits(Q, scale, logits)
         return logits
 
 

@@ -44,3 +44,27 @@ def test_token_interface_learns_and_answers():
     # one token at a time gives what the batch gives
     for i in (0, 100, 255):
         assert torch.equal(m.answer(before[i:i + 1], token[i:i + 1]), m.answer(before, token)[i:i + 1])
+
+
+def test_answers_round_the_head_once_after_its_steps(monkeypatch):
+    """The 8-bit head is made of the table once for any number of answers, and anew after a step."""
+    from paper_2607_01455_amd import ember
+    sys.path.insert(0, os.path.join(ROOT, "examples"))
+    try:
+        import token_interface
+    finally:
+        sys.path.pop(0)
+    m = token_interface.TokenInterface(V=512, D=64, tokens=128)
+    before, token, target = m.batch()
+    rounded = []
+    quantize = ember.ember_quantize_rows
+    monkeypatch.setattr(ember, "ember_quantize_rows", lambda *a: (rounded.append(1), quantize(*a)))
+    first = m.answer(before, token)
+    assert torch.equal(m.answer(before, token), first) and len(rounded) <= 1
+    m.step(before, token, target)
+    rounded.clear()
+    after = m.answer(before, token)
+    assert torch.equal(m.answer(before, token), after) and len(rounded) == 1
+    fresh = ember.HeadQ8.from_table(m.W)
+    assert torch.equal(m.head8.Wq, fresh.Wq) and torch.equal(m.head8.wscale, fresh.wscale)
+    assert not torch.equal(after, first)
