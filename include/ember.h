@@ -444,15 +444,16 @@ int ember_rmsnorm(const void* X, int x_dtype, int64_t ldx, const void* R, int64_
  * The norm's gradient.  S (T x D, x_dtype) is the sum the forward call stored
  * (or its X, without R) and rstd what it wrote; dY (T x D, x_dtype) the gradient
  * of Y; dS (T x D, x_dtype, may be NULL) a gradient that reaches the sum by
- * another way, such as the residual stream.  With u = dy gain:
+ * another way, such as the residual stream.  With u = dy gain and h = s rstd:
  *
- *   dx_j = rstd u_j - rstd^3 mean_k(u_k s_k) s_j + ds_j    -> dX (T x D, x_dtype)
- *   dgain_j = sum_t dy_tj s_tj rstd_t                      -> dgain (D, fp32)
+ *   dx_j = rstd (u_j - mean_k(u_k h_k) h_j) + ds_j    -> dX (T x D, x_dtype)
+ *   dgain_j = sum_t dy_tj h_tj                        -> dgain (D, fp32)
  *
- * dX is the gradient of X and of R; it may be dY, dS or S itself (same ld) and shares no
- * other memory with an argument.  dgain is overwritten (zeros for T = 0); its sum has an order fixed by T and D.  The
- * workspace (device, 256-byte aligned, ember_rmsnorm_grad_workspace_bytes of at
- * least T tokens and this D) needs no initialisation.
+ * dX is the gradient of X and of R; it may be dY, dS or S itself (same ld) and
+ * shares no other memory with an argument.  dgain is overwritten (zeros for T = 0);
+ * its sum has an order fixed by T, D and x_dtype.  The workspace (device, 256-byte
+ * aligned, ember_rmsnorm_grad_workspace_bytes of at least T tokens and this D) needs
+ * no initialisation.
  */
 int ember_rmsnorm_grad_workspace_bytes(int64_t max_tokens, int64_t D, size_t* bytes);
 
@@ -496,7 +497,9 @@ int ember_logits_q8(const int8_t* Xq, int64_t ldx, const float* xscale,
  *
  * and out[0] = norm, out[1] = factor (device, fp32), with no host read: the
  * tables' steps can follow on the stream at once.  A norm that is NaN or
- * infinite gives factor 1.  Squares are summed in float64 in a fixed order.
+ * infinite gives factor 1.  Squares are summed in float64 in a fixed order; of
+ * finite gradients the sum is finite, and so the factor below 1, also where out[0], an
+ * fp32 number, reads infinity.
  *
  * One ember_grad per tensor: rows x cols elements, row i at element i * ld;
  *   src, src_dtype, lds   the gradient, aligned to its element size (views at
