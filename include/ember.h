@@ -490,6 +490,98 @@ int ember_logits_q8(const int8_t* Xq, int64_t ldx, const float* xscale,
                     int64_t T, int64_t V, int64_t D, void* Y, int y_dtype, int64_t ldy, hipStream_t stream);
 
 /*
+ * Tables in 4 bits, for answering: the head and the embedding of a model whose
+ * every token reads them.  A row's columns are in groups of 32, 64 or 128 (the
+ * last one may be shorter), each with a bf16 scale:
+ *
+ *   a = max |x| of the group,  s = bf16(a / 7),  c = rint(x / s) in [-7, 7]
+ *
+ * A group whose a is below 1e-36 (zeros among them) has codes and scale 0; one that
+ * holds an infinity or a NaN has codes 0 and scale NaN.  Codes are in two's
+ * complement, so a table made elsewhere may hold -8 too, and any scales.
+ *
+ * Packing (Wq, Q): the 128 columns from 128 i on take the 64 bytes from 64 i on of
+ * their row.  Byte 16 q + 4 w + b of them (q, w, b in 0..3) holds the code of column
+ * 128 i + 32 w + 4 q + b in its lower half and that of the column 16 further in its
+ * upper half.  A row takes 64 ceil(D / 128) bytes; ember_quantize_rows_q4 writes all of
+ * them (codes 0 past column D), ember_rows_q4 and ember_logits_q4 may read the codes
+ * past column D, but these never affect a stored value, nor does padding.
+ * Layout: codes 16-byte aligned, their row stride in bytes a multiple of 16 below
+ * EMBER_Q8_MAX_LD; scales (bf16 bits, one row of ceil(D / group) for each of the
+ * table's) 16-byte aligned, their row stride a multiple of 8 below EMBER_Q8_MAX_LD.
+ * X, Y: layout rules of W and G.  1 <= V (rows) <= EMBER_MAX_V, 1 <= D <=
+ * EMBER_NORM_MAX_D; outputs share no memory with another argument (EMBER_ERR_ARG), and a
+ * group of another size is EMBER_ERR_ARG too.
+ *
+ * ember_quantize_rows_q4: rows of X in 4 bits.  rows = 0: nothing to do, the pointers
+ * may be NULL.
+ */
+int ember_quantize_rows_q4(const void* X, int x_dtype, int64_t ldx, int64_t rows, int64_t D, int group,
+                           uint8_t* Q, int64_t ldq, uint16_t* gscale, int64_t lds, hipStream_t stream);
+
+/*
+ * Rows read back from 4 bits: Y_i = the values of row tok_i (device int64[n]), or of
+ * row i with tok NULL (then n <= V).  A value is the product of a code and its scale,
+ * rounded once to y_dtype.  A token outside [0, V) gives a row of NaN.  0 <= n <=
+ * EMBER_MAX_TOKENS with tok (0: nothing to do, the pointers may be NULL).
+ */
+int ember_rows_q4(const uint8_t* Wq, int64_t ldw, const uint16_t* wscale, int64_t lds, int group,
+                  int64_t V, int64_t D, const int64_t* tok, int64_t n,
+                  void* Y, int y_dtype, int64_t ldy, hipStream_t stream);
+
+/*
+ * Logits of an LM head held in 4 bits, for T tokens in 8 (Xq and xscale as
+ * ember_logits_q8 has them):
+ *
+ *   Y_tv = xscale_t sum_g wscale_vg (sum_{k in g} Xq_tk c_vk) + bias_v
+ *
+ * A group's sum is exact, the sum over the groups fp32 in an order fixed by the sizes;
+ * the result is rounded once to y_dtype.  bias (V, fp32) may be NULL.  0 <= T <=
+ * EMBER_MAX_TOKENS (0: nothing to do, the pointers may be NULL).
+ */
+int ember_logits_q4(const int8_t* Xq, int64_t ldx, const float* xscale,
+                    const uint8_t* Wq, int64_t ldw, const uint16_t* wscale, int64_t lds, int group,
+                    const float* bias, int64_t T, int64_t V, int64_t D,
+                    void* Y, int y_dtype, int64_t ldy, hipStream_t stream);
+
+/*
+ * A token drawn from each of T rows of V logits (L, T x V, of l_dtype; minus infinity:
+ * a token that is not allowed).  Row t has a temperature, top-k, top-p, min-p (arrays
+ * of T on the device, each NULL if no row has it) and a random number u_t.  With
+ * e_i = exp((l_i - max l) / temperature):
+ *
+ *   top-k   keeps the k first tokens in falling order of l (equal ones by index); 0: all
+ *   top-p   of those, the shortest prefix whose e sum to p times their sum at least (the
+ *           first token always); 1: all
+ *   min-p   of those, the tokens with e_i >= min_p; 0: all
+ *   id      the first token, by index, at which the running sum of the kept e is above
+ *           u times their sum
+ *
+ * Temperature 0 takes the first of the largest logits (temperature 1 and k = 1).
+ * Outputs: ids (T, int64); logp (T, may be NULL): the log of e_id over the sum of all
+ * e, that is before the filters; kept (T, may be NULL): the number of tokens kept.  A
+ * row that has nothing to draw from (no logit above minus infinity), that holds a NaN
+ * or an infinity, or whose parameters are out of range (temperature >= 0 and finite,
+ * k >= 0, 0 <= p <= 1, 0 <= min_p <= 1, 0 <= u < 1) has id -1, logp NaN and kept 0.
+ * e are held in fixed point, exact to half of 2^-n with n = min(48, 62 - ceil(log2 V)):
+ * a token whose e is below that is never drawn.  The result depends on a row's logits
+ * and parameters alone, and has the same bits on every run.
+ * Layout: L as W and G; 0 <= T <= EMBER_MAX_TOKENS (0: nothing to do, the pointers may
+ * be NULL), 1 <= V <= EMBER_SAMPLE_MAX_V.  Outputs and the workspace share no memory
+ * with another argument (EMBER_ERR_ARG).  The workspace (device, 256-byte aligned,
+ * ember_sample_workspace_bytes of at least T tokens and this V) needs no
+ * initialisation; calls that share one must not run at once.
+ */
+#define EMBER_SAMPLE_MAX_V ((int64_t)1 << 24)
+
+int ember_sample_workspace_bytes(int64_t max_tokens, int64_t V, size_t* bytes);
+
+int ember_sample(const void* L, int l_dtype, int64_t ldl, int64_t T, int64_t V, const float* temperature,
+                 const int32_t* top_k, const float* top_p, const float* min_p, const float* u,
+                 int64_t* ids, float* logp, int32_t* kept,
+                 void* ws, size_t ws_bytes, hipStream_t stream);
+
+/*
  * Global gradient norm and clipping.  Over all n_grads tensors together
  *
  *   norm = sqrt(sum g^2),   factor = max_norm / norm if norm > max_norm, else 1

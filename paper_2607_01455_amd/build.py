@@ -15,7 +15,7 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libember.so")
 SOURCES = ["ember_kernels.hip", "ember_coalesce.hip", "ember_lmhead.hip", "ember_norm.hip", "ember_q8.hip",
-           "ember_clip.hip", "ember_probe.hip", "ember_api.cpp"]
+           "ember_q4.hip", "ember_sample.hip", "ember_clip.hip", "ember_probe.hip", "ember_api.cpp"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"

@@ -277,7 +277,7 @@ hipError_t run_phase(const std::vector<const StepArgs*>& order, Key key, Launch 
 }
 
 // ---------------------------------------------------------------------------
-// norm, 8-bit rows and logits, clipping
+// norm, 8-bit and 4-bit rows and logits, sampling, clipping
 // ---------------------------------------------------------------------------
 
 int check_tokens(int64_t T, int64_t D) {
@@ -297,6 +297,16 @@ int check_codes(const int8_t* q, int64_t ld, const float* scale, int64_t D, bool
     if (q == nullptr || scale == nullptr) return EMBER_ERR_ARG;
     if (ld < D || ld >= EMBER_Q8_MAX_LD) return EMBER_ERR_SHAPE;
     return aligned(q, 16) && ld % 16 == 0 && aligned(scale, 4) ? EMBER_OK : EMBER_ERR_ALIGN;
+}
+
+// Rows of 4-bit codes and the scales of their groups; either may be NULL where there are no rows.
+int64_t code_bytes(int64_t D) { return (D + 127) / 128 * 64; }
+int check_codes4(const void* q, int64_t ldq, const void* scale, int64_t lds, int group, int64_t D, bool no_rows) {
+    if (group != 32 && group != 64 && group != 128) return EMBER_ERR_ARG;
+    if (q == nullptr || scale == nullptr) return no_rows ? EMBER_OK : EMBER_ERR_ARG;
+    if (ldq < code_bytes(D) || ldq >= EMBER_Q8_MAX_LD || lds < (D + group - 1) / group || lds >= EMBER_Q8_MAX_LD)
+        return EMBER_ERR_SHAPE;
+    return aligned(q, 16) && ldq % 16 == 0 && aligned(scale, 16) && lds % 8 == 0 ? EMBER_OK : EMBER_ERR_ALIGN;
 }
 
 // Memory of an argument: rows of `width` bytes, `ld` bytes apart (no rows: no argument).
@@ -920,6 +930,93 @@ int ember_logits_q8(const int8_t* Xq, int64_t ldx, const float* xscale, const in
     if (bad_overlap(outs, 1, ins, 5)) return EMBER_ERR_ARG;
     const ember::LogitsArgs a{Xq, ldx, xscale, Wq, ldw, wscale, bias, T, V, D, Y, y_dtype, ldy};
     const hipError_t e = timed("ember_logits_q8", stream, [&] { return ember::launch_logits(a, stream); });
+    return e == hipSuccess ? EMBER_OK : EMBER_ERR_HIP;
+}
+
+int ember_quantize_rows_q4(const void* X, int x_dtype, int64_t ldx, int64_t rows, int64_t D, int group, uint8_t* Q,
+                           int64_t ldq, uint16_t* gscale, int64_t lds, hipStream_t stream) {
+    if (rows < 0 || rows > EMBER_MAX_V || D < 1 || D > EMBER_NORM_MAX_D) return EMBER_ERR_SHAPE;
+    int st = check_matrix(X, x_dtype, ldx, D, rows == 0);
+    if (st == EMBER_OK) st = check_codes4(Q, ldq, gscale, lds, group, D, rows == 0);
+    if (st != EMBER_OK || rows == 0) return st;
+    const Operand outs[] = {{matrix_of(Q, rows, ldq, code_bytes(D), 1), 0},
+                            {matrix_of(gscale, rows, lds, (D + group - 1) / group, 2), 0}};
+    const Operand ins[] = {{matrix_of(X, rows, ldx, D, dtype_size(x_dtype)), 0}};
+    if (bad_overlap(outs, 2, ins, 1)) return EMBER_ERR_ARG;
+    const ember::Quant4Args a{X, x_dtype, ldx, rows, D, group, Q, ldq, gscale, lds};
+    const hipError_t e = timed("ember_quantize_rows_q4", stream, [&] { return ember::launch_quantize4(a, stream); });
+    return e == hipSuccess ? EMBER_OK : EMBER_ERR_HIP;
+}
+
+int ember_rows_q4(const uint8_t* Wq, int64_t ldw, const uint16_t* wscale, int64_t lds, int group, int64_t V, int64_t D,
+                  const int64_t* tok, int64_t n, void* Y, int y_dtype, int64_t ldy, hipStream_t stream) {
+    if (V < 1 || V > EMBER_MAX_V || D < 1 || D > EMBER_NORM_MAX_D) return EMBER_ERR_SHAPE;
+    if (n < 0 || (tok == nullptr ? n > V : n > EMBER_MAX_TOKENS)) return EMBER_ERR_SHAPE;
+    int st = check_codes4(Wq, ldw, wscale, lds, group, D, n == 0);
+    if (st == EMBER_OK) st = check_matrix(Y, y_dtype, ldy, D, n == 0);
+    if (st == EMBER_OK && !aligned(tok, 8)) st = EMBER_ERR_ALIGN;
+    if (st != EMBER_OK || n == 0) return st;
+    const Operand outs[] = {{matrix_of(Y, n, ldy, D, dtype_size(y_dtype)), 0}};
+    const Operand ins[] = {{matrix_of(Wq, V, ldw, code_bytes(D), 1), 0},
+                           {matrix_of(wscale, V, lds, (D + group - 1) / group, 2), 0},
+                           {array_of(tok, (size_t)n * 8), 0}};
+    if (bad_overlap(outs, 1, ins, 3)) return EMBER_ERR_ARG;
+    const ember::Rows4Args a{Wq, ldw, wscale, lds, group, V, D, tok, n, Y, y_dtype, ldy};
+    const hipError_t e = timed("ember_rows_q4", stream, [&] { return ember::launch_rows4(a, stream); });
+    return e == hipSuccess ? EMBER_OK : EMBER_ERR_HIP;
+}
+
+int ember_logits_q4(const int8_t* Xq, int64_t ldx, const float* xscale, const uint8_t* Wq, int64_t ldw,
+                    const uint16_t* wscale, int64_t lds, int group, const float* bias, int64_t T, int64_t V, int64_t D,
+                    void* Y, int y_dtype, int64_t ldy, hipStream_t stream) {
+    int st = check_tokens(T, D);
+    if (st == EMBER_OK && (V < 1 || V > EMBER_MAX_V)) st = EMBER_ERR_SHAPE;
+    if (st == EMBER_OK) st = check_codes(Xq, ldx, xscale, D, false, T == 0);
+    if (st == EMBER_OK) st = check_codes4(Wq, ldw, wscale, lds, group, D, T == 0);
+    if (st == EMBER_OK) st = check_matrix(Y, y_dtype, ldy, V, T == 0);
+    if (st == EMBER_OK && bias != nullptr && !aligned(bias, 4)) st = EMBER_ERR_ALIGN;
+    if (st != EMBER_OK || T == 0) return st;
+    const Operand outs[] = {{matrix_of(Y, T, ldy, V, dtype_size(y_dtype)), 0}};
+    const Operand ins[] = {{matrix_of(Xq, T, ldx, D, 1), 0},
+                           {matrix_of(Wq, V, ldw, code_bytes(D), 1), 0},
+                           {matrix_of(wscale, V, lds, (D + group - 1) / group, 2), 0},
+                           {array_of(xscale, (size_t)T * 4), 0},
+                           {array_of(bias, (size_t)V * 4), 0}};
+    if (bad_overlap(outs, 1, ins, 5)) return EMBER_ERR_ARG;
+    const ember::Logits4Args a{Xq, ldx, xscale, Wq, ldw, wscale, lds, group, bias, T, V, D, Y, y_dtype, ldy};
+    const hipError_t e = timed("ember_logits_q4", stream, [&] { return ember::launch_logits4(a, stream); });
+    return e == hipSuccess ? EMBER_OK : EMBER_ERR_HIP;
+}
+
+int ember_sample_workspace_bytes(int64_t max_tokens, int64_t V, size_t* bytes) {
+    if (bytes == nullptr) return EMBER_ERR_ARG;
+    if (max_tokens < 0 || max_tokens > EMBER_MAX_TOKENS || V < 1 || V > EMBER_SAMPLE_MAX_V) return EMBER_ERR_SHAPE;
+    *bytes = ember::sample_ws_bytes(max_tokens, V);
+    return EMBER_OK;
+}
+
+int ember_sample(const void* L, int l_dtype, int64_t ldl, int64_t T, int64_t V, const float* temperature,
+                 const int32_t* top_k, const float* top_p, const float* min_p, const float* u, int64_t* ids,
+                 float* logp, int32_t* kept, void* ws, size_t ws_bytes, hipStream_t stream) {
+    if (T < 0 || T > EMBER_MAX_TOKENS || V < 1 || V > EMBER_SAMPLE_MAX_V) return EMBER_ERR_SHAPE;
+    const int st = check_matrix(L, l_dtype, ldl, V, T == 0);
+    if (st != EMBER_OK) return st;
+    if (T > 0 && (u == nullptr || ids == nullptr || ws == nullptr)) return EMBER_ERR_ARG;
+    for (const void* x : {(const void*)temperature, (const void*)top_k, (const void*)top_p, (const void*)min_p,
+                          (const void*)u, (const void*)logp, (const void*)kept})
+        if (!aligned(x, 4)) return EMBER_ERR_ALIGN;
+    if (!aligned(ids, 8) || !aligned(ws, 256)) return EMBER_ERR_ALIGN;
+    if (T == 0) return EMBER_OK;
+    const size_t need = ember::sample_ws_bytes(T, V);
+    if (ws_bytes < need) return EMBER_ERR_WORKSPACE;
+    const size_t n = (size_t)T * 4;
+    const Operand outs[] = {{array_of(ids, 2 * n), 0}, {array_of(logp, n), 0}, {array_of(kept, n), 0}, {array_of(ws, need), 0}};
+    const Operand ins[] = {{matrix_of(L, T, ldl, V, dtype_size(l_dtype)), 0}, {array_of(temperature, n), 0},
+                           {array_of(top_k, n), 0}, {array_of(top_p, n), 0}, {array_of(min_p, n), 0}, {array_of(u, n), 0}};
+    if (bad_overlap(outs, 4, ins, 6)) return EMBER_ERR_ARG;
+    const ember::SampleArgs a{L,     l_dtype, ldl, T,   V,    temperature, top_k,
+                              top_p, min_p,   u,   ids, logp, kept,        static_cast<char*>(ws)};
+    const hipError_t e = timed("ember_sample", stream, [&] { return ember::launch_sample(a, stream); });
     return e == hipSuccess ? EMBER_OK : EMBER_ERR_HIP;
 }
 

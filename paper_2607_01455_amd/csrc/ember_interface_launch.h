@@ -1,4 +1,4 @@
-// Launchers of the norm, the 8-bit logits and the clipping, for ember_api.cpp:
+// Launchers of the norm, the 8-bit and 4-bit tables, sampling and the clipping, for ember_api.cpp:
 // arguments checked, all work enqueued on s.
 #pragma once
 
@@ -72,6 +72,74 @@ struct LogitsArgs {
     int64_t ldy;
 };
 hipError_t launch_logits(const LogitsArgs& a, hipStream_t s);
+
+// Tables in 4 bits: rows to them and back, logits (ember_q4.hip).  Scales: bf16 bits.
+struct Quant4Args {
+    const void* X;
+    int x_dtype;
+    int64_t ldx;
+    int64_t rows;
+    int64_t D;
+    int group;
+    uint8_t* Q;
+    int64_t ldq;      // bytes
+    uint16_t* gscale;
+    int64_t ldg;      // scales
+};
+hipError_t launch_quantize4(const Quant4Args& a, hipStream_t s);
+struct Rows4Args {
+    const uint8_t* Wq;
+    int64_t ldw;
+    const uint16_t* wscale;
+    int64_t ldg;
+    int group;
+    int64_t V;
+    int64_t D;
+    const int64_t* tok;
+    int64_t n;
+    void* Y;
+    int y_dtype;
+    int64_t ldy;
+};
+hipError_t launch_rows4(const Rows4Args& a, hipStream_t s);
+struct Logits4Args {
+    const int8_t* Xq;
+    int64_t ldx;
+    const float* xscale;
+    const uint8_t* Wq;
+    int64_t ldw;
+    const uint16_t* wscale;
+    int64_t ldg;
+    int group;
+    const float* bias;
+    int64_t T;
+    int64_t V;
+    int64_t D;
+    void* Y;
+    int y_dtype;
+    int64_t ldy;
+};
+hipError_t launch_logits4(const Logits4Args& a, hipStream_t s);
+
+// A token a row of logits (ember_sample.hip).
+struct SampleArgs {
+    const void* L;
+    int l_dtype;
+    int64_t ldl;
+    int64_t T;
+    int64_t V;
+    const float* temperature;
+    const int* top_k;
+    const float* top_p;
+    const float* min_p;
+    const float* u;
+    int64_t* ids;
+    float* logp;
+    int* kept;
+    char* ws;
+};
+size_t sample_ws_bytes(int64_t T, int64_t V);
+hipError_t launch_sample(const SampleArgs& a, hipStream_t s);
 
 // Global gradient norm and clipping (ember_clip.hip).
 size_t clip_ws_bytes(int64_t n);

@@ -34,7 +34,8 @@ EXPORTED = ("ember_workspace_bytes", "ember_init_state", "ember_step_dense",
             "ember_rowonly_step_sparse_rows", "ember_step_sparse_rows_devn",
             "ember_rowonly_step_sparse_rows_devn", "ember_coalesce_workspace_bytes", "ember_coalesce_rows",
             "ember_lmhead_step", "ember_rmsnorm", "ember_rmsnorm_grad_workspace_bytes", "ember_rmsnorm_grad",
-            "ember_quantize_rows", "ember_logits_q8", "ember_clip_workspace_bytes", "ember_clip_grads",
+            "ember_quantize_rows", "ember_logits_q8", "ember_quantize_rows_q4", "ember_rows_q4", "ember_logits_q4",
+            "ember_sample_workspace_bytes", "ember_sample", "ember_clip_workspace_bytes", "ember_clip_grads",
             "ember_step_multi", "ember_get_error", "ember_strerror",
             "ember_profile_enable", "ember_profile_collect", "ember_stream_probe",
             "ember_set_barrier_wait_ticks",
@@ -103,6 +104,11 @@ def _load(path: str = _LIB_PATH) -> ctypes.CDLL:
     lib.ember_rmsnorm_grad.argtypes = [vp, i64, vp, i32, i64, vp, i32, vp, vp, i64, i64, i64, vp, i64, vp, vp, sz, vp]
     lib.ember_quantize_rows.argtypes = [vp, i32, i64, i64, i64, vp, i64, vp, vp]
     lib.ember_logits_q8.argtypes = [vp, i64, vp, vp, i64, vp, vp, i64, i64, i64, vp, i32, i64, vp]
+    lib.ember_quantize_rows_q4.argtypes = [vp, i32, i64, i64, i64, i32, vp, i64, vp, i64, vp]
+    lib.ember_rows_q4.argtypes = [vp, i64, vp, i64, i32, i64, i64, vp, i64, vp, i32, i64, vp]
+    lib.ember_logits_q4.argtypes = [vp, i64, vp, vp, i64, vp, i64, i32, vp, i64, i64, i64, vp, i32, i64, vp]
+    lib.ember_sample_workspace_bytes.argtypes = [i64, i64, ctypes.POINTER(sz)]
+    lib.ember_sample.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.ember_clip_workspace_bytes.argtypes = [i64, ctypes.POINTER(sz)]
     lib.ember_clip_grads.argtypes = [ctypes.POINTER(Grad), i64, f32, vp, vp, sz, vp]
     lib.ember_step_multi.argtypes = [ctypes.POINTER(TableStep), i32, vp]
@@ -125,7 +131,7 @@ LIB = _load()
 
 
 _DTYPES = {torch.float32: EMBER_F32, torch.bfloat16: EMBER_BF16}
-_CHUNK = {torch.float32: 4, torch.bfloat16: 8, torch.int8: 16}   # elements of 16 bytes
+_CHUNK = {torch.float32: 4, torch.bfloat16: 8, torch.int8: 16, torch.uint8: 16}   # elements of 16 bytes
 
 
 def _dtype(t: torch.Tensor) -> int:
@@ -474,6 +480,81 @@ def ember_logits_q8(Xq: torch.Tensor, xscale: torch.Tensor, Wq: torch.Tensor, ws
            "ember_logits_q8")
 
 
+def q4_shapes(V: int, D: int, group: int):
+    """Shapes of a V x D table's codes (uint8) and scales (bf16) in 4 bits; rows of
+    either start on 16-byte boundaries."""
+    if group not in (32, 64, 128):
+        raise ValueError(f"group {group}: 32, 64 or 128 columns share a scale")
+    return (V, (D + 127) // 128 * 64), (V, (D + group - 1) // group)
+
+
+def _table4(Wq, wscale, V, D, group, dev):
+    """Addresses and row strides of a table's codes and scales."""
+    codes, scales = q4_shapes(V, D, group)
+    return *_matrix("Wq", Wq, codes, dev, torch.uint8), *_matrix("wscale", wscale, scales, dev, torch.bfloat16)
+
+
+def ember_quantize_rows_q4(X: torch.Tensor, Q: torch.Tensor, gscale: torch.Tensor, group: int) -> None:
+    """Rows of X in 4 bits: codes Q, packed, and a bf16 scale for each group of columns."""
+    (rows, D), dev = X.shape, X.get_device()
+    x, ldx = _matrix("X", X, X.shape, dev)
+    q, ldq, s, lds = _table4(Q, gscale, rows, D, group, dev)
+    _check(LIB.ember_quantize_rows_q4(x, _dtype(X), ldx, rows, D, group, q, ldq, s, lds, _stream(X)),
+           "ember_quantize_rows_q4")
+
+
+def ember_rows_q4(Wq: torch.Tensor, wscale: torch.Tensor, Y: torch.Tensor, group: int,
+                  tok: torch.Tensor | None = None) -> None:
+    """Y = the rows of a 4-bit table that tok (int64) names, or (None) its first ones."""
+    V, dev = Wq.shape[0], Wq.get_device()
+    n, D = Y.shape
+    w, ldw, s, lds = _table4(Wq, wscale, V, D, group, dev)
+    y, ldy = _matrix("Y", Y, Y.shape, dev)
+    _check(LIB.ember_rows_q4(w, ldw, s, lds, group, V, D, _vector("tok", tok, (n,), dev, torch.int64), n, y,
+                             _dtype(Y), ldy, _stream(Wq)), "ember_rows_q4")
+
+
+def ember_logits_q4(Xq: torch.Tensor, xscale: torch.Tensor, Wq: torch.Tensor, wscale: torch.Tensor,
+                    Y: torch.Tensor, group: int, bias: torch.Tensor | None = None) -> None:
+    """Logits of T tokens from 8-bit hidden states and a table in 4 bits with a scale
+    a group of columns."""
+    T, D = Xq.shape
+    V, dev = Wq.shape[0], Wq.get_device()
+    x, ldx = _matrix("Xq", Xq, (T, D), dev, torch.int8)
+    w, ldw, s, lds = _table4(Wq, wscale, V, D, group, dev)
+    y, ldy = _matrix("Y", Y, (T, V), dev)
+    _check(LIB.ember_logits_q4(x, ldx, _vector("xscale", xscale, (T,), dev), w, ldw, s, lds, group,
+                               _vector("bias", bias, (V,), dev), T, V, D, y, _dtype(Y), ldy, _stream(Wq)),
+           "ember_logits_q4")
+
+
+def ember_sample_workspace_bytes(max_tokens: int, V: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(LIB.ember_sample_workspace_bytes(int(max_tokens), int(V), ctypes.byref(out)),
+           "ember_sample_workspace_bytes")
+    return out.value
+
+
+def ember_sample(L: torch.Tensor, u: torch.Tensor, ids: torch.Tensor, ws: torch.Tensor,
+                 temperature: torch.Tensor | None = None, top_k: torch.Tensor | None = None,
+                 top_p: torch.Tensor | None = None, min_p: torch.Tensor | None = None,
+                 logp: torch.Tensor | None = None, kept: torch.Tensor | None = None) -> None:
+    """A token of each row of logits L, drawn with the random numbers u in [0, 1): ids
+    (int64), and, where wanted, their log-probabilities before the filters and the
+    number of tokens that the filters keep (int32).  Parameters: a value a row, on the
+    device (top_k int32)."""
+    (T, V), dev = L.shape, L.get_device()
+    l, ldl = _matrix("L", L, L.shape, dev)
+    rows = (T,)
+    w, w_bytes = _workspace(ws, dev)
+    _check(LIB.ember_sample(l, _dtype(L), ldl, T, V, _vector("temperature", temperature, rows, dev),
+                            _vector("top_k", top_k, rows, dev, torch.int32), _vector("top_p", top_p, rows, dev),
+                            _vector("min_p", min_p, rows, dev), _vector("u", u, rows, dev),
+                            _vector("ids", ids, rows, dev, torch.int64), _vector("logp", logp, rows, dev),
+                            _vector("kept", kept, rows, dev, torch.int32), w, w_bytes, _stream(L)),
+           "ember_sample")
+
+
 def ember_clip_workspace_bytes(n_grads: int) -> int:
     out = ctypes.c_size_t(0)
     _check(LIB.ember_clip_workspace_bytes(int(n_grads), ctypes.byref(out)), "ember_clip_workspace_bytes")
@@ -572,6 +653,56 @@ class HeadQ8:
 
     def logits(self, Xq: torch.Tensor, xscale: torch.Tensor, Y: torch.Tensor) -> None:
         ember_logits_q8(Xq, xscale, self.Wq, self.wscale, Y, self.bias)
+
+
+class HeadQ4:
+    """A token table in 4 bits, an LM head's or an embedding's (or one for both): packed
+    codes Wq and the scales wscale of groups of columns, D columns, and, if the head has
+    one, a bias."""
+
+    def __init__(self, Wq: torch.Tensor, wscale: torch.Tensor, D: int, group: int = 128,
+                 bias: torch.Tensor | None = None):
+        self.Wq, self.wscale, self.D, self.group, self.bias = Wq, wscale, int(D), int(group), bias
+        self.V = Wq.shape[0]
+
+    @classmethod
+    def from_table(cls, W: torch.Tensor, group: int = 128, bias: torch.Tensor | None = None) -> "HeadQ4":
+        """The head of a table (V x D, fp32 or bf16)."""
+        codes, (V, groups) = q4_shapes(*W.shape, group)
+        Wq = torch.empty(codes, dtype=torch.uint8, device=W.device)
+        wscale = torch.empty(V, (groups + 7) // 8 * 8, dtype=torch.bfloat16, device=W.device)[:, :groups]
+        head = cls(Wq, wscale, W.shape[1], group, bias)
+        head.load(W)
+        return head
+
+    def load(self, W: torch.Tensor) -> None:
+        """Take the table's present rows (after steps on it)."""
+        ember_quantize_rows_q4(W, self.Wq, self.wscale, self.group)
+
+    def logits(self, Xq: torch.Tensor, xscale: torch.Tensor, Y: torch.Tensor) -> None:
+        if Xq.shape[1] != self.D:
+            raise ValueError(f"Xq has {Xq.shape[1]} columns, the head {self.D}")
+        ember_logits_q4(Xq, xscale, self.Wq, self.wscale, Y, self.group, self.bias)
+
+    def rows(self, tok: torch.Tensor | None, Y: torch.Tensor) -> None:
+        """Y = the rows of the tokens tok (int64), or (None) the first ones."""
+        if Y.shape[1] != self.D:
+            raise ValueError(f"Y has {Y.shape[1]} columns, the table {self.D}")
+        ember_rows_q4(self.Wq, self.wscale, Y, self.group, tok)
+
+
+class Sampler:
+    """Draws a token from each of up to max_tokens rows of V logits; holds the
+    workspace.  Call it as ember_sample, without the workspace."""
+
+    def __init__(self, max_tokens: int, V: int, device="cuda"):
+        self.max_tokens, self.V = int(max_tokens), int(V)
+        nbytes = ember_sample_workspace_bytes(self.max_tokens, self.V)
+        self.ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+    def __call__(self, L: torch.Tensor, u: torch.Tensor, ids: torch.Tensor, temperature=None, top_k=None, top_p=None,
+                 min_p=None, logp=None, kept=None) -> None:
+        ember_sample(L, u, ids, self.ws, temperature, top_k, top_p, min_p, logp, kept)
 
 
 class GradClipper:
