@@ -8,17 +8,22 @@
 // met differently in fp64 is as rare as a difference of 2^-45.
 //
 // The three filters each keep a prefix of the tokens in falling order (equal logits
-// by index), so what is kept is the shortest of three prefixes, and one (logit,
-// index) says where it ends.  Four launches:
+// by index), so what is kept is the shortest of three prefixes, and one place (logit
+// and index in one number) says where it ends.  The token is then the one at which
+// the running sum, by index, of the kept weights passes u times their sum.
+//
+// Rows of up to 16384 tokens: one launch, a block a row, which holds it in registers.
+// Longer ones take four:
 //   1  the largest and smallest logit of each part of a row;
 //   2  weights, their sum for every chunk of 512 tokens, and, where top-k or top-p
 //      is on, a histogram over z of counts and weights;
 //   3  from the histogram the bins in which the prefixes end: their tokens go to
-//      a list; sums of the tokens before them for every chunk;
-//   4  a block a row sorts the list, finds the end of the prefix, finds the chunk
-//      in which the random number falls, and in it the token.
-// A list that does not fit (thousands of equal logits where a prefix ends) is
-// replaced by a search for the prefix's end by halving, over the whole row.
+//      a list; for every chunk the sum of the tokens before them;
+//   4  a block a row finds the prefix's end among the listed, the chunk in which
+//      the random number falls, and in it the token.
+// An end is found by histograms over the places, each over one bin of the last.  A
+// list that does not fit (thousands of equal logits where a prefix ends) is
+// replaced by a search over the whole row by halving.
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -35,16 +40,20 @@ typedef unsigned long long u64;
 
 constexpr int kThreads = 512;                     // launches 1 to 3
 constexpr int kWavesB = kThreads / kWave;
-constexpr int kLastThreads = 1024;                // launch 4
+constexpr int kRowThreads = 1024;                 // a block that has a row
 constexpr int kPerLane = 8;                       // logits a lane
 constexpr int kChunk = kWave * kPerLane;          // tokens of a chunk
 constexpr int kBins = 1024;
 constexpr int kList = 8192;                       // tokens of a row's list
+constexpr int kPartList = 2048;                   // of a part's
 constexpr int kMaxParts = 64;                     // of a row
 constexpr int64_t kMaxRows = 512;                 // of a launch
+constexpr int64_t kOneBlock = 16384;              // tokens of a row that a block holds
+constexpr int kSteps = 32;                        // of a halving of the weight: z counts these
 constexpr double kLog2e = 1.4426950408889634;
 constexpr double kLn2 = 0.6931471805599453;
-constexpr double kFar = 64.0;                     // a z from which on a weight is 0
+constexpr double kFar = 64.0 * kSteps;            // a z from which on a weight is 0
+static_assert(kBins == kRowThreads, "a bin a thread");
 
 struct Part {            // of a row's logits
     float top, low;      // of those above minus infinity
@@ -70,7 +79,8 @@ struct Space {           // a launch's rows in the workspace
     u64* weight;         // kBins a row
     int* count;          // kBins a row
     u64* list;           // kList a row
-    u64* chunk;          // chunks a row
+    u64* chunk;          // chunks a row: sums of weights
+    float* peak;         // chunks a row: largest logits
 };
 
 struct Params {
@@ -80,6 +90,7 @@ struct Params {
     int parts;           // of a row, and their chunks
     int part_chunks;
     int bits;            // behind the weights' point
+    int width;           // bits of an index
 };
 
 size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
@@ -98,15 +109,64 @@ size_t space_of(char* ws, int64_t rows, int64_t V, Space* s) {
     char* const count = take((size_t)rows * kBins * 4);
     char* const list = take((size_t)rows * kList * 8);
     char* const chunk = take((size_t)rows * (size_t)chunks_of(V) * 8);
+    char* const peak = take((size_t)rows * (size_t)chunks_of(V) * 4);
     if (s)
         *s = Space{reinterpret_cast<Part*>(parts), reinterpret_cast<RowState*>(state), reinterpret_cast<u64*>(weight),
-                   reinterpret_cast<int*>(count),  reinterpret_cast<u64*>(list),       reinterpret_cast<u64*>(chunk)};
+                   reinterpret_cast<int*>(count),  reinterpret_cast<u64*>(list),       reinterpret_cast<u64*>(chunk),
+                   reinterpret_cast<float*>(peak)};
     return at;
+}
+
+// The value of another lane of the row of 16, or of an earlier row's end; `none` where there is none.
+template <int kCtrl, int kRows>
+__device__ __forceinline__ int from_lane(int x, int none) {
+    return __builtin_amdgcn_update_dpp(none, x, kCtrl, kRows, 0xF, false);
+}
+template <int kCtrl, int kRows>
+__device__ __forceinline__ float from_lane(float x, float none) {
+    return __int_as_float(from_lane<kCtrl, kRows>(__float_as_int(x), __float_as_int(none)));
+}
+template <int kCtrl, int kRows>
+__device__ __forceinline__ u64 from_lane(u64 x, u64 none) {
+    const uint32_t lo = (uint32_t)from_lane<kCtrl, kRows>((int)(uint32_t)x, (int)(uint32_t)none);
+    const uint32_t hi = (uint32_t)from_lane<kCtrl, kRows>((int)(uint32_t)(x >> 32), (int)(uint32_t)(none >> 32));
+    return (u64)hi << 32 | lo;
+}
+// Inclusive sums over a wave: shifts by 1, 2, 4 and 8 within rows of 16 lanes, then the
+// sums of the row before and of the half before.  (Exchanges through the LDS took most
+// of launch 4's time.)
+template <typename V>
+__device__ __forceinline__ V wave_scan(V x) {
+    x += from_lane<0x111, 0xF>(x, (V)0);
+    x += from_lane<0x112, 0xF>(x, (V)0);
+    x += from_lane<0x114, 0xF>(x, (V)0);
+    x += from_lane<0x118, 0xF>(x, (V)0);
+    x += from_lane<0x142, 0xA>(x, (V)0);
+    x += from_lane<0x143, 0xC>(x, (V)0);
+    return x;
+}
+__device__ __forceinline__ int last_lane(int x) { return __builtin_amdgcn_readlane(x, kWave - 1); }
+__device__ __forceinline__ float last_lane(float x) { return __int_as_float(last_lane(__float_as_int(x))); }
+__device__ __forceinline__ u64 last_lane(u64 x) {
+    return (u64)(uint32_t)last_lane((int)(uint32_t)(x >> 32)) << 32 | (uint32_t)last_lane((int)(uint32_t)x);
+}
+template <typename V>
+__device__ __forceinline__ V wave_sum(V x) { return last_lane(wave_scan(x)); }
+// The result over a wave of an operation for which twice the same is once, such as a maximum.
+template <typename V, typename Op>
+__device__ __forceinline__ V wave_one(V x, Op op) {
+    x = op(x, from_lane<0x111, 0xF>(x, x));
+    x = op(x, from_lane<0x112, 0xF>(x, x));
+    x = op(x, from_lane<0x114, 0xF>(x, x));
+    x = op(x, from_lane<0x118, 0xF>(x, x));
+    x = op(x, from_lane<0x142, 0xA>(x, x));
+    x = op(x, from_lane<0x143, 0xC>(x, x));
+    return last_lane(x);
 }
 
 // What one row asks for.
 struct Ask {
-    double heat;         // log2(e) / temperature
+    double heat;         // steps of z a unit of logit
     int k;               // 0: off
     float p;
     float floor;         // min-p
@@ -125,65 +185,96 @@ __device__ __forceinline__ Ask ask_of(const SampleArgs& a, int64_t t) {
               q.floor >= 0.0f && q.floor <= 1.0f && q.u >= 0.0f && q.u < 1.0f;
     // temperature 0: the first of the largest logits
     if (temperature == 0.0f) q.k = 1;
-    q.heat = kLog2e / (temperature == 0.0f ? 1.0 : (double)temperature);
-    q.far = q.floor > 0.0f ? -log2((double)q.floor) : 1e300;
+    q.heat = kSteps * kLog2e / (temperature == 0.0f ? 1.0 : (double)temperature);
+    q.far = q.floor > 0.0f ? -kSteps * log2((double)q.floor) : 1e300;
     return q;
 }
 
-// What is known of a row after launch 1.
+// What is known of a row once its range is.
 struct Row {
     Ask ask;
     double top;
-    double scale;        // bins a unit of z
+    double scale;        // bins a step of z
     int some;
     bool fine;           // there is something to draw from
 };
-__device__ __forceinline__ Row row_of(const Params& p, int64_t t, int r) {
+// The same in all lanes: kept in scalar registers.
+__device__ __forceinline__ double uniform(double x) {
+    const u64 b = (u64)__double_as_longlong(x);
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((int)(uint32_t)b);
+    const uint32_t hi = __builtin_amdgcn_readfirstlane((int)(uint32_t)(b >> 32));
+    return __longlong_as_double((long long)((u64)hi << 32 | lo));
+}
+__device__ __forceinline__ Row row_of(const Params& p, int64_t t, const Part& q) {
     Row x;
     x.ask = ask_of(p.a, t);
-    float top = -__builtin_inff(), low = __builtin_inff();
-    int some = 0, bad = 0;
-    for (int c = threadIdx.x & (kWave - 1); c < p.parts; c += kWave) {
-        const Part q = p.s.parts[(int64_t)r * kMaxParts + c];
-        top = fmaxf(top, q.top);
-        low = fminf(low, q.low);
-        some += q.some;
-        bad |= q.bad;
-    }
-    top = wave_all(top, [](float x, float y) { return fmaxf(x, y); });
-    low = wave_all(low, [](float x, float y) { return fminf(x, y); });
-    x.some = wave_all(some, [](int x, int y) { return x + y; });
-    bad = wave_all(bad, [](int x, int y) { return x | y; });
-    x.fine = x.ask.right && !bad && x.some > 0;
-    x.top = top;
-    const double span = fmin(((double)top - (double)low) * x.ask.heat, (double)p.bits + 1.0);
-    x.scale = x.fine && span > 0.0 ? kBins / span : 0.0;
+    x.ask.heat = uniform(x.ask.heat);
+    x.ask.far = uniform(x.ask.far);
+    x.some = __builtin_amdgcn_readfirstlane(q.some);
+    x.fine = __builtin_amdgcn_readfirstlane(x.ask.right && !q.bad && q.some > 0);
+    x.top = uniform(q.top);
+    const double span = fmin(((double)q.top - (double)q.low) * x.ask.heat, (p.bits + 1.0) * kSteps);
+    x.scale = uniform(x.fine && span > 0.0 ? kBins / span : 0.0);
     return x;
+}
+__device__ __forceinline__ Part join(const Part& a, const Part& b) {
+    return Part{fmaxf(a.top, b.top), fminf(a.low, b.low), a.some + b.some, a.bad | b.bad};
+}
+__device__ __forceinline__ Part wave_join(Part x) {
+    return Part{wave_one(x.top, [](float a, float b) { return fmaxf(a, b); }),
+                wave_one(x.low, [](float a, float b) { return fminf(a, b); }), wave_sum(x.some),
+                wave_one(x.bad, [](int a, int b) { return a | b; })};
+}
+template <int kN>
+__device__ __forceinline__ Part block_join(Part x, Part* red) {
+    x = wave_join(x);
+    if ((threadIdx.x & (kWave - 1)) == 0) red[threadIdx.x / kWave] = x;
+    __syncthreads();
+    x = red[0];
+#pragma unroll
+    for (int w = 1; w < kN / kWave; ++w) x = join(x, red[w]);
+    return x;
+}
+constexpr float kInf = __builtin_inff();
+__device__ __forceinline__ void see(Part& q, float l) {
+    q.bad |= !(l < kInf);
+    q.top = fmaxf(q.top, l);
+    q.low = l != -kInf ? fminf(q.low, l) : q.low;
+    q.some += l != -kInf;
+}
+// Launches 2 to 4: from the parts of launch 1.
+__device__ __forceinline__ Row row_at(const Params& p, int64_t t, int r) {
+    const int c = threadIdx.x & (kWave - 1);
+    static_assert(kMaxParts == kWave, "a part a lane");
+    return row_of(p, t, wave_join(c < p.parts ? p.s.parts[(int64_t)r * kMaxParts + c] : Part{-kInf, kInf, 0, 0}));
 }
 __device__ __forceinline__ double z_of(const Row& x, float l) { return fmin((x.top - (double)l) * x.ask.heat, kFar); }
 __device__ __forceinline__ int bin_of(const Row& x, double z) { return min(kBins - 1, (int)(z * x.scale)); }
 
-// 2^-z in fixed point.  2^f for |f| <= 1/2 is the sum of (f ln 2)^n / n!, whose
-// terms from the 13th on are below 2^-52; adding 2^52 leaves the integer in the
+// 2^-(z / kSteps) in fixed point.  With n the nearest whole step it is the table's
+// 2^(bits - (n mod kSteps) / kSteps), times a power of two, times e^y, |y| <= ln 2 / 64, whose
+// series' terms from the 7th on are below 2^-58.  Adding 2^52 leaves the integer in the
 // low bits of the fp64 number, rounded to nearest.
-__device__ __forceinline__ u64 weight_of(double z, int bits) {
-    const double k = rint(-z);
-    const double y = (-z - k) * kLn2;
-    double e = 1.0 / 479001600.0;
-    e = fma(e, y, 1.0 / 39916800.0);
-    e = fma(e, y, 1.0 / 3628800.0);
-    e = fma(e, y, 1.0 / 362880.0);
-    e = fma(e, y, 1.0 / 40320.0);
-    e = fma(e, y, 1.0 / 5040.0);
-    e = fma(e, y, 1.0 / 720.0);
+__device__ __forceinline__ u64 weight_of(double z, const double* table) {
+    const double n = rint(z);
+    const double y = (n - z) * (kLn2 / kSteps);
+    double e = 1.0 / 720.0;
     e = fma(e, y, 1.0 / 120.0);
     e = fma(e, y, 1.0 / 24.0);
     e = fma(e, y, 1.0 / 6.0);
     e = fma(e, y, 0.5);
     e = fma(e, y, 1.0);
     e = fma(e, y, 1.0);
-    const double v = ldexp(e, (int)k + bits) + 4503599627370496.0;
+    // the table's exponent less the whole halvings, k / kSteps of them
+    const uint32_t k = (uint32_t)n;
+    u64 two = (u64)__double_as_longlong(table[k & (kSteps - 1)]);
+    two -= (u64)(k << 15 & 0xFFF00000u) << 32;
+    const double v = fma(e, __longlong_as_double((long long)two), 4503599627370496.0);
     return (u64)__double_as_longlong(v) & 0xFFFFFFFFFFFFFull;
+}
+static_assert(kSteps == 32, "a shift by 20 - 5");
+__device__ __forceinline__ void fill_table(double* table, int bits) {
+    if (threadIdx.x < kSteps) table[threadIdx.x] = exp2(bits - threadIdx.x * (1.0 / kSteps));
 }
 
 // Place of a token in falling order: its logit, turned so that larger ones have
@@ -192,10 +283,18 @@ __device__ __forceinline__ uint32_t fall_of(float l) {
     const uint32_t b = __float_as_uint(l == 0.0f ? 0.0f : l);     // both zeros are one
     return b & 0x80000000u ? b : ~(b | 0x80000000u);
 }
-__device__ __forceinline__ u64 place_of(float l, uint32_t i) { return (u64)fall_of(l) << 32 | i; }
-__device__ __forceinline__ float logit_of(u64 place) {
-    const uint32_t f = (uint32_t)(place >> 32);
-    return __uint_as_float(f & 0x80000000u ? f : ~f & 0x7FFFFFFFu);
+__device__ __forceinline__ float logit_of_fall(uint32_t f) { return __uint_as_float(f & 0x80000000u ? f : ~f & 0x7FFFFFFFu); }
+// (of a bf16 logit's turned bits the lower half follows from the upper)
+template <typename T> constexpr int kFallBits = 8 * (int)sizeof(T);
+template <typename T>
+__device__ __forceinline__ u64 place_of(float l, uint32_t i, int width) {
+    return (u64)(fall_of(l) >> (32 - kFallBits<T>)) << width | i;
+}
+template <typename T>
+__device__ __forceinline__ float logit_of(u64 place, int width) {
+    const uint32_t f = (uint32_t)(place >> width);
+    if constexpr (sizeof(T) == 4) return logit_of_fall(f);
+    else return logit_of_fall(f << 16 | (f & 0x8000u ? 0u : 0xFFFFu));
 }
 
 // Eight logits from an index on (a multiple of 8); minus infinity past the row.
@@ -215,28 +314,21 @@ __device__ __forceinline__ void load8(const T* l, int64_t i, int64_t V, float (&
     }
 }
 
-__device__ __forceinline__ u64 wave_sum(u64 x) {
-    return wave_all(x, [](u64 a, u64 b) { return a + b; });
-}
-
 // Inclusive sums over the threads of a block, and their total.  red: a slot a wave.
 template <int kN, typename V>
 __device__ __forceinline__ V block_scan(V x, V* red, V& total) {
-    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-#pragma unroll
-    for (int m = 1; m < kWave; m <<= 1) {
-        const V y = __shfl_up(x, m);
-        if (lane >= m) x += y;
-    }
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    x = wave_scan(x);
     __syncthreads();
-    if (lane == kWave - 1) red[wave] = x;
+    if ((threadIdx.x & (kWave - 1)) == kWave - 1) red[wave] = x;
     __syncthreads();
     V before = 0;
     total = 0;
 #pragma unroll
     for (int w = 0; w < kN / kWave; ++w) {
-        if (w < wave) before += red[w];
-        total += red[w];
+        const V y = red[w];
+        before += w < wave ? y : 0;
+        total += y;
     }
     return before + x;
 }
@@ -248,16 +340,252 @@ __device__ __forceinline__ V block_sum(V x, V* red) {
 }
 
 // ---------------------------------------------------------------------------
-// launches 1 to 3: part blockIdx.x of row blockIdx.y
+// where a prefix ends
 // ---------------------------------------------------------------------------
+
+struct Select {
+    u64 weight[kBins];
+    int count[kBins];
+    u64 red[kRowThreads / kWave];
+    int redi[kRowThreads / kWave];
+    u64 lo, hi;                  // places among which the end is
+    u64 w;                       // weights before them
+    int n;                       // tokens there
+    int in;                      // tokens among them
+};
+constexpr u64 kNone = ~(u64)0;   // past every place
+
+// The first place up to which the candidates' count (or their weights) reaches
+// `need`, of 1 at least and at most what there is.  A block's threads have kOwn
+// tokens each, of which those in the mask are candidates; every pass makes a
+// histogram over one bin of the last, until a bin holds one.  n, w: what there is
+// up to the place, it included.
+template <bool kWeights, int kOwn, typename F, typename G>
+__device__ u64 end_of(F place, G weight, uint32_t mask, u64 need, Select& s, int& n, u64& w) {
+    u64 lo = kNone, hi = 0;
+#pragma unroll
+    for (int q = 0; q < kOwn; ++q) {
+        if (!(mask >> q & 1)) continue;
+        lo = min(lo, place(q));
+        hi = max(hi, place(q));
+    }
+    lo = wave_one(lo, [](u64 a, u64 b) { return a < b ? a : b; });
+    hi = wave_one(hi, [](u64 a, u64 b) { return a > b ? a : b; });
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        s.lo = kNone;
+        s.hi = 0;
+        s.w = 0;
+        s.n = 0;
+    }
+    s.weight[threadIdx.x] = 0;
+    s.count[threadIdx.x] = 0;
+    __syncthreads();
+    if ((threadIdx.x & (kWave - 1)) == 0) {
+        atomicMin(&s.lo, lo);
+        atomicMax(&s.hi, hi);
+    }
+    // a pass leaves ten bits less of at most 56
+    for (int pass = 0; pass < 7; ++pass) {
+        __syncthreads();
+        const u64 from = s.lo, to = s.hi, w0 = s.w;
+        const int n0 = s.n;
+        if (pass > 0 && s.in == 1) break;
+        const u64 wide = to - from;
+        const int shift = wide < kBins ? 0 : 64 - __clzll(wide) - 10;
+#pragma unroll
+        for (int q = 0; q < kOwn; ++q) {
+            if (!(mask >> q & 1) || place(q) < from || place(q) > to) continue;
+            const int b = (int)((place(q) - from) >> shift);
+            atomicAdd(&s.weight[b], weight(q));
+            atomicAdd(&s.count[b], 1);
+        }
+        __syncthreads();
+        const u64 wb = s.weight[threadIdx.x];
+        const int nb = s.count[threadIdx.x];
+        s.weight[threadIdx.x] = 0;
+        s.count[threadIdx.x] = 0;
+        u64 w1 = wave_scan(wb);
+        int n1 = wave_scan(nb);
+        if ((threadIdx.x & (kWave - 1)) == kWave - 1) {
+            s.red[wave] = w1;
+            s.redi[wave] = n1;
+        }
+        __syncthreads();
+        w1 += w0;
+        n1 += n0;
+#pragma unroll
+        for (int q = 0; q < kRowThreads / kWave; ++q) {
+            w1 += q < wave ? s.red[q] : 0;
+            n1 += q < wave ? s.redi[q] : 0;
+        }
+        const u64 before = kWeights ? w1 - wb : (u64)(n1 - nb), after = kWeights ? w1 : (u64)n1;
+        if (nb > 0 && before < need && after >= need) {
+            s.lo = from + ((u64)threadIdx.x << shift);
+            s.hi = min(to, s.lo + (((u64)1 << shift) - 1));
+            s.w = w1 - wb;
+            s.n = n1 - nb;
+            s.in = nb;
+        }
+    }
+    __syncthreads();
+    const u64 from = s.lo, to = s.hi;
+    n = s.n + 1;
+    const u64 w0 = s.w;
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < kOwn; ++q) {
+        if ((mask >> q & 1) && place(q) >= from && place(q) <= to) {
+            s.lo = place(q);
+            s.w = w0 + weight(q);
+        }
+    }
+    __syncthreads();
+    w = s.w;
+    return s.lo;
+}
+
+// The row's p-th part of a sum: what comes before a token that top-p keeps is below it.
+__device__ __forceinline__ u64 part_of(u64 total, float p) { return (u64)ceil((double)total * (double)p); }
+__device__ __forceinline__ bool ranked(const Ask& q) { return q.k > 0 || q.p < 1.0f; }   // an end has to be found
+
+__device__ __forceinline__ void no_token(const SampleArgs& a, int64_t t) {
+    a.ids[t] = -1;
+    if (a.logp) a.logp[t] = __uint_as_float(0x7FC00000u);
+    if (a.kept) a.kept[t] = 0;
+}
+__device__ __forceinline__ void token(const Params& p, int64_t t, int64_t i, double z, u64 all, int kept) {
+    p.a.ids[t] = i;
+    if (p.a.logp) p.a.logp[t] = (float)((p.bits - z / kSteps) * kLn2 - log((double)all));
+    if (p.a.kept) p.a.kept[t] = kept;
+}
+
+// ---------------------------------------------------------------------------
+// one launch: row blockIdx.x, eight tokens a thread side by side, kPieces times
+// ---------------------------------------------------------------------------
+
+template <typename T, int kPieces>
+__global__ __launch_bounds__(kRowThreads) void ember_sample_row(Params p) {
+    constexpr int kOwn = kPieces * kPerLane;
+    __shared__ Select s;
+    __shared__ double table[kSteps];
+    __shared__ Part redp[kRowThreads / kWave];
+    const int64_t t = blockIdx.x;
+    const T* const l = static_cast<const T*>(p.a.L) + t * p.a.ldl;
+    fill_table(table, p.bits);
+    float x[kOwn];
+    Part part{-kInf, kInf, 0, 0};
+#pragma unroll
+    for (int q = 0; q < kPieces; ++q) {
+        float y[kPerLane];
+        load8(l, (int64_t)(q * kRowThreads + threadIdx.x) * kPerLane, p.a.V, y);
+#pragma unroll
+        for (int e = 0; e < kPerLane; ++e) {
+            x[q * kPerLane + e] = y[e];
+            see(part, y[e]);
+        }
+    }
+    const Row row = row_of(p, t, block_join<kRowThreads>(part, redp));
+    if (!row.fine) {
+        if (threadIdx.x == 0) no_token(p.a, t);
+        return;
+    }
+    // where the registers do not hold them all, weights are formed where they are used
+    constexpr bool kHeld = kPieces == 1;
+    u64 held[kHeld ? kOwn : 1], all = 0;
+    const auto weight = [&](int q) {
+        if constexpr (kHeld) return held[q];
+        else return weight_of(z_of(row, x[q]), table);
+    };
+    uint32_t mask = 0;                    // tokens of this thread that have a weight, then those that are kept
+    int near = 0;
+#pragma unroll
+    for (int q = 0; q < kOwn; ++q) {
+        const double z = z_of(row, x[q]);
+        const u64 w = weight_of(z, table);
+        if constexpr (kHeld) held[q] = w;
+        all += w;
+        mask |= (uint32_t)(w != 0) << q;
+        near += x[q] != -kInf && z <= row.ask.far;
+    }
+    all = block_sum<kRowThreads>(all, s.red);
+    int kept = row.some;
+    if (ranked(row.ask)) {
+        const auto place = [&](int q) {
+            const uint32_t i = (q / kPerLane * kRowThreads + threadIdx.x) * kPerLane + q % kPerLane;
+            return place_of<T>(x[q], i, p.width);
+        };
+        const int positive = block_sum<kRowThreads>((int)__popc(mask), s.redi);
+        u64 last = kNone, total = all;    // the last place that is kept, and the weights up to it
+        int n;
+        if (row.ask.k > 0) {
+            kept = min(kept, row.ask.k);
+            if (row.ask.k < positive) last = end_of<false, kOwn>(place, weight, mask, (u64)row.ask.k, s, n, total);
+        }
+        if (row.ask.p < 1.0f) {
+            const u64 need = part_of(total, row.ask.p);
+            last = end_of<true, kOwn>(place, weight, mask, need > 0 ? need : 1, s, n, total);
+            kept = n;
+        }
+#pragma unroll
+        for (int q = 0; q < kOwn; ++q) mask &= ~((uint32_t)(place(q) > last) << q);
+    }
+    if (row.ask.floor > 0.0f) {
+        kept = min(kept, block_sum<kRowThreads>(near, s.redi));
+#pragma unroll
+        for (int q = 0; q < kOwn; ++q) mask &= ~((uint32_t)(z_of(row, x[q]) > row.ask.far) << q);
+    }
+    // running sums by index: a piece is a whole run of the row
+    u64 end[kPieces], total = 0;
+#pragma unroll
+    for (int q = 0; q < kPieces; ++q) {
+        u64 sum = 0, piece;
+#pragma unroll
+        for (int e = 0; e < kPerLane; ++e) sum += mask >> (q * kPerLane + e) & 1 ? weight(q * kPerLane + e) : 0;
+        end[q] = total + block_scan<kRowThreads>(sum, s.red, piece);
+        total += piece;
+    }
+    const u64 target = (u64)((double)total * (double)row.ask.u);
+#pragma unroll
+    for (int q = 0; q < kPieces; ++q) {
+        u64 run = end[q];
+#pragma unroll
+        for (int e = kPerLane - 1; e >= 0; --e) {
+            const int o = q * kPerLane + e;
+            const u64 after = run;
+            run -= mask >> o & 1 ? weight(o) : 0;
+            if (run <= target && target < after)
+                token(p, t, (q * kRowThreads + threadIdx.x) * kPerLane + e, z_of(row, x[o]), all, kept);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// launches 1 to 3 of longer rows: part blockIdx.x of row blockIdx.y
+// ---------------------------------------------------------------------------
+
+// A wave's chunks from j on, every kWavesB-th: f(chunk, this lane's logits), with the next
+// chunk's loads ahead.
+template <typename T, typename F>
+__device__ __forceinline__ void each_chunk(const T* l, int64_t V, int j, int end, F f) {
+    const int lane = threadIdx.x & (kWave - 1);
+    float x[kPerLane], y[kPerLane];
+    if (j < end) load8(l, (int64_t)j * kChunk + lane * kPerLane, V, x);
+    for (; j < end; j += kWavesB) {
+        if (j + kWavesB < end) load8(l, (int64_t)(j + kWavesB) * kChunk + lane * kPerLane, V, y);
+        f(j, x);
+#pragma unroll
+        for (int e = 0; e < kPerLane; ++e) x[e] = y[e];
+    }
+}
 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void ember_sample_range(Params p, int64_t t0) {
-    __shared__ float redf[kWavesB];
-    __shared__ int redi[kWavesB];
+    __shared__ Part redp[kWavesB];
     const int c = blockIdx.x, r = blockIdx.y;
     const T* const l = static_cast<const T*>(p.a.L) + (t0 + r) * p.a.ldl;
-    const int wave = threadIdx.x / kWave, lane = threadIdx.x & (kWave - 1);
+    const int wave = threadIdx.x / kWave;
     // what launches 2 and 3 add to
     const int share = (kBins + p.parts - 1) / p.parts;
     for (int b = c * share + threadIdx.x; b < min((c + 1) * share, kBins); b += kThreads) {
@@ -270,73 +598,68 @@ __global__ __launch_bounds__(kThreads) void ember_sample_range(Params p, int64_t
         s.listed = 0;
         s.near = 0;
     }
-    float top = -__builtin_inff(), low = __builtin_inff();
-    int some = 0, bad = 0;
+    Part part{-kInf, kInf, 0, 0};
     const int end = min((c + 1) * p.part_chunks, p.chunks);
-    for (int j = c * p.part_chunks + wave; j < end; j += kWavesB) {
-        float x[kPerLane];
-        load8(l, (int64_t)j * kChunk + lane * kPerLane, p.a.V, x);
+    each_chunk(l, p.a.V, c * p.part_chunks + wave, end, [&](int, const float (&x)[kPerLane]) {
 #pragma unroll
-        for (int e = 0; e < kPerLane; ++e) {
-            const bool is = x[e] != -__builtin_inff();
-            bad |= !(x[e] < __builtin_inff());
-            top = fmaxf(top, x[e]);
-            low = is ? fminf(low, x[e]) : low;
-            some += is;
-        }
-    }
-    top = row_all<kThreads>(top, [](float x, float y) { return fmaxf(x, y); }, redf);
-    some = row_all<kThreads>(some, [](int x, int y) { return x + y; }, redi);
-    __syncthreads();
-    low = row_all<kThreads>(low, [](float x, float y) { return fminf(x, y); }, redf);
-    bad = row_all<kThreads>(bad, [](int x, int y) { return x | y; }, redi);
-    if (threadIdx.x == 0) p.s.parts[(int64_t)r * kMaxParts + c] = Part{top, low, some, bad};
+        for (int e = 0; e < kPerLane; ++e) see(part, x[e]);
+    });
+    part = block_join<kThreads>(part, redp);
+    if (threadIdx.x == 0) p.s.parts[(int64_t)r * kMaxParts + c] = part;
 }
-
-__device__ __forceinline__ bool ranked(const Ask& q) { return q.k > 0 || q.p < 1.0f; }   // a histogram is needed
 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void ember_sample_weights(Params p, int64_t t0) {
     __shared__ u64 weight[kBins];
     __shared__ int count[kBins];
+    __shared__ double table[kSteps];
     __shared__ u64 red[kWavesB];
     __shared__ int redi[kWavesB];
     const int c = blockIdx.x, r = blockIdx.y;
     const T* const l = static_cast<const T*>(p.a.L) + (t0 + r) * p.a.ldl;
-    const Row row = row_of(p, t0 + r, r);
+    const Row row = row_at(p, t0 + r, r);
     if (!row.fine) return;
     const int wave = threadIdx.x / kWave, lane = threadIdx.x & (kWave - 1);
-    const bool hist = ranked(row.ask);
+    const bool hist = ranked(row.ask), floored = row.ask.floor > 0.0f;
+    fill_table(table, p.bits);
     if (hist) {
         for (int b = threadIdx.x; b < kBins; b += kThreads) {
             weight[b] = 0;
             count[b] = 0;
         }
-        __syncthreads();
     }
+    __syncthreads();
     u64 all = 0;
     int near = 0;
     const int end = min((c + 1) * p.part_chunks, p.chunks);
-    for (int j = c * p.part_chunks + wave; j < end; j += kWavesB) {
-        float x[kPerLane];
-        load8(l, (int64_t)j * kChunk + lane * kPerLane, p.a.V, x);
+    each_chunk(l, p.a.V, c * p.part_chunks + wave, end, [&](int j, const float (&x)[kPerLane]) {
         u64 sum = 0;
 #pragma unroll
         for (int e = 0; e < kPerLane; ++e) {
             const double z = z_of(row, x[e]);
-            const u64 w = weight_of(z, p.bits);
+            const u64 w = weight_of(z, table);
             sum += w;
-            near += x[e] != -__builtin_inff() && z <= row.ask.far;
             if (hist && w) {
                 const int b = bin_of(row, z);
                 atomicAdd(&weight[b], w);
                 atomicAdd(&count[b], 1);
             }
         }
+        if (floored) {
+#pragma unroll
+            for (int e = 0; e < kPerLane; ++e) near += x[e] != -kInf && z_of(row, x[e]) <= row.ask.far;
+        }
         sum = wave_sum(sum);
-        if (lane == 0) p.s.chunk[(int64_t)r * p.chunks + j] = sum;
+        float peak = x[0];
+#pragma unroll
+        for (int e = 1; e < kPerLane; ++e) peak = fmaxf(peak, x[e]);
+        peak = wave_one(peak, [](float a, float b) { return fmaxf(a, b); });
+        if (lane == 0) {
+            p.s.chunk[(int64_t)r * p.chunks + j] = sum;
+            p.s.peak[(int64_t)r * p.chunks + j] = peak;
+        }
         all += sum;
-    }
+    });
     all = block_sum<kThreads>(lane == 0 ? all : 0, red);
     near = block_sum<kThreads>(near, redi);
     if (threadIdx.x == 0) {
@@ -353,22 +676,46 @@ __global__ __launch_bounds__(kThreads) void ember_sample_weights(Params p, int64
     }
 }
 
-// The row's p-th part of a sum: what comes before a token that top-p keeps is below it.
-__device__ __forceinline__ u64 part_of(u64 total, float p) { return (u64)ceil((double)total * (double)p); }
+// The smallest logit for which `is` holds, where it holds for the larger ones of two
+// and for the row's largest: 64 candidates at a time, one a lane.
+template <typename F>
+__device__ __forceinline__ float smallest(float top, F is) {
+    const int lane = threadIdx.x & (kWave - 1);
+    uint32_t lo = fall_of(top), hi = 0xFF7FFFFFu;      // is(lo) holds; the lowest finite logit
+    while (lo < hi) {
+        const uint32_t step = (hi - lo + kWave - 1) / kWave;
+        const uint32_t f = (uint32_t)min((u64)hi, (u64)lo + (u64)step * (lane + 1));
+        const int n = __popcll(__ballot(is(logit_of_fall(f))));      // the first n candidates hold
+        const uint32_t last = n ? (uint32_t)min((u64)hi, (u64)lo + (u64)step * n) : lo;
+        hi = n == kWave ? hi : (uint32_t)min((u64)hi, (u64)lo + (u64)step * (n + 1)) - 1;
+        lo = last;
+        if (n == kWave) break;
+    }
+    return logit_of_fall(lo);
+}
 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void ember_sample_list(Params p, int64_t t0) {
+    __shared__ double table[kSteps];
     __shared__ u64 red[kWavesB];
     __shared__ int redi[kWavesB];
     __shared__ RowState found;
+    __shared__ float edge[7];
+    __shared__ float dense[kWavesB][kChunk];
+    __shared__ uint16_t index[kWavesB][kChunk];
+    __shared__ u64 list[kPartList];
+    __shared__ int listed;
+    __shared__ unsigned joined;
     const int c = blockIdx.x, r = blockIdx.y;
     const T* const l = static_cast<const T*>(p.a.L) + (t0 + r) * p.a.ldl;
-    const Row row = row_of(p, t0 + r, r);
+    const Row row = row_at(p, t0 + r, r);
     const bool hist = ranked(row.ask);
     if (!row.fine || (!hist && row.ask.floor == 0.0f)) return;
     const int wave = threadIdx.x / kWave, lane = threadIdx.x & (kWave - 1);
+    fill_table(table, p.bits);
 
     if (threadIdx.x == 0) {
+        listed = 0;
         found.bin_k = found.bin_p = kBins;
         found.bin_p1 = -1;
         found.w_k = found.w_p = 0;
@@ -426,12 +773,21 @@ __global__ __launch_bounds__(kThreads) void ember_sample_list(Params p, int64_t 
                 nb += n[q];
             }
         }
-        __syncthreads();
-    } else {
-        __syncthreads();
     }
+    __syncthreads();
     const int bin_k = found.bin_k, bin_p = found.bin_p, bin_p1 = found.bin_p1;
     const int sure = min(bin_k, bin_p);
+    // the bins' edges as logits: the smallest one before a bin
+    if (wave < 7) {
+        const int b = wave == 0 ? sure : wave == 1 ? bin_k : wave == 2 ? bin_k + 1 : wave == 3 ? bin_p : bin_p1 + 1;
+        // (bin 0: none, past the largest)
+        // (5, 6: the smallest that min-p keeps, and one below which there is no weight)
+        const double far = wave == 5 ? row.ask.far : (p.bits + 1.0) * kSteps + 1.0;
+        const float at = wave >= 5 ? smallest((float)row.top, [&](float x) { return z_of(row, x) <= far; })
+                         : b <= 0  ? kInf
+                                   : smallest((float)row.top, [&](float x) { return bin_of(row, z_of(row, x)) < b; });
+        if (lane == 0) edge[wave] = at;
+    }
     RowState& s = p.s.rows[r];
     if (c == 0 && threadIdx.x == 0) {
         s.w_k = found.w_k;
@@ -443,26 +799,68 @@ __global__ __launch_bounds__(kThreads) void ember_sample_list(Params p, int64_t 
         s.bin_p1 = bin_p1;
         s.sure = sure;
     }
+    __syncthreads();
+    const float from = fmaxf(edge[0], edge[5]);                // kept for certain: from this logit on
+    const float k0 = edge[1], k1 = bin_k < kBins ? fmaxf(edge[2], edge[6]) : kInf;      // listed: [k1, k0) and [p1, p0)
+    const float p0 = edge[3], p1 = bin_p < kBins ? fmaxf(edge[4], edge[6]) : kInf;
     const int end = min((c + 1) * p.part_chunks, p.chunks);
-    for (int j = c * p.part_chunks + wave; j < end; j += kWavesB) {
-        float x[kPerLane];
-        const int64_t i = (int64_t)j * kChunk + lane * kPerLane;
-        load8(l, i, p.a.V, x);
-        u64 sum = 0;
+    const float least = fminf(from, fminf(k1, p1));            // below it nothing counts
+    // A wave's chunks, every kWavesB-th, 64 at a time; those with a logit that counts are
+    // gone through: their tokens that count side by side in LDS, then a token a lane.
+    for (int j0 = c * p.part_chunks + wave; j0 < end; j0 += kWavesB * kWave) {
+        const int mine = j0 + lane * kWavesB;
+        const int64_t at = (int64_t)r * p.chunks + mine;
+        const bool some = mine < end && p.s.peak[at] >= least;
+        if (mine < end && !some) p.s.chunk[at] = 0;
+        u64 todo = __ballot(some);
+        float x[kPerLane], y[kPerLane];
+        auto chunk_of = [&](u64 m) { return j0 + (__ffsll(m) - 1) * kWavesB; };
+        if (todo) load8(l, (int64_t)chunk_of(todo) * kChunk + lane * kPerLane, p.a.V, x);
+        while (todo) {
+            const int j = chunk_of(todo);
+            todo &= todo - 1;
+            if (todo) load8(l, (int64_t)chunk_of(todo) * kChunk + lane * kPerLane, p.a.V, y);
+            int n = 0;
 #pragma unroll
-        for (int e = 0; e < kPerLane; ++e) {
-            const double z = z_of(row, x[e]);
-            const int b = bin_of(row, z);
-            if (b < sure) {
-                if (z <= row.ask.far) sum += weight_of(z, p.bits);
-            } else if ((b == bin_k || (b >= bin_p && b <= bin_p1)) && weight_of(z, p.bits)) {
-                const unsigned at = atomicAdd(&s.listed, 1u);
-                if (at < (unsigned)kList) p.s.list[(int64_t)r * kList + at] = place_of(x[e], (uint32_t)(i + e));
+            for (int e = 0; e < kPerLane; ++e) n += x[e] >= least;
+            int put = wave_scan(n);
+            const int total = last_lane(put);
+            put -= n;
+#pragma unroll
+            for (int e = 0; e < kPerLane; ++e) {
+                if (x[e] >= least) {
+                    dense[wave][put] = x[e];
+                    index[wave][put++] = (uint16_t)(lane * kPerLane + e);
+                }
             }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            u64 sum = 0;
+            for (int q = lane; q < total; q += kWave) {
+                const float v = dense[wave][q];
+                if (v >= from) {
+                    sum += weight_of(z_of(row, v), table);
+                } else if ((v >= k1 && v < k0) || (v >= p1 && v < p0)) {
+                    const int to = atomicAdd(&listed, 1);
+                    if (to < kPartList) list[to] = place_of<T>(v, (uint32_t)(j * kChunk + index[wave][q]), p.width);
+                }
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            sum = wave_sum(sum);
+            if (lane == 0) p.s.chunk[(int64_t)r * p.chunks + j] = sum;
+#pragma unroll
+            for (int e = 0; e < kPerLane; ++e) x[e] = y[e];
         }
-        sum = wave_sum(sum);
-        if (lane == 0) p.s.chunk[(int64_t)r * p.chunks + j] = sum;
     }
+    // the block's list joins the row's
+    __syncthreads();
+    const int n = listed;
+    if (n == 0) return;
+    if (threadIdx.x == 0) joined = atomicAdd(&s.listed, n > kPartList ? (unsigned)kList + 1 : (unsigned)n);
+    __syncthreads();
+    for (int q = threadIdx.x; q < min(n, kPartList); q += kThreads)
+        if (joined + q < (unsigned)kList) p.s.list[(int64_t)r * kList + joined + q] = list[q];
 }
 
 // ---------------------------------------------------------------------------
@@ -471,86 +869,80 @@ __global__ __launch_bounds__(kThreads) void ember_sample_list(Params p, int64_t 
 
 // Tokens up to a place in falling order, or (weights) their weights.
 template <bool kWeights, typename T>
-__device__ u64 up_to(const Params& p, const Row& row, const T* l, u64 place, u64* red) {
+__device__ u64 up_to(const Params& p, const Row& row, const T* l, u64 place, Select& s, const double* table) {
     u64 sum = 0;
-    for (int64_t i = threadIdx.x * kPerLane; i < p.a.V; i += kLastThreads * kPerLane) {
+    for (int64_t i = threadIdx.x * kPerLane; i < p.a.V; i += kRowThreads * kPerLane) {
         float x[kPerLane];
         load8(l, i, p.a.V, x);
 #pragma unroll
         for (int e = 0; e < kPerLane; ++e) {
-            if (x[e] != -__builtin_inff() && place_of(x[e], (uint32_t)(i + e)) <= place)
-                sum += kWeights ? weight_of(z_of(row, x[e]), p.bits) : 1;
+            if (x[e] != -kInf && place_of<T>(x[e], (uint32_t)(i + e), p.width) <= place)
+                sum += kWeights ? weight_of(z_of(row, x[e]), table) : 1;
         }
     }
-    return block_sum<kLastThreads>(sum, red);
+    return block_sum<kRowThreads>(sum, s.red);
 }
 
-// The first place up to which there is `need`, 1 at least, by halving: the logit, then the index.
+// The first place up to which there is `need`, 1 at least, by halving.
 template <bool kWeights, typename T>
-__device__ u64 reach(const Params& p, const Row& row, const T* l, u64 need, u64* red) {
-    u64 low = 0, high = ~(u64)0;      // the answer is in [low, high]
-    for (int half = 0; half < 2; ++half) {
-        // logits first: places that end in all ones
-        const u64 fine = half == 0 ? 0xFFFFFFFFull : 0;
-        while ((low | fine) < (high | fine)) {
-            const u64 mid = (low + (high - low) / 2) | fine;
-            if (up_to<kWeights>(p, row, l, mid, red) >= need) high = mid;
-            else low = mid + 1;
-        }
-        if (half == 0) {
-            low = high & ~0xFFFFFFFFull;
-            high = low | (uint32_t)(p.a.V - 1);
-        }
+__device__ u64 reach(const Params& p, const Row& row, const T* l, u64 need, Select& s, const double* table) {
+    u64 low = place_of<T>((float)row.top, 0, p.width), high = ((u64)1 << (kFallBits<T> + p.width)) - 1;      // the answer is in [low, high]
+    while (low < high) {
+        const u64 mid = low + (high - low) / 2;
+        if (up_to<kWeights>(p, row, l, mid, s, table) >= need) high = mid;
+        else low = mid + 1;
     }
     return high;
 }
 
 template <typename T>
-__global__ __launch_bounds__(kLastThreads) void ember_sample_draw(Params p, int64_t t0) {
-    __shared__ u64 entry[kList];
-    __shared__ u64 red[kLastThreads / kWave];
-    __shared__ int redi[kLastThreads / kWave];
-    __shared__ u64 found_at;
-    __shared__ u64 found_before;
+__global__ __launch_bounds__(kRowThreads) void ember_sample_draw(Params p, int64_t t0) {
+    __shared__ Select s;
+    __shared__ double table[kSteps];
+    __shared__ u64 more[kRowThreads];      // what is kept of a thread's chunks beside their sums
     const int r = blockIdx.x;
     const int64_t t = t0 + r;
     const T* const l = static_cast<const T*>(p.a.L) + t * p.a.ldl;
-    const Row row = row_of(p, t, r);
+    const Row row = row_at(p, t, r);
     if (!row.fine) {
-        if (threadIdx.x == 0) {
-            p.a.ids[t] = -1;
-            if (p.a.logp) p.a.logp[t] = __uint_as_float(0x7FC00000u);
-            if (p.a.kept) p.a.kept[t] = 0;
-        }
+        if (threadIdx.x == 0) no_token(p.a, t);
         return;
     }
-    const bool hist = ranked(row.ask), floored = row.ask.floor > 0.0f;
-    u64* const chunk = p.s.chunk + (int64_t)r * p.chunks;
-    const RowState& s = p.s.rows[r];
+    // what is needed later, ahead: this thread's chunks, the first of the list
+    const bool hist = ranked(row.ask);
+    const int own = (p.chunks + kRowThreads - 1) / kRowThreads;      // chunks a thread
+    u64 sum = 0;
+    for (int j = threadIdx.x * own; j < min((int)(threadIdx.x + 1) * own, p.chunks); ++j)
+        sum += p.s.chunk[(int64_t)r * p.chunks + j];
+    const u64 first = hist ? p.s.list[(int64_t)r * kList + threadIdx.x] : 0;
+    const RowState st = p.s.rows[r];
+    fill_table(table, p.bits);
+    more[threadIdx.x] = 0;
+    __syncthreads();
+    const u64 all = st.all;
     u64 last = 0;                     // the last place that is kept, where the bins alone do not say it
     int sure = kBins;                 // tokens of bins before it are kept
     int kept = row.some;              // before min-p
     if (hist) {
-        sure = s.sure;
-        const int k = row.ask.k > 0 ? min(row.ask.k, row.some) : row.some;
-        kept = k;
-        const bool has_k = s.bin_k < kBins, has_p = s.bin_p < kBins;
-        const int n = (int)min(s.listed, (unsigned)kList + 1);
+        sure = st.sure;
+        if (row.ask.k > 0) kept = min(kept, row.ask.k);
+        const bool has_k = st.bin_k < kBins, has_p = st.bin_p < kBins;
+        const int n = (int)min(st.listed, (unsigned)kList + 1);
+        u64 total = all;
         if (n > kList) {
             // too many for the list: search the row, then sum its chunks again
-            last = ~(u64)0;
-            u64 total = s.all;
+            last = kNone;
             if (has_k) {
-                last = reach<false>(p, row, l, (u64)row.ask.k, red);
-                total = up_to<true>(p, row, l, last, red);
+                last = reach<false>(p, row, l, (u64)row.ask.k, s, table);
+                total = up_to<true>(p, row, l, last, s, table);
             }
             if (has_p) {
                 const u64 need = part_of(total, row.ask.p);
-                last = min(last, reach<true>(p, row, l, need > 0 ? need : 1, red));
-                kept = (int)up_to<false>(p, row, l, last, red);
+                last = min(last, reach<true>(p, row, l, need > 0 ? need : 1, s, table));
+                kept = (int)up_to<false>(p, row, l, last, s, table);
             }
             const int wave = threadIdx.x / kWave, lane = threadIdx.x & (kWave - 1);
-            for (int j = wave; j < p.chunks; j += kLastThreads / kWave) {
+            for (int j = wave; j < p.chunks; j += kRowThreads / kWave) {
                 float x[kPerLane];
                 const int64_t i = (int64_t)j * kChunk + lane * kPerLane;
                 load8(l, i, p.a.V, x);
@@ -558,123 +950,89 @@ __global__ __launch_bounds__(kLastThreads) void ember_sample_draw(Params p, int6
 #pragma unroll
                 for (int e = 0; e < kPerLane; ++e) {
                     const double z = z_of(row, x[e]);
-                    if (place_of(x[e], (uint32_t)(i + e)) <= last && z <= row.ask.far) sum += weight_of(z, p.bits);
+                    if (place_of<T>(x[e], (uint32_t)(i + e), p.width) <= last && z <= row.ask.far)
+                        sum += weight_of(z, table);
                 }
                 sum = wave_sum(sum);
-                if (lane == 0) __hip_atomic_store(&chunk[j], sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                if (lane == 0) atomicAdd(&more[j / own], sum);
             }
             sure = 0;
-            __threadfence();
         } else if (n > 0) {
-            int n2 = 2;
-            while (n2 < n) n2 *= 2;
-            for (int i = threadIdx.x; i < n2; i += kLastThreads)
-                entry[i] = i < n ? p.s.list[(int64_t)r * kList + i] : ~(u64)0;
-            __syncthreads();
-            for (int size = 2; size <= n2; size *= 2) {
-                for (int step = size / 2; step > 0; step /= 2) {
-                    for (int q = threadIdx.x; q < n2 / 2; q += kLastThreads) {
-                        const int i = (q / step) * 2 * step + q % step, j = i + step;
-                        const u64 x = entry[i], y = entry[j];
-                        if ((x > y) == ((i & size) == 0)) {
-                            entry[i] = y;
-                            entry[j] = x;
-                        }
-                    }
-                    __syncthreads();
-                }
-            }
-            // this thread's entries and their weights
-            constexpr int kOwn = kList / kLastThreads;
-            u64 w[kOwn], w_list = 0, w_k = 0;
-            int bin[kOwn], before_k = 0;
+            constexpr int kOwn = kList / kRowThreads;
+            u64 at[kOwn], w[kOwn];
+            uint32_t in_k = 0, in_p = 0;
+            const auto place = [&](int q) { return at[q]; };
+            const auto weight = [&](int q) { return w[q]; };
+            const auto logit = [&](int q) { return logit_of<T>(at[q], p.width); };
 #pragma unroll
             for (int q = 0; q < kOwn; ++q) {
-                const int i = threadIdx.x * kOwn + q;
-                const double z = i < n ? z_of(row, logit_of(entry[i])) : kFar;
-                w[q] = i < n ? weight_of(z, p.bits) : 0;
-                bin[q] = i < n ? bin_of(row, z) : kBins;
-                before_k += bin[q] < s.bin_k;
-                w_list += w[q];
+                at[q] = kNone;
+                w[q] = 0;
+                if (q * kRowThreads >= n) continue;
+                const int i = q * kRowThreads + threadIdx.x;
+                if (i < n) at[q] = q == 0 ? first : p.s.list[(int64_t)r * kList + i];
+                const double z = i < n ? z_of(row, logit(q)) : kFar;
+                w[q] = weight_of(z, table);
+                const int b = bin_of(row, z);
+                if (w[q] == 0) at[q] = kNone;
+                in_k |= (uint32_t)(w[q] && b == st.bin_k) << q;
+                in_p |= (uint32_t)(w[q] && b >= st.bin_p && b <= st.bin_p1) << q;
             }
-            int first_k = n, end_k = n;       // of the list: bin_k's first entry, and the first that top-k drops
-            u64 total = s.all;
+            int found;
+            u64 sum;
             if (has_k) {
-                first_k = block_sum<kLastThreads>(before_k, redi);
-                end_k = min(n, first_k + (row.ask.k - s.n_k));
-#pragma unroll
-                for (int q = 0; q < kOwn; ++q) {
-                    const int i = threadIdx.x * kOwn + q;
-                    if (i >= first_k && i < end_k) w_k += w[q];
-                }
-                total = s.w_k + block_sum<kLastThreads>(w_k, red);
+                last = end_of<false, kOwn>(place, weight, in_k, (u64)(row.ask.k - st.n_k), s, found, sum);
+                total = st.w_k + sum;
             }
-            int take = has_k ? end_k : 0;     // entries that are kept
             if (has_p) {
+                // what the bins before keep is below this part, and at bin_p1's end it is reached
                 const u64 need = part_of(total, row.ask.p);
-                u64 all;
-                u64 before = s.w_p + block_scan<kLastThreads>(w_list, red, all) - w_list;
-                int mine = 0;
-#pragma unroll
-                for (int q = 0; q < kOwn; ++q) {
-                    const int i = threadIdx.x * kOwn + q;
-                    // the largest logit is kept whatever top-p is
-                    mine += i < end_k && bin[q] <= s.bin_p1 && (before < need || (i == 0 && s.n_p == 0));
-                    before += w[q];
-                }
-                take = block_sum<kLastThreads>(mine, redi);
-                kept = s.n_p + take;
+                last = end_of<true, kOwn>(place, weight, in_p, need > st.w_p ? need - st.w_p : 1, s, found, sum);
+                kept = st.n_p + found;
             }
-            if (take > 0) last = entry[take - 1];
-            // the kept entries join their chunks' sums
-            __syncthreads();
+            // the kept ones join their chunks' sums
 #pragma unroll
             for (int q = 0; q < kOwn; ++q) {
-                const int i = threadIdx.x * kOwn + q;
-                if (i < take && z_of(row, logit_of(entry[i])) <= row.ask.far)
-                    atomicAdd(&chunk[(uint32_t)entry[i] / kChunk], w[q]);
+                if (at[q] <= last && z_of(row, logit(q)) <= row.ask.far)
+                    atomicAdd(&more[(uint32_t)(at[q] & (((u64)1 << p.width) - 1)) / (kChunk * own)], w[q]);
             }
-            __threadfence();
         }
-        __syncthreads();
-    }
-    if (floored) kept = min(kept, s.near);
-
-    // the chunk in which u falls
-    auto sum_of = [&](int64_t j) { return __hip_atomic_load(&chunk[j], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
-    const int own = (p.chunks + kLastThreads - 1) / kLastThreads, j0 = threadIdx.x * own, j1 = min(j0 + own, p.chunks);
-    u64 sum = 0, total;
-    for (int j = j0; j < j1; ++j) sum += sum_of(j);
-    u64 before = block_scan<kLastThreads>(sum, red, total) - sum;
-    const u64 target = (u64)((double)total * (double)row.ask.u);
-    if (before <= target && target < before + sum) {
-        int j = j0;
-        for (; j < j1 - 1; ++j) {
-            const u64 x = sum_of(j);
-            if (target < before + x) break;
-            before += x;
-        }
-        found_at = j;
-        found_before = before;
     }
     __syncthreads();
-    // and the token: one a thread
-    const int64_t i = (int64_t)found_at * kChunk + threadIdx.x;
-    const u64 base = found_before;
-    u64 w = 0;
-    double z = 0.0;
-    if (threadIdx.x < kChunk && i < p.a.V) {
-        const float x = load_elem(l, i, sizeof(T) == 2);
-        z = z_of(row, x);
-        const bool keep = bin_of(row, z) < sure || place_of(x, (uint32_t)i) <= last;
-        if (keep && z <= row.ask.far) w = weight_of(z, p.bits);
+    if (row.ask.floor > 0.0f) kept = min(kept, st.near);
+
+    // the thread in whose chunks u falls
+    u64 kept_sum;
+    sum = (sure > 0 ? sum : 0) + more[threadIdx.x];
+    if (threadIdx.x == 0) s.lo = kNone;
+    const u64 end = block_scan<kRowThreads>(sum, s.red, kept_sum);
+    const u64 target = (u64)((double)kept_sum * (double)row.ask.u);
+    if (end - sum <= target && target < end) {
+        s.lo = threadIdx.x;
+        s.w = end - sum;
     }
-    u64 in_chunk;
-    const u64 end = base + block_scan<kLastThreads>(w, red, in_chunk);
-    if (end - w <= target && target < end) {
-        p.a.ids[t] = i;
-        if (p.a.logp) p.a.logp[t] = (float)((p.bits - z) * kLn2 - log((double)s.all));
-        if (p.a.kept) p.a.kept[t] = kept;
+    __syncthreads();
+    if (s.lo == kNone) {      // not met: the largest logit is always kept
+        if (threadIdx.x == 0) no_token(p.a, t);
+        return;
+    }
+    // and the token in them, one a thread
+    int64_t i = (int64_t)s.lo * own * kChunk + threadIdx.x;
+    u64 before = s.w;
+    for (int q = 0; q < own * kChunk; q += kRowThreads, i += kRowThreads) {
+        u64 w = 0;
+        double z = 0.0;
+        if (q + (int)threadIdx.x < own * kChunk && i < p.a.V) {
+            const float x = load_elem(l, i, sizeof(T) == 2);
+            z = z_of(row, x);
+            const bool keep = bin_of(row, z) < sure || place_of<T>(x, (uint32_t)i, p.width) <= last;
+            if (keep && z <= row.ask.far) w = weight_of(z, table);
+        }
+        u64 piece;
+        const u64 to = before + block_scan<kRowThreads>(w, s.red, piece);
+        if (to - w <= target && target < to) token(p, t, i, z, all, kept);
+        before += piece;
+        if (target < before) break;
     }
 }
 
@@ -684,7 +1042,15 @@ hipError_t launch(const Params& p, int64_t t0, int rows, bool list, hipStream_t 
     ember_sample_range<T><<<grid, kThreads, 0, s>>>(p, t0);
     ember_sample_weights<T><<<grid, kThreads, 0, s>>>(p, t0);
     if (list) ember_sample_list<T><<<grid, kThreads, 0, s>>>(p, t0);
-    ember_sample_draw<T><<<rows, kLastThreads, 0, s>>>(p, t0);
+    ember_sample_draw<T><<<rows, kRowThreads, 0, s>>>(p, t0);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_row(const Params& p, hipStream_t s) {
+    const unsigned rows = (unsigned)p.a.T;
+    if (p.a.V <= kOneBlock / 2) ember_sample_row<T, 1><<<rows, kRowThreads, 0, s>>>(p);
+    else ember_sample_row<T, 2><<<rows, kRowThreads, 0, s>>>(p);
     return hipGetLastError();
 }
 
@@ -695,14 +1061,15 @@ size_t sample_ws_bytes(int64_t T, int64_t V) { return space_of(nullptr, std::min
 hipError_t launch_sample(const SampleArgs& a, hipStream_t s) {
     Params p;
     p.a = a;
+    p.width = 0;
+    while (((int64_t)1 << p.width) < a.V) ++p.width;
+    p.bits = std::min(48, 62 - p.width);
+    if (a.V <= kOneBlock) return a.l_dtype == EMBER_F32 ? launch_row<float>(p, s) : launch_row<uint16_t>(p, s);
     const int64_t rows = std::min(a.T, kMaxRows);
     space_of(a.ws, rows, a.V, &p.s);
     p.chunks = (int)chunks_of(a.V);
-    int width = 0;
-    while (((int64_t)1 << width) < a.V) ++width;
-    p.bits = std::min(48, 62 - width);
-    // about 1024 blocks, of a chunk a wave at least
-    const int64_t want = std::min<int64_t>({(1024 + rows - 1) / rows, (p.chunks + kWavesB - 1) / kWavesB, kMaxParts});
+    // about 1024 blocks, of two chunks a wave at least
+    const int64_t want = std::min<int64_t>({(1024 + rows - 1) / rows, (p.chunks + 2 * kWavesB - 1) / (2 * kWavesB), kMaxParts});
     p.part_chunks = (int)((p.chunks + want - 1) / want);
     p.parts = (p.chunks + p.part_chunks - 1) / p.part_chunks;
     const bool list = a.top_k || a.top_p || a.min_p || a.temperature;
