@@ -177,93 +177,95 @@ void launch_rows(const RowsParams& p, unsigned grid, hipStream_t s) {
 // logits of few tokens
 // ---------------------------------------------------------------------------
 
-constexpr int kFewWaves = 16;
-constexpr int kFewThreads = kFewWaves * kWave;
-constexpr int kStrip = 16;                     // channels of a strip
+constexpr int kUnit = 4;                       // blocks of codes a unit: 512 columns
 constexpr int kFewLds = 152 * 1024;
+
+// kWide: 32 x 32 tiles, MT of them over the tokens; else one of 16 x 16.
+template <bool kWide_, int MT_>
+struct Stream {
+    static constexpr bool kWide = kWide_;
+    static constexpr int MT = MT_;
+    static constexpr int kRows = kWide ? 32 : 16;           // channels of a strip, tokens of a tile
+    static constexpr int kTokens = kRows * MT;
+    static constexpr int kWaves = kWide ? 8 : 16;
+    static constexpr int kThreads = kWaves * kWave;
+    static constexpr int kDepth = kWide ? 2 : 3;            // units in registers
+    static constexpr int kLoadsW = kWide ? 2 * kUnit : kUnit;    // 16-byte loads of a unit's codes
+    static constexpr int kAcc = kWide ? 16 : 4;             // values of a tile a lane
+    static constexpr int kLanes = kWide ? 2 : 4;            // lanes of a row
+};
 
 struct Few4Params {
     Logits4Args a;
     int nblk;            // blocks of codes a row
     int groups;
+    int units;           // of a row
     int pitch;           // bytes of a token in LDS
-    int64_t units;       // of `strips` strips each
-    int strips;
+    int window;          // units that the LDS holds of each token
+    int share;           // waves that share a strip: each takes every share-th unit
+    int64_t strips;
+    int together;        // neighbouring strips of a block (where a wave goes through several)
+    bool several;        // a wave goes through several strips
+    int tiles;           // of tokens
+    int blocks;          // of a tile of tokens
 };
 
-// Up to 16 NB tokens whose codes fit the LDS: bound by the table's bytes.  The
-// block holds the tokens in LDS, in the order of the table's operands; each wave
-// streams strips of 16 channels, CH blocks of codes a chunk straight from memory
-// into registers, with the next chunk's loads in flight.  The tokens are the rows
-// of the MFMA tiles, so a lane's values are all of one channel, the one whose codes
-// it loads, and need that channel's scale alone.
-template <int NB, int G, int CH, typename YT>
-__global__ __launch_bounds__(kFewThreads) void ember_logits_q4_few(Few4Params p) {
+// Few tokens, 16 to 64 a block: bound by the table's bytes.  A block holds the tokens'
+// codes in LDS, in the order of the table's operands (all columns, or a window of them
+// after the other); each wave streams strips of 16 or 32 channels straight from memory
+// into registers, the next units' loads in flight.  The tokens are the rows of the
+// MFMA tiles, so a lane's values are all of one channel, the one whose codes it
+// loads, and need that channel's scale alone.  Where a table has few strips several
+// waves share one, unit by unit, and add up in LDS.  Blocks of the same channels and
+// other tokens are neighbours on one XCD, whose L2 then has the codes.  The order of
+// a logit's sum depends on V and D, not on the number of tokens.
+template <typename C, int G, typename YT>
+__global__ __launch_bounds__(C::kThreads) void ember_logits_q4_few(Few4Params p) {
     const Logits4Args& a = p.a;
-    constexpr int kPer = kBlockCols / G;                // groups a block
-    constexpr int kScaleLoads = CH * kPer * 2 / 16;     // 16-byte loads of a chunk's scales
-    static_assert(CH * kPer * 2 % 16 == 0, "whole loads of scales");
+    constexpr int kPer = kBlockCols / G;                    // groups a block
+    constexpr int kScaleBytes = kUnit * kPer * 2;           // of a unit: 8, 16 or 32
+    constexpr int kScaleWords = kScaleBytes / 4;
+    typedef int acc_t __attribute__((ext_vector_type(C::kAcc)));
+    typedef float facc_t __attribute__((ext_vector_type(C::kAcc)));
     __shared__ __attribute__((aligned(16))) uint8_t lds[kFewLds];
+    __shared__ float xs[64];
     const int lane = threadIdx.x & (kWave - 1);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int row = lane & 15, quarter = lane >> 4;
-    const int nblk = p.nblk, D = (int)a.D, T = (int)a.T;
+    const int row = lane % C::kRows, part = lane / C::kRows;
+    const int nblk = p.nblk, D = (int)a.D;
+    // block -> tile of tokens and block of channels: on an XCD the tiles of the same channels side by side
+    const int in_xcd = blockIdx.x / kXcds, block = in_xcd / p.tiles * kXcds + blockIdx.x % kXcds;
+    const int64_t t0 = (int64_t)(in_xcd % p.tiles) * C::kTokens;
+    const int T = (int)min((int64_t)C::kTokens, a.T - t0);
+    if (block >= p.blocks) return;
 
-    // the tokens' codes, 16 columns a thread: columns 4 q .. of the 16 go to the 16 bytes
-    // that quarter q reads
-    for (int i = threadIdx.x; i < T * nblk * 8; i += kFewThreads) {
-        const int t = i / (nblk * 8), c = i - t * (nblk * 8), k = c * 16;
-        i32x4 x = {0, 0, 0, 0};
-        if (k < D) {   // the padding up to 16 columns is readable
-            x = *reinterpret_cast<const i32x4*>(a.Xq + t * a.ldx + k);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int n = D - k - 4 * j;
-                x[j] &= n >= 4 ? -1 : n <= 0 ? 0 : (int)((1u << (8 * n)) - 1);
-            }
-        }
-        const int s = c / 8, w = c % 8 / 2, h = c % 2;
-        uint8_t* at = lds + t * p.pitch + s * kBlockCols + (w >> 1) * 64 + ((w & 1) * 2 + h) * 4;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) *reinterpret_cast<int*>(at + 16 * j) = x[j];
+    // this wave's strips and units
+    const int per_block = C::kWaves / p.share, mate = wave % p.share, place = wave / p.share;
+    int64_t first, pass;
+    if (p.several) {
+        // `together` neighbours, then those of the grid's other blocks
+        first = ((int64_t)block + (int64_t)p.blocks * (place / p.together)) * p.together + place % p.together;
+        pass = (int64_t)p.blocks * per_block;
+    } else {
+        first = (int64_t)block * per_block + place;
+        pass = p.strips;
     }
-    float xs[NB][4];
-    uint32_t at_x[NB];
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int t = 16 * b + 4 * quarter + e;
-            xs[b][e] = t < T ? a.xscale[t] * 0.0625f : 0.0f;     // the operands are 16 times the codes
-        }
-        at_x[b] = (uint32_t)(min(16 * b + row, T - 1) * p.pitch + quarter * 16);   // rows past T: any token
-    }
-    __syncthreads();
-
-    const int chunks = (nblk + CH - 1) / CH;
-    // this wave's strips: wave % strips of each of its units
-    const int per_pass = kFewWaves / p.strips;
-    const int64_t unit0 = blockIdx.x + (int64_t)gridDim.x * (wave / p.strips);
-    const int mine = unit0 < p.units ? (int)((p.units - 1 - unit0) / ((int64_t)gridDim.x * per_pass)) + 1 : 0;
-    if (mine == 0) return;
-    auto channel = [&](int i) {
-        return ((unit0 + (int64_t)i * gridDim.x * per_pass) * p.strips + wave % p.strips) * kStrip;
-    };
+    const int mine = first < p.strips ? (int)((p.strips - 1 - first) / pass) + 1 : 0;
+    auto channel = [&](int i) { return (first + i * pass) * C::kRows; };
     const int64_t row_bytes = (int64_t)nblk * kBlockBytes;
-    const uint32_t off_w = (uint32_t)row * (uint32_t)a.ldw + quarter * 16;
+    const uint32_t off_w = (uint32_t)row * (uint32_t)a.ldw + part * (kBlockBytes / C::kLanes);
     const uint32_t off_s = (uint32_t)row * (uint32_t)a.ldg * 2;
-
     auto buffer = [&](const void* base, int64_t bytes) {
         return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0,
                                                  (int)(bytes < kBufferMax ? bytes : kBufferMax), kBufferWord3);
     };
-    struct Chunk {
-        i32x4 w[CH];
-        u32x4_t s[kScaleLoads];
+    struct Unit {
+        i32x4 w[C::kLoadsW];
+        uint32_t s[kScaleWords];
         float bias;
     };
-    // chunk c of strip i: zeros past the table (also for strips past it) and past the row
-    auto load = [&](int i, int c, Chunk& k) {
+    // unit u of strip i: zeros past the table (also for strips past it) and past the row
+    auto load = [&](int i, int u, Unit& k) {
         const int64_t v = channel(i);
         const bool in = i < mine && v < a.V;
         const int64_t v_in = in ? v : 0, left = in ? a.V - 1 - v : 0;
@@ -271,111 +273,208 @@ __global__ __launch_bounds__(kFewThreads) void ember_logits_q4_few(Few4Params p)
         const auto rs = buffer(a.wscale + v_in * a.ldg, in ? (left * a.ldg + (p.groups + 7) / 8 * 8) * 2 : 0);
         const auto rb = buffer(a.bias ? a.bias + v_in : a.xscale, in && a.bias ? (left + 1) * 4 : 0);
 #pragma unroll
-        for (int b = 0; b < CH; ++b) {
-            const int s = c * CH + b;
-            const uint32_t off = s < nblk ? off_w + s * kBlockBytes : kBufferMax;
+        for (int b = 0; b < C::kLoadsW; ++b) {
+            const int s = u * kUnit + b / (C::kLoadsW / kUnit);
+            const uint32_t off = s < nblk ? off_w + s * kBlockBytes + b % (C::kLoadsW / kUnit) * 16 : kBufferMax;
             k.w[b] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, off, 0, 0));
         }
+        // (16 bytes at a time where there are as many; groups past the row's are not used)
+        const uint32_t off = u * kUnit * kPer < p.groups ? off_s + u * kScaleBytes : kBufferMax;
+        if constexpr (kScaleBytes == 8) {
+            const u32x2_t d = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_raw_buffer_load_b64(rs, off, 0, 0));
+            k.s[0] = d[0];
+            k.s[1] = d[1];
+        } else {
 #pragma unroll
-        for (int b = 0; b < kScaleLoads; ++b) {
-            const int g = c * CH * kPer + 8 * b;
-            const uint32_t off = g < p.groups ? off_s + g * 2 : kBufferMax;
-            k.s[b] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rs, off, 0, 0));
+            for (int q = 0; q < kScaleWords; q += 4) {
+                const u32x4_t d = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rs, off + 4 * q, 0, 0));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) k.s[q + e] = d[e];
+            }
         }
         k.bias = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rb, row * 4, 0, 0));
     };
 
-    f32x4 f[NB];
-    auto multiply = [&](int c, const Chunk& k) {
+    uint32_t at_x[C::MT];
 #pragma unroll
-        for (int b = 0; b < CH; ++b) {
-            const int s = c * CH + b;
+    for (int m = 0; m < C::MT; ++m)       // rows past T: any token
+        at_x[m] = (uint32_t)(min(C::kRows * m + row, T - 1) * p.pitch + part * 16);
+
+    facc_t f[C::MT];
+    auto clear = [&] {
+#pragma unroll
+        for (int m = 0; m < C::MT; ++m)
+#pragma unroll
+            for (int e = 0; e < C::kAcc; ++e) f[m][e] = 0.0f;
+    };
+    // u0: the unit that the LDS begins with
+    auto multiply = [&](int u, int u0, const Unit& k) {
+#pragma unroll
+        for (int b = 0; b < kUnit; ++b) {
+            const int s = u * kUnit + b;
             if (s >= nblk) continue;
-            i32x4 op[2];
+            // A block's operands.  16 x 16 tiles: two of 64 columns, or four of 32; a lane's quarter
+            // of the block's bytes holds them.  32 x 32 tiles: four of 32 columns, each a dword of
+            // both quarters that a lane has.
+            i32x4 op[C::kWide ? 4 : 2];
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-                op[h] = i32x4{(int)low_codes(k.w[b][2 * h]), (int)high_codes(k.w[b][2 * h]),
-                              (int)low_codes(k.w[b][2 * h + 1]), (int)high_codes(k.w[b][2 * h + 1])};
+            for (int h = 0; h < (C::kWide ? 4 : 2); ++h) {
+                const uint32_t d0 = C::kWide ? k.w[2 * b][h] : k.w[b][2 * h % 4];
+                const uint32_t d1 = C::kWide ? k.w[2 * b + 1 < C::kLoadsW ? 2 * b + 1 : 0][h] : k.w[b][(2 * h + 1) % 4];
+                op[h] = i32x4{(int)low_codes(d0), (int)high_codes(d0), (int)low_codes(d1), (int)high_codes(d1)};
+            }
             float scale[kPer];
 #pragma unroll
             for (int j = 0; j < kPer; ++j) {
                 const int g = b * kPer + j;
-                const uint32_t d = k.s[g / 8][g % 8 / 2];
-                scale[j] = __uint_as_float((g & 1) ? d & 0xFFFF0000u : d << 16);
+                scale[j] = __uint_as_float((g & 1) ? k.s[g / 2] & 0xFFFF0000u : k.s[g / 2] << 16);
             }
 #pragma unroll
-            for (int n = 0; n < NB; ++n) {
-                const uint8_t* x = lds + at_x[n] + s * kBlockCols;
-                const i32x4 x0 = *reinterpret_cast<const i32x4*>(x);
-                const i32x4 x1 = *reinterpret_cast<const i32x4*>(x + 64);
-                const i32x4 zero = {0, 0, 0, 0};
-                i32x4 sum[kPer];
-                if constexpr (G == 128) {
-                    sum[0] = __builtin_amdgcn_mfma_i32_16x16x64_i8(x0, op[0], zero, 0, 0, 0);
-                    sum[0] = __builtin_amdgcn_mfma_i32_16x16x64_i8(x1, op[1], sum[0], 0, 0, 0);
-                } else if constexpr (G == 64) {
-                    sum[0] = __builtin_amdgcn_mfma_i32_16x16x64_i8(x0, op[0], zero, 0, 0, 0);
-                    sum[1] = __builtin_amdgcn_mfma_i32_16x16x64_i8(x1, op[1], zero, 0, 0, 0);
-                } else {
-                    typedef int i32x2 __attribute__((ext_vector_type(2)));
-                    auto half = [](const i32x4& r, int h) {
-                        return __builtin_bit_cast(long, h ? i32x2{r[2], r[3]} : i32x2{r[0], r[1]});
-                    };
+            for (int m = 0; m < C::MT; ++m) {
+                const uint8_t* x = lds + at_x[m] + (s - u0 * kUnit) * kBlockCols;
+                acc_t zero;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        sum[j] = __builtin_amdgcn_mfma_i32_16x16x32_i8(half(j < 2 ? x0 : x1, j & 1),
-                                                                       half(op[j >> 1], j & 1), zero, 0, 0, 0);
+                for (int e = 0; e < C::kAcc; ++e) zero[e] = 0;
+                acc_t sum[kPer];
+                if constexpr (C::kWide) {
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        const i32x4 xw = *reinterpret_cast<const i32x4*>(x + 32 * w);
+                        const int j = w * kPer / 4;
+                        sum[j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(xw, op[w], w % (4 / kPer) == 0 ? zero : sum[j], 0, 0, 0);
+                    }
+                } else {
+                    const i32x4 x0 = *reinterpret_cast<const i32x4*>(x);
+                    const i32x4 x1 = *reinterpret_cast<const i32x4*>(x + 64);
+                    if constexpr (G == 128) {
+                        sum[0] = __builtin_amdgcn_mfma_i32_16x16x64_i8(x0, op[0], zero, 0, 0, 0);
+                        sum[0] = __builtin_amdgcn_mfma_i32_16x16x64_i8(x1, op[1], sum[0], 0, 0, 0);
+                    } else if constexpr (G == 64) {
+                        sum[0] = __builtin_amdgcn_mfma_i32_16x16x64_i8(x0, op[0], zero, 0, 0, 0);
+                        sum[1] = __builtin_amdgcn_mfma_i32_16x16x64_i8(x1, op[1], zero, 0, 0, 0);
+                    } else {
+                        typedef int i32x2 __attribute__((ext_vector_type(2)));
+                        auto half = [](const i32x4& r, int h) {
+                            return __builtin_bit_cast(long, h ? i32x2{r[2], r[3]} : i32x2{r[0], r[1]});
+                        };
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            sum[j] = __builtin_amdgcn_mfma_i32_16x16x32_i8(half(j < 2 ? x0 : x1, j & 1),
+                                                                           half(op[j >> 1], j & 1), zero, 0, 0, 0);
+                    }
                 }
 #pragma unroll
                 for (int j = 0; j < kPer; ++j) {
                     // no group: what stands in its place is not a scale
                     if (kPer > 1 && s * kPer + j >= p.groups) continue;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) f[n][e] += (float)sum[j][e] * scale[j];
+                    for (int e = 0; e < C::kAcc; ++e) f[m][e] = fmaf((float)sum[j][e], scale[j], f[m][e]);
                 }
+                if (C::kWide) __builtin_amdgcn_sched_barrier(0);    // more tiles at once take more registers
             }
         }
     };
     auto store = [&](int i, float bias) {
-        const int64_t v = channel(i) + row;
+        int l = lane;
+        asm volatile("" : "+v"(l));   // what follows from it is not kept in registers over the loop
+        const int64_t v = channel(i) + l % C::kRows;
         if (i >= mine || v >= a.V) return;
+        const int tl = l / C::kRows * 4;
+        YT* const y0 = static_cast<YT*>(a.Y) + t0 * a.ldy + v;
 #pragma unroll
-        for (int n = 0; n < NB; ++n) {
+        for (int m = 0; m < C::MT; ++m) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int t = 16 * n + 4 * quarter + e;
+            for (int e = 0; e < C::kAcc; ++e) {
+                const int t = C::kWide ? 32 * m + 8 * (e / 4) + tl + e % 4 : tl + e;
                 if (t >= T) continue;
-                const float y = f[n][e] * xs[n][e] + bias;
-                if constexpr (sizeof(YT) == 4) static_cast<float*>(a.Y)[t * a.ldy + v] = y;
-                else static_cast<uint16_t*>(a.Y)[t * a.ldy + v] = (uint16_t)pack_bf16(y, 0.0f);
+                const float y = fmaf(f[m][e], xs[t], bias);
+                if constexpr (sizeof(YT) == 4) y0[t * a.ldy] = y;
+                else y0[t * a.ldy] = (uint16_t)pack_bf16(y, 0.0f);
             }
         }
     };
 
-    Chunk k0, k1;
-    int i = 0, c = 0;
-    auto next = [&](int& i, int& c) {
-        if (++c == chunks) c = 0, ++i;
+    Unit k[C::kDepth];
+    int i = 0, u = mate;         // the next unit to multiply
+    int il = 0, ul = mate;       // and to load
+    const int slots = p.several ? p.units : (p.units + p.window - 1) / p.window * p.window;
+    auto next = [&](int& i, int& u) {
+        if ((u += p.share) >= slots) u = mate, ++i;
     };
-    load(0, 0, k0);
-    auto go = [&](const Chunk& now, Chunk& then) {
-        int in = i, cn = c;
-        next(in, cn);
-        load(in, cn, then);
-        __builtin_amdgcn_sched_barrier(0);
-        if (c == 0) {
 #pragma unroll
-            for (int n = 0; n < NB; ++n) f[n] = f32x4{0, 0, 0, 0};
+    for (int d = 0; d < C::kDepth - 1; ++d) {
+        load(il, ul, k[d]);
+        next(il, ul);
+    }
+    if ((int)threadIdx.x < T) xs[threadIdx.x] = a.xscale[t0 + threadIdx.x] * 0.0625f;    // operands are 16 times the codes
+    clear();
+    float bias = 0.0f;
+    for (int u0 = 0; u0 < p.units; u0 += p.window) {
+        // the tokens' codes of the window, 16 columns a thread: columns 4 q .. of the 16 go to
+        // the 16 bytes that their lane reads
+        if (u0 > 0) __syncthreads();
+        const int cols = min(p.window, p.units - u0) * kUnit * 8;     // of 16 columns
+        for (int n = threadIdx.x; n < T * cols; n += C::kThreads) {
+            const int t = n / cols, c = n - t * cols, k0 = (u0 * kUnit * 8 + c) * 16;
+            i32x4 x = {0, 0, 0, 0};
+            if (k0 < D) {   // the padding up to 16 columns is readable
+                x = *reinterpret_cast<const i32x4*>(a.Xq + (t0 + t) * a.ldx + k0);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int left = D - k0 - 4 * j;
+                    x[j] &= left >= 4 ? -1 : left <= 0 ? 0 : (int)((1u << (8 * left)) - 1);
+                }
+            }
+            const int w = c % 8 / 2, h = c % 2;
+            uint8_t* at = lds + t * p.pitch + c / 8 * kBlockCols;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int to = C::kWide ? w * 32 + (j >> 1) * 16 + ((j & 1) * 2 + h) * 4
+                                        : (w >> 1) * 64 + j * 16 + ((w & 1) * 2 + h) * 4;
+                *reinterpret_cast<int*>(at + to) = x[j];
+            }
         }
-        multiply(c, now);
-        if (c == chunks - 1) store(i, now.bias);
-        __builtin_amdgcn_sched_barrier(0);
-        i = in, c = cn;
-    };
-    const int total = mine * chunks;
-    for (int j = 0; j < total; j += 2) {
-        go(k0, k1);
-        go(k1, k0);      // past the last one: nothing is read or stored
+        __syncthreads();
+        // as many steps for each wave, a multiple of the depth: past its units (of its strips) they are empty
+        const int total = p.several ? mine * p.units : p.window / p.share;
+        for (int n = 0; n < total; n += C::kDepth) {
+#pragma unroll
+            for (int d = 0; d < C::kDepth; ++d) {
+                load(il, ul, k[(d + C::kDepth - 1) % C::kDepth]);
+                next(il, ul);
+                __builtin_amdgcn_sched_barrier(0);
+                multiply(u, u0, k[d]);
+                if (u < p.units && u + p.share >= p.units) {
+                    bias = k[d].bias;
+                    if (p.share == 1) {
+                        store(i, bias);
+                        clear();
+                    }
+                }
+                next(i, u);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+    }
+    if (p.share > 1) {
+        // the others' sums join the first's, in order
+        float* const sums = reinterpret_cast<float*>(lds);
+        __syncthreads();
+#pragma unroll
+        for (int m = 0; m < C::MT; ++m)
+#pragma unroll
+            for (int e = 0; e < C::kAcc; ++e) sums[((wave * C::MT + m) * C::kAcc + e) * kWave + lane] = f[m][e];
+        __syncthreads();
+        if (mate > 0) return;
+        const int64_t v = channel(0) + row;
+        bias = a.bias && v < a.V && mine ? a.bias[v] : 0.0f;
+        for (int q = 1; q < p.share; ++q) {
+#pragma unroll
+            for (int m = 0; m < C::MT; ++m)
+#pragma unroll
+                for (int e = 0; e < C::kAcc; ++e) f[m][e] += sums[(((wave + q) * C::MT + m) * C::kAcc + e) * kWave + lane];
+        }
+        store(0, bias);
     }
 }
 
@@ -407,6 +506,7 @@ struct Tile4 {
     static constexpr int kStageBytes = kX + kW + kS;
     static constexpr int kLds = kStages * kStageBytes;
     static_assert(BM % (8 * kWavesB) == 0 && BN % (16 * kWavesB) == 0 && kWavesB % 2 == 0, "equal loads a wave");
+    static_assert(BM <= kThreads, "a thread a token's row");
     static_assert(BN % 64 == 0 && kWavesB % (BN / 64) == 0, "loads of the scales");
     static_assert(kStages >= 2 && (kStages - 2) * kLoads < 64, "vmcnt range");
     static_assert((int64_t)std::max(BM, BN) * EMBER_Q8_MAX_LD < (int64_t)1 << 31, "32-bit load offsets");
@@ -416,9 +516,7 @@ struct Tile4 {
 // BM tokens x BN channels a block, a block of 128 columns a step.  A ring of LDS
 // stages holds the tokens' codes, the table's, and 16 bytes of scales a channel
 // (eight groups, among them the step's).
-// kMask: D is not a multiple of 16, so the last chunk of a token's row holds
-// columns that do not count.
-template <typename C, int G, typename YT, bool kMask>
+template <typename C, int G, typename YT>
 __global__ __launch_bounds__(C::kThreads) void ember_logits_q4(Tile4Params p) {
     __shared__ __attribute__((aligned(1024))) uint8_t lds[C::kLds];
     const Logits4Args& a = p.a;
@@ -476,6 +574,21 @@ __global__ __launch_bounds__(C::kThreads) void ember_logits_q4(Tile4Params p) {
         // the barrier everyone's have, and no one reads the stage of step i - 1 any more
         wait_step<(C::kStages - 2) * C::kLoads>();
         issue(i + C::kStages - 1, fill);
+        if (D % 16 != 0 && i == p.nk - 1) {
+            // the last chunk of a token's row holds columns that do not count
+            const int c = D % kBlockCols / 16, r = threadIdx.x;
+            if (r < C::BM) {
+                auto* const x = (__attribute__((address_space(3))) i32x4*)(uintptr_t)(st + r * kBlockCols + (c ^ swizzle<8>(r)) * 16);
+                i32x4 y = *x;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int b = D % 16 - 4 * e;
+                    y[e] &= b >= 4 ? -1 : b <= 0 ? 0 : (int)((1u << (8 * b)) - 1);
+                }
+                *x = y;
+            }
+            wait_step<63>();
+        }
         i32x4 wd[C::NT][4];
         float scale[C::NT][kPer];
 #pragma unroll
@@ -500,17 +613,7 @@ __global__ __launch_bounds__(C::kThreads) void ember_logits_q4(Tile4Params p) {
                 for (int g = 0; g < 4 / kPer; ++g) {
                     const int w = j * (4 / kPer) + g;
                     const int r = rx0 + 32 * m;
-                    i32x4 x = lds_at(st + r * kBlockCols + (((2 * w + half) ^ swizzle<8>(r)) * 16));
-                    if constexpr (kMask) {
-                        if (i == p.nk - 1) {
-                            const int left = D - i * kBlockCols - 32 * w - 16 * half;
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const int b = left - 4 * e;
-                                x[e] &= b >= 4 ? -1 : b <= 0 ? 0 : (int)((1u << (8 * b)) - 1);
-                            }
-                        }
-                    }
+                    const i32x4 x = lds_at(st + r * kBlockCols + (((2 * w + half) ^ swizzle<8>(r)) * 16));
 #pragma unroll
                     for (int n = 0; n < C::NT; ++n) {
                         i32x4 op;
@@ -553,27 +656,45 @@ __global__ __launch_bounds__(C::kThreads) void ember_logits_q4(Tile4Params p) {
     }
 }
 
-template <int NB, int G>
-hipError_t launch_few(const Logits4Args& a, int pitch, hipStream_t s) {
-    constexpr int CH = G == 32 ? 4 : 8;
+// Bytes of a token's units in LDS.  They end 16 bytes past a multiple of the banks: the
+// lanes of a part read different ones.
+int64_t few_pitch(int64_t units) { return (units * kUnit * kBlockCols + 255) / 256 * 256 + 16; }
+static_assert(16 * (4 * 3 * kUnit * kBlockCols + 16) <= kFewLds, "16 tokens: a window for four waves, three units deep");
+
+template <typename C, int G>
+hipError_t launch_few(const Logits4Args& a, hipStream_t s) {
     Few4Params p;
     p.a = a;
     p.nblk = (int)((a.D + kBlockCols - 1) / kBlockCols);
     p.groups = (int)((a.D + G - 1) / G);
-    p.pitch = pitch;
-    const int64_t strips = (a.V + kStrip - 1) / kStrip;
-    p.strips = strips >= 4 * kCus ? 4 : 1;
-    p.units = (strips + p.strips - 1) / p.strips;
-    const dim3 grid((unsigned)std::min<int64_t>(p.units, kCus));
-    if (a.y_dtype == EMBER_F32) ember_logits_q4_few<NB, G, CH, float><<<grid, kFewThreads, 0, s>>>(p);
-    else ember_logits_q4_few<NB, G, CH, uint16_t><<<grid, kFewThreads, 0, s>>>(p);
+    p.units = (p.nblk + kUnit - 1) / kUnit;
+    // Waves that share a strip of 32 channels (of 16: as many, so that the order of the sums
+    // is the same): up to four, where there would be fewer than 1024 at work.
+    const int64_t strips32 = (a.V + 31) / 32;
+    p.share = 1;
+    while (p.share < 4 && p.share * 2 <= p.units && strips32 * p.share < 1024) p.share *= 2;
+    p.strips = (a.V + C::kRows - 1) / C::kRows;
+    p.tiles = (int)((a.T + C::kTokens - 1) / C::kTokens);
+    const int64_t T = std::min<int64_t>(a.T, C::kTokens);
+    p.several = p.share == 1 && T * few_pitch(p.units) <= kFewLds;
+    const int step = p.share * C::kDepth;      // a window has whole rounds of the registers' units
+    p.window = p.several ? p.units : (p.units + step - 1) / step * step;
+    while (!p.several && p.window > 0 && T * few_pitch(p.window) > kFewLds) p.window -= step;
+    if (p.window < step && !p.several) return hipErrorInvalidValue;
+    p.pitch = (int)few_pitch(p.window);
+    const int64_t per_block = C::kWaves / p.share;
+    p.together = p.strips >= 4 * kCus ? 4 : 1;
+    const int64_t all = p.several ? (p.strips + p.together - 1) / p.together : (p.strips + per_block - 1) / per_block;
+    p.blocks = (int)(p.several ? std::min<int64_t>(all, std::max(1, kCus / p.tiles)) : all);
+    const dim3 grid((unsigned)((p.blocks + kXcds - 1) / kXcds * kXcds * p.tiles));
+    if (a.y_dtype == EMBER_F32) ember_logits_q4_few<C, G, float><<<grid, C::kThreads, 0, s>>>(p);
+    else ember_logits_q4_few<C, G, uint16_t><<<grid, C::kThreads, 0, s>>>(p);
     return hipGetLastError();
 }
 
 template <typename C, int G, typename YT>
 void launch_tile(const Tile4Params& p, unsigned grid, hipStream_t s) {
-    if (p.a.D % 16 != 0) ember_logits_q4<C, G, YT, true><<<grid, C::kThreads, 0, s>>>(p);
-    else ember_logits_q4<C, G, YT, false><<<grid, C::kThreads, 0, s>>>(p);
+    ember_logits_q4<C, G, YT><<<grid, C::kThreads, 0, s>>>(p);
 }
 
 template <typename C, int G>
@@ -599,22 +720,19 @@ hipError_t launch_tiles(const Logits4Args& a, hipStream_t s) {
     return hipSuccess;
 }
 
-using T64x128 = Tile4<64, 128, 1, 4, 3>;
-using T256x128 = Tile4<256, 128, 2, 2, 3>;
+using T128x128 = Tile4<128, 128, 4, 2, 3>;
+using T256x256 = Tile4<256, 256, 2, 4, 3>;
 
-// Tokens whose codes fit the LDS take the streaming form, up to 64 of them.
 template <int G>
 hipError_t launch_group(const Logits4Args& a, hipStream_t s) {
-    const int64_t nblk = (a.D + kBlockCols - 1) / kBlockCols;
-    // rows of 16 bytes past a multiple of the banks: the lanes of a quarter read different ones
-    const int64_t pitch = (nblk * kBlockCols + 255) / 256 * 256 + 16;
-    if (a.T * pitch <= kFewLds) {
-        if (a.T <= 16) return launch_few<1, G>(a, (int)pitch, s);
-        if (a.T <= 32) return launch_few<2, G>(a, (int)pitch, s);
-        if (a.T <= 64) return launch_few<4, G>(a, (int)pitch, s);
+    if (a.T <= 64) {
+        const int64_t pitch = few_pitch((a.D + 511) / 512);
+        if (a.T <= 16 || a.V < 16384 || 32 * pitch > kFewLds) return launch_few<Stream<false, 1>, G>(a, s);
+        if (a.T <= 32 || 64 * pitch > kFewLds) return launch_few<Stream<true, 1>, G>(a, s);
+        return launch_few<Stream<true, 2>, G>(a, s);
     }
-    if (a.T <= 128) return launch_tiles<T64x128, G>(a, s);
-    return launch_tiles<T256x128, G>(a, s);
+    if (a.T <= 512 || a.V <= 16384) return launch_tiles<T128x128, G>(a, s);
+    return launch_tiles<T256x256, G>(a, s);
 }
 
 } // namespace
