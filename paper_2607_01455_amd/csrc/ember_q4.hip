@@ -19,6 +19,8 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <cmath>
+#include <type_traits>
 
 #include "ember_device.h"
 #include "ember_interface_launch.h"
@@ -187,9 +189,9 @@ struct Stream {
     static constexpr int MT = MT_;
     static constexpr int kRows = kWide ? 32 : 16;           // channels of a strip, tokens of a tile
     static constexpr int kTokens = kRows * MT;
-    static constexpr int kWaves = kWide ? 8 : 16;
+    static constexpr int kWaves = kWide ? 8 : 16;           // at most
     static constexpr int kThreads = kWaves * kWave;
-    static constexpr int kDepth = kWide ? 2 : 3;            // units in registers
+    static constexpr int kDepth = 2;                        // units in registers
     static constexpr int kLoadsW = kWide ? 2 * kUnit : kUnit;    // 16-byte loads of a unit's codes
     static constexpr int kAcc = kWide ? 16 : 4;             // values of a tile a lane
     static constexpr int kLanes = kWide ? 2 : 4;            // lanes of a row
@@ -203,6 +205,7 @@ struct Few4Params {
     int pitch;           // bytes of a token in LDS
     int window;          // units that the LDS holds of each token
     int share;           // waves that share a strip: each takes every share-th unit
+    int waves;           // of a block
     int64_t strips;
     int together;        // neighbouring strips of a block (where a wave goes through several)
     bool several;        // a wave goes through several strips
@@ -225,6 +228,9 @@ __global__ __launch_bounds__(C::kThreads) void ember_logits_q4_few(Few4Params p)
     constexpr int kPer = kBlockCols / G;                    // groups a block
     constexpr int kScaleBytes = kUnit * kPer * 2;           // of a unit: 8, 16 or 32
     constexpr int kScaleWords = kScaleBytes / 4;
+    // A row's lanes load a part of its scales each, where all of them are more than 8 bytes (16 x 128256 x
+    // 4096, groups of 32: 57 us, 59 when each loads all 32 bytes).
+    constexpr int kScaleParts = kScaleWords == 2 ? 1 : C::kWide ? 2 : 4;
     typedef int acc_t __attribute__((ext_vector_type(C::kAcc)));
     typedef float facc_t __attribute__((ext_vector_type(C::kAcc)));
     __shared__ __attribute__((aligned(16))) uint8_t lds[kFewLds];
@@ -240,7 +246,7 @@ __global__ __launch_bounds__(C::kThreads) void ember_logits_q4_few(Few4Params p)
     if (block >= p.blocks) return;
 
     // this wave's strips and units
-    const int per_block = C::kWaves / p.share, mate = wave % p.share, place = wave / p.share;
+    const int per_block = p.waves / p.share, mate = wave % p.share, place = wave / p.share;
     int64_t first, pass;
     if (p.several) {
         // `together` neighbours, then those of the grid's other blocks
@@ -254,14 +260,14 @@ __global__ __launch_bounds__(C::kThreads) void ember_logits_q4_few(Few4Params p)
     auto channel = [&](int i) { return (first + i * pass) * C::kRows; };
     const int64_t row_bytes = (int64_t)nblk * kBlockBytes;
     const uint32_t off_w = (uint32_t)row * (uint32_t)a.ldw + part * (kBlockBytes / C::kLanes);
-    const uint32_t off_s = (uint32_t)row * (uint32_t)a.ldg * 2;
+    const uint32_t off_s = (uint32_t)row * (uint32_t)a.ldg * 2 + lane / (kWave / kScaleParts) * (kScaleBytes / kScaleParts);
     auto buffer = [&](const void* base, int64_t bytes) {
         return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0,
                                                  (int)(bytes < kBufferMax ? bytes : kBufferMax), kBufferWord3);
     };
     struct Unit {
         i32x4 w[C::kLoadsW];
-        uint32_t s[kScaleWords];
+        uint32_t s[kScaleWords / kScaleParts];
         float bias;
     };
     // unit u of strip i: zeros past the table (also for strips past it) and past the row
@@ -278,19 +284,19 @@ __global__ __launch_bounds__(C::kThreads) void ember_logits_q4_few(Few4Params p)
             const uint32_t off = s < nblk ? off_w + s * kBlockBytes + b % (C::kLoadsW / kUnit) * 16 : kBufferMax;
             k.w[b] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, off, 0, 0));
         }
-        // (16 bytes at a time where there are as many; groups past the row's are not used)
+        // (groups past the row's are not used)
         const uint32_t off = u * kUnit * kPer < p.groups ? off_s + u * kScaleBytes : kBufferMax;
-        if constexpr (kScaleBytes == 8) {
+        constexpr int kWords = kScaleWords / kScaleParts;      // 1, 2 or 4
+        if constexpr (kWords == 1) {
+            k.s[0] = __builtin_amdgcn_raw_buffer_load_b32(rs, off, 0, 0);
+        } else if constexpr (kWords == 2) {
             const u32x2_t d = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_raw_buffer_load_b64(rs, off, 0, 0));
             k.s[0] = d[0];
             k.s[1] = d[1];
         } else {
+            const u32x4_t d = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rs, off, 0, 0));
 #pragma unroll
-            for (int q = 0; q < kScaleWords; q += 4) {
-                const u32x4_t d = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rs, off + 4 * q, 0, 0));
-#pragma unroll
-                for (int e = 0; e < 4; ++e) k.s[q + e] = d[e];
-            }
+            for (int e = 0; e < 4; ++e) k.s[e] = d[e];
         }
         k.bias = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rb, row * 4, 0, 0));
     };
@@ -309,6 +315,28 @@ __global__ __launch_bounds__(C::kThreads) void ember_logits_q4_few(Few4Params p)
     };
     // u0: the unit that the LDS begins with
     auto multiply = [&](int u, int u0, const Unit& k) {
+        // all lanes of a row get all of its scales: halves of the wave, then quarters exchanged
+        uint32_t sw[kScaleWords];
+        constexpr int kWords = kScaleWords / kScaleParts;
+#pragma unroll
+        for (int r = 0; r < kWords; ++r) {
+            if constexpr (kScaleParts == 1) {
+                sw[r] = k.s[r];
+                continue;
+            }
+            const auto h = __builtin_amdgcn_permlane32_swap(k.s[r], k.s[r], false, false);
+            if constexpr (kScaleParts == 2) {
+                sw[r] = h[0];
+                sw[kWords + r] = h[1];
+            } else {
+                const auto q0 = __builtin_amdgcn_permlane16_swap(h[0], h[0], false, false);
+                const auto q2 = __builtin_amdgcn_permlane16_swap(h[1], h[1], false, false);
+                sw[r] = q0[0];
+                sw[kWords + r] = q0[1];
+                sw[2 * kWords + r] = q2[0];
+                sw[3 * kWords + r] = q2[1];
+            }
+        }
 #pragma unroll
         for (int b = 0; b < kUnit; ++b) {
             const int s = u * kUnit + b;
@@ -327,7 +355,7 @@ __global__ __launch_bounds__(C::kThreads) void ember_logits_q4_few(Few4Params p)
 #pragma unroll
             for (int j = 0; j < kPer; ++j) {
                 const int g = b * kPer + j;
-                scale[j] = __uint_as_float((g & 1) ? k.s[g / 2] & 0xFFFF0000u : k.s[g / 2] << 16);
+                scale[j] = __uint_as_float((g & 1) ? sw[g / 2] & 0xFFFF0000u : sw[g / 2] << 16);
             }
 #pragma unroll
             for (int m = 0; m < C::MT; ++m) {
@@ -414,24 +442,31 @@ __global__ __launch_bounds__(C::kThreads) void ember_logits_q4_few(Few4Params p)
         // the 16 bytes that their lane reads
         if (u0 > 0) __syncthreads();
         const int cols = min(p.window, p.units - u0) * kUnit * 8;     // of 16 columns
-        for (int n = threadIdx.x; n < T * cols; n += C::kThreads) {
-            const int t = n / cols, c = n - t * cols, k0 = (u0 * kUnit * 8 + c) * 16;
-            i32x4 x = {0, 0, 0, 0};
-            if (k0 < D) {   // the padding up to 16 columns is readable
-                x = *reinterpret_cast<const i32x4*>(a.Xq + (t0 + t) * a.ldx + k0);
+        const int all = T * cols, threads = p.waves * kWave;
+        for (int n0 = threadIdx.x; n0 < all; n0 += 4 * threads) {      // four loads in flight
+            i32x4 x[4];
+            uint32_t to[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                if (__builtin_amdgcn_readfirstlane(n0) + q * threads >= all) break;      // for the whole wave
+                const int n = min(n0 + q * threads, all - 1), t = n / cols, c = n - t * cols;
+                const int k0 = (u0 * kUnit * 8 + c) * 16;
+                // (the padding up to 16 columns is readable)
+                x[q] = *reinterpret_cast<const i32x4*>(a.Xq + (t0 + t) * a.ldx + (k0 < D ? k0 : 0));
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const int left = D - k0 - 4 * j;
-                    x[j] &= left >= 4 ? -1 : left <= 0 ? 0 : (int)((1u << (8 * left)) - 1);
+                    x[q][j] &= left >= 4 ? -1 : left <= 0 ? 0 : (int)((1u << (8 * left)) - 1);
                 }
+                const int w = c % 8 / 2, h = c % 2;
+                to[q] = t * p.pitch + c / 8 * kBlockCols + (C::kWide ? w * 32 : (w >> 1) * 64 + (w & 1) * 8) + h * 4;
             }
-            const int w = c % 8 / 2, h = c % 2;
-            uint8_t* at = lds + t * p.pitch + c / 8 * kBlockCols;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int to = C::kWide ? w * 32 + (j >> 1) * 16 + ((j & 1) * 2 + h) * 4
-                                        : (w >> 1) * 64 + j * 16 + ((w & 1) * 2 + h) * 4;
-                *reinterpret_cast<int*>(at + to) = x[j];
+            for (int q = 0; q < 4; ++q) {
+                if (n0 + q * threads >= all) continue;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    *reinterpret_cast<int*>(lds + to[q] + (C::kWide ? (j >> 1) * 16 + (j & 1) * 8 : j * 16)) = x[q][j];
             }
         }
         __syncthreads();
@@ -492,30 +527,36 @@ struct Tile4Params {
     int group_m;
 };
 
-template <int BM_, int BN_, int WM_, int WN_, int STAGES_>
+// BM tokens x 32 channels a wave, WN waves side by side.
+template <int BM_, int WN_, int STAGES_>
 struct Tile4 {
-    static constexpr int BM = BM_, BN = BN_;       // tokens, channels a block
-    static constexpr int WM = WM_, WN = WN_;       // wavefronts over them
+    static constexpr int BM = BM_, BN = 32 * WN_;  // tokens, channels a block
     static constexpr int kStages = STAGES_;
-    static constexpr int kWavesB = WM * WN;
-    static constexpr int kThreads = kWavesB * kWave;
-    static constexpr int MT = BM / WM / 32, NT = BN / WN / 32;   // MFMA tiles a wave
-    static constexpr int kX = BM * kBlockCols, kW = BN * kBlockBytes, kS = BN * 16;   // bytes of a stage
-    static constexpr int kLoadsX = BM / 8 / kWavesB, kLoadsW = BN / 16 / kWavesB;     // a wave and step
+    static constexpr int kWaves = WN_;
+    static constexpr int kThreads = kWaves * kWave;
+    static constexpr int MT = BM / 32;             // MFMA tiles a wave
+    static constexpr int kX = BM * kBlockCols, kW = BN * kBlockBytes;                 // bytes of a stage
+    static constexpr int kS = BN * 16, kScales = 3;                                   // of a period's scales, and of these
+    static constexpr int kLoadsX = BM / 8 / kWaves, kLoadsW = BN / 16 / kWaves;       // a wave and step
     static constexpr int kLoads = kLoadsX + kLoadsW + 1;
-    static constexpr int kStageBytes = kX + kW + kS;
-    static constexpr int kLds = kStages * kStageBytes;
-    static_assert(BM % (8 * kWavesB) == 0 && BN % (16 * kWavesB) == 0 && kWavesB % 2 == 0, "equal loads a wave");
-    static_assert(BM <= kThreads, "a thread a token's row");
-    static_assert(BN % 64 == 0 && kWavesB % (BN / 64) == 0, "loads of the scales");
-    static_assert(kStages >= 2 && (kStages - 2) * kLoads < 64, "vmcnt range");
+    static constexpr int kStageBytes = kX + kW;
+    static constexpr int kRing = kStages * kStageBytes, kNone = kRing + kScales * kS;    // kNone: what loads outside a buffer write
+    static constexpr int kXs = kNone + 1024, kLds = kXs + BM * 4;
+    static_assert(BM % (8 * kWaves) == 0 && kWaves % 2 == 0 && MT % 2 == 0, "equal loads a wave, even tiles");
+    static_assert(kStages >= 2 && kStages <= 4 && (kStages - 2) * kLoads < 64, "vmcnt range, scales of the steps ahead");
+    static_assert(BN % kWave == 0 && BN / kWave <= kWaves, "the scales' loads");
     static_assert((int64_t)std::max(BM, BN) * EMBER_Q8_MAX_LD < (int64_t)1 << 31, "32-bit load offsets");
     static_assert(kLds <= 160 * 1024, "LDS of one CU");
 };
 
 // BM tokens x BN channels a block, a block of 128 columns a step.  A ring of LDS
-// stages holds the tokens' codes, the table's, and 16 bytes of scales a channel
-// (eight groups, among them the step's).
+// stages holds the tokens' codes and the table's; beside it are 16 bytes of scales a
+// channel (eight groups: two to eight steps), loaded with the first of their steps.  Every group's sum has to be turned into
+// fp32, scaled and added: 32 vector instructions for each 32 x 32 tile, as long as
+// the MFMAs of 128 columns take.  So these are laid between the next sum's MFMAs,
+// each wave has all of the block's tokens (the codes' halves are taken apart once),
+// and the step barrier sits before the last tile of tokens, whose operands are in
+// registers by then.
 template <typename C, int G, typename YT>
 __global__ __launch_bounds__(C::kThreads) void ember_logits_q4(Tile4Params p) {
     __shared__ __attribute__((aligned(1024))) uint8_t lds[C::kLds];
@@ -523,7 +564,6 @@ __global__ __launch_bounds__(C::kThreads) void ember_logits_q4(Tile4Params p) {
     constexpr int kPer = kBlockCols / G;
     const int lane = threadIdx.x & (kWave - 1);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int wm = wave % C::WM, wn = wave / C::WM;
     const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
     const int64_t l = p.tile0 + (int64_t)(blockIdx.x % kXcds) * p.per_xcd + blockIdx.x / kXcds;
     if (l >= min(p.tile0 + (int64_t)(blockIdx.x % kXcds + 1) * p.per_xcd, p.tile1)) return;
@@ -535,131 +575,197 @@ __global__ __launch_bounds__(C::kThreads) void ember_logits_q4(Tile4Params p) {
 
     const int row_x = wave * 8 + lane / 8, row_w = wave * 16 + lane / 4;
     const int k_x = ((lane % 8) ^ swizzle<8>(row_x)) * 16, k_w = ((lane % 4) ^ swizzle<4>(row_w)) * 16;
-    const int row_s = wave % (C::BN / 64) * 64 + lane;
+    const int row_s = wave * kWave + lane;                 // of the first waves
     const uint32_t off_x = row_x * (uint32_t)a.ldx + k_x, off_w = row_w * (uint32_t)a.ldw + k_w;
     const uint32_t off_s = row_s * (uint32_t)(2 * a.ldg);
+    // all of a load's place in the offset that the buffer's range is checked against; past the
+    // last step they are outside it
+    const i32x4 rx = rsrc(a.Xq + t0 * a.ldx, (a.T - t0) * a.ldx);
+    const i32x4 rw = rsrc(a.Wq + v0 * a.ldw, (a.V - v0) * a.ldw);
+    const i32x4 rs = rsrc(a.wscale + v0 * a.ldg, (a.V - v0) * a.ldg * 2);
     auto issue = [&](int kt, uint32_t st) {
-        const bool in = kt < p.nk;
-        const int64_t kx = in ? (int64_t)kt * kBlockCols : 0, kw = in ? (int64_t)kt * kBlockBytes : 0;
-        const int64_t ks = in ? (int64_t)kt * kPer / 8 * 8 : 0;
-        const i32x4 rx = rsrc(a.Xq + t0 * a.ldx + kx, in ? (a.T - t0) * a.ldx - kx : 0);
-        const i32x4 rw = rsrc(a.Wq + v0 * a.ldw + kw, in ? (a.V - v0) * a.ldw - kw : 0);
-        const i32x4 rs = rsrc(a.wscale + v0 * a.ldg + ks, in ? ((a.V - v0) * a.ldg - ks) * 2 : 0);
-        const uint32_t ox = k_x < D - (int)kx ? off_x : kBufferMax;
+        const uint32_t ox = kt * kBlockCols + k_x < D ? off_x + kt * kBlockCols : kBufferMax;
+        const uint32_t ow = off_w + (kt < p.nk ? (uint32_t)kt * kBlockBytes : kBufferMax);
+        // Scales: 16 bytes of a row each, so 64 rows a load, and slow.  In the other steps (and waves)
+        // the load stays, outside the buffer, so that all steps have as many.
+        constexpr int kPeriod = 8 / kPer;
+        const bool scales = kt % kPeriod == 0 && kt < p.nk && wave < C::BN / kWave;
+        const uint32_t os = off_s + (scales ? (uint32_t)(kt / kPeriod * 16) : kBufferMax);
+        const uint32_t to_s = scales ? C::kRing + kt / kPeriod % C::kScales * C::kS + wave * 1024 : C::kNone;
+        load_to_lds(rs, lds_base + to_s, os);
 #pragma unroll
         for (int j = 0; j < C::kLoadsX; ++j)
-            load_to_lds(rx, st + (wave + C::kWavesB * j) * 1024, ox + j * (C::kWavesB * 8 * (uint32_t)a.ldx));
+            load_to_lds(rx, lds_base + st + (wave + C::kWaves * j) * 1024, ox + j * (C::kWaves * 8 * (uint32_t)a.ldx));
 #pragma unroll
         for (int j = 0; j < C::kLoadsW; ++j)
-            load_to_lds(rw, st + C::kX + (wave + C::kWavesB * j) * 1024, off_w + j * (C::kWavesB * 16 * (uint32_t)a.ldw));
-        load_to_lds(rs, st + C::kX + C::kW + wave % (C::BN / 64) * 1024, off_s);
+            load_to_lds(rw, lds_base + st + C::kX + (wave + C::kWaves * j) * 1024, ow + j * (C::kWaves * 16 * (uint32_t)a.ldw));
     };
-    const int half = lane >> 5, sh = half ? 0 : 4;
-    const int rx0 = wm * (C::MT * 32) + (lane & 31), rw0 = wn * (C::NT * 32) + (lane & 31);
-    auto lds_at = [](uint32_t at) { return *(const __attribute__((address_space(3))) i32x4*)(uintptr_t)at; };
+    const int half = lane >> 5, sh = half ? 0 : 4, col = lane & 31, ch = wave * 32 + col;
+    const auto* const ring = (const __attribute__((address_space(3))) uint8_t*)lds;      // stages: offsets in it
+    auto lds_at = [&](uint32_t at, int more) { return *(const __attribute__((address_space(3))) i32x4*)(ring + at + more); };
+    // operands: a tile's tokens, 32 columns each; a block's codes, dword w of quarter t; scales
+    uint32_t at_x[4];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) at_x[w] = col * kBlockCols + (((2 * w + half) ^ swizzle<8>(col)) * 16);
+    uint32_t at_w[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) at_w[t] = ch * kBlockBytes + ((t ^ swizzle<4>(ch)) * 16);
+    // (masked: the last step of a D that is not a multiple of 16, whose last chunk holds columns that do not count)
+    uint32_t here[4];       // of the stage
+#pragma unroll
+    for (int w = 0; w < 4; ++w) here[w] = at_x[w];
+    auto read_x = [&](int m, i32x4 (&x)[4], bool masked) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            x[w] = lds_at(here[w], m * (32 * kBlockCols));
+            if (!masked) continue;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int b = D - (p.nk - 1) * kBlockCols - 32 * w - 16 * half - 4 * e;
+                x[w][e] &= b >= 4 ? -1 : b <= 0 ? 0 : (int)((1u << (8 * b)) - 1);
+            }
+        }
+    };
+    auto read_w = [&](uint32_t st, i32x4 (&wd)[4]) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) wd[t] = lds_at(st + at_w[t], C::kX);
+    };
+    auto read_s = [&](int kt, float (&s)[kPer]) {
+        const uint32_t at = kt * kPer / 8 % C::kScales * C::kS + ch * 16 + kt * kPer % 8 * 2;
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            const uint32_t h = *(const __attribute__((address_space(3))) uint16_t*)(ring + at + (C::kRing + 2 * j));
+            // no group: what stands in its place is not a scale
+            s[j] = kPer == 1 || kt * kPer + j < p.groups ? bf16_bits_f32(h) : 0.0f;
+        }
+    };
+    auto take_apart = [&](const i32x4 (&wd)[4], i32x4 (&op)[4]) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) op[w][t] = (int)(((uint32_t)wd[t][w] << sh) & 0xF0F0F0F0u);
+    };
 
-    f32x16 f[C::MT][C::NT];
+    f32x16 f[C::MT];
+    i32x16 sum[2], zero;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) zero[e] = sum[0][e] = sum[1][e] = 0;
 #pragma unroll
     for (int m = 0; m < C::MT; ++m)
 #pragma unroll
-        for (int n = 0; n < C::NT; ++n)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) f[m][n][e] = 0.0f;
+        for (int e = 0; e < 16; ++e) f[m][e] = 0.0f;
 
+    // for the epilogue, ahead of everything; the operands are 16 times the codes
+    const int64_t my_t = t0 + threadIdx.x, my_v = v0 + ch;
+    const float my_xs = (int)threadIdx.x < C::BM && my_t < a.T ? a.xscale[my_t] * 0.0625f : 0.0f;
+    const float bias = a.bias && my_v < a.V ? a.bias[my_v] : 0.0f;
+    float* const xs = reinterpret_cast<float*>(lds + C::kXs);
+    if ((int)threadIdx.x < C::BM) xs[threadIdx.x] = my_xs;
 #pragma unroll
-    for (int q = 0; q < C::kStages - 1; ++q) issue(q, lds_base + q * C::kStageBytes);
-    uint32_t st = lds_base, fill = lds_base + (C::kStages - 1) * C::kStageBytes;
-    for (int i = 0; i < p.nk; ++i) {
-        // this wave's loads of step i have landed (those of later steps may be out), and past
-        // the barrier everyone's have, and no one reads the stage of step i - 1 any more
-        wait_step<(C::kStages - 2) * C::kLoads>();
-        issue(i + C::kStages - 1, fill);
-        if (D % 16 != 0 && i == p.nk - 1) {
-            // the last chunk of a token's row holds columns that do not count
-            const int c = D % kBlockCols / 16, r = threadIdx.x;
-            if (r < C::BM) {
-                auto* const x = (__attribute__((address_space(3))) i32x4*)(uintptr_t)(st + r * kBlockCols + (c ^ swizzle<8>(r)) * 16);
-                i32x4 y = *x;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int b = D % 16 - 4 * e;
-                    y[e] &= b >= 4 ? -1 : b <= 0 ? 0 : (int)((1u << (8 * b)) - 1);
-                }
-                *x = y;
-            }
-            wait_step<63>();
-        }
-        i32x4 wd[C::NT][4];
-        float scale[C::NT][kPer];
-#pragma unroll
-        for (int n = 0; n < C::NT; ++n) {
-            const int r = rw0 + 32 * n;
-#pragma unroll
-            for (int t = 0; t < 4; ++t) wd[n][t] = lds_at(st + C::kX + r * kBlockBytes + ((t ^ swizzle<4>(r)) * 16));
-#pragma unroll
-            for (int j = 0; j < kPer; ++j) {
-                const uint32_t at = st + C::kX + C::kW + r * 16 + (i * kPer + j) % 8 * 2;
-                const uint32_t h = *(const __attribute__((address_space(3))) uint16_t*)(uintptr_t)at;
-                // no group: what stands in its place is not a scale
-                scale[n][j] = kPer == 1 || i * kPer + j < p.groups ? bf16_bits_f32(h) : 0.0f;
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < kPer; ++j) {
-#pragma unroll
-            for (int m = 0; m < C::MT; ++m) {
-                i32x16 sum[C::NT];
-#pragma unroll
-                for (int g = 0; g < 4 / kPer; ++g) {
-                    const int w = j * (4 / kPer) + g;
-                    const int r = rx0 + 32 * m;
-                    const i32x4 x = lds_at(st + r * kBlockCols + (((2 * w + half) ^ swizzle<8>(r)) * 16));
-#pragma unroll
-                    for (int n = 0; n < C::NT; ++n) {
-                        i32x4 op;
-#pragma unroll
-                        for (int t = 0; t < 4; ++t) op[t] = (int)(((uint32_t)wd[n][t][w] << sh) & 0xF0F0F0F0u);
-                        i32x16 zero;
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) zero[e] = 0;
-                        sum[n] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x, op, g == 0 ? zero : sum[n], 0, 0, 0);
-                    }
-                }
-#pragma unroll
-                for (int n = 0; n < C::NT; ++n)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) f[m][n][e] += (float)sum[n][e] * scale[n][j];
-            }
-        }
-        st = st + C::kStageBytes == lds_base + C::kLds ? lds_base : st + C::kStageBytes;
-        fill = fill + C::kStageBytes == lds_base + C::kLds ? lds_base : fill + C::kStageBytes;
-    }
-    wait_step<0>();    // the zero-filling loads past the end have landed
-
-    // a lane holds 16 tokens of a channel
-#pragma unroll
-    for (int n = 0; n < C::NT; ++n) {
-        const int64_t v = v0 + rw0 + 32 * n;
-        if (v >= a.V) continue;
-        const float bias = a.bias ? a.bias[v] : 0.0f;
+    for (int q = 0; q < C::kStages; ++q) issue(q, q * C::kStageBytes);
+    wait_step<(C::kStages - 1) * C::kLoads>();
+    i32x4 op[4], wd[4], x[2][4];
+    float scale[kPer], last = 0.0f;       // this step's, and that of the sum that is not added yet
+    read_w(0, wd);
+    read_s(0, scale);
+    read_x(0, x[0], p.nk == 1);
+    take_apart(wd, op);
+    uint32_t st = 0;
+    auto step = [&](int i, auto is_last) {
+        constexpr bool kLast = decltype(is_last)::value;
+        const uint32_t next = st + C::kStageBytes == C::kRing ? 0 : st + C::kStageBytes;
+        float then[kPer];
 #pragma unroll
         for (int m = 0; m < C::MT; ++m) {
+            if (m + 1 < C::MT) {
+                read_x(m + 1, x[(m + 1) & 1], kLast);
+            } else if (!kLast) {
+                // Everyone's operands of this stage are in registers, so step i + kStages may fill
+                // it; of each wave's loads those of step i + 2 and later may be out.
+                wait_step<(C::kStages - 2) * C::kLoads>();
+                issue(i + C::kStages, st);
+                read_w(next, wd);
+                read_s(i + 1, then);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int64_t t = t0 + (wm * C::MT + m) * 32 + 8 * (e / 4) + 4 * half + e % 4;
-                if (t >= a.T) continue;
-                const float y = f[m][n][e] * (a.xscale[t] * 0.0625f) + bias;
-                if constexpr (sizeof(YT) == 4) static_cast<float*>(a.Y)[t * a.ldy + v] = y;
-                else static_cast<uint16_t*>(a.Y)[t * a.ldy + v] = (uint16_t)pack_bf16(y, 0.0f);
+                for (int w = 0; w < 4; ++w) here[w] = next + at_x[w];
+                read_x(0, x[0], false);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                constexpr int kRun = 4 / kPer;                 // MFMAs of a group
+                const int n = (m * 4 + w) / kRun, cur = n & 1;
+                sum[cur] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x[m & 1][w], op[w], w % kRun == 0 ? zero : sum[cur], 0, 0, 0);
+                // a part of the sum before
+                const int before = (n + C::MT * kPer - 1) % (C::MT * kPer);
+                const float s = n == 0 ? last : scale[before % kPer];
+#pragma unroll
+                for (int e = 0; e < 16 / kRun; ++e) {
+                    const int q = w % kRun * (16 / kRun) + e;
+                    f[before / kPer][q] = fmaf((float)sum[cur ^ 1][q], s, f[before / kPer][q]);
+                }
+                asm volatile("" : "+v"(f[before / kPer]));     // here, not past the step
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
+        last = scale[kPer - 1];
+        if (kLast) return;
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) scale[j] = then[j];
+        take_apart(wd, op);
+        st = next;
+    };
+    for (int i = 0; i < p.nk - 1; ++i) step(i, std::false_type());
+    if (p.nk > 1) read_x(0, x[0], true);
+    step(p.nk - 1, std::true_type());
+#pragma unroll
+    for (int e = 0; e < 16; ++e) f[C::MT - 1][e] = fmaf((float)sum[1][e], last, f[C::MT - 1][e]);
+    wait_step<0>();    // the zero-filling loads past the end have landed, and everyone is done with the stages
+
+    // A lane holds 16 tokens of a channel: through a strip of LDS of the wave's own, 32
+    // tokens x 32 channels, each token's are stored side by side.
+    constexpr int kEs = (int)sizeof(YT), kPitch = 32 * kEs + 16, kEpc = 16 / kEs, kPerRow = 32 / kEpc;
+    static_assert(C::kWaves * 32 * kPitch <= C::kLds, "the strips");
+    uint8_t* const strip = lds + wave * (32 * kPitch);
+    int el = lane;
+    asm volatile("" : "+v"(el));   // what follows from it is not kept in registers over the loop above
+    const int eh = el >> 5, ec = el & 31;
+#pragma unroll
+    for (int m = 0; m < C::MT; ++m) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int r = 8 * (e / 4) + 4 * eh + e % 4;
+            const float y = fmaf(f[m][e], xs[32 * m + r], bias);
+            if constexpr (kEs == 4) *reinterpret_cast<float*>(strip + r * kPitch + ec * 4) = y;
+            else *reinterpret_cast<uint16_t*>(strip + r * kPitch + ec * 2) = (uint16_t)pack_bf16(y, 0.0f);
+        }
+        wave_lds_order();
+#pragma unroll
+        for (int q = 0; q < 32 * kPerRow / kWave; ++q) {
+            const int r = (q * kWave + el) / kPerRow, c = el % kPerRow * kEpc;
+            const int64_t t = t0 + 32 * m + r, v = v0 + wave * 32 + c;
+            const u32x4_t y = *reinterpret_cast<const u32x4_t*>(strip + r * kPitch + c * kEs);
+            if (t >= a.T) continue;
+            YT* const to = static_cast<YT*>(a.Y) + t * a.ldy + v;
+            if (v + kEpc <= a.V) {
+                *reinterpret_cast<u32x4_t*>(to) = y;
+            } else {
+#pragma unroll
+                for (int e = 0; e < kEpc; ++e) {
+                    if (v + e >= a.V) continue;
+                    if constexpr (kEs == 4) reinterpret_cast<uint32_t*>(to)[e] = y[e];
+                    else reinterpret_cast<uint16_t*>(to)[e] = (uint16_t)(y[e >> 1] >> (16 * (e & 1)));
+                }
+            }
+        }
+        wave_lds_order();
     }
 }
 
 // Bytes of a token's units in LDS.  They end 16 bytes past a multiple of the banks: the
 // lanes of a part read different ones.
 int64_t few_pitch(int64_t units) { return (units * kUnit * kBlockCols + 255) / 256 * 256 + 16; }
-static_assert(16 * (4 * 3 * kUnit * kBlockCols + 16) <= kFewLds, "16 tokens: a window for four waves, three units deep");
+static_assert(16 * (4 * 2 * kUnit * kBlockCols + 16) <= kFewLds, "16 tokens: a window for four waves, two units deep");
 
 template <typename C, int G>
 hipError_t launch_few(const Logits4Args& a, hipStream_t s) {
@@ -682,13 +788,16 @@ hipError_t launch_few(const Logits4Args& a, hipStream_t s) {
     while (!p.several && p.window > 0 && T * few_pitch(p.window) > kFewLds) p.window -= step;
     if (p.window < step && !p.several) return hipErrorInvalidValue;
     p.pitch = (int)few_pitch(p.window);
-    const int64_t per_block = C::kWaves / p.share;
+    // few waves to a block where there would be less than a block for each compute unit
+    p.waves = C::kWaves;
+    while (p.waves > 8 && p.strips * p.share * p.tiles < (int64_t)p.waves * kCus * 3 / 4) p.waves /= 2;
+    const int64_t per_block = p.waves / p.share;
     p.together = p.strips >= 4 * kCus ? 4 : 1;
     const int64_t all = p.several ? (p.strips + p.together - 1) / p.together : (p.strips + per_block - 1) / per_block;
     p.blocks = (int)(p.several ? std::min<int64_t>(all, std::max(1, kCus / p.tiles)) : all);
     const dim3 grid((unsigned)((p.blocks + kXcds - 1) / kXcds * kXcds * p.tiles));
-    if (a.y_dtype == EMBER_F32) ember_logits_q4_few<C, G, float><<<grid, C::kThreads, 0, s>>>(p);
-    else ember_logits_q4_few<C, G, uint16_t><<<grid, C::kThreads, 0, s>>>(p);
+    if (a.y_dtype == EMBER_F32) ember_logits_q4_few<C, G, float><<<grid, p.waves * kWave, 0, s>>>(p);
+    else ember_logits_q4_few<C, G, uint16_t><<<grid, p.waves * kWave, 0, s>>>(p);
     return hipGetLastError();
 }
 
@@ -720,19 +829,36 @@ hipError_t launch_tiles(const Logits4Args& a, hipStream_t s) {
     return hipSuccess;
 }
 
-using T128x128 = Tile4<128, 128, 4, 2, 3>;
-using T256x256 = Tile4<256, 256, 2, 4, 3>;
+using T128x256 = Tile4<128, 8, 4>;
+using T64x128 = Tile4<64, 4, 3>;       // two a compute unit
 
+// What a launch of a tiling takes, in us: rounds of the chip's compute units, each of D
+// / 128 steps (fitted to 1024 x 128256 x 4096, 512 x 32000 x 4096, 256 x 128256 x 4096 and
+// 1024 x 32000 x 2048; times by group size).
+template <typename C, int G>
+double tiles_us(const Logits4Args& a) {
+    constexpr bool kLarge = C::BN == 256;
+    constexpr double kStep = kLarge ? (G == 128 ? 1.55 : G == 64 ? 2.1 : 2.8) : (G == 128 ? 0.65 : G == 64 ? 0.8 : 1.3);
+    const double tiles = (double)((a.T + C::BM - 1) / C::BM) * (double)((a.V + C::BN - 1) / C::BN) / kCus;
+    // the small tiling: the second block of a compute unit costs 0.6 of the first
+    const double rounds = kLarge ? std::ceil(tiles) : 0.8 * std::ceil(tiles) + 0.2 * (tiles <= 1 ? 1 : 0);
+    return rounds * (double)((a.D + kBlockCols - 1) / kBlockCols) * kStep;
+}
+
+// Up to 64 tokens the streaming form, in the largest tile of tokens whose codes fit the LDS
+// (us: 64 tokens x 100000 x 1000 in tiles of 64 27, of 16 34, the smaller tiling 34); small tables,
+// where several tiles' blocks fill the chip and the codes come from the caches, in tiles of 16
+// (64 x 1500 x 4096: 11; 16 in tiles of 32, 31 with the tiling).  A large table whose 33 to 64 tokens do not fit goes through the tiling
+// (64 x 128256 x 4096: 78; 85 in tiles of 32).
 template <int G>
 hipError_t launch_group(const Logits4Args& a, hipStream_t s) {
-    if (a.T <= 64) {
-        const int64_t pitch = few_pitch((a.D + 511) / 512);
-        if (a.T <= 16 || a.V < 16384 || 32 * pitch > kFewLds) return launch_few<Stream<false, 1>, G>(a, s);
-        if (a.T <= 32 || 64 * pitch > kFewLds) return launch_few<Stream<true, 1>, G>(a, s);
-        return launch_few<Stream<true, 2>, G>(a, s);
-    }
-    if (a.T <= 512 || a.V <= 16384) return launch_tiles<T128x128, G>(a, s);
-    return launch_tiles<T256x256, G>(a, s);
+    const int64_t pitch = few_pitch((a.D + kUnit * kBlockCols - 1) / (kUnit * kBlockCols));
+    const bool small = a.V < 16384;
+    if (a.T <= 16 || (a.T <= 64 && small)) return launch_few<Stream<false, 1>, G>(a, s);
+    if (a.T <= 32) return 32 * pitch <= kFewLds ? launch_few<Stream<true, 1>, G>(a, s) : launch_few<Stream<false, 1>, G>(a, s);
+    if (a.T <= 64 && 64 * pitch <= kFewLds) return launch_few<Stream<true, 2>, G>(a, s);
+    if (a.T > 64 && tiles_us<T128x256, G>(a) <= tiles_us<T64x128, G>(a)) return launch_tiles<T128x256, G>(a, s);
+    return launch_tiles<T64x128, G>(a, s);
 }
 
 } // namespace
