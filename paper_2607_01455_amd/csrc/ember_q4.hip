@@ -48,29 +48,25 @@ uint32_t magic_of(uint32_t d) { return d == 1 ? 0 : (uint32_t)((((uint64_t)1 << 
 // ---------------------------------------------------------------------------
 
 constexpr int kRowThreads = 256;
+constexpr int64_t kPastBytes = (int64_t)128 << 20;        // of rows: from here on they are stored past the caches
 constexpr int kUnitLanes = 16;                            // lanes a block of codes, one dword each
 constexpr int kUnitsPerPass = kRowThreads / kUnitLanes;   // blocks of codes side by side
+constexpr int kAhead = 4;                                 // of a thread, whose loads go out together
+constexpr float kSmall = 1e-28f;                          // below it a quotient's remainder may not be exact
 
-// Columns [col, col + 4) of a row, zeros past D.
-template <typename T>
-__device__ __forceinline__ f32x4 load4(const T* row, int col, int D) {
-    f32x4 v = {0, 0, 0, 0};
-    if (col + 4 <= D) {
-        if constexpr (sizeof(T) == 4) {
-            v = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(row + col));
-        } else {
-            const u32x2_t w = __builtin_nontemporal_load(reinterpret_cast<const u32x2_t*>(row + col));
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                v[e] = __uint_as_float((e & 1) ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16);
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (col + e < D) v[e] = load_elem(row, col + e, sizeof(T) == 2);
-    }
-    return v;
+// A lane (w, q) of a block has dword 16 q + 4 w of its codes.  In memory order the pair of lanes with q
+// = 2 i and 2 i + 1 has 16 columns: the even lane takes the 8 from 32 w + 8 i on (the lower halves of both
+// dwords), the odd one the 8 from 32 w + 16 + 8 i on (the upper halves), 16 bytes of bf16 each.
+__device__ __forceinline__ int first_col(int s, int lane) {
+    return s * kBlockCols + 32 * (lane >> 2) + 4 * (lane & 2) + 16 * (lane & 1);
 }
+
+// The value of another lane of the row of 16.
+template <int kCtrl>
+__device__ __forceinline__ uint32_t of_lane(uint32_t x) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kCtrl, 0xF, 0xF, true);
+}
+constexpr int kPair = 0xB1, kQuad = 0x4E, kHalfRow = 0x141, kRow = 0x140;    // lane ^ 1, ^ 2; mirrored in 8, in 16
 
 struct QuantParams {
     Quant4Args a;
@@ -80,43 +76,75 @@ struct QuantParams {
     int rows_per_block;
 };
 
-// A lane rounds the eight columns of one dword; a group is 4, 8 or 16 lanes.
+// A group is 4, 8 or 16 lanes.  The quotient x / s is rounded correctly, and so is the code at a
+// tie: with r = 1 / s correctly rounded, q = x r and the remainder e = x - q s (exact), q + e r is
+// (Markstein).  128256 x 4096 bf16 (1.3 GB read and written): 235 us; with divisions 390.
 template <typename T, int G>
 __global__ __launch_bounds__(kRowThreads) void ember_quantize_q4(QuantParams p) {
     const Quant4Args& a = p.a;
+    constexpr int kChunks = 8 / kChunkElems<T>;
     const int lane = threadIdx.x % kUnitLanes, w = lane / 4, q = lane % 4;
     const int64_t row0 = (int64_t)blockIdx.x * p.rows_per_block;
     const int rows = (int)min((int64_t)p.rows_per_block, a.rows - row0);
     const int units = rows * p.nblk, D = (int)a.D;
-    for (int u = threadIdx.x / kUnitLanes; u < units; u += kUnitsPerPass) {
-        const int r = (int)div_small(u, p.magic), s = u - r * p.nblk;
-        const T* x = static_cast<const T*>(a.X) + (row0 + r) * a.ldx;
-        const int col = s * kBlockCols + 32 * w + 4 * q;
-        const f32x4 lo = load4(x, col, D), hi = load4(x, col + 16, D);
-        float top = 0.0f;
-        bool fine = true;
+    for (int u0 = threadIdx.x / kUnitLanes; u0 < units; u0 += kAhead * kUnitsPerPass) {
+        u32x4_t x[kAhead][kChunks];
+        int r[kAhead], s[kAhead];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            top = fmaxf(top, fmaxf(fabsf(lo[e]), fabsf(hi[e])));
-            fine = fine && isfinite(lo[e]) && isfinite(hi[e]);
+        for (int i = 0; i < kAhead; ++i) {
+            const int u = min(u0 + i * kUnitsPerPass, units - 1);
+            r[i] = (int)div_small(u, p.magic);
+            s[i] = u - r[i] * p.nblk;
+            const T* row = static_cast<const T*>(a.X) + (row0 + r[i]) * a.ldx;
+            const bool follows = row0 + r[i] + 1 < a.rows;
+            const int col = first_col(s[i], lane);
+#pragma unroll
+            for (int c = 0; c < kChunks; ++c) x[i][c] = load_chunk(row, col + c * kChunkElems<T>, D, follows);
         }
-        top = fine ? top : __builtin_inff();      // a maximum passes over a NaN
 #pragma unroll
-        for (int m = 1; m < G / 8; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
-        const uint32_t bits = pack_bf16(top / 7.0f, 0.0f) & 0xFFFFu;
-        const float scale = bf16_bits_f32(bits);
-        const bool some = top >= kTiny && top < __builtin_inff();
-        uint32_t codes = 0;
+        for (int i = 0; i < kAhead; ++i) {
+            if (u0 + i * kUnitsPerPass >= units) break;
+            const int col = first_col(s[i], lane);
+            float v[8];
+            uint32_t top = 0;              // of the magnitudes' bits: those of a NaN are above infinity's
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int cl = some ? (int)rintf(lo[e] / scale) : 0, ch = some ? (int)rintf(hi[e] / scale) : 0;
-            codes |= (uint32_t)((cl & 15) | (ch & 15) << 4) << (8 * e);
+            for (int c = 0; c < kChunks; ++c) {
+                if (col + (c + 1) * kChunkElems<T> > D) x[i][c] &= kept_words<T>(col + c * kChunkElems<T>, D);
+#pragma unroll
+                for (int e = 0; e < kChunkElems<T>; ++e) {
+                    v[c * kChunkElems<T> + e] = elem<T>(x[i][c], e);
+                    top = max(top, __float_as_uint(v[c * kChunkElems<T> + e]) & 0x7FFFFFFFu);
+                }
+            }
+            top = max(top, of_lane<kPair>(top));
+            top = max(top, of_lane<kQuad>(top));
+            if constexpr (G >= 64) top = max(top, of_lane<kHalfRow>(top));
+            if constexpr (G == 128) top = max(top, of_lane<kRow>(top));
+            const float most = __uint_as_float(top);
+            const uint32_t bits = pack_bf16(most / 7.0f, 0.0f) & 0xFFFFu;
+            const float scale = bf16_bits_f32(bits), inv = 1.0f / scale;
+            const bool fine = top < 0x7F800000u, some = fine && most >= kTiny;
+            uint32_t half[2] = {0, 0};     // codes of the first four columns, of the others, in the lower halves of bytes
+            // (whole numbers by adding 1.5 * 2^23, whose low bits then are the code's)
+            if (__ballot(most < kSmall && most > 0.0f)) {
+#pragma unroll 1
+                for (int e = 0; e < 8; ++e) half[e / 4] |= (__float_as_uint(v[e] / scale + 12582912.0f) & 15u) << (8 * (e % 4));
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float y = v[e] * inv, more = fmaf(fmaf(-y, scale, v[e]), inv, y);
+                    half[e / 4] |= (__float_as_uint(more + 12582912.0f) & 15u) << (8 * (e % 4));
+                }
+            }
+            // the even lane gives its second half for the odd one's first
+            const uint32_t other = of_lane<kPair>(q & 1 ? half[0] : half[1]);
+            const uint32_t codes = q & 1 ? other | half[1] << 4 : half[0] | other << 4;
+            uint8_t* out = a.Q + (row0 + r[i]) * a.ldq + s[i] * kBlockBytes + 16 * q + 4 * w;
+            *reinterpret_cast<uint32_t*>(out) = some ? codes : 0u;
+            const int g = (s[i] * kBlockCols + 32 * w) / G;
+            if (lane % (G / 8) == 0 && g < p.groups)
+                a.gscale[(row0 + r[i]) * a.ldg + g] = (uint16_t)(some ? bits : fine ? 0u : 0x7FC0u);
         }
-        uint8_t* out = a.Q + (row0 + r) * a.ldq + s * kBlockBytes + 16 * q + 4 * w;
-        *reinterpret_cast<uint32_t*>(out) = codes;
-        const int g = (s * kBlockCols + 32 * w) / G;
-        if (lane % (G / 8) == 0 && g < p.groups)
-            a.gscale[(row0 + r) * a.ldg + g] = (uint16_t)(some ? bits : top < kTiny ? 0u : 0x7FC0u);
     }
 }
 
@@ -128,34 +156,62 @@ struct RowsParams {
 };
 
 // Rows of the table, or those of given tokens: the exact product of a code (4 bits)
-// and its scale (8), rounded once.  A token outside the table has NaN.
-template <typename T, int G>
+// and its scale (8), rounded once.  A token outside the table has NaN.  Each store of
+// a block's 16 lanes is 256 bytes side by side: of bf16 the pairs' eight columns a lane;
+// of fp32 four, for which a lane loads two dwords.  kPast: stored past the caches.
+template <typename T, int G, bool kPast>
 __global__ __launch_bounds__(kRowThreads) void ember_rows_q4(RowsParams p) {
     const Rows4Args& a = p.a;
-    const int lane = threadIdx.x % kUnitLanes, w = lane / 4, q = lane % 4;
+    constexpr int kPieces = sizeof(T) / 2, kCols = 8 / kPieces;      // stores a lane, columns of each
+    const int lane = threadIdx.x % kUnitLanes, q = lane % 4, w = kPieces == 1 ? lane / 4 : lane / 8;
     const int64_t row0 = (int64_t)blockIdx.x * p.rows_per_block;
     const int rows = (int)min((int64_t)p.rows_per_block, a.n - row0);
     const int units = rows * p.nblk, D = (int)a.D;
-    for (int u = threadIdx.x / kUnitLanes; u < units; u += kUnitsPerPass) {
-        const int r = (int)div_small(u, p.magic), s = u - r * p.nblk;
-        const int64_t v = a.tok ? a.tok[row0 + r] : row0 + r;
-        const bool in = v >= 0 && v < a.V;
-        const int col = s * kBlockCols + 32 * w + 4 * q;
-        uint32_t codes = 0;
-        float scale = __uint_as_float(0x7FC00000u);
-        if (in && col < D) {
-            codes = *reinterpret_cast<const uint32_t*>(a.Wq + v * a.ldw + s * kBlockBytes + 16 * q + 4 * w);
-            scale = bf16_bits_f32(a.wscale[v * a.ldg + (s * kBlockCols + 32 * w) / G]);
-        }
-        float lo[4], hi[4];
+    for (int u0 = threadIdx.x / kUnitLanes; u0 < units; u0 += kAhead * kUnitsPerPass) {
+        uint32_t codes[kAhead][kPieces], scale[kAhead][kPieces];
+        int r[kAhead], s[kAhead];
+        int64_t v[kAhead];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            lo[e] = (float)((int)(codes << (28 - 8 * e)) >> 28) * scale;
-            hi[e] = (float)((int)(codes << (24 - 8 * e)) >> 28) * scale;
+        for (int i = 0; i < kAhead; ++i) {
+            const int u = min(u0 + i * kUnitsPerPass, units - 1);
+            r[i] = (int)div_small(u, p.magic);
+            s[i] = u - r[i] * p.nblk;
+            v[i] = a.tok ? a.tok[row0 + r[i]] : row0 + r[i];
         }
-        T* y = static_cast<T*>(a.Y) + (row0 + r) * a.ldy;
-        store_values<T, 4>(y, col, D, lo);
-        store_values<T, 4>(y, col + 16, D, hi);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const bool in = v[i] >= 0 && v[i] < a.V;
+            const int64_t at = in ? v[i] : 0;
+#pragma unroll
+            for (int j = 0; j < kPieces; ++j) {
+                const int wj = w + 2 * j, g = min((s[i] * kBlockCols + 32 * wj) / G, (D - 1) / G);     // past the row: not used
+                codes[i][j] = *reinterpret_cast<const uint32_t*>(a.Wq + at * a.ldw + s[i] * kBlockBytes + 16 * q + 4 * wj);
+                scale[i][j] = in ? a.wscale[at * a.ldg + g] : 0x7FC0u;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            if (u0 + i * kUnitsPerPass >= units) break;
+            T* const y = static_cast<T*>(a.Y) + (row0 + r[i]) * a.ldy;
+            float x[kPieces][kCols];
+#pragma unroll
+            for (int j = 0; j < kPieces; ++j) {
+                // the codes in the upper halves of bytes: of the pair's dwords the same half, or that of lanes 4 .. 7 of 8
+                uint32_t c[2];
+                if constexpr (kPieces == 1) {
+                    const uint32_t other = of_lane<kPair>(codes[i][j]);
+                    c[0] = q & 1 ? other : codes[i][j] << 4;
+                    c[1] = q & 1 ? codes[i][j] : other << 4;
+                } else {
+                    c[0] = lane & 4 ? codes[i][j] : codes[i][j] << 4;
+                }
+                const float f = bf16_bits_f32(scale[i][j]);
+#pragma unroll
+                for (int e = 0; e < kCols; ++e) x[j][e] = (float)((int)(c[e / 4] << (24 - 8 * (e % 4))) >> 28) * f;
+                const int col = kPieces == 1 ? first_col(s[i], lane) : s[i] * kBlockCols + 64 * j + 4 * lane;
+                store_values<T, kCols, kPast>(y, col, D, x[j]);
+            }
+        }
     }
 }
 
@@ -168,11 +224,11 @@ void launch_quantize(const QuantParams& p, unsigned grid, hipStream_t s) {
     else if (p.a.group == 64) ember_quantize_q4<T, 64><<<grid, kRowThreads, 0, s>>>(p);
     else ember_quantize_q4<T, 128><<<grid, kRowThreads, 0, s>>>(p);
 }
-template <typename T>
+template <typename T, bool kPast>
 void launch_rows(const RowsParams& p, unsigned grid, hipStream_t s) {
-    if (p.a.group == 32) ember_rows_q4<T, 32><<<grid, kRowThreads, 0, s>>>(p);
-    else if (p.a.group == 64) ember_rows_q4<T, 64><<<grid, kRowThreads, 0, s>>>(p);
-    else ember_rows_q4<T, 128><<<grid, kRowThreads, 0, s>>>(p);
+    if (p.a.group == 32) ember_rows_q4<T, 32, kPast><<<grid, kRowThreads, 0, s>>>(p);
+    else if (p.a.group == 64) ember_rows_q4<T, 64, kPast><<<grid, kRowThreads, 0, s>>>(p);
+    else ember_rows_q4<T, 128, kPast><<<grid, kRowThreads, 0, s>>>(p);
 }
 
 // ---------------------------------------------------------------------------
@@ -883,8 +939,9 @@ hipError_t launch_rows4(const Rows4Args& a, hipStream_t s) {
     p.magic = magic_of(p.nblk);
     p.rows_per_block = rows_per_block(p.nblk);
     const unsigned grid = (unsigned)((a.n + p.rows_per_block - 1) / p.rows_per_block);
-    if (a.y_dtype == EMBER_F32) launch_rows<float>(p, grid, s);
-    else launch_rows<uint16_t>(p, grid, s);
+    const bool past = a.n * a.D * (a.y_dtype == EMBER_F32 ? 4 : 2) >= kPastBytes;
+    if (a.y_dtype == EMBER_F32) past ? launch_rows<float, true>(p, grid, s) : launch_rows<float, false>(p, grid, s);
+    else past ? launch_rows<uint16_t, true>(p, grid, s) : launch_rows<uint16_t, false>(p, grid, s);
     return hipGetLastError();
 }
 
