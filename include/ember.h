@@ -494,8 +494,10 @@ int ember_logits_q8(const int8_t* Xq, int64_t ldx, const float* xscale,
  * every token reads them.  A row's columns are in groups of 32, 64 or 128 (the
  * last one may be shorter), each with a bf16 scale:
  *
- *   a = max |x| of the group,  s = bf16(a / 7),  c = rint(x / s) in [-7, 7]
+ *   a = max |x| of the group,  s = bf16(a (1/7)),  c = rint(x / s) in [-7, 7]
  *
+ * in fp32: the product with the fp32 nearest 1/7 is rounded to fp32, then to bf16, the
+ * quotient correctly rounded to fp32, then to the nearest integer, to even at a tie.
  * A group whose a is below 1e-36 (zeros among them) has codes and scale 0; one that
  * holds an infinity or a NaN has codes 0 and scale NaN.  Codes are in two's
  * complement, so a table made elsewhere may hold -8 too, and any scales.

@@ -121,7 +121,7 @@ __global__ __launch_bounds__(kRowThreads) void ember_quantize_q4(QuantParams p) 
             if constexpr (G >= 64) top = max(top, of_lane<kHalfRow>(top));
             if constexpr (G == 128) top = max(top, of_lane<kRow>(top));
             const float most = __uint_as_float(top);
-            const uint32_t bits = pack_bf16(most / 7.0f, 0.0f) & 0xFFFFu;
+            const uint32_t bits = pack_bf16(most * (1.0f / 7.0f), 0.0f) & 0xFFFFu;
             const float scale = bf16_bits_f32(bits), inv = 1.0f / scale;
             const bool fine = top < 0x7F800000u, some = fine && most >= kTiny;
             uint32_t half[2] = {0, 0};     // codes of the first four columns, of the others, in the lower halves of bytes

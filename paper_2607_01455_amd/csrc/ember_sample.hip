@@ -45,7 +45,8 @@ constexpr int kPerLane = 8;                       // logits a lane
 constexpr int kChunk = kWave * kPerLane;          // tokens of a chunk
 constexpr int kBins = 1024;
 constexpr int kList = 8192;                       // tokens of a row's list
-constexpr int kPartList = 2048;                   // of a part's
+constexpr int kPartList = 1536;                   // of a part's (launch 3: four blocks a compute unit)
+constexpr int kRanked = 128;                      // of a list that is ranked at once: eight lanes a token
 constexpr int kMaxParts = 64;                     // of a row
 constexpr int64_t kMaxRows = 512;                 // of a launch
 constexpr int64_t kOneBlock = 16384;              // tokens of a row that a block holds
@@ -345,6 +346,7 @@ __device__ __forceinline__ V block_sum(V x, V* red) {
 
 struct Select {
     u64 weight[kBins];
+    u64 place[kRanked];
     int count[kBins];
     u64 red[kRowThreads / kWave];
     int redi[kRowThreads / kWave];
@@ -957,6 +959,50 @@ __global__ __launch_bounds__(kRowThreads) void ember_sample_draw(Params p, int64
                 if (lane == 0) atomicAdd(&more[j / own], sum);
             }
             sure = 0;
+        } else if (n > 0 && n <= kRanked) {
+            // eight lanes an entry: its rank and the weights before it, from all entries in LDS
+            // (entries without a weight do not count)
+            if ((int)threadIdx.x < n) {
+                const u64 x = weight_of(z_of(row, logit_of<T>(first, p.width)), table);
+                s.weight[threadIdx.x] = x;
+                s.place[threadIdx.x] = x ? first : kNone;
+            }
+            __syncthreads();
+            const int e = threadIdx.x / 8;
+            u64 at = e < n ? s.place[e] : kNone, w = e < n ? s.weight[e] : 0, before = 0;
+            const int bin = at != kNone ? bin_of(row, z_of(row, logit_of<T>(at, p.width))) : kBins;
+            int rank = 0;
+            for (int q = threadIdx.x % 8; q < n; q += 8) {
+                const bool less = s.place[q] < at;
+                rank += less;
+                before += less ? s.weight[q] : 0;
+            }
+            rank += from_lane<0xB1, 0xF>(rank, 0);         // of lane ^ 1, lane ^ 2, and 7 - lane of eight
+            rank += from_lane<0x4E, 0xF>(rank, 0);
+            rank += from_lane<0x141, 0xF>(rank, 0);
+            before += from_lane<0xB1, 0xF>(before, (u64)0);
+            before += from_lane<0x4E, 0xF>(before, (u64)0);
+            before += from_lane<0x141, 0xF>(before, (u64)0);
+            if (threadIdx.x % 8) at = kNone;               // one lane counts
+            // bin_k's first entry, and the first that top-k drops
+            const int first_k = has_k ? block_sum<kRowThreads>((int)(at != kNone && bin < st.bin_k), s.redi) : n;
+            const int end_k = has_k ? first_k + (row.ask.k - st.n_k) : n;
+            const bool in = at != kNone && rank < end_k;
+            if (has_k) total = st.w_k + block_sum<kRowThreads>(in && rank >= first_k ? w : 0, s.red);
+            bool mine = has_k && in;
+            if (has_p) {
+                // the largest logit is kept whatever top-p is
+                mine = in && bin <= st.bin_p1 && (st.w_p + before < part_of(total, row.ask.p) || (rank == 0 && st.n_p == 0));
+                kept = st.n_p + block_sum<kRowThreads>((int)mine, s.redi);
+            }
+            const u64 end = wave_one(mine ? at : 0, [](u64 a, u64 b) { return a > b ? a : b; });
+            if (threadIdx.x == 0) s.hi = 0;
+            __syncthreads();
+            if ((threadIdx.x & (kWave - 1)) == 0 && end) atomicMax(&s.hi, end);
+            if (mine && z_of(row, logit_of<T>(at, p.width)) <= row.ask.far)
+                atomicAdd(&more[(uint32_t)(at & (((u64)1 << p.width) - 1)) / (kChunk * own)], w);
+            __syncthreads();
+            last = s.hi;
         } else if (n > 0) {
             constexpr int kOwn = kList / kRowThreads;
             u64 at[kOwn], w[kOwn];

@@ -88,7 +88,7 @@ def rounded(X, group):
     rows, D = X.shape
     x = torch.nn.functional.pad(X.float(), (0, -D % group)).view(rows, -1, group)
     a = x.abs().amax(dim=2)
-    s = (a / torch.full_like(a, 7)).to(BF)     # a division: by a host number torch multiplies with its reciprocal
+    s = (a * (1 / 7)).to(BF)                   # the fp32 nearest 1/7, a product rounded to fp32, then to bf16
     c = torch.round(x / s.float()[:, :, None])
     c = torch.where((a >= 1e-36)[:, :, None], c, 0.0)
     return c.view(rows, -1)[:, :D].long(), torch.where(a >= 1e-36, s, 0.0)
