@@ -1,4 +1,5 @@
-"""Trains the token tables of a toy language model and answers from them in 8 bits.
+"""Trains the token tables of a toy language model, answers from them in 8 bits and
+generates from them in 4.
 
 The model is its token interface alone: the embedding of a token is the hidden
 state, a part of that of the one before it the residual stream, and they go
@@ -14,7 +15,9 @@ would:
 
 with no value read back to the host.  Answering takes the norm's 8-bit output and
 the head in 8 bits (HeadQ8), which takes the table's present rows once after the steps
-on it.
+on it.  Generating holds both tables in 4 bits (HeadQ4): a step reads the last tokens' rows,
+goes through the norm and the head and draws the next tokens (Sampler), all of it in one
+HIP graph that is replayed for every token.
 
     python examples/token_interface.py [--steps N]
 """
@@ -107,6 +110,42 @@ class TokenInterface:
         self.head8.logits(Q, scale, logits)
         return logits
 
+    def generate(self, before, token, u, temperature=None, top_k=None, top_p=None, min_p=None):
+        """Tokens that follow n pairs, one after the other, from both tables in 4 bits: u (steps x n)
+        holds the random numbers, the others are the sampler's, a value a sequence.  Returns the tokens and
+        their log-probabilities, steps x n each."""
+        steps, n = u.shape
+        dev = self.E.device
+        tables = [ember.HeadQ4.from_table(t, group=64) for t in (self.E, self.W)]
+        sampler = ember.Sampler(n, self.V, device=dev)
+        D8 = (self.D + 15) // 16 * 16
+        X, R, S = (torch.empty(n, D8, dtype=torch.bfloat16, device=dev)[:, :self.D] for _ in range(3))     # 16-byte rows
+        Q = torch.empty(n, D8, dtype=torch.int8, device=dev)[:, :self.D]
+        L = torch.empty(n, (self.V + 7) // 8 * 8, dtype=torch.bfloat16, device=dev)[:, :self.V]
+        scale, logp, u_now = (torch.empty(n, device=dev) for _ in range(3))
+        last, ids = before.clone(), token.clone()
+        norm = ember.HeadNorm(self.gain, eps=self.norm.eps)
+
+        def step():
+            tables[0].rows(ids, X)
+            tables[0].rows(last, R)
+            R.mul_(self.BEFORE)
+            norm(X, R, S=S, Q=Q, qscale=scale)
+            tables[1].logits(Q, scale, L)
+            last.copy_(ids)
+            sampler(L, u_now, ids, temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p, logp=logp)
+
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            step()
+        out, out_logp = torch.empty(steps, n, dtype=torch.int64, device=dev), torch.empty(steps, n, device=dev)
+        for i in range(steps):
+            u_now.copy_(u[i])
+            graph.replay()
+            out[i], out_logp[i] = ids, logp
+        return out, out_logp
+
 
 def main():
     ap = argparse.ArgumentParser(description=__doc__.splitlines()[0])
@@ -123,6 +162,13 @@ def main():
     one = m.answer(before[:1], token[:1]).argmax(dim=1).item()
     print(f"answers in 8 bits: {right:.3f} right; after token {token[0].item()} comes {one} "
           f"(the language's: {m.follows[token[0]].item()})")
+    n, steps = 4, 8
+    u = torch.rand(steps, n, generator=m.g, device=m.E.device)
+    ids, logp = m.generate(before[:n], token[:n], u, top_p=torch.full((n,), 0.9, device=m.E.device))
+    chain = torch.cat([token[None, :n], ids])
+    right = (m.follows[chain[:-1]] == ids).float().mean().item()
+    print(f"generated from tables in 4 bits: {ids[:, 0].tolist()}, {right:.3f} of {n} x {steps} as the language has them, "
+          f"log-probability {logp.mean().item():.2f} a token")
 
 
 if __name__ == "__main__":
