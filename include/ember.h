@@ -565,8 +565,8 @@ int ember_logits_q4(const int8_t* Xq, int64_t ldx, const float* xscale,
  * row that has nothing to draw from (no logit above minus infinity), that holds a NaN
  * or an infinity, or whose parameters are out of range (temperature >= 0 and finite,
  * k >= 0, 0 <= p <= 1, 0 <= min_p <= 1, 0 <= u < 1) has id -1, logp NaN and kept 0.
- * e are held in fixed point, exact to half of 2^-n with n = min(48, 62 - ceil(log2 V)):
- * a token whose e is below that is never drawn.  The result depends on a row's logits
+ * e are held in fixed point, to less than 2^-n with n = min(48, 62 - ceil(log2 V)):
+ * a token whose e is below half of that is never drawn.  The result depends on a row's logits
  * and parameters alone, and has the same bits on every run.
  * Layout: L as W and G; 0 <= T <= EMBER_MAX_TOKENS (0: nothing to do, the pointers may
  * be NULL), 1 <= V <= EMBER_SAMPLE_MAX_V.  Outputs and the workspace share no memory

@@ -12,7 +12,7 @@
 // and index in one number) says where it ends.  The token is then the one at which
 // the running sum, by index, of the kept weights passes u times their sum.
 //
-// Rows of up to 16384 tokens: one launch, a block a row, which holds it in registers.
+// Rows of up to 8192 tokens: one launch, a block a row, which holds it in registers.
 // Longer ones take four:
 //   1  the largest and smallest logit of each part of a row;
 //   2  weights, their sum for every chunk of 512 tokens, and, where top-k or top-p
@@ -21,9 +21,9 @@
 //      a list; for every chunk the sum of the tokens before them;
 //   4  a block a row finds the prefix's end among the listed, the chunk in which
 //      the random number falls, and in it the token.
-// An end is found by histograms over the places, each over one bin of the last.  A
-// list that does not fit (thousands of equal logits where a prefix ends) is
-// replaced by a search over the whole row by halving.
+// An end is found by histograms over the places, each over one bin of the last: of the
+// listed, or, where they do not fit (thousands of equal logits at a prefix's end), of
+// the whole row.
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -49,7 +49,7 @@ constexpr int kPartList = 1536;                   // of a part's (launch 3: four
 constexpr int kRanked = 128;                      // of a list that is ranked at once: eight lanes a token
 constexpr int kMaxParts = 64;                     // of a row
 constexpr int64_t kMaxRows = 512;                 // of a launch
-constexpr int64_t kOneBlock = 16384;              // tokens of a row that a block holds
+constexpr int64_t kOneBlock = kRowThreads * kPerLane;   // tokens of a row that a block holds
 constexpr int kSteps = 32;                        // of a halving of the weight: z counts these
 constexpr double kLog2e = 1.4426950408889634;
 constexpr double kLn2 = 0.6931471805599453;
@@ -358,19 +358,16 @@ struct Select {
 constexpr u64 kNone = ~(u64)0;   // past every place
 
 // The first place up to which the candidates' count (or their weights) reaches
-// `need`, of 1 at least and at most what there is.  A block's threads have kOwn
-// tokens each, of which those in the mask are candidates; every pass makes a
-// histogram over one bin of the last, until a bin holds one.  n, w: what there is
-// up to the place, it included.
-template <bool kWeights, int kOwn, typename F, typename G>
-__device__ u64 end_of(F place, G weight, uint32_t mask, u64 need, Select& s, int& n, u64& w) {
+// `need`, of 1 at least and at most what there is.  each(f) calls f(place, weight) for
+// the candidates of a thread; every pass makes a histogram over one bin of the last,
+// until a bin holds one.  n, w: what there is up to the place, it included.
+template <bool kWeights, typename Each>
+__device__ u64 end_of(Each each, u64 need, Select& s, int& n, u64& w) {
     u64 lo = kNone, hi = 0;
-#pragma unroll
-    for (int q = 0; q < kOwn; ++q) {
-        if (!(mask >> q & 1)) continue;
-        lo = min(lo, place(q));
-        hi = max(hi, place(q));
-    }
+    each([&](u64 place, auto) {
+        lo = min(lo, place);
+        hi = max(hi, place);
+    });
     lo = wave_one(lo, [](u64 a, u64 b) { return a < b ? a : b; });
     hi = wave_one(hi, [](u64 a, u64 b) { return a > b ? a : b; });
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -396,13 +393,12 @@ __device__ u64 end_of(F place, G weight, uint32_t mask, u64 need, Select& s, int
         if (pass > 0 && s.in == 1) break;
         const u64 wide = to - from;
         const int shift = wide < kBins ? 0 : 64 - __clzll(wide) - 10;
-#pragma unroll
-        for (int q = 0; q < kOwn; ++q) {
-            if (!(mask >> q & 1) || place(q) < from || place(q) > to) continue;
-            const int b = (int)((place(q) - from) >> shift);
-            atomicAdd(&s.weight[b], weight(q));
+        each([&](u64 place, auto weight) {
+            if (place < from || place > to) return;
+            const int b = (int)((place - from) >> shift);
+            atomicAdd(&s.weight[b], weight());
             atomicAdd(&s.count[b], 1);
-        }
+        });
         __syncthreads();
         const u64 wb = s.weight[threadIdx.x];
         const int nb = s.count[threadIdx.x];
@@ -436,13 +432,11 @@ __device__ u64 end_of(F place, G weight, uint32_t mask, u64 need, Select& s, int
     n = s.n + 1;
     const u64 w0 = s.w;
     __syncthreads();
-#pragma unroll
-    for (int q = 0; q < kOwn; ++q) {
-        if ((mask >> q & 1) && place(q) >= from && place(q) <= to) {
-            s.lo = place(q);
-            s.w = w0 + weight(q);
-        }
-    }
+    each([&](u64 place, auto weight) {
+        if (place < from || place > to) return;
+        s.lo = place;
+        s.w = w0 + weight();
+    });
     __syncthreads();
     w = s.w;
     return s.lo;
@@ -464,102 +458,79 @@ __device__ __forceinline__ void token(const Params& p, int64_t t, int64_t i, dou
 }
 
 // ---------------------------------------------------------------------------
-// one launch: row blockIdx.x, eight tokens a thread side by side, kPieces times
+// one launch: a block a row, eight tokens a thread side by side
 // ---------------------------------------------------------------------------
 
-template <typename T, int kPieces>
-__global__ __launch_bounds__(kRowThreads) void ember_sample_row(Params p) {
-    constexpr int kOwn = kPieces * kPerLane;
+template <typename T>
+__global__ __launch_bounds__(kRowThreads) void ember_sample_row(Params p, int64_t t0) {
     __shared__ Select s;
     __shared__ double table[kSteps];
     __shared__ Part redp[kRowThreads / kWave];
-    const int64_t t = blockIdx.x;
+    const int64_t t = t0 + blockIdx.x;
     const T* const l = static_cast<const T*>(p.a.L) + t * p.a.ldl;
     fill_table(table, p.bits);
-    float x[kOwn];
+    float x[kPerLane];
     Part part{-kInf, kInf, 0, 0};
+    const uint32_t i0 = threadIdx.x * kPerLane;
+    load8(l, i0, p.a.V, x);
 #pragma unroll
-    for (int q = 0; q < kPieces; ++q) {
-        float y[kPerLane];
-        load8(l, (int64_t)(q * kRowThreads + threadIdx.x) * kPerLane, p.a.V, y);
-#pragma unroll
-        for (int e = 0; e < kPerLane; ++e) {
-            x[q * kPerLane + e] = y[e];
-            see(part, y[e]);
-        }
-    }
+    for (int e = 0; e < kPerLane; ++e) see(part, x[e]);
     const Row row = row_of(p, t, block_join<kRowThreads>(part, redp));
     if (!row.fine) {
         if (threadIdx.x == 0) no_token(p.a, t);
         return;
     }
-    // where the registers do not hold them all, weights are formed where they are used
-    constexpr bool kHeld = kPieces == 1;
-    u64 held[kHeld ? kOwn : 1], all = 0;
-    const auto weight = [&](int q) {
-        if constexpr (kHeld) return held[q];
-        else return weight_of(z_of(row, x[q]), table);
-    };
+    u64 w[kPerLane], all = 0;
     uint32_t mask = 0;                    // tokens of this thread that have a weight, then those that are kept
     int near = 0;
 #pragma unroll
-    for (int q = 0; q < kOwn; ++q) {
-        const double z = z_of(row, x[q]);
-        const u64 w = weight_of(z, table);
-        if constexpr (kHeld) held[q] = w;
-        all += w;
-        mask |= (uint32_t)(w != 0) << q;
-        near += x[q] != -kInf && z <= row.ask.far;
+    for (int e = 0; e < kPerLane; ++e) {
+        const double z = z_of(row, x[e]);
+        w[e] = weight_of(z, table);
+        all += w[e];
+        mask |= (uint32_t)(w[e] != 0) << e;
+        near += x[e] != -kInf && z <= row.ask.far;
     }
     all = block_sum<kRowThreads>(all, s.red);
     int kept = row.some;
     if (ranked(row.ask)) {
-        const auto place = [&](int q) {
-            const uint32_t i = (q / kPerLane * kRowThreads + threadIdx.x) * kPerLane + q % kPerLane;
-            return place_of<T>(x[q], i, p.width);
+        const auto place = [&](int e) { return place_of<T>(x[e], i0 + e, p.width); };
+        const auto each = [&](auto f) {
+#pragma unroll
+            for (int e = 0; e < kPerLane; ++e)
+                if (mask >> e & 1) f(place(e), [&] { return w[e]; });
         };
         const int positive = block_sum<kRowThreads>((int)__popc(mask), s.redi);
         u64 last = kNone, total = all;    // the last place that is kept, and the weights up to it
         int n;
         if (row.ask.k > 0) {
             kept = min(kept, row.ask.k);
-            if (row.ask.k < positive) last = end_of<false, kOwn>(place, weight, mask, (u64)row.ask.k, s, n, total);
+            if (row.ask.k < positive) last = end_of<false>(each, (u64)row.ask.k, s, n, total);
         }
         if (row.ask.p < 1.0f) {
             const u64 need = part_of(total, row.ask.p);
-            last = end_of<true, kOwn>(place, weight, mask, need > 0 ? need : 1, s, n, total);
+            last = end_of<true>(each, need > 0 ? need : 1, s, n, total);
             kept = n;
         }
 #pragma unroll
-        for (int q = 0; q < kOwn; ++q) mask &= ~((uint32_t)(place(q) > last) << q);
+        for (int e = 0; e < kPerLane; ++e) mask &= ~((uint32_t)(place(e) > last) << e);
     }
     if (row.ask.floor > 0.0f) {
         kept = min(kept, block_sum<kRowThreads>(near, s.redi));
 #pragma unroll
-        for (int q = 0; q < kOwn; ++q) mask &= ~((uint32_t)(z_of(row, x[q]) > row.ask.far) << q);
+        for (int e = 0; e < kPerLane; ++e) mask &= ~((uint32_t)(z_of(row, x[e]) > row.ask.far) << e);
     }
-    // running sums by index: a piece is a whole run of the row
-    u64 end[kPieces], total = 0;
+    // running sums by index
+    u64 sum = 0, total;
 #pragma unroll
-    for (int q = 0; q < kPieces; ++q) {
-        u64 sum = 0, piece;
-#pragma unroll
-        for (int e = 0; e < kPerLane; ++e) sum += mask >> (q * kPerLane + e) & 1 ? weight(q * kPerLane + e) : 0;
-        end[q] = total + block_scan<kRowThreads>(sum, s.red, piece);
-        total += piece;
-    }
+    for (int e = 0; e < kPerLane; ++e) sum += mask >> e & 1 ? w[e] : 0;
+    u64 run = block_scan<kRowThreads>(sum, s.red, total);
     const u64 target = (u64)((double)total * (double)row.ask.u);
 #pragma unroll
-    for (int q = 0; q < kPieces; ++q) {
-        u64 run = end[q];
-#pragma unroll
-        for (int e = kPerLane - 1; e >= 0; --e) {
-            const int o = q * kPerLane + e;
-            const u64 after = run;
-            run -= mask >> o & 1 ? weight(o) : 0;
-            if (run <= target && target < after)
-                token(p, t, (q * kRowThreads + threadIdx.x) * kPerLane + e, z_of(row, x[o]), all, kept);
-        }
+    for (int e = kPerLane - 1; e >= 0; --e) {
+        const u64 after = run;
+        run -= mask >> e & 1 ? w[e] : 0;
+        if (run <= target && target < after) token(p, t, i0 + e, z_of(row, x[e]), all, kept);
     }
 }
 
@@ -869,34 +840,6 @@ __global__ __launch_bounds__(kThreads) void ember_sample_list(Params p, int64_t 
 // launch 4: row blockIdx.x
 // ---------------------------------------------------------------------------
 
-// Tokens up to a place in falling order, or (weights) their weights.
-template <bool kWeights, typename T>
-__device__ u64 up_to(const Params& p, const Row& row, const T* l, u64 place, Select& s, const double* table) {
-    u64 sum = 0;
-    for (int64_t i = threadIdx.x * kPerLane; i < p.a.V; i += kRowThreads * kPerLane) {
-        float x[kPerLane];
-        load8(l, i, p.a.V, x);
-#pragma unroll
-        for (int e = 0; e < kPerLane; ++e) {
-            if (x[e] != -kInf && place_of<T>(x[e], (uint32_t)(i + e), p.width) <= place)
-                sum += kWeights ? weight_of(z_of(row, x[e]), table) : 1;
-        }
-    }
-    return block_sum<kRowThreads>(sum, s.red);
-}
-
-// The first place up to which there is `need`, 1 at least, by halving.
-template <bool kWeights, typename T>
-__device__ u64 reach(const Params& p, const Row& row, const T* l, u64 need, Select& s, const double* table) {
-    u64 low = place_of<T>((float)row.top, 0, p.width), high = ((u64)1 << (kFallBits<T> + p.width)) - 1;      // the answer is in [low, high]
-    while (low < high) {
-        const u64 mid = low + (high - low) / 2;
-        if (up_to<kWeights>(p, row, l, mid, s, table) >= need) high = mid;
-        else low = mid + 1;
-    }
-    return high;
-}
-
 template <typename T>
 __global__ __launch_bounds__(kRowThreads) void ember_sample_draw(Params p, int64_t t0) {
     __shared__ Select s;
@@ -931,34 +874,42 @@ __global__ __launch_bounds__(kRowThreads) void ember_sample_draw(Params p, int64
         const bool has_k = st.bin_k < kBins, has_p = st.bin_p < kBins;
         const int n = (int)min(st.listed, (unsigned)kList + 1);
         u64 total = all;
-        if (n > kList) {
-            // too many for the list: search the row, then sum its chunks again
-            last = kNone;
+        // each(first, last bin, f): this thread's tokens of a weight in them, as end_of takes them
+        const auto find_ends = [&](auto each) {
+            int found;
+            u64 sum;
             if (has_k) {
-                last = reach<false>(p, row, l, (u64)row.ask.k, s, table);
-                total = up_to<true>(p, row, l, last, s, table);
+                last = end_of<false>([&](auto f) { each(st.bin_k, st.bin_k, f); }, (u64)(row.ask.k - st.n_k), s, found, sum);
+                total = st.w_k + sum;
             }
             if (has_p) {
+                // what the bins before keep is below this part, and at bin_p1's end it is reached
                 const u64 need = part_of(total, row.ask.p);
-                last = min(last, reach<true>(p, row, l, need > 0 ? need : 1, s, table));
-                kept = (int)up_to<false>(p, row, l, last, s, table);
+                last = end_of<true>([&](auto f) { each(st.bin_p, st.bin_p1, f); }, need > st.w_p ? need - st.w_p : 1, s,
+                                    found, sum);
+                kept = st.n_p + found;
             }
-            const int wave = threadIdx.x / kWave, lane = threadIdx.x & (kWave - 1);
-            for (int j = wave; j < p.chunks; j += kRowThreads / kWave) {
-                float x[kPerLane];
-                const int64_t i = (int64_t)j * kChunk + lane * kPerLane;
-                load8(l, i, p.a.V, x);
-                u64 sum = 0;
+        };
+        if (n > kList) {
+            const auto each = [&](int first, int last, auto f) {
+                for (int64_t i = threadIdx.x * kPerLane; i < p.a.V; i += kRowThreads * kPerLane) {
+                    float x[kPerLane];
+                    load8(l, i, p.a.V, x);
 #pragma unroll
-                for (int e = 0; e < kPerLane; ++e) {
-                    const double z = z_of(row, x[e]);
-                    if (place_of<T>(x[e], (uint32_t)(i + e), p.width) <= last && z <= row.ask.far)
-                        sum += weight_of(z, table);
+                    for (int e = 0; e < kPerLane; ++e) {
+                        const double z = z_of(row, x[e]);
+                        const int b = bin_of(row, z);
+                        if (b < first || b > last) continue;
+                        const u64 w = weight_of(z, table);
+                        if (w) f(place_of<T>(x[e], (uint32_t)(i + e), p.width), [&] { return w; });
+                    }
                 }
-                sum = wave_sum(sum);
-                if (lane == 0) atomicAdd(&more[j / own], sum);
-            }
-            sure = 0;
+            };
+            find_ends(each);
+            each(sure, kBins - 1, [&](u64 at, auto weight) {
+                if (at <= last && z_of(row, logit_of<T>(at, p.width)) <= row.ask.far)
+                    atomicAdd(&more[(uint32_t)(at & (((u64)1 << p.width) - 1)) / (kChunk * own)], weight());
+            });
         } else if (n > 0 && n <= kRanked) {
             // eight lanes an entry: its rank and the weights before it, from all entries in LDS
             // (entries without a weight do not count)
@@ -1006,36 +957,27 @@ __global__ __launch_bounds__(kRowThreads) void ember_sample_draw(Params p, int64
         } else if (n > 0) {
             constexpr int kOwn = kList / kRowThreads;
             u64 at[kOwn], w[kOwn];
-            uint32_t in_k = 0, in_p = 0;
-            const auto place = [&](int q) { return at[q]; };
-            const auto weight = [&](int q) { return w[q]; };
+            int bin[kOwn];
             const auto logit = [&](int q) { return logit_of<T>(at[q], p.width); };
 #pragma unroll
             for (int q = 0; q < kOwn; ++q) {
                 at[q] = kNone;
                 w[q] = 0;
+                bin[q] = kBins;
                 if (q * kRowThreads >= n) continue;
                 const int i = q * kRowThreads + threadIdx.x;
-                if (i < n) at[q] = q == 0 ? first : p.s.list[(int64_t)r * kList + i];
-                const double z = i < n ? z_of(row, logit(q)) : kFar;
+                if (i >= n) continue;
+                at[q] = q == 0 ? first : p.s.list[(int64_t)r * kList + i];
+                const double z = z_of(row, logit(q));
                 w[q] = weight_of(z, table);
-                const int b = bin_of(row, z);
-                if (w[q] == 0) at[q] = kNone;
-                in_k |= (uint32_t)(w[q] && b == st.bin_k) << q;
-                in_p |= (uint32_t)(w[q] && b >= st.bin_p && b <= st.bin_p1) << q;
+                if (w[q]) bin[q] = bin_of(row, z);
+                else at[q] = kNone;
             }
-            int found;
-            u64 sum;
-            if (has_k) {
-                last = end_of<false, kOwn>(place, weight, in_k, (u64)(row.ask.k - st.n_k), s, found, sum);
-                total = st.w_k + sum;
-            }
-            if (has_p) {
-                // what the bins before keep is below this part, and at bin_p1's end it is reached
-                const u64 need = part_of(total, row.ask.p);
-                last = end_of<true, kOwn>(place, weight, in_p, need > st.w_p ? need - st.w_p : 1, s, found, sum);
-                kept = st.n_p + found;
-            }
+            find_ends([&](int first, int last, auto f) {
+#pragma unroll
+                for (int q = 0; q < kOwn; ++q)
+                    if (bin[q] >= first && bin[q] <= last) f(at[q], [&] { return w[q]; });
+            });
             // the kept ones join their chunks' sums
 #pragma unroll
             for (int q = 0; q < kOwn; ++q) {
@@ -1094,10 +1036,12 @@ hipError_t launch(const Params& p, int64_t t0, int rows, bool list, hipStream_t 
 
 template <typename T>
 hipError_t launch_row(const Params& p, hipStream_t s) {
-    const unsigned rows = (unsigned)p.a.T;
-    if (p.a.V <= kOneBlock / 2) ember_sample_row<T, 1><<<rows, kRowThreads, 0, s>>>(p);
-    else ember_sample_row<T, 2><<<rows, kRowThreads, 0, s>>>(p);
-    return hipGetLastError();
+    for (int64_t t0 = 0; t0 < p.a.T; t0 += kMaxGridBlocks) {
+        ember_sample_row<T><<<(unsigned)std::min(kMaxGridBlocks, p.a.T - t0), kRowThreads, 0, s>>>(p, t0);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 } // namespace

@@ -239,6 +239,38 @@ def test_more_rows_than_a_launch(em, T, V):
     check(em, L, u, k=[5] * T, p=[0.9] * T)
 
 
+def test_more_rows_than_a_grid(em):
+    """More than 2^20 rows that are a block each: the same as in two calls."""
+    T, V = (1 << 20) + 70, 5
+    print(f"sample T={T} V={V}", flush=True)
+    L, u = zipf(T, V, F, 3)
+    k = torch.full((T,), 3, dtype=torch.int32, device=DEV)
+    whole = draw(em, L, u, k=k)
+    half = T // 2
+    for a, b in ((0, half), (half, T)):
+        for x, y in zip(draw(em, L[a:b], u[a:b], k=k[a:b]), whole):
+            assert torch.equal(x, y[a:b])
+    check(em, L[-50:], u[-50:], k=[3] * 50)
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_few_values(em, dtype):
+    """Thousands of tokens of each of a few logits, at random places: ends among more than a list holds."""
+    T, V = 12, 128256
+    print(f"sample few values {dtype}", flush=True)
+    L = logits(T, V, dtype)
+    L.copy_(20 + torch.randint(-3, 4, (T, V), generator=gen(1), device=DEV) * 0.125)
+    u = torch.rand(T, generator=gen(2), device=DEV)
+    k = [1, 2, 100, 5000, 20000, 60000, 100000, V, 0, 0, 0, 0]
+    p = [1.0, 0.9, 0.5, 0.99, 1.0, 0.7, 0.95, 0.999, 0.01, 0.3, 0.9, 0.99]
+    check(em, L, u, k=k)
+    check(em, L, u, p=p)
+    check(em, L, u, k=k, p=p, floor=[0.0, 0.5, 0.7, 0.8, 0.9, 0.95] * 2)
+    L[:, 0] = -1e4                       # the bins are 2^-10 of a wide range
+    L[:, V // 2] = 21.0
+    check(em, L, u, k=k, p=p)
+
+
 def test_row_alone_and_among_others(em):
     """A row's token depends on the row alone, in how many parts it may be worked on."""
     L, u = zipf(300, 40000, F, 8)
