@@ -29,7 +29,6 @@
 namespace ember {
 namespace {
 
-typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int kBlockCols = 128;      // columns of a block of codes
@@ -150,6 +149,7 @@ __global__ __launch_bounds__(kRowThreads) void ember_quantize_q4(QuantParams p) 
 
 struct RowsParams {
     Rows4Args a;
+    int64_t first;       // row of the first, without tokens
     int nblk;
     uint32_t magic;
     int rows_per_block;
@@ -176,7 +176,7 @@ __global__ __launch_bounds__(kRowThreads) void ember_rows_q4(RowsParams p) {
             const int u = min(u0 + i * kUnitsPerPass, units - 1);
             r[i] = (int)div_small(u, p.magic);
             s[i] = u - r[i] * p.nblk;
-            v[i] = a.tok ? a.tok[row0 + r[i]] : row0 + r[i];
+            v[i] = a.tok ? a.tok[row0 + r[i]] : p.first + row0 + r[i];
         }
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
@@ -631,7 +631,7 @@ __global__ __launch_bounds__(C::kThreads) void ember_logits_q4(Tile4Params p) {
 
     const int row_x = wave * 8 + lane / 8, row_w = wave * 16 + lane / 4;
     const int k_x = ((lane % 8) ^ swizzle<8>(row_x)) * 16, k_w = ((lane % 4) ^ swizzle<4>(row_w)) * 16;
-    const int row_s = wave * kWave + lane;                 // of the first waves
+    const int row_s = wave < C::BN / kWave ? wave * kWave + lane : 0;      // the first waves load the scales
     const uint32_t off_x = row_x * (uint32_t)a.ldx + k_x, off_w = row_w * (uint32_t)a.ldw + k_w;
     const uint32_t off_s = row_s * (uint32_t)(2 * a.ldg);
     // all of a load's place in the offset that the buffer's range is checked against; past the
@@ -781,7 +781,7 @@ __global__ __launch_bounds__(C::kThreads) void ember_logits_q4(Tile4Params p) {
     // A lane holds 16 tokens of a channel: through a strip of LDS of the wave's own, 32
     // tokens x 32 channels, each token's are stored side by side.
     constexpr int kEs = (int)sizeof(YT), kPitch = 32 * kEs + 16, kEpc = 16 / kEs, kPerRow = 32 / kEpc;
-    static_assert(C::kWaves * 32 * kPitch <= C::kLds, "the strips");
+    static_assert(C::kWaves * 32 * kPitch <= C::kXs, "the strips");
     uint8_t* const strip = lds + wave * (32 * kPitch);
     int el = lane;
     asm volatile("" : "+v"(el));   // what follows from it is not kept in registers over the loop above
@@ -919,6 +919,7 @@ hipError_t launch_group(const Logits4Args& a, hipStream_t s) {
 
 } // namespace
 
+// (a launch's blocks are limited, so rows go in parts)
 hipError_t launch_quantize4(const Quant4Args& a, hipStream_t s) {
     QuantParams p;
     p.a = a;
@@ -926,10 +927,19 @@ hipError_t launch_quantize4(const Quant4Args& a, hipStream_t s) {
     p.groups = (int)((a.D + a.group - 1) / a.group);
     p.magic = magic_of(p.nblk);
     p.rows_per_block = rows_per_block(p.nblk);
-    const unsigned grid = (unsigned)((a.rows + p.rows_per_block - 1) / p.rows_per_block);
-    if (a.x_dtype == EMBER_F32) launch_quantize<float>(p, grid, s);
-    else launch_quantize<uint16_t>(p, grid, s);
-    return hipGetLastError();
+    const int64_t part = kMaxGridBlocks * p.rows_per_block;
+    for (int64_t row = 0; row < a.rows; row += part) {
+        p.a.X = static_cast<const char*>(a.X) + row * a.ldx * (a.x_dtype == EMBER_F32 ? 4 : 2);
+        p.a.Q = a.Q + row * a.ldq;
+        p.a.gscale = a.gscale + row * a.ldg;
+        p.a.rows = std::min(part, a.rows - row);
+        const unsigned grid = (unsigned)((p.a.rows + p.rows_per_block - 1) / p.rows_per_block);
+        if (a.x_dtype == EMBER_F32) launch_quantize<float>(p, grid, s);
+        else launch_quantize<uint16_t>(p, grid, s);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 hipError_t launch_rows4(const Rows4Args& a, hipStream_t s) {
@@ -938,11 +948,21 @@ hipError_t launch_rows4(const Rows4Args& a, hipStream_t s) {
     p.nblk = (int)((a.D + kBlockCols - 1) / kBlockCols);
     p.magic = magic_of(p.nblk);
     p.rows_per_block = rows_per_block(p.nblk);
-    const unsigned grid = (unsigned)((a.n + p.rows_per_block - 1) / p.rows_per_block);
-    const bool past = a.n * a.D * (a.y_dtype == EMBER_F32 ? 4 : 2) >= kPastBytes;
-    if (a.y_dtype == EMBER_F32) past ? launch_rows<float, true>(p, grid, s) : launch_rows<float, false>(p, grid, s);
-    else past ? launch_rows<uint16_t, true>(p, grid, s) : launch_rows<uint16_t, false>(p, grid, s);
-    return hipGetLastError();
+    const int es = a.y_dtype == EMBER_F32 ? 4 : 2;
+    const bool past = a.n * a.D * es >= kPastBytes;
+    const int64_t part = kMaxGridBlocks * p.rows_per_block;
+    for (int64_t row = 0; row < a.n; row += part) {
+        p.a.Y = static_cast<char*>(a.Y) + row * a.ldy * es;
+        if (a.tok) p.a.tok = a.tok + row;
+        p.first = row;
+        p.a.n = std::min(part, a.n - row);
+        const unsigned grid = (unsigned)((p.a.n + p.rows_per_block - 1) / p.rows_per_block);
+        if (a.y_dtype == EMBER_F32) past ? launch_rows<float, true>(p, grid, s) : launch_rows<float, false>(p, grid, s);
+        else past ? launch_rows<uint16_t, true>(p, grid, s) : launch_rows<uint16_t, false>(p, grid, s);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 hipError_t launch_logits4(const Logits4Args& a, hipStream_t s) {

@@ -319,6 +319,42 @@ def test_wide_strides(em):
         near(Y, codes[:V], s[:V], 32, Xq, xs, None)
 
 
+def test_wide_scale_strides(em):
+    """Scales at the largest strides, the rows between them NaN."""
+    ld, n = (1 << 22) - 8, 300
+    codes, Q, st = table(n, 1000, 32, 1, 0)
+    s = torch.full((n * ld,), float("nan"), dtype=BF, device=DEV).as_strided((n, 32), (ld, 1))
+    s.copy_(st)
+    for T in (1, 20, 70, 300, 1000):
+        print(f"q4 wide scale strides T={T}", flush=True)
+        Xq, xs = tokens(T, 1000, T)
+        Y = mat(T, n, F, 0)
+        em.ember_logits_q4(Xq, xs, Q, s, Y, 32)
+        near(Y, codes, st, 32, Xq, xs, None)
+    Y = mat(n, 1000, F)
+    em.ember_rows_q4(Q, s, Y, 32)
+    assert torch.equal(Y, values(codes, st, 32).float())
+
+
+def test_more_rows_than_a_launch(em):
+    """2^20 blocks of 64 rows and some more: the rows behind them are where those before are."""
+    V, D = (1 << 26) + 3000, 8
+    print("q4 rows V=2^26 + 3000", flush=True)
+    X = torch.randn(V, D, generator=gen(3), device=DEV).to(BF)
+    Q = torch.full((V, 64), 0x5A, dtype=torch.uint8, device=DEV)
+    s = torch.full((V, 8), 7.0, dtype=BF, device=DEV)
+    em.ember_quantize_rows_q4(X, Q, s[:, :1], 32)
+    Y = torch.full((V, D), float("nan"), dtype=BF, device=DEV)
+    em.ember_rows_q4(Q, s[:, :1], Y, 32)
+    for a, b in ((0, 5000), (V - 5000, V)):
+        c, sc = rounded(X[a:b], 32)
+        assert torch.equal(unpack(Q[a:b], D), c) and torch.equal(s[a:b, :1], sc)
+        assert torch.equal(Y[a:b], values(c, sc, 32).to(BF))
+    # a code is off by half a step at most, the scale by 2^-8: 7 * 2^-8 of a step more
+    err = (X.float() - Y.float()).abs().amax(dim=1)
+    assert (err <= s[:, 0].float() * (0.5 + 7 * 2.0 ** -8) * (1 + 2.0 ** -7)).all()
+
+
 def test_a_part_of_a_table(em):
     """Channels of a larger table: what lies behind them is not read into them."""
     codes, Q, s = table(500, 300, 64, 2)
