@@ -480,6 +480,16 @@ def ember_logits_q8(Xq: torch.Tensor, xscale: torch.Tensor, Wq: torch.Tensor, ws
            "ember_logits_q8")
 
 
+def _run(where, dev, f, *args):
+    """The entry point f with the GPU dev current: a launch on the null stream goes to the current one."""
+    if torch._C._cuda_getDevice() == dev:
+        st = f(*args)
+    else:
+        with torch.cuda.device(dev):
+            st = f(*args)
+    _check(st, where)
+
+
 def q4_shapes(V: int, D: int, group: int):
     """Shapes of a V x D table's codes (uint8) and scales (bf16) in 4 bits; rows of
     either start on 16-byte boundaries."""
@@ -499,8 +509,8 @@ def ember_quantize_rows_q4(X: torch.Tensor, Q: torch.Tensor, gscale: torch.Tenso
     (rows, D), dev = X.shape, X.get_device()
     x, ldx = _matrix("X", X, X.shape, dev)
     q, ldq, s, lds = _table4(Q, gscale, rows, D, group, dev)
-    _check(LIB.ember_quantize_rows_q4(x, _dtype(X), ldx, rows, D, group, q, ldq, s, lds, _stream(X)),
-           "ember_quantize_rows_q4")
+    _run("ember_quantize_rows_q4", dev, LIB.ember_quantize_rows_q4, x, _dtype(X), ldx, rows, D, group, q, ldq, s, lds,
+         _stream(X))
 
 
 def ember_rows_q4(Wq: torch.Tensor, wscale: torch.Tensor, Y: torch.Tensor, group: int,
@@ -510,8 +520,8 @@ def ember_rows_q4(Wq: torch.Tensor, wscale: torch.Tensor, Y: torch.Tensor, group
     n, D = Y.shape
     w, ldw, s, lds = _table4(Wq, wscale, V, D, group, dev)
     y, ldy = _matrix("Y", Y, Y.shape, dev)
-    _check(LIB.ember_rows_q4(w, ldw, s, lds, group, V, D, _vector("tok", tok, (n,), dev, torch.int64), n, y,
-                             _dtype(Y), ldy, _stream(Wq)), "ember_rows_q4")
+    _run("ember_rows_q4", dev, LIB.ember_rows_q4, w, ldw, s, lds, group, V, D,
+         _vector("tok", tok, (n,), dev, torch.int64), n, y, _dtype(Y), ldy, _stream(Wq))
 
 
 def ember_logits_q4(Xq: torch.Tensor, xscale: torch.Tensor, Wq: torch.Tensor, wscale: torch.Tensor,
@@ -523,9 +533,8 @@ def ember_logits_q4(Xq: torch.Tensor, xscale: torch.Tensor, Wq: torch.Tensor, ws
     x, ldx = _matrix("Xq", Xq, (T, D), dev, torch.int8)
     w, ldw, s, lds = _table4(Wq, wscale, V, D, group, dev)
     y, ldy = _matrix("Y", Y, (T, V), dev)
-    _check(LIB.ember_logits_q4(x, ldx, _vector("xscale", xscale, (T,), dev), w, ldw, s, lds, group,
-                               _vector("bias", bias, (V,), dev), T, V, D, y, _dtype(Y), ldy, _stream(Wq)),
-           "ember_logits_q4")
+    _run("ember_logits_q4", dev, LIB.ember_logits_q4, x, ldx, _vector("xscale", xscale, (T,), dev), w, ldw, s, lds,
+         group, _vector("bias", bias, (V,), dev), T, V, D, y, _dtype(Y), ldy, _stream(Wq))
 
 
 def ember_sample_workspace_bytes(max_tokens: int, V: int) -> int:
@@ -547,12 +556,10 @@ def ember_sample(L: torch.Tensor, u: torch.Tensor, ids: torch.Tensor, ws: torch.
     l, ldl = _matrix("L", L, L.shape, dev)
     rows = (T,)
     w, w_bytes = _workspace(ws, dev)
-    _check(LIB.ember_sample(l, _dtype(L), ldl, T, V, _vector("temperature", temperature, rows, dev),
-                            _vector("top_k", top_k, rows, dev, torch.int32), _vector("top_p", top_p, rows, dev),
-                            _vector("min_p", min_p, rows, dev), _vector("u", u, rows, dev),
-                            _vector("ids", ids, rows, dev, torch.int64), _vector("logp", logp, rows, dev),
-                            _vector("kept", kept, rows, dev, torch.int32), w, w_bytes, _stream(L)),
-           "ember_sample")
+    _run("ember_sample", dev, LIB.ember_sample, l, _dtype(L), ldl, T, V, _vector("temperature", temperature, rows, dev),
+         _vector("top_k", top_k, rows, dev, torch.int32), _vector("top_p", top_p, rows, dev),
+         _vector("min_p", min_p, rows, dev), _vector("u", u, rows, dev), _vector("ids", ids, rows, dev, torch.int64),
+         _vector("logp", logp, rows, dev), _vector("kept", kept, rows, dev, torch.int32), w, w_bytes, _stream(L))
 
 
 def ember_clip_workspace_bytes(n_grads: int) -> int:
