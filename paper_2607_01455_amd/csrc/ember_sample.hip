@@ -14,9 +14,10 @@
 //
 // Rows of up to 8192 tokens: one launch, a block a row, which holds it in registers.
 // Longer ones take four:
-//   1  the largest and smallest logit of each part of a row;
-//   2  weights, their sum for every chunk of 512 tokens, and, where top-k or top-p
-//      is on, a histogram over z of counts and weights;
+//   1  the largest and smallest logit of each part of a row, and, for a row that has a
+//      filter, the largest of every chunk of 1024 tokens;
+//   2  weights and their sum, of every chunk where no filter is on, and, where top-k or
+//      top-p is, a histogram over z of counts and weights;
 //   3  from the histogram the bins in which the prefixes end: their tokens go to
 //      a list; for every chunk the sum of the tokens before them;
 //   4  a block a row finds the prefix's end among the listed, the chunk in which
@@ -42,10 +43,11 @@ constexpr int kThreads = 512;                     // launches 1 to 3
 constexpr int kWavesB = kThreads / kWave;
 constexpr int kRowThreads = 1024;                 // a block that has a row
 constexpr int kPerLane = 8;                       // logits a lane
-constexpr int kChunk = kWave * kPerLane;          // tokens of a chunk
+constexpr int kSub = kWave * kPerLane;            // tokens of a wave's loads
+constexpr int kChunk = 2 * kSub;                  // and of a chunk
 constexpr int kBins = 1024;
 constexpr int kList = 8192;                       // tokens of a row's list
-constexpr int kPartList = 1536;                   // of a part's (launch 3: four blocks a compute unit)
+constexpr int kPartList = 1280;                   // of a part's (launch 3: four blocks a compute unit)
 constexpr int kRanked = 128;                      // of a list that is ranked at once: eight lanes a token
 constexpr int kMaxParts = 64;                     // of a row
 constexpr int64_t kMaxRows = 512;                 // of a launch
@@ -54,6 +56,7 @@ constexpr int kSteps = 32;                        // of a halving of the weight:
 constexpr double kLog2e = 1.4426950408889634;
 constexpr double kLn2 = 0.6931471805599453;
 constexpr double kFar = 64.0 * kSteps;            // a z from which on a weight is 0
+constexpr double kWhole = 6755399441055744.0;     // 1.5 * 2^52: numbers about it are whole
 static_assert(kBins == kRowThreads, "a bin a thread");
 
 struct Part {            // of a row's logits
@@ -90,8 +93,10 @@ struct Params {
     int chunks;          // of a row
     int parts;           // of a row, and their chunks
     int part_chunks;
+    int weight_chunks;   // of a block of launch 2
     int bits;            // behind the weights' point
     int width;           // bits of an index
+    bool list;           // a row may have a filter: launch 3
 };
 
 size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
@@ -168,6 +173,7 @@ __device__ __forceinline__ V wave_one(V x, Op op) {
 // What one row asks for.
 struct Ask {
     double heat;         // steps of z a unit of logit
+    double cool;         // and units of logit a step
     int k;               // 0: off
     float p;
     float floor;         // min-p
@@ -186,7 +192,9 @@ __device__ __forceinline__ Ask ask_of(const SampleArgs& a, int64_t t) {
               q.floor >= 0.0f && q.floor <= 1.0f && q.u >= 0.0f && q.u < 1.0f;
     // temperature 0: the first of the largest logits
     if (temperature == 0.0f) q.k = 1;
-    q.heat = kSteps * kLog2e / (temperature == 0.0f ? 1.0 : (double)temperature);
+    const double by = temperature == 0.0f ? 1.0 : (double)temperature;
+    q.heat = kSteps * kLog2e / by;
+    q.cool = by * (1.0 / (kSteps * kLog2e));
     q.far = q.floor > 0.0f ? -kSteps * log2((double)q.floor) : 1e300;
     return q;
 }
@@ -195,7 +203,9 @@ __device__ __forceinline__ Ask ask_of(const SampleArgs& a, int64_t t) {
 struct Row {
     Ask ask;
     double top;
-    double scale;        // bins a step of z
+    double reach;        // logits further below the largest count as this far
+    double none;         // and from here on have no weight
+    double scale;        // bins a unit of logit
     int some;
     bool fine;           // there is something to draw from
 };
@@ -214,8 +224,10 @@ __device__ __forceinline__ Row row_of(const Params& p, int64_t t, const Part& q)
     x.some = __builtin_amdgcn_readfirstlane(q.some);
     x.fine = __builtin_amdgcn_readfirstlane(x.ask.right && !q.bad && q.some > 0);
     x.top = uniform(q.top);
-    const double span = fmin(((double)q.top - (double)q.low) * x.ask.heat, (p.bits + 1.0) * kSteps);
-    x.scale = uniform(x.fine && span > 0.0 ? kBins / span : 0.0);
+    x.reach = uniform(kFar * x.ask.cool);
+    x.none = uniform((p.bits + 1.0) * kSteps * x.ask.cool);
+    const double span = fmin((double)q.top - (double)q.low, x.none);
+    x.scale = uniform(x.fine && span > 0.0 ? kBins * (1.0 - 0x1p-20) / span : 0.0);
     return x;
 }
 __device__ __forceinline__ Part join(const Part& a, const Part& b) {
@@ -249,33 +261,38 @@ __device__ __forceinline__ Row row_at(const Params& p, int64_t t, int r) {
     static_assert(kMaxParts == kWave, "a part a lane");
     return row_of(p, t, wave_join(c < p.parts ? p.s.parts[(int64_t)r * kMaxParts + c] : Part{-kInf, kInf, 0, 0}));
 }
-__device__ __forceinline__ double z_of(const Row& x, float l) { return fmin((x.top - (double)l) * x.ask.heat, kFar); }
-__device__ __forceinline__ int bin_of(const Row& x, double z) { return min(kBins - 1, (int)(z * x.scale)); }
+// How far a logit is below the largest, z times a step, and whether min-p keeps it.
+__device__ __forceinline__ double gap_of(const Row& x, float l) { return fmin(x.top - (double)l, x.reach); }
+__device__ __forceinline__ bool near_of(const Row& x, float l) { return (x.top - (double)l) * x.ask.heat <= x.ask.far; }
+// (up to a gap that has a weight the bins are 0 .. kBins - 1 by the scale alone)
+__device__ __forceinline__ int bin_of(const Row& x, double gap) { return min(kBins - 1, (int)(gap * x.scale)); }
 
-// 2^-(z / kSteps) in fixed point.  With n the nearest whole step it is the table's
-// 2^(bits - (n mod kSteps) / kSteps), times a power of two, times e^y, |y| <= ln 2 / 64, whose
-// series' terms from the 7th on are below 2^-58.  Adding 2^52 leaves the integer in the
-// low bits of the fp64 number, rounded to nearest.
-__device__ __forceinline__ u64 weight_of(double z, const double* table) {
-    const double n = rint(z);
-    const double y = (n - z) * (kLn2 / kSteps);
-    double e = 1.0 / 720.0;
-    e = fma(e, y, 1.0 / 120.0);
-    e = fma(e, y, 1.0 / 24.0);
-    e = fma(e, y, 1.0 / 6.0);
-    e = fma(e, y, 0.5);
+// 2^(-z / kSteps) in fixed point, z = gap heat.  With n the whole number of steps nearest -z, in
+// the low bits of a sum with 1.5 * 2^52, it is the table's 2^(bits + (n mod kSteps) / kSteps), times a
+// power of two, times e^(c y) with y = -z - n, |y| <= 1/2, c = ln 2 / 32, whose series' terms
+// from the 7th on are below 2^-58.  Adding 2^52 leaves the integer in the low bits of the
+// fp64 number, rounded to nearest.  (A table of 256 saves two terms, but its reads meet in the
+// LDS banks; 32 numbers of 8 bytes lie in one each.)
+__device__ __forceinline__ u64 weight_of(const Row& x, double gap, const double* table) {
+    constexpr double c = kLn2 / kSteps;
+    const double t = fma(gap, -x.ask.heat, kWhole);
+    const double y = fma(gap, -x.ask.heat, kWhole - t);
+    double e = c * c * c * c * c * c / 720.0;
+    e = fma(e, y, c * c * c * c * c / 120.0);
+    e = fma(e, y, c * c * c * c / 24.0);
+    e = fma(e, y, c * c * c / 6.0);
+    e = fma(e, y, c * c / 2.0);
+    e = fma(e, y, c);
     e = fma(e, y, 1.0);
-    e = fma(e, y, 1.0);
-    // the table's exponent less the whole halvings, k / kSteps of them
-    const uint32_t k = (uint32_t)n;
-    u64 two = (u64)__double_as_longlong(table[k & (kSteps - 1)]);
-    two -= (u64)(k << 15 & 0xFFF00000u) << 32;
+    const uint32_t n = (uint32_t)(u64)__double_as_longlong(t);
+    u64 two = (u64)__double_as_longlong(table[n & (kSteps - 1)]);
+    two += (u64)((n & ~(kSteps - 1u)) << 15) << 32;
     const double v = fma(e, __longlong_as_double((long long)two), 4503599627370496.0);
     return (u64)__double_as_longlong(v) & 0xFFFFFFFFFFFFFull;
 }
 static_assert(kSteps == 32, "a shift by 20 - 5");
 __device__ __forceinline__ void fill_table(double* table, int bits) {
-    if (threadIdx.x < kSteps) table[threadIdx.x] = exp2(bits - threadIdx.x * (1.0 / kSteps));
+    if (threadIdx.x < kSteps) table[threadIdx.x] = exp2(bits + threadIdx.x * (1.0 / kSteps));
 }
 
 // Place of a token in falling order: its logit, turned so that larger ones have
@@ -451,9 +468,9 @@ __device__ __forceinline__ void no_token(const SampleArgs& a, int64_t t) {
     if (a.logp) a.logp[t] = __uint_as_float(0x7FC00000u);
     if (a.kept) a.kept[t] = 0;
 }
-__device__ __forceinline__ void token(const Params& p, int64_t t, int64_t i, double z, u64 all, int kept) {
+__device__ __forceinline__ void token(const Params& p, const Row& x, int64_t t, int64_t i, float l, u64 all, int kept) {
     p.a.ids[t] = i;
-    if (p.a.logp) p.a.logp[t] = (float)((p.bits - z / kSteps) * kLn2 - log((double)all));
+    if (p.a.logp) p.a.logp[t] = (float)((p.bits - gap_of(x, l) * x.ask.heat / kSteps) * kLn2 - log((double)all));
     if (p.a.kept) p.a.kept[t] = kept;
 }
 
@@ -485,11 +502,10 @@ __global__ __launch_bounds__(kRowThreads) void ember_sample_row(Params p, int64_
     int near = 0;
 #pragma unroll
     for (int e = 0; e < kPerLane; ++e) {
-        const double z = z_of(row, x[e]);
-        w[e] = weight_of(z, table);
+        w[e] = weight_of(row, gap_of(row, x[e]), table);
         all += w[e];
         mask |= (uint32_t)(w[e] != 0) << e;
-        near += x[e] != -kInf && z <= row.ask.far;
+        near += x[e] != -kInf && near_of(row, x[e]);
     }
     all = block_sum<kRowThreads>(all, s.red);
     int kept = row.some;
@@ -518,7 +534,7 @@ __global__ __launch_bounds__(kRowThreads) void ember_sample_row(Params p, int64_
     if (row.ask.floor > 0.0f) {
         kept = min(kept, block_sum<kRowThreads>(near, s.redi));
 #pragma unroll
-        for (int e = 0; e < kPerLane; ++e) mask &= ~((uint32_t)(z_of(row, x[e]) > row.ask.far) << e);
+        for (int e = 0; e < kPerLane; ++e) mask &= ~((uint32_t)!near_of(row, x[e]) << e);
     }
     // running sums by index
     u64 sum = 0, total;
@@ -530,7 +546,7 @@ __global__ __launch_bounds__(kRowThreads) void ember_sample_row(Params p, int64_
     for (int e = kPerLane - 1; e >= 0; --e) {
         const u64 after = run;
         run -= mask >> e & 1 ? w[e] : 0;
-        if (run <= target && target < after) token(p, t, i0 + e, z_of(row, x[e]), all, kept);
+        if (run <= target && target < after) token(p, row, t, i0 + e, x[e], all, kept);
     }
 }
 
@@ -538,18 +554,19 @@ __global__ __launch_bounds__(kRowThreads) void ember_sample_row(Params p, int64_
 // launches 1 to 3 of longer rows: part blockIdx.x of row blockIdx.y
 // ---------------------------------------------------------------------------
 
-// A wave's chunks from j on, every kWavesB-th: f(chunk, this lane's logits), with the next
-// chunk's loads ahead.
-template <typename T, typename F>
-__device__ __forceinline__ void each_chunk(const T* l, int64_t V, int j, int end, F f) {
-    const int lane = threadIdx.x & (kWave - 1);
+// A wave's chunks from j on, every kWavesB-th: f(this lane's logits) for both of its halves, with
+// the next loads ahead, then g(chunk).
+template <typename T, typename F, typename G>
+__device__ __forceinline__ void each_chunk(const T* l, int64_t V, int j, int end, F f, G g) {
+    const int at = threadIdx.x % kWave * kPerLane;
     float x[kPerLane], y[kPerLane];
-    if (j < end) load8(l, (int64_t)j * kChunk + lane * kPerLane, V, x);
+    if (j < end) load8(l, (int64_t)j * kChunk + at, V, x);
     for (; j < end; j += kWavesB) {
-        if (j + kWavesB < end) load8(l, (int64_t)(j + kWavesB) * kChunk + lane * kPerLane, V, y);
-        f(j, x);
-#pragma unroll
-        for (int e = 0; e < kPerLane; ++e) x[e] = y[e];
+        load8(l, (int64_t)j * kChunk + kSub + at, V, y);
+        f(x);
+        if (j + kWavesB < end) load8(l, (int64_t)(j + kWavesB) * kChunk + at, V, x);
+        f(y);
+        g(j);
     }
 }
 
@@ -573,10 +590,22 @@ __global__ __launch_bounds__(kThreads) void ember_sample_range(Params p, int64_t
     }
     Part part{-kInf, kInf, 0, 0};
     const int end = min((c + 1) * p.part_chunks, p.chunks);
-    each_chunk(l, p.a.V, c * p.part_chunks + wave, end, [&](int, const float (&x)[kPerLane]) {
+    float peak = -kInf;
+    each_chunk(
+        l, p.a.V, c * p.part_chunks + wave, end,
+        [&](const float (&x)[kPerLane]) {
 #pragma unroll
-        for (int e = 0; e < kPerLane; ++e) see(part, x[e]);
-    });
+            for (int e = 0; e < kPerLane; ++e) {
+                see(part, x[e]);
+                peak = fmaxf(peak, x[e]);
+            }
+        },
+        [&](int j) {
+            if (!p.list) return;
+            peak = wave_one(peak, [](float a, float b) { return fmaxf(a, b); });
+            if (threadIdx.x % kWave == 0) p.s.peak[(int64_t)r * p.chunks + j] = peak;
+            peak = -kInf;
+        });
     part = block_join<kThreads>(part, redp);
     if (threadIdx.x == 0) p.s.parts[(int64_t)r * kMaxParts + c] = part;
 }
@@ -602,38 +631,44 @@ __global__ __launch_bounds__(kThreads) void ember_sample_weights(Params p, int64
         }
     }
     __syncthreads();
-    u64 all = 0;
+    u64 all = 0, sum = 0;
     int near = 0;
-    const int end = min((c + 1) * p.part_chunks, p.chunks);
-    each_chunk(l, p.a.V, c * p.part_chunks + wave, end, [&](int j, const float (&x)[kPerLane]) {
-        u64 sum = 0;
+    const int end = min((c + 1) * p.weight_chunks, p.chunks);
+    each_chunk(
+        l, p.a.V, c * p.weight_chunks + wave, end,
+        [&](const float (&x)[kPerLane]) {
+            u64 w[kPerLane];
+            int b[kPerLane];
 #pragma unroll
-        for (int e = 0; e < kPerLane; ++e) {
-            const double z = z_of(row, x[e]);
-            const u64 w = weight_of(z, table);
-            sum += w;
-            if (hist && w) {
-                const int b = bin_of(row, z);
-                atomicAdd(&weight[b], w);
-                atomicAdd(&count[b], 1);
+            for (int e = 0; e < kPerLane; ++e) {
+                const double gap = gap_of(row, x[e]);
+                w[e] = weight_of(row, gap, table);
+                b[e] = (int)(gap * row.scale);
+                sum += w[e];
             }
-        }
-        if (floored) {
+            if (hist) {
 #pragma unroll
-            for (int e = 0; e < kPerLane; ++e) near += x[e] != -kInf && z_of(row, x[e]) <= row.ask.far;
-        }
-        sum = wave_sum(sum);
-        float peak = x[0];
+                for (int e = 0; e < kPerLane; ++e) {
+                    if (!w[e]) continue;
+                    atomicAdd(&weight[b[e]], w[e]);
+                    atomicAdd(&count[b[e]], 1);
+                }
+            }
+            if (floored) {
 #pragma unroll
-        for (int e = 1; e < kPerLane; ++e) peak = fmaxf(peak, x[e]);
-        peak = wave_one(peak, [](float a, float b) { return fmaxf(a, b); });
-        if (lane == 0) {
-            p.s.chunk[(int64_t)r * p.chunks + j] = sum;
-            p.s.peak[(int64_t)r * p.chunks + j] = peak;
-        }
-        all += sum;
-    });
-    all = block_sum<kThreads>(lane == 0 ? all : 0, red);
+                for (int e = 0; e < kPerLane; ++e) near += x[e] != -kInf && near_of(row, x[e]);
+            }
+        },
+        [&](int j) {
+            if (hist || floored) return;      // launch 3 does it
+            sum = wave_sum(sum);
+            if (lane == 0) {
+                p.s.chunk[(int64_t)r * p.chunks + j] = sum;
+                all += sum;
+            }
+            sum = 0;
+        });
+    all = block_sum<kThreads>(all + sum, red);
     near = block_sum<kThreads>(near, redi);
     if (threadIdx.x == 0) {
         atomicAdd(&p.s.rows[r].all, all);
@@ -649,33 +684,14 @@ __global__ __launch_bounds__(kThreads) void ember_sample_weights(Params p, int64
     }
 }
 
-// The smallest logit for which `is` holds, where it holds for the larger ones of two
-// and for the row's largest: 64 candidates at a time, one a lane.
-template <typename F>
-__device__ __forceinline__ float smallest(float top, F is) {
-    const int lane = threadIdx.x & (kWave - 1);
-    uint32_t lo = fall_of(top), hi = 0xFF7FFFFFu;      // is(lo) holds; the lowest finite logit
-    while (lo < hi) {
-        const uint32_t step = (hi - lo + kWave - 1) / kWave;
-        const uint32_t f = (uint32_t)min((u64)hi, (u64)lo + (u64)step * (lane + 1));
-        const int n = __popcll(__ballot(is(logit_of_fall(f))));      // the first n candidates hold
-        const uint32_t last = n ? (uint32_t)min((u64)hi, (u64)lo + (u64)step * n) : lo;
-        hi = n == kWave ? hi : (uint32_t)min((u64)hi, (u64)lo + (u64)step * (n + 1)) - 1;
-        lo = last;
-        if (n == kWave) break;
-    }
-    return logit_of_fall(lo);
-}
-
 template <typename T>
-__global__ __launch_bounds__(kThreads) void ember_sample_list(Params p, int64_t t0) {
+__global__ __launch_bounds__(kThreads, 8) void ember_sample_list(Params p, int64_t t0) {
     __shared__ double table[kSteps];
     __shared__ u64 red[kWavesB];
     __shared__ int redi[kWavesB];
     __shared__ RowState found;
-    __shared__ float edge[7];
-    __shared__ float dense[kWavesB][kChunk];
-    __shared__ uint16_t index[kWavesB][kChunk];
+    __shared__ float dense[kWavesB][kSub + kWave];
+    __shared__ uint16_t index[kWavesB][kSub + kWave];
     __shared__ u64 list[kPartList];
     __shared__ int listed;
     __shared__ unsigned joined;
@@ -750,17 +766,6 @@ __global__ __launch_bounds__(kThreads) void ember_sample_list(Params p, int64_t 
     __syncthreads();
     const int bin_k = found.bin_k, bin_p = found.bin_p, bin_p1 = found.bin_p1;
     const int sure = min(bin_k, bin_p);
-    // the bins' edges as logits: the smallest one before a bin
-    if (wave < 7) {
-        const int b = wave == 0 ? sure : wave == 1 ? bin_k : wave == 2 ? bin_k + 1 : wave == 3 ? bin_p : bin_p1 + 1;
-        // (bin 0: none, past the largest)
-        // (5, 6: the smallest that min-p keeps, and one below which there is no weight)
-        const double far = wave == 5 ? row.ask.far : (p.bits + 1.0) * kSteps + 1.0;
-        const float at = wave >= 5 ? smallest((float)row.top, [&](float x) { return z_of(row, x) <= far; })
-                         : b <= 0  ? kInf
-                                   : smallest((float)row.top, [&](float x) { return bin_of(row, z_of(row, x)) < b; });
-        if (lane == 0) edge[wave] = at;
-    }
     RowState& s = p.s.rows[r];
     if (c == 0 && threadIdx.x == 0) {
         s.w_k = found.w_k;
@@ -773,11 +778,15 @@ __global__ __launch_bounds__(kThreads) void ember_sample_list(Params p, int64_t 
         s.sure = sure;
     }
     __syncthreads();
-    const float from = fmaxf(edge[0], edge[5]);                // kept for certain: from this logit on
-    const float k0 = edge[1], k1 = bin_k < kBins ? fmaxf(edge[2], edge[6]) : kInf;      // listed: [k1, k0) and [p1, p0)
-    const float p0 = edge[3], p1 = bin_p < kBins ? fmaxf(edge[4], edge[6]) : kInf;
+    // A logit below which nothing counts, with a margin for its rounding: whether a token counts
+    // its bin says.
+    const auto gap_to = [&](int b) { return row.scale > 0.0 ? b / row.scale : row.none; };
+    double gap = fmin(gap_to(sure), row.ask.far * row.ask.cool);
+    if (bin_k < kBins) gap = fmax(gap, gap_to(bin_k + 1));
+    if (bin_p < kBins) gap = fmax(gap, gap_to(bin_p1 + 1));
+    float least = (float)(row.top - fmin(gap, row.none));
+    least = fmaxf(least - fabsf(least) * 0x1p-22f - 1e-37f, -3.4028235e38f);
     const int end = min((c + 1) * p.part_chunks, p.chunks);
-    const float least = fminf(from, fminf(k1, p1));            // below it nothing counts
     // A wave's chunks, every kWavesB-th, 64 at a time; those with a logit that counts are
     // gone through: their tokens that count side by side in LDS, then a token a lane.
     for (int j0 = c * p.part_chunks + wave; j0 < end; j0 += kWavesB * kWave) {
@@ -786,44 +795,56 @@ __global__ __launch_bounds__(kThreads) void ember_sample_list(Params p, int64_t 
         const bool some = mine < end && p.s.peak[at] >= least;
         if (mine < end && !some) p.s.chunk[at] = 0;
         u64 todo = __ballot(some);
-        float x[kPerLane], y[kPerLane];
         auto chunk_of = [&](u64 m) { return j0 + (__ffsll(m) - 1) * kWavesB; };
-        if (todo) load8(l, (int64_t)chunk_of(todo) * kChunk + lane * kPerLane, p.a.V, x);
-        while (todo) {
-            const int j = chunk_of(todo);
-            todo &= todo - 1;
-            if (todo) load8(l, (int64_t)chunk_of(todo) * kChunk + lane * kPerLane, p.a.V, y);
-            int n = 0;
-#pragma unroll
-            for (int e = 0; e < kPerLane; ++e) n += x[e] >= least;
-            int put = wave_scan(n);
-            const int total = last_lane(put);
-            put -= n;
+        u64 sum = 0;
+        int n = 0, j = 0;
+        // a half's tokens that count join the n there are
+        auto put = [&](const float (&x)[kPerLane], int first) {
 #pragma unroll
             for (int e = 0; e < kPerLane; ++e) {
+                const u64 m = __ballot(x[e] >= least);
                 if (x[e] >= least) {
-                    dense[wave][put] = x[e];
-                    index[wave][put++] = (uint16_t)(lane * kPerLane + e);
+                    const int to = n + __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0));
+                    dense[wave][to] = x[e];
+                    index[wave][to] = (uint16_t)(first + lane * kPerLane + e);
                 }
+                n += __popcll(m);
             }
+        };
+        auto take = [&] {
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
-            u64 sum = 0;
-            for (int q = lane; q < total; q += kWave) {
+            for (int q = lane; q < n; q += kWave) {
                 const float v = dense[wave][q];
-                if (v >= from) {
-                    sum += weight_of(z_of(row, v), table);
-                } else if ((v >= k1 && v < k0) || (v >= p1 && v < p0)) {
+                const double gap = gap_of(row, v);
+                const int b = bin_of(row, gap);
+                const u64 w = weight_of(row, gap, table);
+                if (b < sure) {
+                    sum += near_of(row, v) ? w : 0;
+                } else if (w && (b == bin_k || (b >= bin_p && b <= bin_p1))) {
                     const int to = atomicAdd(&listed, 1);
                     if (to < kPartList) list[to] = place_of<T>(v, (uint32_t)(j * kChunk + index[wave][q]), p.width);
                 }
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
+            n = 0;
+        };
+        float x[kPerLane], y[kPerLane];
+        const int own = lane * kPerLane;
+        if (todo) load8(l, (int64_t)chunk_of(todo) * kChunk + own, p.a.V, x);
+        while (todo) {
+            j = chunk_of(todo);
+            todo &= todo - 1;
+            load8(l, (int64_t)j * kChunk + kSub + own, p.a.V, y);
+            put(x, 0);
+            if (todo) load8(l, (int64_t)chunk_of(todo) * kChunk + own, p.a.V, x);
+            if (n > kWave) take();
+            put(y, kSub);
+            take();
             sum = wave_sum(sum);
             if (lane == 0) p.s.chunk[(int64_t)r * p.chunks + j] = sum;
-#pragma unroll
-            for (int e = 0; e < kPerLane; ++e) x[e] = y[e];
+            sum = 0;
         }
     }
     // the block's list joins the row's
@@ -897,31 +918,31 @@ __global__ __launch_bounds__(kRowThreads) void ember_sample_draw(Params p, int64
                     load8(l, i, p.a.V, x);
 #pragma unroll
                     for (int e = 0; e < kPerLane; ++e) {
-                        const double z = z_of(row, x[e]);
-                        const int b = bin_of(row, z);
+                        const double gap = gap_of(row, x[e]);
+                        const int b = bin_of(row, gap);
                         if (b < first || b > last) continue;
-                        const u64 w = weight_of(z, table);
+                        const u64 w = weight_of(row, gap, table);
                         if (w) f(place_of<T>(x[e], (uint32_t)(i + e), p.width), [&] { return w; });
                     }
                 }
             };
             find_ends(each);
             each(sure, kBins - 1, [&](u64 at, auto weight) {
-                if (at <= last && z_of(row, logit_of<T>(at, p.width)) <= row.ask.far)
+                if (at <= last && near_of(row, logit_of<T>(at, p.width)))
                     atomicAdd(&more[(uint32_t)(at & (((u64)1 << p.width) - 1)) / (kChunk * own)], weight());
             });
         } else if (n > 0 && n <= kRanked) {
             // eight lanes an entry: its rank and the weights before it, from all entries in LDS
             // (entries without a weight do not count)
             if ((int)threadIdx.x < n) {
-                const u64 x = weight_of(z_of(row, logit_of<T>(first, p.width)), table);
+                const u64 x = weight_of(row, gap_of(row, logit_of<T>(first, p.width)), table);
                 s.weight[threadIdx.x] = x;
                 s.place[threadIdx.x] = x ? first : kNone;
             }
             __syncthreads();
             const int e = threadIdx.x / 8;
             u64 at = e < n ? s.place[e] : kNone, w = e < n ? s.weight[e] : 0, before = 0;
-            const int bin = at != kNone ? bin_of(row, z_of(row, logit_of<T>(at, p.width))) : kBins;
+            const int bin = at != kNone ? bin_of(row, gap_of(row, logit_of<T>(at, p.width))) : kBins;
             int rank = 0;
             for (int q = threadIdx.x % 8; q < n; q += 8) {
                 const bool less = s.place[q] < at;
@@ -950,7 +971,7 @@ __global__ __launch_bounds__(kRowThreads) void ember_sample_draw(Params p, int64
             if (threadIdx.x == 0) s.hi = 0;
             __syncthreads();
             if ((threadIdx.x & (kWave - 1)) == 0 && end) atomicMax(&s.hi, end);
-            if (mine && z_of(row, logit_of<T>(at, p.width)) <= row.ask.far)
+            if (mine && near_of(row, logit_of<T>(at, p.width)))
                 atomicAdd(&more[(uint32_t)(at & (((u64)1 << p.width) - 1)) / (kChunk * own)], w);
             __syncthreads();
             last = s.hi;
@@ -968,9 +989,9 @@ __global__ __launch_bounds__(kRowThreads) void ember_sample_draw(Params p, int64
                 const int i = q * kRowThreads + threadIdx.x;
                 if (i >= n) continue;
                 at[q] = q == 0 ? first : p.s.list[(int64_t)r * kList + i];
-                const double z = z_of(row, logit(q));
-                w[q] = weight_of(z, table);
-                if (w[q]) bin[q] = bin_of(row, z);
+                const double gap = gap_of(row, logit(q));
+                w[q] = weight_of(row, gap, table);
+                if (w[q]) bin[q] = bin_of(row, gap);
                 else at[q] = kNone;
             }
             find_ends([&](int first, int last, auto f) {
@@ -981,7 +1002,7 @@ __global__ __launch_bounds__(kRowThreads) void ember_sample_draw(Params p, int64
             // the kept ones join their chunks' sums
 #pragma unroll
             for (int q = 0; q < kOwn; ++q) {
-                if (at[q] <= last && z_of(row, logit(q)) <= row.ask.far)
+                if (at[q] <= last && near_of(row, logit(q)))
                     atomicAdd(&more[(uint32_t)(at[q] & (((u64)1 << p.width) - 1)) / (kChunk * own)], w[q]);
             }
         }
@@ -1009,27 +1030,27 @@ __global__ __launch_bounds__(kRowThreads) void ember_sample_draw(Params p, int64
     u64 before = s.w;
     for (int q = 0; q < own * kChunk; q += kRowThreads, i += kRowThreads) {
         u64 w = 0;
-        double z = 0.0;
+        float x = 0.0f;
         if (q + (int)threadIdx.x < own * kChunk && i < p.a.V) {
-            const float x = load_elem(l, i, sizeof(T) == 2);
-            z = z_of(row, x);
-            const bool keep = bin_of(row, z) < sure || place_of<T>(x, (uint32_t)i, p.width) <= last;
-            if (keep && z <= row.ask.far) w = weight_of(z, table);
+            x = load_elem(l, i, sizeof(T) == 2);
+            const double gap = gap_of(row, x);
+            const bool keep = bin_of(row, gap) < sure || place_of<T>(x, (uint32_t)i, p.width) <= last;
+            if (keep && near_of(row, x)) w = weight_of(row, gap, table);
         }
         u64 piece;
         const u64 to = before + block_scan<kRowThreads>(w, s.red, piece);
-        if (to - w <= target && target < to) token(p, t, i, z, all, kept);
+        if (to - w <= target && target < to) token(p, row, t, i, x, all, kept);
         before += piece;
         if (target < before) break;
     }
 }
 
 template <typename T>
-hipError_t launch(const Params& p, int64_t t0, int rows, bool list, hipStream_t s) {
+hipError_t launch(const Params& p, int64_t t0, int rows, hipStream_t s) {
     const dim3 grid((unsigned)p.parts, (unsigned)rows);
     ember_sample_range<T><<<grid, kThreads, 0, s>>>(p, t0);
-    ember_sample_weights<T><<<grid, kThreads, 0, s>>>(p, t0);
-    if (list) ember_sample_list<T><<<grid, kThreads, 0, s>>>(p, t0);
+    ember_sample_weights<T><<<dim3((unsigned)((p.chunks + p.weight_chunks - 1) / p.weight_chunks), (unsigned)rows), kThreads, 0, s>>>(p, t0);
+    if (p.list) ember_sample_list<T><<<grid, kThreads, 0, s>>>(p, t0);
     ember_sample_draw<T><<<rows, kRowThreads, 0, s>>>(p, t0);
     return hipGetLastError();
 }
@@ -1058,14 +1079,18 @@ hipError_t launch_sample(const SampleArgs& a, hipStream_t s) {
     const int64_t rows = std::min(a.T, kMaxRows);
     space_of(a.ws, rows, a.V, &p.s);
     p.chunks = (int)chunks_of(a.V);
-    // about 1024 blocks, of two chunks a wave at least
-    const int64_t want = std::min<int64_t>({(1024 + rows - 1) / rows, (p.chunks + 2 * kWavesB - 1) / (2 * kWavesB), kMaxParts});
-    p.part_chunks = (int)((p.chunks + want - 1) / want);
+    // about 1024 blocks (launch 2: 512, which are there at once), of a chunk a wave at least
+    const auto chunks_a_block = [&](int64_t blocks) {
+        const int64_t n = std::min<int64_t>({(blocks + rows - 1) / rows, (p.chunks + kWavesB - 1) / kWavesB, kMaxParts});
+        return (int)((p.chunks + n - 1) / n);
+    };
+    p.part_chunks = chunks_a_block(1024);
+    p.weight_chunks = chunks_a_block(512);
     p.parts = (p.chunks + p.part_chunks - 1) / p.part_chunks;
-    const bool list = a.top_k || a.top_p || a.min_p || a.temperature;
+    p.list = a.top_k || a.top_p || a.min_p || a.temperature;
     for (int64_t t0 = 0; t0 < a.T; t0 += kMaxRows) {
         const int n = (int)std::min(kMaxRows, a.T - t0);
-        const hipError_t e = a.l_dtype == EMBER_F32 ? launch<float>(p, t0, n, list, s) : launch<uint16_t>(p, t0, n, list, s);
+        const hipError_t e = a.l_dtype == EMBER_F32 ? launch<float>(p, t0, n, s) : launch<uint16_t>(p, t0, n, s);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;

@@ -271,6 +271,15 @@ def test_few_values(em, dtype):
     check(em, L, u, k=k, p=p)
 
 
+@pytest.mark.parametrize("V", [1000, 30000])
+def test_tiny_min_p(em, V):
+    """Tokens that min-p keeps although their weights round to nothing count as kept."""
+    L, u = zipf(6, V, F, 4)
+    L.copy_(-300 * torch.rand(6, V, generator=gen(6), device=DEV))
+    check(em, L, u, floor=[1e-30, 1e-20, 1e-38, 1e-10, 1e-44, 1.0])
+    check(em, L, u, floor=[1e-30] * 6, k=[0, 3, 2 ** 31 - 1, V // 2, 500, 1], temperature=[0.5, 1.0, 2.0, 3.0, 0.0, 1.0])
+
+
 def test_row_alone_and_among_others(em):
     """A row's token depends on the row alone, in how many parts it may be worked on."""
     L, u = zipf(300, 40000, F, 8)
