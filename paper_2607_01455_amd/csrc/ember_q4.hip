@@ -579,7 +579,7 @@ struct Tile4Params {
     int groups;
     int MT;
     int64_t NT;
-    int64_t tile0, tile1, per_xcd;
+    int64_t tiles, per_xcd;
     int group_m;
 };
 
@@ -602,7 +602,8 @@ struct Tile4 {
     static_assert(kStages >= 2 && kStages <= 4 && (kStages - 2) * kLoads < 64, "vmcnt range, scales of the steps ahead");
     static_assert(BN % kWave == 0 && BN / kWave <= kWaves, "the scales' loads");
     static_assert((int64_t)std::max(BM, BN) * EMBER_Q8_MAX_LD < (int64_t)1 << 31, "32-bit load offsets");
-    static_assert(kLds <= 160 * 1024, "LDS of one CU");
+    static constexpr int kBlocks = 160 * 1024 / kLds;    // a compute unit
+    static_assert(kBlocks > 0, "LDS of one CU");
 };
 
 // BM tokens x BN channels a block, a block of 128 columns a step.  A ring of LDS
@@ -621,12 +622,10 @@ __global__ __launch_bounds__(C::kThreads) void ember_logits_q4(Tile4Params p) {
     const int lane = threadIdx.x & (kWave - 1);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
-    const int64_t l = p.tile0 + (int64_t)(blockIdx.x % kXcds) * p.per_xcd + blockIdx.x / kXcds;
-    if (l >= min(p.tile0 + (int64_t)(blockIdx.x % kXcds + 1) * p.per_xcd, p.tile1)) return;
-    int tm;
-    int64_t tn;
-    tile_at(p.MT, p.NT, p.group_m, l, tm, tn);
-    const int64_t t0 = (int64_t)tm * C::BM, v0 = tn * C::BN;
+    // this block's tiles: every gridDim.x / kXcds-th of its XCD's
+    const int64_t xcd = blockIdx.x % kXcds, end = min((xcd + 1) * p.per_xcd, p.tiles);
+    int64_t l = xcd * p.per_xcd + blockIdx.x / kXcds;
+    if (l >= end) return;
     const int D = (int)a.D;
 
     const int row_x = wave * 8 + lane / 8, row_w = wave * 16 + lane / 4;
@@ -636,9 +635,17 @@ __global__ __launch_bounds__(C::kThreads) void ember_logits_q4(Tile4Params p) {
     const uint32_t off_s = row_s * (uint32_t)(2 * a.ldg);
     // all of a load's place in the offset that the buffer's range is checked against; past the
     // last step they are outside it
-    const i32x4 rx = rsrc(a.Xq + t0 * a.ldx, (a.T - t0) * a.ldx);
-    const i32x4 rw = rsrc(a.Wq + v0 * a.ldw, (a.V - v0) * a.ldw);
-    const i32x4 rs = rsrc(a.wscale + v0 * a.ldg, (a.V - v0) * a.ldg * 2);
+    int64_t t0, v0;
+    i32x4 rx, rw, rs;
+    auto go_to = [&](int64_t l) {
+        int tm;
+        int64_t tn;
+        tile_at(p.MT, p.NT, p.group_m, l, tm, tn);
+        t0 = (int64_t)tm * C::BM, v0 = tn * C::BN;
+        rx = rsrc(a.Xq + t0 * a.ldx, (a.T - t0) * a.ldx);
+        rw = rsrc(a.Wq + v0 * a.ldw, (a.V - v0) * a.ldw);
+        rs = rsrc(a.wscale + v0 * a.ldg, (a.V - v0) * a.ldg * 2);
+    };
     auto issue = [&](int kt, uint32_t st) {
         const uint32_t ox = kt * kBlockCols + k_x < D ? off_x + kt * kBlockCols : kBufferMax;
         const uint32_t ow = off_w + (kt < p.nk ? (uint32_t)kt * kBlockBytes : kBufferMax);
@@ -668,8 +675,6 @@ __global__ __launch_bounds__(C::kThreads) void ember_logits_q4(Tile4Params p) {
     for (int t = 0; t < 4; ++t) at_w[t] = ch * kBlockBytes + ((t ^ swizzle<4>(ch)) * 16);
     // (masked: the last step of a D that is not a multiple of 16, whose last chunk holds columns that do not count)
     uint32_t here[4];       // of the stage
-#pragma unroll
-    for (int w = 0; w < 4; ++w) here[w] = at_x[w];
     auto read_x = [&](int m, i32x4 (&x)[4], bool masked) {
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
@@ -705,28 +710,19 @@ __global__ __launch_bounds__(C::kThreads) void ember_logits_q4(Tile4Params p) {
     f32x16 f[C::MT];
     i32x16 sum[2], zero;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) zero[e] = sum[0][e] = sum[1][e] = 0;
-#pragma unroll
-    for (int m = 0; m < C::MT; ++m)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) f[m][e] = 0.0f;
+    for (int e = 0; e < 16; ++e) zero[e] = 0;
 
-    // for the epilogue, ahead of everything; the operands are 16 times the codes
-    const int64_t my_t = t0 + threadIdx.x, my_v = v0 + ch;
-    const float my_xs = (int)threadIdx.x < C::BM && my_t < a.T ? a.xscale[my_t] * 0.0625f : 0.0f;
-    const float bias = a.bias && my_v < a.V ? a.bias[my_v] : 0.0f;
+    // for the epilogue; the operands are 16 times the codes
     float* const xs = reinterpret_cast<float*>(lds + C::kXs);
-    if ((int)threadIdx.x < C::BM) xs[threadIdx.x] = my_xs;
-#pragma unroll
-    for (int q = 0; q < C::kStages; ++q) issue(q, q * C::kStageBytes);
-    wait_step<(C::kStages - 1) * C::kLoads>();
+    float my_xs, bias;
+    auto factors = [&] {
+        const int64_t my_t = t0 + threadIdx.x, my_v = v0 + ch;
+        my_xs = (int)threadIdx.x < C::BM && my_t < a.T ? a.xscale[my_t] * 0.0625f : 0.0f;
+        bias = a.bias && my_v < a.V ? a.bias[my_v] : 0.0f;
+    };
     i32x4 op[4], wd[4], x[2][4];
-    float scale[kPer], last = 0.0f;       // this step's, and that of the sum that is not added yet
-    read_w(0, wd);
-    read_s(0, scale);
-    read_x(0, x[0], p.nk == 1);
-    take_apart(wd, op);
-    uint32_t st = 0;
+    float scale[kPer], last;         // this step's, and that of the sum that is not added yet
+    uint32_t st;
     auto step = [&](int i, auto is_last) {
         constexpr bool kLast = decltype(is_last)::value;
         const uint32_t next = st + C::kStageBytes == C::kRing ? 0 : st + C::kStageBytes;
@@ -771,50 +767,91 @@ __global__ __launch_bounds__(C::kThreads) void ember_logits_q4(Tile4Params p) {
         take_apart(wd, op);
         st = next;
     };
-    for (int i = 0; i < p.nk - 1; ++i) step(i, std::false_type());
-    if (p.nk > 1) read_x(0, x[0], true);
-    step(p.nk - 1, std::true_type());
-#pragma unroll
-    for (int e = 0; e < 16; ++e) f[C::MT - 1][e] = fmaf((float)sum[1][e], last, f[C::MT - 1][e]);
-    wait_step<0>();    // the zero-filling loads past the end have landed, and everyone is done with the stages
-
     // A lane holds 16 tokens of a channel: through a strip of LDS of the wave's own, 32
-    // tokens x 32 channels, each token's are stored side by side.
+    // tokens x 32 channels, each token's are stored side by side.  The strips take the ring's
+    // last stages; the first of the next tile are loaded meanwhile.
     constexpr int kEs = (int)sizeof(YT), kPitch = 32 * kEs + 16, kEpc = 16 / kEs, kPerRow = 32 / kEpc;
-    static_assert(C::kWaves * 32 * kPitch <= C::kXs, "the strips");
-    uint8_t* const strip = lds + wave * (32 * kPitch);
+    constexpr int kAhead = C::kStages - (C::kWaves * 32 * kPitch + C::kStageBytes - 1) / C::kStageBytes;
+    static_assert(kAhead >= 1, "the strips");
+    uint8_t* const strip = lds + kAhead * C::kStageBytes + wave * (32 * kPitch);
     int el = lane;
-    asm volatile("" : "+v"(el));   // what follows from it is not kept in registers over the loop above
-    const int eh = el >> 5, ec = el & 31;
+    auto store = [&](int64_t t0, int64_t v0, float bias) {
+        asm volatile("" : "+v"(el));   // what follows from it is not kept in registers over the steps
+        const int eh = el >> 5, ec = el & 31;
 #pragma unroll
-    for (int m = 0; m < C::MT; ++m) {
+        for (int m = 0; m < C::MT; ++m) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const int r = 8 * (e / 4) + 4 * eh + e % 4;
-            const float y = fmaf(f[m][e], xs[32 * m + r], bias);
-            if constexpr (kEs == 4) *reinterpret_cast<float*>(strip + r * kPitch + ec * 4) = y;
-            else *reinterpret_cast<uint16_t*>(strip + r * kPitch + ec * 2) = (uint16_t)pack_bf16(y, 0.0f);
-        }
-        wave_lds_order();
+            for (int e = 0; e < 16; ++e) {
+                const int r = 8 * (e / 4) + 4 * eh + e % 4;
+                const float y = fmaf(f[m][e], xs[32 * m + r], bias);
+                if constexpr (kEs == 4) *reinterpret_cast<float*>(strip + r * kPitch + ec * 4) = y;
+                else *reinterpret_cast<uint16_t*>(strip + r * kPitch + ec * 2) = (uint16_t)pack_bf16(y, 0.0f);
+            }
+            wave_lds_order();
 #pragma unroll
-        for (int q = 0; q < 32 * kPerRow / kWave; ++q) {
-            const int r = (q * kWave + el) / kPerRow, c = el % kPerRow * kEpc;
-            const int64_t t = t0 + 32 * m + r, v = v0 + wave * 32 + c;
-            const u32x4_t y = *reinterpret_cast<const u32x4_t*>(strip + r * kPitch + c * kEs);
-            if (t >= a.T) continue;
-            YT* const to = static_cast<YT*>(a.Y) + t * a.ldy + v;
-            if (v + kEpc <= a.V) {
-                *reinterpret_cast<u32x4_t*>(to) = y;
-            } else {
+            for (int q = 0; q < 32 * kPerRow / kWave; ++q) {
+                const int r = (q * kWave + el) / kPerRow, c = el % kPerRow * kEpc;
+                const int64_t t = t0 + 32 * m + r, v = v0 + wave * 32 + c;
+                const u32x4_t y = *reinterpret_cast<const u32x4_t*>(strip + r * kPitch + c * kEs);
+                if (t >= a.T) continue;
+                YT* const to = static_cast<YT*>(a.Y) + t * a.ldy + v;
+                if (v + kEpc <= a.V) {
+                    *reinterpret_cast<u32x4_t*>(to) = y;
+                } else {
 #pragma unroll
-                for (int e = 0; e < kEpc; ++e) {
-                    if (v + e >= a.V) continue;
-                    if constexpr (kEs == 4) reinterpret_cast<uint32_t*>(to)[e] = y[e];
-                    else reinterpret_cast<uint16_t*>(to)[e] = (uint16_t)(y[e >> 1] >> (16 * (e & 1)));
+                    for (int e = 0; e < kEpc; ++e) {
+                        if (v + e >= a.V) continue;
+                        if constexpr (kEs == 4) reinterpret_cast<uint32_t*>(to)[e] = y[e];
+                        else reinterpret_cast<uint16_t*>(to)[e] = (uint16_t)(y[e >> 1] >> (16 * (e & 1)));
+                    }
                 }
             }
+            wave_lds_order();
         }
-        wave_lds_order();
+    };
+
+    go_to(l);
+    factors();
+#pragma unroll
+    for (int q = 0; q < C::kStages; ++q) issue(q, q * C::kStageBytes);
+    for (;;) {
+        if ((int)threadIdx.x < C::BM) xs[threadIdx.x] = my_xs;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sum[0][e] = sum[1][e] = 0;
+#pragma unroll
+        for (int m = 0; m < C::MT; ++m)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) f[m][e] = 0.0f;
+        last = 0.0f;
+        st = 0;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) here[w] = at_x[w];
+        wait_step<(C::kStages - 1) * C::kLoads>();
+        read_w(0, wd);
+        read_s(0, scale);
+        read_x(0, x[0], p.nk == 1);
+        take_apart(wd, op);
+        for (int i = 0; i < p.nk - 1; ++i) step(i, std::false_type());
+        if (p.nk > 1) read_x(0, x[0], true);
+        step(p.nk - 1, std::true_type());
+#pragma unroll
+        for (int e = 0; e < 16; ++e) f[C::MT - 1][e] = fmaf((float)sum[1][e], last, f[C::MT - 1][e]);
+        wait_step<0>();    // the zero-filling loads past the end have landed, and everyone is done with the stages
+        const int64_t t_done = t0, v_done = v0;
+        const float bias_done = bias;
+        l += gridDim.x / kXcds;
+        const bool more = l < end;
+        if (more) {
+            go_to(l);
+            factors();
+#pragma unroll
+            for (int q = 0; q < kAhead; ++q) issue(q, q * C::kStageBytes);
+        }
+        store(t_done, v_done, bias_done);
+        if (!more) return;
+        wait_step<63>();   // everyone is done with the strips and xs (no load is waited for)
+#pragma unroll
+        for (int q = kAhead; q < C::kStages; ++q) issue(q, q * C::kStageBytes);
     }
 }
 
@@ -871,18 +908,16 @@ hipError_t launch_tiles(const Logits4Args& a, hipStream_t s) {
     p.MT = (int)((a.T + C::BM - 1) / C::BM);
     p.NT = (a.V + C::BN - 1) / C::BN;
     p.group_m = 4;
-    const int64_t total = (int64_t)p.MT * p.NT;
-    for (int64_t t0 = 0; t0 < total; t0 += kMaxGridBlocks) {
-        p.tile0 = t0;
-        p.tile1 = std::min(t0 + kMaxGridBlocks, total);
-        p.per_xcd = (p.tile1 - t0 + kXcds - 1) / kXcds;
-        const unsigned grid = (unsigned)(p.per_xcd * kXcds);
-        if (a.y_dtype == EMBER_F32) launch_tile<C, G, float>(p, grid, s);
-        else launch_tile<C, G, uint16_t>(p, grid, s);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    }
-    return hipSuccess;
+    p.tiles = (int64_t)p.MT * p.NT;
+    p.per_xcd = (p.tiles + kXcds - 1) / kXcds;
+    // The blocks that are there at once go through the tiles, so that the next one's first loads are
+    // out while one is stored (1024 x 131072: 721 us at D = 4096 and 239 at 1024; a tile a block 764
+    // and 251); of few steps, with nothing to hide the stores behind, a tile a block (168 at 512; 181).
+    const int64_t blocks = p.nk < 6 ? kMaxGridBlocks : kCus * C::kBlocks;
+    const unsigned grid = (unsigned)(std::min<int64_t>(p.per_xcd, blocks / kXcds) * kXcds);
+    if (a.y_dtype == EMBER_F32) launch_tile<C, G, float>(p, grid, s);
+    else launch_tile<C, G, uint16_t>(p, grid, s);
+    return hipGetLastError();
 }
 
 using T128x256 = Tile4<128, 8, 4>;
