@@ -923,24 +923,23 @@ hipError_t launch_tiles(const Logits4Args& a, hipStream_t s) {
 using T128x256 = Tile4<128, 8, 4>;
 using T64x128 = Tile4<64, 4, 3>;       // two a compute unit
 
-// What a launch of a tiling takes, in us: rounds of the chip's compute units, each of D
-// / 128 steps (fitted to 1024 x 128256 x 4096, 512 x 32000 x 4096, 256 x 128256 x 4096 and
-// 1024 x 32000 x 2048; times by group size).
-template <typename C, int G>
-double tiles_us(const Logits4Args& a) {
-    constexpr bool kLarge = C::BN == 256;
-    constexpr double kStep = kLarge ? (G == 128 ? 1.55 : G == 64 ? 2.1 : 2.8) : (G == 128 ? 0.65 : G == 64 ? 0.8 : 1.3);
-    const double tiles = (double)((a.T + C::BM - 1) / C::BM) * (double)((a.V + C::BN - 1) / C::BN) / kCus;
-    // the small tiling: the second block of a compute unit costs 0.6 of the first
-    const double rounds = kLarge ? std::ceil(tiles) : 0.8 * std::ceil(tiles) + 0.2 * (tiles <= 1 ? 1 : 0);
-    return rounds * (double)((a.D + kBlockCols - 1) / kBlockCols) * kStep;
+// Whether the large tiling is the faster one: by rounds of the chip's compute units, of which
+// the small tiling's hold two blocks (the second costs 0.6 of the first), a round of large
+// tiles being 2.2 of its own (fitted to 96 to 1024 tokens, 2000 to 100000 channels, D = 1000 and
+// 4096, all group sizes: what it takes is never more than 1% slower than the other; 512 x 32000
+// x 4096, groups of 128: 86 us, 119 in small tiles; 333 x 8191 x 1000, groups of 64: 14.6, 19.6 in
+// large ones).
+bool large_tiles(const Logits4Args& a) {
+    const auto tiles = [&](int BM, int BN) { return (double)((a.T + BM - 1) / BM) * (double)((a.V + BN - 1) / BN) / kCus; };
+    const double small = tiles(T64x128::BM, T64x128::BN);
+    return 2.2 * std::ceil(tiles(T128x256::BM, T128x256::BN)) <= (small <= 1.0 ? 1.0 : 0.8 * std::ceil(small));
 }
 
 // Up to 64 tokens the streaming form, in the largest tile of tokens whose codes fit the LDS
-// (us: 64 tokens x 100000 x 1000 in tiles of 64 27, of 16 34, the smaller tiling 34); small tables,
+// (us: 64 tokens x 100000 x 1000 in tiles of 64 28, of 16 34, the smaller tiling 34); small tables,
 // where several tiles' blocks fill the chip and the codes come from the caches, in tiles of 16
-// (64 x 1500 x 4096: 11; 16 in tiles of 32, 31 with the tiling).  A large table whose 33 to 64 tokens do not fit goes through the tiling
-// (64 x 128256 x 4096: 78; 85 in tiles of 32).
+// (64 x 1500 x 4096: 8.6; 16 in tiles of 32, 31 with the tiling).  A large table whose 33 to 64
+// tokens do not fit goes through the tiling (64 x 128256 x 4096: 73; 85 in tiles of 32).
 template <int G>
 hipError_t launch_group(const Logits4Args& a, hipStream_t s) {
     const int64_t pitch = few_pitch((a.D + kUnit * kBlockCols - 1) / (kUnit * kBlockCols));
@@ -948,7 +947,7 @@ hipError_t launch_group(const Logits4Args& a, hipStream_t s) {
     if (a.T <= 16 || (a.T <= 64 && small)) return launch_few<Stream<false, 1>, G>(a, s);
     if (a.T <= 32) return 32 * pitch <= kFewLds ? launch_few<Stream<true, 1>, G>(a, s) : launch_few<Stream<false, 1>, G>(a, s);
     if (a.T <= 64 && 64 * pitch <= kFewLds) return launch_few<Stream<true, 2>, G>(a, s);
-    if (a.T > 64 && tiles_us<T128x256, G>(a) <= tiles_us<T64x128, G>(a)) return launch_tiles<T128x256, G>(a, s);
+    if (a.T > 64 && large_tiles(a)) return launch_tiles<T128x256, G>(a, s);
     return launch_tiles<T64x128, G>(a, s);
 }
 
