@@ -22,9 +22,17 @@
 //      a list; for every chunk the sum of the tokens before them;
 //   4  a block a row finds the prefix's end among the listed, the chunk in which
 //      the random number falls, and in it the token.
-// An end is found by histograms over the places, each over one bin of the last: of the
-// listed, or, where they do not fit (thousands of equal logits at a prefix's end), of
-// the whole row.
+// In the bin an end is found by rank where few tokens are there, or else by histograms over
+// the places, each over one bin of the last: of the listed, or, where they do not fit
+// (thousands of equal logits at a prefix's end), of the whole row.  (Histograms over places
+// alone have most of their bins about 0, where floats are dense: 256 rows of 8192 with top-k
+// and top-p take 20 us, and 31 so.)
+//
+// Bound by: a row of 8192 by the chain of its barriers (7 us, 18 to 20 with filters, 1 or 256
+// rows); few long rows by the chain of the four launches (16 x 128256 bf16: 4 + 9 + 8 + 11 us);
+// many by HBM in launch 1 (256 x 128256 fp32: 23 us, 5.8 TB/s), the vector units and LDS
+// atomics in 2 (41 us: 70% and 40% busy), loads and the rows that keep the most tokens in 3
+// (37 us; 4 takes 13).
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -48,7 +56,7 @@ constexpr int kChunk = 2 * kSub;                  // and of a chunk
 constexpr int kBins = 1024;
 constexpr int kList = 8192;                       // tokens of a row's list
 constexpr int kPartList = 1280;                   // of a part's (launch 3: four blocks a compute unit)
-constexpr int kRanked = 128;                      // of a list that is ranked at once: eight lanes a token
+constexpr int kRanked = kWave;                    // candidates that a wave ranks
 constexpr int kMaxParts = 64;                     // of a row
 constexpr int64_t kMaxRows = 512;                 // of a launch
 constexpr int64_t kOneBlock = kRowThreads * kPerLane;   // tokens of a row that a block holds
@@ -65,16 +73,19 @@ struct Part {            // of a row's logits
     int bad;             // a NaN or an infinity among them
 };
 
+struct Bins {            // where the prefixes end, from a row's histogram
+    u64 w_k, w_p;        // weights before bin_k, before bin_p
+    int n_k, n_p;        // tokens there
+    int in_k, to_p;      // tokens in bin_k; up to bin_p1's end
+    int bin_k;           // bin in which top-k ends (kBins: it is off)
+    int bin_p, bin_p1;   // first and last bin in which top-p may end (kBins, -1: it is off)
+};
+
 struct RowState {
     u64 all;             // sum of the weights
     unsigned listed;     // tokens that belong to the list
     int near;            // tokens that min-p keeps
-    // where the prefixes end, from the histogram
-    u64 w_k, w_p;        // weights before bin_k, before bin_p
-    int n_k, n_p;        // tokens there
-    int bin_k;           // bin in which top-k ends (kBins: it is off)
-    int bin_p, bin_p1;   // first and last bin in which top-p may end (kBins, -1: it is off)
-    int sure;            // tokens of bins before it are kept by both
+    Bins bins;
 };
 
 struct Space {           // a launch's rows in the workspace
@@ -370,91 +381,121 @@ struct Select {
     u64 lo, hi;                  // places among which the end is
     u64 w;                       // weights before them
     int n;                       // tokens there
-    int in;                      // tokens among them
+    int in;                      // tokens among them, then those ranked
 };
 constexpr u64 kNone = ~(u64)0;   // past every place
 
 // The first place up to which the candidates' count (or their weights) reaches
 // `need`, of 1 at least and at most what there is.  each(f) calls f(place, weight) for
-// the candidates of a thread; every pass makes a histogram over one bin of the last,
-// until a bin holds one.  n, w: what there is up to the place, it included.
+// the candidates of a thread, `most` of all threads at most.  Every pass makes a histogram
+// over one bin of the last, until a bin holds no more than a wave ranks: a lane each,
+// which goes through the others.  n, w: what there is up to the place, it included.
 template <bool kWeights, typename Each>
-__device__ u64 end_of(Each each, u64 need, Select& s, int& n, u64& w) {
-    u64 lo = kNone, hi = 0;
-    each([&](u64 place, auto) {
-        lo = min(lo, place);
-        hi = max(hi, place);
-    });
-    lo = wave_one(lo, [](u64 a, u64 b) { return a < b ? a : b; });
-    hi = wave_one(hi, [](u64 a, u64 b) { return a > b ? a : b; });
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+__device__ u64 end_of(Each each, int most, u64 need, Select& s, int& n, u64& w) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x & (kWave - 1);
+    u64 from = 0, to = kNone, w0 = 0;
+    int n0 = 0;
     __syncthreads();
-    if (threadIdx.x == 0) {
-        s.lo = kNone;
-        s.hi = 0;
-        s.w = 0;
-        s.n = 0;
-    }
-    s.weight[threadIdx.x] = 0;
-    s.count[threadIdx.x] = 0;
-    __syncthreads();
-    if ((threadIdx.x & (kWave - 1)) == 0) {
-        atomicMin(&s.lo, lo);
-        atomicMax(&s.hi, hi);
-    }
-    // a pass leaves ten bits less of at most 56
-    for (int pass = 0; pass < 7; ++pass) {
-        __syncthreads();
-        const u64 from = s.lo, to = s.hi, w0 = s.w;
-        const int n0 = s.n;
-        if (pass > 0 && s.in == 1) break;
-        const u64 wide = to - from;
-        const int shift = wide < kBins ? 0 : 64 - __clzll(wide) - 10;
-        each([&](u64 place, auto weight) {
-            if (place < from || place > to) return;
-            const int b = (int)((place - from) >> shift);
-            atomicAdd(&s.weight[b], weight());
-            atomicAdd(&s.count[b], 1);
+    if (most > kRanked) {
+        u64 lo = kNone, hi = 0;
+        each([&](u64 place, auto) {
+            lo = min(lo, place);
+            hi = max(hi, place);
         });
-        __syncthreads();
-        const u64 wb = s.weight[threadIdx.x];
-        const int nb = s.count[threadIdx.x];
+        lo = wave_one(lo, [](u64 a, u64 b) { return a < b ? a : b; });
+        hi = wave_one(hi, [](u64 a, u64 b) { return a > b ? a : b; });
+        if (threadIdx.x == 0) {
+            s.lo = kNone;
+            s.hi = 0;
+        }
         s.weight[threadIdx.x] = 0;
         s.count[threadIdx.x] = 0;
-        u64 w1 = wave_scan(wb);
-        int n1 = wave_scan(nb);
-        if ((threadIdx.x & (kWave - 1)) == kWave - 1) {
-            s.red[wave] = w1;
-            s.redi[wave] = n1;
+        __syncthreads();
+        if (lane == 0) {
+            atomicMin(&s.lo, lo);
+            atomicMax(&s.hi, hi);
         }
         __syncthreads();
-        w1 += w0;
-        n1 += n0;
+        from = s.lo;
+        to = s.hi;
+        // a pass leaves ten bits less of at most 56
+        for (int pass = 0; pass < 6; ++pass) {
+            const u64 wide = to - from;
+            const int shift = wide < kBins ? 0 : 64 - __clzll(wide) - 10;
+            each([&](u64 place, auto weight) {
+                if (place < from || place > to) return;
+                const int b = (int)((place - from) >> shift);
+                atomicAdd(&s.weight[b], weight());
+                atomicAdd(&s.count[b], 1);
+            });
+            __syncthreads();
+            const u64 wb = s.weight[threadIdx.x];
+            const int nb = s.count[threadIdx.x];
+            s.weight[threadIdx.x] = 0;
+            s.count[threadIdx.x] = 0;
+            u64 w1 = wave_scan(wb);
+            int n1 = wave_scan(nb);
+            if (lane == kWave - 1) {
+                s.red[wave] = w1;
+                s.redi[wave] = n1;
+            }
+            __syncthreads();
+            w1 += w0;
+            n1 += n0;
 #pragma unroll
-        for (int q = 0; q < kRowThreads / kWave; ++q) {
-            w1 += q < wave ? s.red[q] : 0;
-            n1 += q < wave ? s.redi[q] : 0;
+            for (int q = 0; q < kRowThreads / kWave; ++q) {
+                w1 += q < wave ? s.red[q] : 0;
+                n1 += q < wave ? s.redi[q] : 0;
+            }
+            const u64 before = kWeights ? w1 - wb : (u64)(n1 - nb), after = kWeights ? w1 : (u64)n1;
+            if (nb > 0 && before < need && after >= need) {
+                s.lo = from + ((u64)threadIdx.x << shift);
+                s.hi = min(to, s.lo + (((u64)1 << shift) - 1));
+                s.w = w1 - wb;
+                s.n = n1 - nb;
+                s.in = nb;
+            }
+            __syncthreads();
+            from = s.lo;
+            to = s.hi;
+            w0 = s.w;
+            n0 = s.n;
+            if (s.in <= kRanked) break;
         }
-        const u64 before = kWeights ? w1 - wb : (u64)(n1 - nb), after = kWeights ? w1 : (u64)n1;
-        if (nb > 0 && before < need && after >= need) {
-            s.lo = from + ((u64)threadIdx.x << shift);
-            s.hi = min(to, s.lo + (((u64)1 << shift) - 1));
-            s.w = w1 - wb;
-            s.n = n1 - nb;
-            s.in = nb;
-        }
+        __syncthreads();
     }
-    __syncthreads();
-    const u64 from = s.lo, to = s.hi;
-    n = s.n + 1;
-    const u64 w0 = s.w;
+    if (threadIdx.x == 0) {
+        s.lo = kNone;
+        s.in = 0;
+    }
     __syncthreads();
     each([&](u64 place, auto weight) {
         if (place < from || place > to) return;
-        s.lo = place;
-        s.w = w0 + weight();
+        const int q = atomicAdd(&s.in, 1);
+        if (q >= kRanked) return;
+        s.place[q] = place;
+        s.weight[q] = weight();
     });
     __syncthreads();
+    if (wave == 0) {
+        const int m = min(s.in, kRanked);
+        const u64 at = lane < m ? s.place[lane] : 0;
+        u64 before = w0;
+        int rank = n0;
+        for (int q = 0; q < m; ++q) {
+            const bool less = s.place[q] < at;
+            before += less ? s.weight[q] : 0;
+            rank += less;
+        }
+        const u64 after = before + (lane < m ? s.weight[lane] : 0);
+        if (lane < m && (kWeights ? before < need && after >= need : (u64)rank < need && (u64)rank + 1 >= need)) {
+            s.lo = at;
+            s.w = after;
+            s.n = rank + 1;
+        }
+    }
+    __syncthreads();
+    n = s.n;
     w = s.w;
     return s.lo;
 }
@@ -462,6 +503,82 @@ __device__ u64 end_of(Each each, u64 need, Select& s, int& n, u64& w) {
 // The row's p-th part of a sum: what comes before a token that top-p keeps is below it.
 __device__ __forceinline__ u64 part_of(u64 total, float p) { return (u64)ceil((double)total * (double)p); }
 __device__ __forceinline__ bool ranked(const Ask& q) { return q.k > 0 || q.p < 1.0f; }   // an end has to be found
+
+// The bins in which the prefixes end, from a histogram of which each of a block's kN threads
+// has kBins / kN bins side by side.  In LDS after the next barrier.
+template <int kN>
+__device__ __forceinline__ void bins_of(const Ask& q, const u64 (&w)[kBins / kN], const int (&n)[kBins / kN], u64* red, int* redi,
+                                        Bins& found) {
+    constexpr int kOwn = kBins / kN;
+    if (threadIdx.x == 0) found = Bins{0, 0, 0, 0, 0, 0, kBins, kBins, -1};
+    u64 sw = 0, all;
+    int sn = 0, positive;
+#pragma unroll
+    for (int o = 0; o < kOwn; ++o) {
+        sw += w[o];
+        sn += n[o];
+    }
+    const u64 w0 = block_scan<kN>(sw, red, all) - sw;        // before this thread's bins
+    const int n0 = block_scan<kN>(sn, redi, positive) - sn;
+    // top-k ends in the bin in which the count reaches k
+    const bool has_k = q.k > 0 && q.k < positive;
+    if (has_k) {
+        u64 wb = w0;
+        int nb = n0;
+#pragma unroll
+        for (int o = 0; o < kOwn; ++o) {
+            if (nb < q.k && nb + n[o] >= q.k) {
+                found.bin_k = threadIdx.x * kOwn + o;
+                found.w_k = wb;
+                found.n_k = nb;
+                found.in_k = n[o];
+                red[0] = wb + w[o];
+            }
+            wb += w[o];
+            nb += n[o];
+        }
+    }
+    __syncthreads();
+    if (q.p >= 1.0f) return;
+    // top-p ends between where it would with the smallest and the largest sum that top-k may keep
+    const u64 least = part_of(has_k ? found.w_k : all, q.p), most = part_of(has_k ? red[0] : all, q.p);
+    u64 wb = w0;
+    int nb = n0;
+#pragma unroll
+    for (int o = 0; o < kOwn; ++o) {
+        const int b = threadIdx.x * kOwn + o;
+        if ((wb < least && wb + w[o] >= least) || (b == 0 && least == 0)) {
+            found.bin_p = b;
+            found.w_p = wb;
+            found.n_p = nb;
+        }
+        if ((wb < most && wb + w[o] >= most) || (b == 0 && most == 0)) {
+            found.bin_p1 = b;
+            found.to_p = nb + n[o];
+        }
+        wb += w[o];
+        nb += n[o];
+    }
+}
+
+// The last place that is kept (kNone: all); `kept` comes as what top-k alone keeps.
+// each(first, last bin, f): a thread's tokens of a weight in these, as end_of takes them.
+template <typename Each>
+__device__ __forceinline__ u64 last_of(const Ask& q, const Bins& b, u64 all, Each each, Select& s, int& kept) {
+    u64 last = kNone, total = all, sum;
+    int n;
+    if (b.bin_k < kBins) {
+        last = end_of<false>([&](auto f) { each(b.bin_k, b.bin_k, f); }, b.in_k, (u64)(q.k - b.n_k), s, n, sum);
+        total = b.w_k + sum;
+    }
+    if (b.bin_p < kBins) {
+        // what the bins before keep is below this part, and at bin_p1's end it is reached
+        const u64 need = part_of(total, q.p);
+        last = end_of<true>([&](auto f) { each(b.bin_p, b.bin_p1, f); }, b.to_p - b.n_p, need > b.w_p ? need - b.w_p : 1, s, n, sum);
+        kept = b.n_p + n;
+    }
+    return last;
+}
 
 __device__ __forceinline__ void no_token(const SampleArgs& a, int64_t t) {
     a.ids[t] = -1;
@@ -481,11 +598,14 @@ __device__ __forceinline__ void token(const Params& p, const Row& x, int64_t t, 
 template <typename T>
 __global__ __launch_bounds__(kRowThreads) void ember_sample_row(Params p, int64_t t0) {
     __shared__ Select s;
+    __shared__ Bins bins;
     __shared__ double table[kSteps];
     __shared__ Part redp[kRowThreads / kWave];
     const int64_t t = t0 + blockIdx.x;
     const T* const l = static_cast<const T*>(p.a.L) + t * p.a.ldl;
     fill_table(table, p.bits);
+    s.weight[threadIdx.x] = 0;
+    s.count[threadIdx.x] = 0;
     float x[kPerLane];
     Part part{-kInf, kInf, 0, 0};
     const uint32_t i0 = threadIdx.x * kPerLane;
@@ -497,37 +617,38 @@ __global__ __launch_bounds__(kRowThreads) void ember_sample_row(Params p, int64_
         if (threadIdx.x == 0) no_token(p.a, t);
         return;
     }
+    const bool hist = ranked(row.ask);
     u64 w[kPerLane], all = 0;
+    int b[kPerLane];
     uint32_t mask = 0;                    // tokens of this thread that have a weight, then those that are kept
     int near = 0;
 #pragma unroll
     for (int e = 0; e < kPerLane; ++e) {
-        w[e] = weight_of(row, gap_of(row, x[e]), table);
+        const double gap = gap_of(row, x[e]);
+        w[e] = weight_of(row, gap, table);
+        b[e] = bin_of(row, gap);
         all += w[e];
         mask |= (uint32_t)(w[e] != 0) << e;
         near += x[e] != -kInf && near_of(row, x[e]);
+        if (!hist || !w[e]) continue;
+        atomicAdd(&s.weight[b[e]], w[e]);
+        atomicAdd(&s.count[b[e]], 1);
     }
     all = block_sum<kRowThreads>(all, s.red);
     int kept = row.some;
-    if (ranked(row.ask)) {
+    if (hist) {
+        const u64 own_w[1] = {s.weight[threadIdx.x]};
+        const int own_n[1] = {s.count[threadIdx.x]};
+        bins_of<kRowThreads>(row.ask, own_w, own_n, s.red, s.redi, bins);
+        __syncthreads();
+        if (row.ask.k > 0) kept = min(kept, row.ask.k);
         const auto place = [&](int e) { return place_of<T>(x[e], i0 + e, p.width); };
-        const auto each = [&](auto f) {
+        const auto each = [&](int first, int last, auto f) {
 #pragma unroll
             for (int e = 0; e < kPerLane; ++e)
-                if (mask >> e & 1) f(place(e), [&] { return w[e]; });
+                if ((mask >> e & 1) && b[e] >= first && b[e] <= last) f(place(e), [&] { return w[e]; });
         };
-        const int positive = block_sum<kRowThreads>((int)__popc(mask), s.redi);
-        u64 last = kNone, total = all;    // the last place that is kept, and the weights up to it
-        int n;
-        if (row.ask.k > 0) {
-            kept = min(kept, row.ask.k);
-            if (row.ask.k < positive) last = end_of<false>(each, (u64)row.ask.k, s, n, total);
-        }
-        if (row.ask.p < 1.0f) {
-            const u64 need = part_of(total, row.ask.p);
-            last = end_of<true>(each, need > 0 ? need : 1, s, n, total);
-            kept = n;
-        }
+        const u64 last = last_of(row.ask, bins, all, each, s, kept);
 #pragma unroll
         for (int e = 0; e < kPerLane; ++e) mask &= ~((uint32_t)(place(e) > last) << e);
     }
@@ -689,7 +810,7 @@ __global__ __launch_bounds__(kThreads, 8) void ember_sample_list(Params p, int64
     __shared__ double table[kSteps];
     __shared__ u64 red[kWavesB];
     __shared__ int redi[kWavesB];
-    __shared__ RowState found;
+    __shared__ Bins found;
     __shared__ float dense[kWavesB][kSub + kWave];
     __shared__ uint16_t index[kWavesB][kSub + kWave];
     __shared__ u64 list[kPartList];
@@ -705,79 +826,24 @@ __global__ __launch_bounds__(kThreads, 8) void ember_sample_list(Params p, int64
 
     if (threadIdx.x == 0) {
         listed = 0;
-        found.bin_k = found.bin_p = kBins;
-        found.bin_p1 = -1;
-        found.w_k = found.w_p = 0;
-        found.n_k = found.n_p = 0;
+        found = Bins{0, 0, 0, 0, 0, 0, kBins, kBins, -1};
     }
     if (hist) {
         constexpr int kOwn = kBins / kThreads;     // bins a thread
-        u64 w[kOwn], sw = 0;
-        int n[kOwn], sn = 0;
+        u64 w[kOwn];
+        int n[kOwn];
 #pragma unroll
         for (int q = 0; q < kOwn; ++q) {
             w[q] = p.s.weight[(int64_t)r * kBins + threadIdx.x * kOwn + q];
             n[q] = p.s.count[(int64_t)r * kBins + threadIdx.x * kOwn + q];
-            sw += w[q];
-            sn += n[q];
         }
-        u64 all;
-        int positive;
-        const u64 w0 = block_scan<kThreads>(sw, red, all) - sw;    // before this thread's bins
-        const int n0 = block_scan<kThreads>(sn, redi, positive) - sn;
-        // top-k ends in the bin in which the count reaches k
-        const int k = row.ask.k;
-        const bool has_k = k > 0 && k < positive;
-        if (has_k) {
-            u64 wb = w0;
-            int nb = n0;
-#pragma unroll
-            for (int q = 0; q < kOwn; ++q) {
-                if (nb < k && nb + n[q] >= k) {
-                    found.bin_k = threadIdx.x * kOwn + q;
-                    found.w_k = wb;
-                    found.n_k = nb;
-                    red[0] = wb + w[q];
-                }
-                wb += w[q];
-                nb += n[q];
-            }
-        }
-        __syncthreads();
-        // top-p ends between where it would with the smallest and the largest sum that top-k may keep
-        if (row.ask.p < 1.0f) {
-            const u64 least = part_of(has_k ? found.w_k : all, row.ask.p), most = part_of(has_k ? red[0] : all, row.ask.p);
-            u64 wb = w0;
-            int nb = n0;
-#pragma unroll
-            for (int q = 0; q < kOwn; ++q) {
-                const int b = threadIdx.x * kOwn + q;
-                if ((wb < least && wb + w[q] >= least) || (b == 0 && least == 0)) {
-                    found.bin_p = b;
-                    found.w_p = wb;
-                    found.n_p = nb;
-                }
-                if ((wb < most && wb + w[q] >= most) || (b == 0 && most == 0)) found.bin_p1 = b;
-                wb += w[q];
-                nb += n[q];
-            }
-        }
+        bins_of<kThreads>(row.ask, w, n, red, redi, found);
     }
     __syncthreads();
     const int bin_k = found.bin_k, bin_p = found.bin_p, bin_p1 = found.bin_p1;
-    const int sure = min(bin_k, bin_p);
+    const int sure = min(bin_k, bin_p);      // tokens of bins before it are kept by both
     RowState& s = p.s.rows[r];
-    if (c == 0 && threadIdx.x == 0) {
-        s.w_k = found.w_k;
-        s.w_p = found.w_p;
-        s.n_k = found.n_k;
-        s.n_p = found.n_p;
-        s.bin_k = bin_k;
-        s.bin_p = bin_p;
-        s.bin_p1 = bin_p1;
-        s.sure = sure;
-    }
-    __syncthreads();
+    if (c == 0 && threadIdx.x == 0) s.bins = found;
     // A logit below which nothing counts, with a margin for its rounding: whether a token counts
     // its bin says.
     const auto gap_to = [&](int b) { return row.scale > 0.0 ? b / row.scale : row.none; };
@@ -890,27 +956,9 @@ __global__ __launch_bounds__(kRowThreads) void ember_sample_draw(Params p, int64
     int sure = kBins;                 // tokens of bins before it are kept
     int kept = row.some;              // before min-p
     if (hist) {
-        sure = st.sure;
+        sure = min(st.bins.bin_k, st.bins.bin_p);
         if (row.ask.k > 0) kept = min(kept, row.ask.k);
-        const bool has_k = st.bin_k < kBins, has_p = st.bin_p < kBins;
         const int n = (int)min(st.listed, (unsigned)kList + 1);
-        u64 total = all;
-        // each(first, last bin, f): this thread's tokens of a weight in them, as end_of takes them
-        const auto find_ends = [&](auto each) {
-            int found;
-            u64 sum;
-            if (has_k) {
-                last = end_of<false>([&](auto f) { each(st.bin_k, st.bin_k, f); }, (u64)(row.ask.k - st.n_k), s, found, sum);
-                total = st.w_k + sum;
-            }
-            if (has_p) {
-                // what the bins before keep is below this part, and at bin_p1's end it is reached
-                const u64 need = part_of(total, row.ask.p);
-                last = end_of<true>([&](auto f) { each(st.bin_p, st.bin_p1, f); }, need > st.w_p ? need - st.w_p : 1, s,
-                                    found, sum);
-                kept = st.n_p + found;
-            }
-        };
         if (n > kList) {
             const auto each = [&](int first, int last, auto f) {
                 for (int64_t i = threadIdx.x * kPerLane; i < p.a.V; i += kRowThreads * kPerLane) {
@@ -926,55 +974,11 @@ __global__ __launch_bounds__(kRowThreads) void ember_sample_draw(Params p, int64
                     }
                 }
             };
-            find_ends(each);
+            last = last_of(row.ask, st.bins, all, each, s, kept);
             each(sure, kBins - 1, [&](u64 at, auto weight) {
                 if (at <= last && near_of(row, logit_of<T>(at, p.width)))
                     atomicAdd(&more[(uint32_t)(at & (((u64)1 << p.width) - 1)) / (kChunk * own)], weight());
             });
-        } else if (n > 0 && n <= kRanked) {
-            // eight lanes an entry: its rank and the weights before it, from all entries in LDS
-            // (entries without a weight do not count)
-            if ((int)threadIdx.x < n) {
-                const u64 x = weight_of(row, gap_of(row, logit_of<T>(first, p.width)), table);
-                s.weight[threadIdx.x] = x;
-                s.place[threadIdx.x] = x ? first : kNone;
-            }
-            __syncthreads();
-            const int e = threadIdx.x / 8;
-            u64 at = e < n ? s.place[e] : kNone, w = e < n ? s.weight[e] : 0, before = 0;
-            const int bin = at != kNone ? bin_of(row, gap_of(row, logit_of<T>(at, p.width))) : kBins;
-            int rank = 0;
-            for (int q = threadIdx.x % 8; q < n; q += 8) {
-                const bool less = s.place[q] < at;
-                rank += less;
-                before += less ? s.weight[q] : 0;
-            }
-            rank += from_lane<0xB1, 0xF>(rank, 0);         // of lane ^ 1, lane ^ 2, and 7 - lane of eight
-            rank += from_lane<0x4E, 0xF>(rank, 0);
-            rank += from_lane<0x141, 0xF>(rank, 0);
-            before += from_lane<0xB1, 0xF>(before, (u64)0);
-            before += from_lane<0x4E, 0xF>(before, (u64)0);
-            before += from_lane<0x141, 0xF>(before, (u64)0);
-            if (threadIdx.x % 8) at = kNone;               // one lane counts
-            // bin_k's first entry, and the first that top-k drops
-            const int first_k = has_k ? block_sum<kRowThreads>((int)(at != kNone && bin < st.bin_k), s.redi) : n;
-            const int end_k = has_k ? first_k + (row.ask.k - st.n_k) : n;
-            const bool in = at != kNone && rank < end_k;
-            if (has_k) total = st.w_k + block_sum<kRowThreads>(in && rank >= first_k ? w : 0, s.red);
-            bool mine = has_k && in;
-            if (has_p) {
-                // the largest logit is kept whatever top-p is
-                mine = in && bin <= st.bin_p1 && (st.w_p + before < part_of(total, row.ask.p) || (rank == 0 && st.n_p == 0));
-                kept = st.n_p + block_sum<kRowThreads>((int)mine, s.redi);
-            }
-            const u64 end = wave_one(mine ? at : 0, [](u64 a, u64 b) { return a > b ? a : b; });
-            if (threadIdx.x == 0) s.hi = 0;
-            __syncthreads();
-            if ((threadIdx.x & (kWave - 1)) == 0 && end) atomicMax(&s.hi, end);
-            if (mine && near_of(row, logit_of<T>(at, p.width)))
-                atomicAdd(&more[(uint32_t)(at & (((u64)1 << p.width) - 1)) / (kChunk * own)], w);
-            __syncthreads();
-            last = s.hi;
         } else if (n > 0) {
             constexpr int kOwn = kList / kRowThreads;
             u64 at[kOwn], w[kOwn];
@@ -994,11 +998,12 @@ __global__ __launch_bounds__(kRowThreads) void ember_sample_draw(Params p, int64
                 if (w[q]) bin[q] = bin_of(row, gap);
                 else at[q] = kNone;
             }
-            find_ends([&](int first, int last, auto f) {
+            const auto each = [&](int first, int last, auto f) {
 #pragma unroll
                 for (int q = 0; q < kOwn; ++q)
                     if (bin[q] >= first && bin[q] <= last) f(at[q], [&] { return w[q]; });
-            });
+            };
+            last = last_of(row.ask, st.bins, all, each, s, kept);
             // the kept ones join their chunks' sums
 #pragma unroll
             for (int q = 0; q < kOwn; ++q) {
