@@ -47,7 +47,7 @@ uint32_t magic_of(uint32_t d) { return d == 1 ? 0 : (uint32_t)((((uint64_t)1 << 
 // ---------------------------------------------------------------------------
 
 constexpr int kRowThreads = 256;
-constexpr int64_t kPastBytes = (int64_t)128 << 20;        // of rows: from here on they are stored past the caches
+constexpr int64_t kPastBytes = (int64_t)192 << 20;        // of rows: from here on they are stored past the caches
 constexpr int kUnitLanes = 16;                            // lanes a block of codes, one dword each
 constexpr int kUnitsPerPass = kRowThreads / kUnitLanes;   // blocks of codes side by side
 constexpr int kAhead = 4;                                 // of a thread, whose loads go out together
@@ -77,7 +77,8 @@ struct QuantParams {
 
 // A group is 4, 8 or 16 lanes.  The quotient x / s is rounded correctly, and so is the code at a
 // tie: with r = 1 / s correctly rounded, q = x r and the remainder e = x - q s (exact), q + e r is
-// (Markstein).  128256 x 4096 bf16 (1.3 GB read and written): 235 us; with divisions 390.
+// (Markstein).  Bound by HBM: 128256 x 4096 bf16 (1.3 GB read and written) 219 to 245 us, 5.4 to
+// 6.0 TB/s; with divisions 390.
 template <typename T, int G>
 __global__ __launch_bounds__(kRowThreads) void ember_quantize_q4(QuantParams p) {
     const Quant4Args& a = p.a;
@@ -158,7 +159,11 @@ struct RowsParams {
 // Rows of the table, or those of given tokens: the exact product of a code (4 bits)
 // and its scale (8), rounded once.  A token outside the table has NaN.  Each store of
 // a block's 16 lanes is 256 bytes side by side: of bf16 the pairs' eight columns a lane;
-// of fp32 four, for which a lane loads two dwords.  kPast: stored past the caches.
+// of fp32 four, for which a lane loads two dwords.  Bound by the stores: 16384 tokens of
+// 128256 x 4096, bf16 (169 MB), 26 us, 6.5 TB/s.
+// kPast: stored past the caches, so that rows beyond the last-level cache do not pass through
+// it (131072 x 4096 bf16 189 us, 359 otherwise); rows that fit are left there for their reader
+// (16384 x 4096: 27 us both, with a sum over them 59 and 71).
 template <typename T, int G, bool kPast>
 __global__ __launch_bounds__(kRowThreads) void ember_rows_q4(RowsParams p) {
     const Rows4Args& a = p.a;
@@ -278,6 +283,9 @@ struct Few4Params {
 // waves share one, unit by unit, and add up in LDS.  Blocks of the same channels and
 // other tokens are neighbours on one XCD, whose L2 then has the codes.  The order of
 // a logit's sum depends on V and D, not on the number of tokens.
+// 128256 x 4096: 1 token, groups of 128, 45 to 48 us (271 MB, 5.6 to 6.0 TB/s; reading alone 6.9);
+// 16 tokens, groups of 32, 57 to 63, where the sums' scaling takes the vector units; 64 x 100000 x
+// 1000 28 (MFMA, scaling and loads of one wave follow each other).
 template <typename C, int G, typename YT>
 __global__ __launch_bounds__(C::kThreads) void ember_logits_q4_few(Few4Params p) {
     const Logits4Args& a = p.a;
@@ -608,12 +616,14 @@ struct Tile4 {
 
 // BM tokens x BN channels a block, a block of 128 columns a step.  A ring of LDS
 // stages holds the tokens' codes and the table's; beside it are 16 bytes of scales a
-// channel (eight groups: two to eight steps), loaded with the first of their steps.  Every group's sum has to be turned into
-// fp32, scaled and added: 32 vector instructions for each 32 x 32 tile, as long as
-// the MFMAs of 128 columns take.  So these are laid between the next sum's MFMAs,
-// each wave has all of the block's tokens (the codes' halves are taken apart once),
-// and the step barrier sits before the last tile of tokens, whose operands are in
-// registers by then.
+// channel (eight groups: two to eight steps), loaded with the first of their steps.
+// Every group's sum has to be turned into fp32, scaled and added: 32 vector instructions
+// for each 32 x 32 tile, as long as the MFMAs of 128 columns take.  So these are laid
+// between the next sum's MFMAs, each wave has all of the block's tokens (the codes' halves
+// are taken apart once), and the step barrier sits before the last tile of tokens, whose
+// operands are in registers by then.  1024 x 128256 x 4096, groups of 128, bf16 logits: 674
+// to 693 us, 1.6 POPS (the int8 library product, without scales: 2.0); the vector units
+// have 55% of the time, the matrix units 36%, and they hardly overlap.
 template <typename C, int G, typename YT>
 __global__ __launch_bounds__(C::kThreads) void ember_logits_q4(Tile4Params p) {
     __shared__ __attribute__((aligned(1024))) uint8_t lds[C::kLds];

@@ -28,7 +28,7 @@
 // alone have most of their bins about 0, where floats are dense: 256 rows of 8192 with top-k
 // and top-p take 20 us, and 31 so.)
 //
-// Bound by: a row of 8192 by the chain of its barriers (7 us, 18 to 20 with filters, 1 or 256
+// Bound by: a row of 8192 by the chain of its barriers (8 to 10 us, 18 to 20 with filters, 1 or 256
 // rows); few long rows by the chain of the four launches (16 x 128256 bf16: 4 + 9 + 8 + 11 us);
 // many by HBM in launch 1 (256 x 128256 fp32: 23 us, 5.8 TB/s), the vector units and LDS
 // atomics in 2 (41 us: 70% and 40% busy), loads and the rows that keep the most tokens in 3
