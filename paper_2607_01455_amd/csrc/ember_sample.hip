@@ -276,7 +276,7 @@ __device__ __forceinline__ Row row_at(const Params& p, int64_t t, int r) {
 __device__ __forceinline__ double gap_of(const Row& x, float l) { return fmin(x.top - (double)l, x.reach); }
 __device__ __forceinline__ bool near_of(const Row& x, float l) { return (x.top - (double)l) * x.ask.heat <= x.ask.far; }
 // (up to a gap that has a weight the bins are 0 .. kBins - 1 by the scale alone)
-__device__ __forceinline__ int bin_of(const Row& x, double gap) { return min(kBins - 1, (int)(gap * x.scale)); }
+__device__ __forceinline__ int bin_of(const Row& x, double gap) { return (int)fmin(gap * x.scale, kBins - 1.0); }
 
 // 2^(-z / kSteps) in fixed point, z = gap heat.  With n the whole number of steps nearest -z, in
 // the low bits of a sum with 1.5 * 2^52, it is the table's 2^(bits + (n mod kSteps) / kSteps), times a
@@ -630,9 +630,15 @@ __global__ __launch_bounds__(kRowThreads) void ember_sample_row(Params p, int64_
         all += w[e];
         mask |= (uint32_t)(w[e] != 0) << e;
         near += x[e] != -kInf && near_of(row, x[e]);
-        if (!hist || !w[e]) continue;
-        atomicAdd(&s.weight[b[e]], w[e]);
-        atomicAdd(&s.count[b[e]], 1);
+        if (e % 4 == 3) __builtin_amdgcn_sched_barrier(0);      // eight at once take more registers
+    }
+    if (hist) {
+#pragma unroll
+        for (int e = 0; e < kPerLane; ++e) {
+            if (!w[e]) continue;
+            atomicAdd(&s.weight[b[e]], w[e]);
+            atomicAdd(&s.count[b[e]], 1);
+        }
     }
     all = block_sum<kRowThreads>(all, s.red);
     int kept = row.some;
@@ -844,13 +850,13 @@ __global__ __launch_bounds__(kThreads, 8) void ember_sample_list(Params p, int64
     const int sure = min(bin_k, bin_p);      // tokens of bins before it are kept by both
     RowState& s = p.s.rows[r];
     if (c == 0 && threadIdx.x == 0) s.bins = found;
-    // A logit below which nothing counts, with a margin for its rounding: whether a token counts
-    // its bin says.
+    // A logit below which nothing counts, with margins for the border's rounding and its own:
+    // whether a token counts its bin says.
     const auto gap_to = [&](int b) { return row.scale > 0.0 ? b / row.scale : row.none; };
     double gap = fmin(gap_to(sure), row.ask.far * row.ask.cool);
     if (bin_k < kBins) gap = fmax(gap, gap_to(bin_k + 1));
     if (bin_p < kBins) gap = fmax(gap, gap_to(bin_p1 + 1));
-    float least = (float)(row.top - fmin(gap, row.none));
+    float least = (float)(row.top - fmin(gap, row.none) * (1.0 + 0x1p-40));
     least = fmaxf(least - fabsf(least) * 0x1p-22f - 1e-37f, -3.4028235e38f);
     const int end = min((c + 1) * p.part_chunks, p.chunks);
     // A wave's chunks, every kWavesB-th, 64 at a time; those with a logit that counts are
