@@ -591,13 +591,14 @@ struct Tile4Params {
     int group_m;
 };
 
-// BM tokens x 32 channels a wave, WN waves side by side.
-template <int BM_, int WN_, int STAGES_>
+// BM tokens x 32 channels a wave, WN waves side by side, GROUPS times: each group of waves
+// takes every GROUPS-th step.
+template <int BM_, int WN_, int STAGES_, int GROUPS_ = 1>
 struct Tile4 {
     static constexpr int BM = BM_, BN = 32 * WN_;  // tokens, channels a block
     static constexpr int kStages = STAGES_;
-    static constexpr int kWaves = WN_;
-    static constexpr int kThreads = kWaves * kWave;
+    static constexpr int kWaves = WN_, kGroups = GROUPS_;
+    static constexpr int kThreads = kGroups * kWaves * kWave;
     static constexpr int MT = BM / 32;             // MFMA tiles a wave
     static constexpr int kX = BM * kBlockCols, kW = BN * kBlockBytes;                 // bytes of a stage
     static constexpr int kS = BN * 16, kScales = 3;                                   // of a period's scales, and of these
@@ -605,9 +606,12 @@ struct Tile4 {
     static constexpr int kLoads = kLoadsX + kLoadsW + 1;
     static constexpr int kStageBytes = kX + kW;
     static constexpr int kRing = kStages * kStageBytes, kNone = kRing + kScales * kS;    // kNone: what loads outside a buffer write
-    static constexpr int kXs = kNone + 1024, kLds = kXs + BM * 4;
+    static constexpr int kGroupLds = kNone + 1024;                                    // a group's
+    static constexpr int kXs = kGroups * kGroupLds, kLds = kXs + BM * 4;
+    static constexpr int kSumBytes = kWaves * MT * 16 * kWave * 4;                    // a group's sums
     static_assert(BM % (8 * kWaves) == 0 && kWaves % 2 == 0 && MT % 2 == 0, "equal loads a wave, even tiles");
     static_assert(kStages >= 2 && kStages <= 4 && (kStages - 2) * kLoads < 64, "vmcnt range, scales of the steps ahead");
+    static_assert(kGroups == 1 || (kGroups == 2 && kSumBytes <= kGroupLds), "whole periods of scales; the second group's sums");
     static_assert(BN % kWave == 0 && BN / kWave <= kWaves, "the scales' loads");
     static_assert((int64_t)std::max(BM, BN) * EMBER_Q8_MAX_LD < (int64_t)1 << 31, "32-bit load offsets");
     static constexpr int kBlocks = 160 * 1024 / kLds;    // a compute unit
@@ -630,8 +634,10 @@ __global__ __launch_bounds__(C::kThreads) void ember_logits_q4(Tile4Params p) {
     const Logits4Args& a = p.a;
     constexpr int kPer = kBlockCols / G;
     const int lane = threadIdx.x & (kWave - 1);
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
+    const int group = C::kGroups == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / (C::kWaves * kWave));
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) - group * C::kWaves;      // of the group
+    uint8_t* const own = lds + group * C::kGroupLds;
+    const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)own;
     // this block's tiles: every gridDim.x / kXcds-th of its XCD's
     const int64_t xcd = blockIdx.x % kXcds, end = min((xcd + 1) * p.per_xcd, p.tiles);
     int64_t l = xcd * p.per_xcd + blockIdx.x / kXcds;
@@ -656,13 +662,17 @@ __global__ __launch_bounds__(C::kThreads) void ember_logits_q4(Tile4Params p) {
         rw = rsrc(a.Wq + v0 * a.ldw, (a.V - v0) * a.ldw);
         rs = rsrc(a.wscale + v0 * a.ldg, (a.V - v0) * a.ldg * 2);
     };
-    auto issue = [&](int kt, uint32_t st) {
+    // step i of the group: the row's step kt
+    auto step_of = [&](int i) { return C::kGroups * i + group; };
+    const int steps = (p.nk + C::kGroups - 1) / C::kGroups;
+    auto issue = [&](int i, uint32_t st) {
+        const int kt = step_of(i);
         const uint32_t ox = kt * kBlockCols + k_x < D ? off_x + kt * kBlockCols : kBufferMax;
         const uint32_t ow = off_w + (kt < p.nk ? (uint32_t)kt * kBlockBytes : kBufferMax);
         // Scales: 16 bytes of a row each, so 64 rows a load, and slow.  In the other steps (and waves)
         // the load stays, outside the buffer, so that all steps have as many.
         constexpr int kPeriod = 8 / kPer;
-        const bool scales = kt % kPeriod == 0 && kt < p.nk && wave < C::BN / kWave;
+        const bool scales = kt % kPeriod == group && kt < p.nk && wave < C::BN / kWave;
         const uint32_t os = off_s + (scales ? (uint32_t)(kt / kPeriod * 16) : kBufferMax);
         const uint32_t to_s = scales ? C::kRing + kt / kPeriod % C::kScales * C::kS + wave * 1024 : C::kNone;
         load_to_lds(rs, lds_base + to_s, os);
@@ -674,7 +684,7 @@ __global__ __launch_bounds__(C::kThreads) void ember_logits_q4(Tile4Params p) {
             load_to_lds(rw, lds_base + st + C::kX + (wave + C::kWaves * j) * 1024, ow + j * (C::kWaves * 16 * (uint32_t)a.ldw));
     };
     const int half = lane >> 5, sh = half ? 0 : 4, col = lane & 31, ch = wave * 32 + col;
-    const auto* const ring = (const __attribute__((address_space(3))) uint8_t*)lds;      // stages: offsets in it
+    const auto* const ring = (const __attribute__((address_space(3))) uint8_t*)own;      // stages: offsets in it
     auto lds_at = [&](uint32_t at, int more) { return *(const __attribute__((address_space(3))) i32x4*)(ring + at + more); };
     // operands: a tile's tokens, 32 columns each; a block's codes, dword w of quarter t; scales
     uint32_t at_x[4];
@@ -683,7 +693,7 @@ __global__ __launch_bounds__(C::kThreads) void ember_logits_q4(Tile4Params p) {
     uint32_t at_w[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) at_w[t] = ch * kBlockBytes + ((t ^ swizzle<4>(ch)) * 16);
-    // (masked: the last step of a D that is not a multiple of 16, whose last chunk holds columns that do not count)
+    // (masked: the group's last step, where a D that is not a multiple of 16 has a chunk of columns that do not count)
     uint32_t here[4];       // of the stage
     auto read_x = [&](int m, i32x4 (&x)[4], bool masked) {
 #pragma unroll
@@ -692,7 +702,7 @@ __global__ __launch_bounds__(C::kThreads) void ember_logits_q4(Tile4Params p) {
             if (!masked) continue;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int b = D - (p.nk - 1) * kBlockCols - 32 * w - 16 * half - 4 * e;
+                const int b = D - step_of(steps - 1) * kBlockCols - 32 * w - 16 * half - 4 * e;
                 x[w][e] &= b >= 4 ? -1 : b <= 0 ? 0 : (int)((1u << (8 * b)) - 1);
             }
         }
@@ -701,13 +711,14 @@ __global__ __launch_bounds__(C::kThreads) void ember_logits_q4(Tile4Params p) {
 #pragma unroll
         for (int t = 0; t < 4; ++t) wd[t] = lds_at(st + at_w[t], C::kX);
     };
-    auto read_s = [&](int kt, float (&s)[kPer]) {
+    auto read_s = [&](int i, float (&s)[kPer]) {
+        const int kt = step_of(i);
         const uint32_t at = kt * kPer / 8 % C::kScales * C::kS + ch * 16 + kt * kPer % 8 * 2;
 #pragma unroll
         for (int j = 0; j < kPer; ++j) {
             const uint32_t h = *(const __attribute__((address_space(3))) uint16_t*)(ring + at + (C::kRing + 2 * j));
             // no group: what stands in its place is not a scale
-            s[j] = kPer == 1 || kt * kPer + j < p.groups ? bf16_bits_f32(h) : 0.0f;
+            s[j] = (kPer == 1 && C::kGroups == 1) || kt * kPer + j < p.groups ? bf16_bits_f32(h) : 0.0f;
         }
     };
     auto take_apart = [&](const i32x4 (&wd)[4], i32x4 (&op)[4]) {
@@ -782,8 +793,9 @@ __global__ __launch_bounds__(C::kThreads) void ember_logits_q4(Tile4Params p) {
     // last stages; the first of the next tile are loaded meanwhile.
     constexpr int kEs = (int)sizeof(YT), kPitch = 32 * kEs + 16, kEpc = 16 / kEs, kPerRow = 32 / kEpc;
     constexpr int kAhead = C::kStages - (C::kWaves * 32 * kPitch + C::kStageBytes - 1) / C::kStageBytes;
+    static_assert(C::kGroups == 1 || C::kSumBytes + C::kWaves * 32 * kPitch <= C::kGroups * C::kGroupLds, "sums and strips");
     static_assert(kAhead >= 1, "the strips");
-    uint8_t* const strip = lds + kAhead * C::kStageBytes + wave * (32 * kPitch);
+    uint8_t* const strip = lds + (C::kGroups == 1 ? kAhead * C::kStageBytes : C::kSumBytes) + wave * (32 * kPitch);
     int el = lane;
     auto store = [&](int64_t t0, int64_t v0, float bias) {
         asm volatile("" : "+v"(el));   // what follows from it is not kept in registers over the steps
@@ -839,14 +851,32 @@ __global__ __launch_bounds__(C::kThreads) void ember_logits_q4(Tile4Params p) {
         wait_step<(C::kStages - 1) * C::kLoads>();
         read_w(0, wd);
         read_s(0, scale);
-        read_x(0, x[0], p.nk == 1);
+        read_x(0, x[0], steps == 1);
         take_apart(wd, op);
-        for (int i = 0; i < p.nk - 1; ++i) step(i, std::false_type());
-        if (p.nk > 1) read_x(0, x[0], true);
-        step(p.nk - 1, std::true_type());
+        for (int i = 0; i < steps - 1; ++i) step(i, std::false_type());
+        if (steps > 1) read_x(0, x[0], true);
+        step(steps - 1, std::true_type());
 #pragma unroll
         for (int e = 0; e < 16; ++e) f[C::MT - 1][e] = fmaf((float)sum[1][e], last, f[C::MT - 1][e]);
         wait_step<0>();    // the zero-filling loads past the end have landed, and everyone is done with the stages
+        if constexpr (C::kGroups > 1) {
+            // one tile: the second group's sums join the first's
+            float* const sums = reinterpret_cast<float*>(lds) + wave * (C::MT * 16 * kWave) + lane;
+            if (group > 0) {
+#pragma unroll
+                for (int m = 0; m < C::MT; ++m)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) sums[(m * 16 + e) * kWave] = f[m][e];
+            }
+            __syncthreads();
+            if (group > 0) return;
+#pragma unroll
+            for (int m = 0; m < C::MT; ++m)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) f[m][e] += sums[(m * 16 + e) * kWave];
+            store(t0, v0, bias);
+            return;
+        }
         const int64_t t_done = t0, v_done = v0;
         const float bias_done = bias;
         l += gridDim.x / kXcds;
@@ -923,7 +953,7 @@ hipError_t launch_tiles(const Logits4Args& a, hipStream_t s) {
     // The blocks that are there at once go through the tiles, so that the next one's first loads are
     // out while one is stored (1024 x 131072: 721 us at D = 4096 and 239 at 1024; a tile a block 764
     // and 251); of few steps, with nothing to hide the stores behind, a tile a block (168 at 512; 181).
-    const int64_t blocks = p.nk < 6 ? kMaxGridBlocks : kCus * C::kBlocks;
+    const int64_t blocks = p.nk < 6 || C::kGroups > 1 ? kMaxGridBlocks : kCus * C::kBlocks;
     const unsigned grid = (unsigned)(std::min<int64_t>(p.per_xcd, blocks / kXcds) * kXcds);
     if (a.y_dtype == EMBER_F32) launch_tile<C, G, float>(p, grid, s);
     else launch_tile<C, G, uint16_t>(p, grid, s);
@@ -932,6 +962,7 @@ hipError_t launch_tiles(const Logits4Args& a, hipStream_t s) {
 
 using T128x256 = Tile4<128, 8, 4>;
 using T64x128 = Tile4<64, 4, 3>;       // two a compute unit
+using T64x128Two = Tile4<64, 4, 3, 2>;
 
 // Whether the large tiling is the faster one: by rounds of the chip's compute units, of which
 // the small tiling's hold two blocks (the second costs 0.6 of the first), a round of large
@@ -958,7 +989,10 @@ hipError_t launch_group(const Logits4Args& a, hipStream_t s) {
     if (a.T <= 32) return 32 * pitch <= kFewLds ? launch_few<Stream<true, 1>, G>(a, s) : launch_few<Stream<false, 1>, G>(a, s);
     if (a.T <= 64 && 64 * pitch <= kFewLds) return launch_few<Stream<true, 2>, G>(a, s);
     if (a.T > 64 && large_tiles(a)) return launch_tiles<T128x256, G>(a, s);
-    return launch_tiles<T64x128, G>(a, s);
+    // where each compute unit has one small tile at most, two groups of waves share its steps (us: 200 x
+    // 8000 x 8192, groups of 32, 55, one group 84; 96 x 8191 x 1000, groups of 64, 10.2 and 11.6)
+    const bool one = (a.T + T64x128::BM - 1) / T64x128::BM * ((a.V + T64x128::BN - 1) / T64x128::BN) <= kCus;
+    return one ? launch_tiles<T64x128Two, G>(a, s) : launch_tiles<T64x128, G>(a, s);
 }
 
 } // namespace

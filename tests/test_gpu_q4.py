@@ -225,6 +225,23 @@ def test_logits(em, T, V, D, group):
     check(em, T, V, D, group, dtype, bias, extra=(T + D) % 2)
 
 
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_logits_of_few_and_odd_steps(em, group):
+    """Tiles of many tokens with 1 to 9 blocks of columns, the last one whole or not."""
+    for T in (70, 700):
+        for D in (1, 128, 129, 250, 256, 300, 384, 500, 513, 640, 768, 800, 1000, 1040):
+            print(f"q4 steps T={T} D={D} group={group}", flush=True)
+            check(em, T, 150, D, group, F, True, seed=D)
+
+
+@pytest.mark.parametrize("T,V,D", [(700, 20001, 1000), (130, 70001, 700), (1000, 33000, 200), (70, 66000, 900)])
+@pytest.mark.parametrize("group,dtype", [(32, BF), (64, F), (128, BF)])
+def test_more_tiles_than_blocks(em, T, V, D, group, dtype):
+    """Blocks that go on to other tiles, and of few steps one a tile."""
+    print(f"q4 tiles T={T} V={V} D={D} group={group} {dtype}", flush=True)
+    check(em, T, V, D, group, dtype, True)
+
+
 @pytest.mark.parametrize("T", [1, 20, 50, 70, 300])
 def test_logits_of_one_scale_are_exact_integers(em, T):
     """Scales that are powers of two: every partial sum is an integer below 2^24."""
