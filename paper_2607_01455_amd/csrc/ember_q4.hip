@@ -976,23 +976,31 @@ bool large_tiles(const Logits4Args& a) {
     return 2.2 * std::ceil(tiles(T128x256::BM, T128x256::BN)) <= (small <= 1.0 ? 1.0 : 0.8 * std::ceil(small));
 }
 
-// Up to 64 tokens the streaming form, in the largest tile of tokens whose codes fit the LDS
-// (us: 64 tokens x 100000 x 1000 in tiles of 64 28, of 16 34, the smaller tiling 34); small tables,
-// where several tiles' blocks fill the chip and the codes come from the caches, in tiles of 16
-// (64 x 1500 x 4096: 8.6; 16 in tiles of 32, 31 with the tiling).  A large table whose 33 to 64
-// tokens do not fit goes through the tiling (64 x 128256 x 4096: 73; 85 in tiles of 32).
+// Up to 16 tokens the streaming form.  Up to 64 it is the faster one
+//   - in tiles of 16 tokens for small tables, as long as these are few: several tiles' blocks fill the
+//     chip and the codes come from the caches (us, D = 2048, groups of 128: 64 x 4000 8.1, 12.4 with the
+//     tiling; 64 x 8000 14.9 and 12.4; groups of 32 16.4 and 17.6, but 64 x 16000 32 and 18);
+//   - in tiles of 32 or 64 tokens whose codes fit the LDS for large ones: of up to 32 tokens (32 x 60000 x
+//     2048 18, 19 with the tiling), of more where the small tiling takes more than one round (64 x 60000
+//     x 2048 24 and 20, 64 x 128256 x 2048, groups of 64, 42 and 45);
+//   - in tiles of 16 for up to 32 tokens that do not fit, where groups of 32 or 64 keep the tiling's vector
+//     units (32 x 60000 x 8192: 88 and 104; groups of 128 82 and 57).
 template <int G>
 hipError_t launch_group(const Logits4Args& a, hipStream_t s) {
     const int64_t pitch = few_pitch((a.D + kUnit * kBlockCols - 1) / (kUnit * kBlockCols));
-    const bool small = a.V < 16384;
-    if (a.T <= 16 || (a.T <= 64 && small)) return launch_few<Stream<false, 1>, G>(a, s);
-    if (a.T <= 32) return 32 * pitch <= kFewLds ? launch_few<Stream<true, 1>, G>(a, s) : launch_few<Stream<false, 1>, G>(a, s);
-    if (a.T <= 64 && 64 * pitch <= kFewLds) return launch_few<Stream<true, 2>, G>(a, s);
+    const int64_t strips = (a.T + 15) / 16 * ((a.V + 15) / 16);
+    const int64_t tiles = (a.T + T64x128::BM - 1) / T64x128::BM * ((a.V + T64x128::BN - 1) / T64x128::BN);
+    if (a.T <= 16) return launch_few<Stream<false, 1>, G>(a, s);
+    if (a.T <= 64 && a.V < 16384 && strips < (G == 128 ? 1500 : 3000)) return launch_few<Stream<false, 1>, G>(a, s);
+    if (a.T <= 32 && a.V >= 16384) {
+        if (32 * pitch <= kFewLds) return launch_few<Stream<true, 1>, G>(a, s);
+        if (G < 128 && tiles > kCus) return launch_few<Stream<false, 1>, G>(a, s);
+    }
+    if (a.T <= 64 && 64 * pitch <= kFewLds && tiles > 2 * kCus) return launch_few<Stream<true, 2>, G>(a, s);
     if (a.T > 64 && large_tiles(a)) return launch_tiles<T128x256, G>(a, s);
     // where each compute unit has one small tile at most, two groups of waves share its steps (us: 200 x
     // 8000 x 8192, groups of 32, 55, one group 84; 96 x 8191 x 1000, groups of 64, 10.2 and 11.6)
-    const bool one = (a.T + T64x128::BM - 1) / T64x128::BM * ((a.V + T64x128::BN - 1) / T64x128::BN) <= kCus;
-    return one ? launch_tiles<T64x128Two, G>(a, s) : launch_tiles<T64x128, G>(a, s);
+    return tiles <= kCus ? launch_tiles<T64x128Two, G>(a, s) : launch_tiles<T64x128, G>(a, s);
 }
 
 } // namespace
