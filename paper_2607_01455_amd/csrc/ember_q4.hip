@@ -47,7 +47,7 @@ uint32_t magic_of(uint32_t d) { return d == 1 ? 0 : (uint32_t)((((uint64_t)1 << 
 // ---------------------------------------------------------------------------
 
 constexpr int kRowThreads = 256;
-constexpr int64_t kPastBytes = (int64_t)192 << 20;        // of rows: from here on they are stored past the caches
+constexpr int64_t kPastBytes = (int64_t)128 << 20;        // of rows: from here on they are stored past the caches
 constexpr int kUnitLanes = 16;                            // lanes a block of codes, one dword each
 constexpr int kUnitsPerPass = kRowThreads / kUnitLanes;   // blocks of codes side by side
 constexpr int kAhead = 4;                                 // of a thread, whose loads go out together
@@ -161,9 +161,9 @@ struct RowsParams {
 // a block's 16 lanes is 256 bytes side by side: of bf16 the pairs' eight columns a lane;
 // of fp32 four, for which a lane loads two dwords.  Bound by the stores: 16384 tokens of
 // 128256 x 4096, bf16 (169 MB), 26 us, 6.5 TB/s.
-// kPast: stored past the caches, so that rows beyond the last-level cache do not pass through
-// it (131072 x 4096 bf16 189 us, 359 otherwise); rows that fit are left there for their reader
-// (16384 x 4096: 27 us both, with a sum over them 59 and 71).
+// kPast: stored past the caches, from where that costs the rows' reader no more than it gains
+// here (other buffers each time, x 4096 bf16, us past the caches and through them: 32768 rows 53 and
+// 93, with a sum over the rows 164 and 173; 16384 27 and 49, 89 and 88; 8192 16 and 27, 52 and 47).
 template <typename T, int G, bool kPast>
 __global__ __launch_bounds__(kRowThreads) void ember_rows_q4(RowsParams p) {
     const Rows4Args& a = p.a;
