@@ -684,6 +684,8 @@ class HeadQ4:
 
     def load(self, W: torch.Tensor) -> None:
         """Take the table's present rows (after steps on it)."""
+        if W.shape[1] != self.D:
+            raise ValueError(f"W has {W.shape[1]} columns, the table {self.D}")
         ember_quantize_rows_q4(W, self.Wq, self.wscale, self.group)
 
     def logits(self, Xq: torch.Tensor, xscale: torch.Tensor, Y: torch.Tensor) -> None:

@@ -176,3 +176,12 @@ def test_binding_refuses_tensors_that_do_not_fit(em):
                dict(top_k=torch.zeros(3))):
         with pytest.raises((ValueError, TypeError)):
             em.ember_sample(**{**dict(L=L, u=u, ids=ids, ws=ws), **kw})
+
+
+def test_head_takes_a_table_of_its_own_columns(em):
+    """250 columns have as many bytes of codes and as many groups as 200: only the head knows which it has."""
+    head = em.HeadQ4(torch.zeros(4, 128, dtype=torch.uint8), torch.zeros(4, 8, dtype=torch.bfloat16)[:, :4], 200, 64)
+    assert em.q4_shapes(4, 250, 64) == em.q4_shapes(4, 200, 64)
+    for D in (193, 199, 201, 250, 256):
+        with pytest.raises(ValueError, match=f"{D} columns"):
+            head.load(torch.zeros(4, D))
