@@ -572,7 +572,8 @@ int ember_logits_q4(const int8_t* Xq, int64_t ldx, const float* xscale,
  * be NULL), 1 <= V <= EMBER_SAMPLE_MAX_V.  Outputs and the workspace share no memory
  * with another argument (EMBER_ERR_ARG).  The workspace (device, 256-byte aligned,
  * ember_sample_workspace_bytes of at least T tokens and this V) needs no
- * initialisation; calls that share one must not run at once.
+ * initialisation; calls that share one must not run at once.  Rows of up to 8192
+ * tokens leave it as it is, and 4 KiB serve any number of them.
  */
 #define EMBER_SAMPLE_MAX_V ((int64_t)1 << 24)
 

@@ -60,6 +60,7 @@ constexpr int kRanked = kWave;                    // candidates that a wave rank
 constexpr int kMaxParts = 64;                     // of a row
 constexpr int64_t kMaxRows = 512;                 // of a launch
 constexpr int64_t kOneBlock = kRowThreads * kPerLane;   // tokens of a row that a block holds
+constexpr size_t kLeastBytes = 4096;              // of a workspace
 constexpr int kSteps = 32;                        // of a halving of the weight: z counts these
 constexpr double kLog2e = 1.4426950408889634;
 constexpr double kLn2 = 0.6931471805599453;
@@ -1078,7 +1079,10 @@ hipError_t launch_row(const Params& p, hipStream_t s) {
 
 } // namespace
 
-size_t sample_ws_bytes(int64_t T, int64_t V) { return space_of(nullptr, std::min(T, kMaxRows), V, nullptr); }
+// (a block's rows need none of it: 4 KiB for any number of them, so that a call's workspace is never empty)
+size_t sample_ws_bytes(int64_t T, int64_t V) {
+    return V <= kOneBlock ? kLeastBytes : std::max(kLeastBytes, space_of(nullptr, std::min(T, kMaxRows), V, nullptr));
+}
 
 hipError_t launch_sample(const SampleArgs& a, hipStream_t s) {
     Params p;

@@ -185,3 +185,20 @@ def test_head_takes_a_table_of_its_own_columns(em):
     for D in (193, 199, 201, 250, 256):
         with pytest.raises(ValueError, match=f"{D} columns"):
             head.load(torch.zeros(4, D))
+
+
+def test_short_rows_ask_for_no_workspace_of_their_own(em):
+    """Rows of up to 8192 tokens are one launch without scratch memory: the same 4 KiB for any number of them."""
+    out = ctypes.c_size_t(0)
+    for V in (1, 64, 5000, 8192):
+        for T in (0, 1, 512, 1 << 26):
+            assert em.LIB.ember_sample_workspace_bytes(T, V, ctypes.byref(out)) == em.EMBER_OK and out.value == 4096
+    assert _sample(em, V=8192, ldl=8192, T=1 << 20, wsb=4095) == em.EMBER_ERR_WORKSPACE
+    # longer rows ask for their bins, lists and chunks, and are refused with less
+    for T in (0, 1, 600):
+        assert em.LIB.ember_sample_workspace_bytes(T, 8193, ctypes.byref(out)) == em.EMBER_OK
+        assert out.value >= max(4096, min(T, 512) * (1024 * 12 + 8192 * 8))
+        if T:
+            args = dict(T=T, V=8193, ldl=8200)
+            assert _sample(em, wsb=out.value - 1, **args) == em.EMBER_ERR_WORKSPACE
+            assert _sample(em, wsb=4096, **args) == em.EMBER_ERR_WORKSPACE

@@ -355,3 +355,21 @@ def test_streams_and_graphs(em):
             g.replay()
         torch.cuda.synchronize()
         assert torch.equal(outs[0], want[0]) and torch.equal(outs[1], want[1]), i
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_short_rows_leave_the_workspace_alone(em, dtype):
+    """Rows of up to 8192 tokens with the 4 KiB they ask for, as many rows as there are; nothing of it or
+    behind it is written."""
+    for T, V in ((1, 8192), (700, 8192), (3000, 40)):
+        print(f"sample workspace T={T} V={V} {dtype}", flush=True)
+        L, u = zipf(T, V, dtype, V)
+        k, p = vec([50] * T, torch.int32), vec([0.9] * T)
+        assert em.ember_sample_workspace_bytes(T, V) == 4096
+        buf = torch.full((4096 * 2,), 0xA5, dtype=torch.uint8, device=DEV)
+        ids, logp, kept = torch.empty(T, dtype=torch.int64, device=DEV), torch.empty(T, device=DEV), vec([0] * T, torch.int32)
+        em.ember_sample(L, u, ids, buf[:4096], top_k=k, top_p=p, logp=logp, kept=kept)
+        assert (buf == 0xA5).all()
+        for t in range(0, T, 97):
+            i, lp, n = one_row(L[t], u[t].double().item(), 1.0, 50, vec([0.9])[0].item())
+            assert (ids[t].item(), kept[t].item()) == (i, n), t
