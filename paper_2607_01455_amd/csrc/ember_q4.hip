@@ -47,7 +47,7 @@ uint32_t magic_of(uint32_t d) { return d == 1 ? 0 : (uint32_t)((((uint64_t)1 << 
 // ---------------------------------------------------------------------------
 
 constexpr int kRowThreads = 256;
-constexpr int64_t kPastBytes = (int64_t)128 << 20;        // of rows: from here on they are stored past the caches
+constexpr int64_t kPastBytes = (int64_t)96 << 20;         // of rows: from here on they are stored past the caches
 constexpr int kUnitLanes = 16;                            // lanes a block of codes, one dword each
 constexpr int kUnitsPerPass = kRowThreads / kUnitLanes;   // blocks of codes side by side
 constexpr int kAhead = 4;                                 // of a thread, whose loads go out together
@@ -161,9 +161,16 @@ struct RowsParams {
 // a block's 16 lanes is 256 bytes side by side: of bf16 the pairs' eight columns a lane;
 // of fp32 four, for which a lane loads two dwords.  Bound by the stores: 16384 tokens of
 // 128256 x 4096, bf16 (169 MB), 26 us, 6.5 TB/s.
-// kPast: stored past the caches, from where that costs the rows' reader no more than it gains
-// here (other buffers each time, x 4096 bf16, us past the caches and through them: 32768 rows 53 and
-// 93, with a sum over the rows 164 and 173; 16384 27 and 49, 89 and 88; 8192 16 and 27, 52 and 47).
+// kPast: stored past the caches, which is the faster form at every size where nothing reads the rows next, but a
+// reader that does finds them in the memory-side cache otherwise.  The limit is where the rows and the norm of them with
+// its residual, as a model goes on, together stop losing by it.  Time through the caches against past them, mean (least to
+// most) of ten tables of 32000 to 262144 rows and 1000 to 8192 columns, bf16 and fp32; the same buffers every time or
+// others make no difference with a reader:
+//   rows         80 MiB              96                   128                  144                 192
+//   alone        +10% (0 to +22)     +17 (+10 to +25)     +23 (+8 to +32)      +27 (+8 to +37)     +36 (+12 to +48)
+//   norm of sum  -0.6 (-5 to +4)     -0.2 (-4 to +5)      0.0 (-4 to +5)       +1.2 (-4 to +6)     +5 (-3 to +10)
+//   norm alone   -3.3 (-7 to +1)     -3.0 (-7 to +2)      -1.9 (-7 to +4)      +0.3 (-6 to +7)     +7 (-3 to +14)
+// The most is lost with 8192 columns of 128256 rows: of 128 MiB, and a norm alone, 86 us, 80 through the caches.
 template <typename T, int G, bool kPast>
 __global__ __launch_bounds__(kRowThreads) void ember_rows_q4(RowsParams p) {
     const Rows4Args& a = p.a;

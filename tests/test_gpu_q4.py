@@ -436,3 +436,24 @@ def test_no_tokens(em):
     _, Q, s = table(10, 40, 32, 1)
     em.ember_logits_q4(torch.empty(0, 48, dtype=torch.int8, device=DEV)[:, :40], torch.empty(0, device=DEV), Q, s,
                        torch.empty(0, 10, device=DEV), 32)
+
+
+@pytest.mark.parametrize("D,group", [(4096, 128), (1000, 64), (1001, 32), (8191, 128)])
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_rows_on_both_sides_of_the_store_limit(em, D, group, dtype):
+    """About 96 MiB of rows, where stores past the caches begin: each row is its token's, the padding is left alone,
+    and a reader next on the stream has them."""
+    V = 700
+    codes, Q, s = table(V, D, group, 6)
+    want = values(codes, s, group).to(dtype)
+    limit = -(-(96 << 20) // (D * (4 if dtype == F else 2)))
+    for n in (limit - 1, limit, limit + 1):
+        print(f"q4 rows D={D} n={n} {dtype}", flush=True)
+        tok = torch.randint(0, V, (n,), generator=gen(n), device=DEV)
+        tok[n // 3] = V
+        Y = mat(n, D, dtype)
+        em.ember_rows_q4(Q, s, Y, group, tok)
+        same = Y == want[tok.clamp(max=V - 1)]
+        same[n // 3] = torch.isnan(Y[n // 3].float())
+        assert same.all()
+        assert torch.isnan(Y._base[:, D:].float()).all()
