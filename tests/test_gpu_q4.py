@@ -438,6 +438,81 @@ def test_no_tokens(em):
                        torch.empty(0, 10, device=DEV), 32)
 
 
+# Shapes by the form that answers them: the streaming form in tiles of 32 tokens (waves that share strips up to 32736
+# channels, several strips a wave from there), in two such tiles, in tiles of 16 for 17 to 32 tokens of more columns than
+# the LDS holds of 32 (groups of 128: tiles), and in windows of the columns where it does not hold 16 or fewer either,
+# a strip a wave.
+STREAMED = [(17, 16385, 1000), (18, 16384, 512), (25, 20000, 96), (31, 20001, 4097), (32, 33000, 2047), (24, 40003, 640),
+            (32, 32737, 4600), (17, 131073, 200),
+            (33, 65665, 1000), (64, 70001, 2047), (63, 65537, 130), (48, 131072, 512), (40, 99999, 33),
+            (20, 40001, 8192), (17, 32769, 4700), (32, 33001, 12000),
+            (16, 40001, 12000), (5, 33001, 32768), (13, 32737, 15000)]
+
+
+@pytest.mark.parametrize("T,V,D", STREAMED)
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_logits_of_few_tokens_and_many_channels(em, T, V, D, group, dtype):
+    print(f"q4 streamed T={T} V={V} D={D} group={group} {dtype}", flush=True)
+    check(em, T, V, D, group, dtype, (T + V + group // 32) % 2 == 0, extra=(V + D) % 2)
+
+
+@pytest.mark.parametrize("V,D,counts", [(16384, 1000, (1, 16, 17, 31)), (33000, 4500, (2, 16, 17, 32)),
+                                        (70000, 1000, (1, 15, 16, 17, 32, 33, 63)), (66000, 2048, (1, 16, 32, 48))])
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_same_bits_in_every_streaming_form(em, V, D, counts, group):
+    """Tiles of 16, of 32 and of twice 32 tokens add a logit's groups in one order."""
+    print(f"q4 streamed bits V={V} D={D} group={group}", flush=True)
+    codes, Q, s = table(V, D, group, 2)
+    del codes
+    most = max(counts) + 1 if max(counts) % 32 else max(counts)
+    Xq, xs = tokens(most, D, 7)
+    whole = mat(most, V, F)
+    em.ember_logits_q4(Xq, xs, Q, s, whole, group)
+    for n in counts:
+        Y = mat(n, V, F)
+        em.ember_logits_q4(Xq[most - n:], xs[most - n:], Q, s, Y, group)
+        assert torch.equal(Y, whole[most - n:]), n
+
+
+def test_scales_that_are_not_finite_of_many_channels(em):
+    """What stands behind a row's scales, or in another row's, does not reach a channel (widest tiles and windows)."""
+    for T, V, D in ((20, 16400, 200), (50, 66000, 200), (12, 33000, 13000), (30, 33000, 5000)):
+        print(f"q4 streamed scales T={T} V={V} D={D}", flush=True)
+        codes, Q, s = table(V, D, 32, 4)                  # the scales' padding is NaN
+        Xq, xs = tokens(T, D, 3)
+        xs[2] = float("nan")
+        s[7, 6], s[V - 1, 0] = float("inf"), float("nan")
+        Y = mat(T, V, F)
+        em.ember_logits_q4(Xq, xs, Q, s, Y, 32)
+        assert torch.isnan(Y[2]).all() and torch.isnan(Y[:, V - 1]).all()
+        rest = torch.arange(T, device=DEV) != 2
+        cols = (torch.arange(V, device=DEV) != 7) & (torch.arange(V, device=DEV) != V - 1)
+        near(Y[rest][:, cols], codes[cols], s[cols], 32, Xq[rest], xs[rest], None)
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_scales_against_a_seventh_of_the_largest(em, group, dtype):
+    """s = a / 7 (1 + d1) (1 + d2) (1 + d3): the constant and the product within 2^-24 each, bf16 to the nearest of
+    what that gives: |s - a / 7| <= half a step of bf16 + a / 7 (2^-23 + 2^-47), below 2^-22 a / 7 more than half a step."""
+    V, D = 4000, 8 * group
+    X = torch.randn(V, D, generator=gen(group), device=DEV) * torch.rand(V, 1, generator=gen(1), device=DEV) * 10
+    if dtype == F:
+        # ties of a / 7 between two scales, and the fp32 next to them
+        k = torch.arange(128, 256, device=DEV, dtype=torch.float64)
+        tie = (7 * (2 * k + 1)).float()
+        X[:128] *= 1e-3
+        X[:128, 0], X[:128, group] = tie, torch.nextafter(tie, torch.zeros_like(tie))
+        X[:128, 2 * group] = torch.nextafter(tie, tie * 2)
+    X = X.to(dtype)
+    head = em.HeadQ4.from_table(X, group)
+    a = X.double().view(V, 8, group).abs().amax(dim=2)
+    s = head.wscale.double()
+    half = torch.exp2(torch.floor(torch.log2(a / 7)) - 8)
+    assert ((s - a / 7).abs() <= half + a / 7 * 2.0 ** -22).all()
+
+
 @pytest.mark.parametrize("D,group", [(4096, 128), (1000, 64), (1001, 32), (8191, 128)])
 @pytest.mark.parametrize("dtype", [BF, F])
 def test_rows_on_both_sides_of_the_store_limit(em, D, group, dtype):
