@@ -373,3 +373,90 @@ def test_short_rows_leave_the_workspace_alone(em, dtype):
         for t in range(0, T, 97):
             i, lp, n = one_row(L[t], u[t].double().item(), 1.0, 50, vec([0.9])[0].item())
             assert (ids[t].item(), kept[t].item()) == (i, n), t
+
+
+@pytest.mark.parametrize("T,V,dtype", [(513, 8193, F), (1030, 9001, BF), (520, 30000, BF)])
+def test_more_long_rows_than_a_launch(em, T, V, dtype):
+    """Rows past the 512 of a launch have their own parameters, in a workspace that the ones before left full."""
+    print(f"sample long rows T={T} V={V} {dtype}", flush=True)
+    L, u = zipf(T, V, dtype, T)
+    r = [torch.rand(T, generator=gen(T + i), device=DEV) for i in range(4)]
+    temperature = 0.3 + 1.4 * r[0]
+    temperature[::11] = 0
+    k = torch.where(r[1] < 0.4, 0, (10 ** (3.5 * r[1])).int())
+    p = torch.where(r[2] < 0.3, 1.0, 0.5 + 0.5 * r[2])
+    floor = torch.where(r[3] < 0.6, 0.0, 0.1 * (r[3] - 0.6))
+    L[::13] = torch.randint(0, 3, (len(L[::13]), V), generator=gen(9), device=DEV).to(dtype) * 0.25      # ends among equal ones
+    L[5::17, V // 2:] = -INF
+    L[512:, V - 1] = -INF
+    L[-1] = -INF
+    check(em, L, u, temperature, k, p, floor)
+    check(em, L, u)
+
+
+def ends(V, dtype):
+    low, top = torch.finfo(dtype).min, torch.finfo(dtype).max
+    L, u = zipf(12, V, dtype, 3)
+    L[0] = low
+    L[1, 1:] = low
+    L[2, ::2] = low
+    L[3] = 0.0
+    L[3, ::2] = -0.0
+    L[4, V - 7] = top
+    L[5] = low
+    L[5, V // 2] = top
+    L[6] = top
+    L[7] = -INF
+    L[7, ::5] = low
+    L[8] = torch.linspace(-1e38, 1e38, V, device=DEV).to(dtype)
+    L[9] = -torch.rand(V, generator=gen(5), device=DEV) * 1e-37          # a border about the smallest normal numbers
+    L[10] = (torch.rand(V, generator=gen(6), device=DEV) - 0.5) * 1e-40  # subnormal in both types
+    L[11] = low
+    L[11, V - 1] = torch.nextafter(torch.tensor(low, dtype=dtype), torch.tensor(0.0, dtype=dtype))
+    return L, u
+
+
+@pytest.mark.parametrize("V", [8193, 20000])
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_values_at_the_ends_of_long_rows(em, V, dtype):
+    print(f"sample ends V={V} {dtype}", flush=True)
+    L, u = ends(V, dtype)
+    T = len(L)
+    for kw in (dict(), dict(k=[5] * T), dict(p=[0.7] * T), dict(floor=[0.3] * T), dict(temperature=[0.0] * T),
+               dict(temperature=[3e38] * T, p=[0.7] * T), dict(temperature=[1e-38] * T, k=[7] * T),
+               dict(temperature=[1e-30] * T, p=[0.9] * T), dict(k=[V // 2] * T, p=[0.6] * T, floor=[0.01] * T),
+               dict(temperature=[1e-44] * T, floor=[0.5] * T)):
+        check(em, L, u, **kw)
+
+
+@pytest.mark.parametrize("V", [8193, 20000, 128256])
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_long_rows_without_a_token(em, V, dtype):
+    """NaN or infinity in the first, a middle or the last part of a row, nothing allowed, parameters out of range: -1 there, the
+    other rows as they are."""
+    T = 20
+    print(f"sample without V={V} {dtype}", flush=True)
+    L, u = zipf(T, V, dtype, 4)
+    want0 = draw(em, L, u)
+    bad = logits(T, V, dtype)
+    bad.copy_(L)
+    for t, (i, x) in enumerate(((0, float("nan")), (V // 2, float("nan")), (V - 1, float("nan")), (0, INF), (V // 2, INF), (V - 1, INF))):
+        bad[t, i] = x
+    bad[6] = -INF
+    bad[7, V // 3] = -float("nan")
+    for kw in (dict(), dict(k=vec([9] * T, torch.int32)), dict(p=vec([0.9] * T)), dict(floor=vec([0.05] * T))):
+        want = draw(em, L, u, **kw)
+        got = draw(em, bad, u, **kw)
+        assert (got[0][:8] == -1).all() and torch.isnan(got[1][:8]).all() and (got[2][:8] == 0).all()
+        for a, b in zip(got, want):
+            assert torch.equal(a[8:], b[8:])
+    u2, temp, k = u.clone(), torch.ones(T, device=DEV), torch.zeros(T, dtype=torch.int32, device=DEV)
+    p, floor = torch.ones(T, device=DEV), torch.zeros(T, device=DEV)
+    u2[0], u2[1], u2[2] = 1.0, -1e-9, float("nan")
+    temp[3], temp[4], temp[5] = -1.0, INF, float("nan")
+    k[6] = -1
+    p[7], p[8], p[9] = -0.1, 1.0001, float("nan")
+    floor[10], floor[11], floor[12] = -0.1, 1.5, float("nan")
+    ids, logp, kept = draw(em, L, u2, temp, k, p, floor)
+    assert (ids[:13] == -1).all() and torch.isnan(logp[:13]).all() and (kept[:13] == 0).all()
+    assert torch.equal(ids[13:], want0[0][13:]) and torch.equal(logp[13:], want0[1][13:]) and (kept[13:] == V).all()
