@@ -537,9 +537,10 @@ int ember_rows_q4(const uint8_t* Wq, int64_t ldw, const uint16_t* wscale, int64_
  *
  *   Y_tv = xscale_t sum_g wscale_vg (sum_{k in g} Xq_tk c_vk) + bias_v
  *
- * A group's sum is exact, the sum over the groups fp32 in an order fixed by the sizes;
- * the result is rounded once to y_dtype.  bias (V, fp32) may be NULL.  0 <= T <=
- * EMBER_MAX_TOKENS (0: nothing to do, the pointers may be NULL).
+ * A group's sum is exact, the sum over the groups fp32 in an order fixed by the sizes
+ * (held times 16: one of 2^124 and more is an infinity); the result is rounded once to
+ * y_dtype.  bias (V, fp32) may be NULL.  0 <= T <= EMBER_MAX_TOKENS (0: nothing to do,
+ * the pointers may be NULL).
  */
 int ember_logits_q4(const int8_t* Xq, int64_t ldx, const float* xscale,
                     const uint8_t* Wq, int64_t ldw, const uint16_t* wscale, int64_t lds, int group,

@@ -290,9 +290,10 @@ struct Few4Params {
 // waves share one, unit by unit, and add up in LDS.  Blocks of the same channels and
 // other tokens are neighbours on one XCD, whose L2 then has the codes.  The order of
 // a logit's sum depends on V and D, not on the number of tokens.
-// 128256 x 4096: 1 token, groups of 128, 45 to 48 us (271 MB, 5.6 to 6.0 TB/s; reading alone 6.9);
-// 16 tokens, groups of 32, 57 to 63, where the sums' scaling takes the vector units; 64 x 100000 x
-// 1000 28 (MFMA, scaling and loads of one wave follow each other).
+// 128256 x 4096: 1 token, groups of 128, 44 to 48 us (271 MB, 5.6 to 6.1 TB/s; reading alone 6.9); 16 tokens,
+// groups of 32, 54 to 63, where no unit is full: the vector units work for 41% of the time (half of it on the sums'
+// scaling), the matrix units for 10%, and a wave's loads, operands, MFMAs and scaling follow each other; 64 x 100000 x
+// 1000, groups of 64, 26.
 template <typename C, int G, typename YT>
 __global__ __launch_bounds__(C::kThreads) void ember_logits_q4_few(Few4Params p) {
     const Logits4Args& a = p.a;
@@ -632,9 +633,9 @@ struct Tile4 {
 // for each 32 x 32 tile, as long as the MFMAs of 128 columns take.  So these are laid
 // between the next sum's MFMAs, each wave has all of the block's tokens (the codes' halves
 // are taken apart once), and the step barrier sits before the last tile of tokens, whose
-// operands are in registers by then.  1024 x 128256 x 4096, groups of 128, bf16 logits: 674
-// to 693 us, 1.6 POPS (the int8 library product, without scales: 2.0); the vector units
-// have 55% of the time, the matrix units 36%, and they hardly overlap.
+// operands are in registers by then.  1024 x 128256 x 4096, groups of 128, bf16 logits: 660 to
+// 720 us by card (the first dozen launches 715 to 750), 1.5 to 1.6 POPS (the int8 library product, without scales:
+// 2.0); the vector units have 55% of the time, the matrix units 36%, and they hardly overlap.
 template <typename C, int G, typename YT>
 __global__ __launch_bounds__(C::kThreads) void ember_logits_q4(Tile4Params p) {
     __shared__ __attribute__((aligned(1024))) uint8_t lds[C::kLds];
@@ -958,8 +959,8 @@ hipError_t launch_tiles(const Logits4Args& a, hipStream_t s) {
     p.tiles = (int64_t)p.MT * p.NT;
     p.per_xcd = (p.tiles + kXcds - 1) / kXcds;
     // The blocks that are there at once go through the tiles, so that the next one's first loads are
-    // out while one is stored (1024 x 131072: 721 us at D = 4096 and 239 at 1024; a tile a block 764
-    // and 251); of few steps, with nothing to hide the stores behind, a tile a block (168 at 512; 181).
+    // out while one is stored (1024 x 131072: 690 us at D = 4096 and 230 at 1024; a tile a block 720
+    // and 245); of few steps, with nothing to hide the stores behind, a tile a block (172 at 512; 181).
     const int64_t blocks = p.nk < 6 || C::kGroups > 1 ? kMaxGridBlocks : kCus * C::kBlocks;
     const unsigned grid = (unsigned)(std::min<int64_t>(p.per_xcd, blocks / kXcds) * kXcds);
     if (a.y_dtype == EMBER_F32) launch_tile<C, G, float>(p, grid, s);
@@ -975,8 +976,8 @@ using T64x128Two = Tile4<64, 4, 3, 2>;
 // the small tiling's hold two blocks (the second costs 0.6 of the first), a round of large
 // tiles being 2.2 of its own (fitted to 96 to 1024 tokens, 2000 to 100000 channels, D = 1000 and
 // 4096, all group sizes: what it takes is never more than 1% slower than the other; 512 x 32000
-// x 4096, groups of 128: 86 us, 119 in small tiles; 333 x 8191 x 1000, groups of 64: 14.6, 19.6 in
-// large ones).
+// x 4096, groups of 128: 82 us, 115 in small tiles; 333 x 8191 x 1000, groups of 64, in small ones: bf16 logits
+// 14.8, 19.4 in large; fp32 with a bias 16.9 and 21.7).
 bool large_tiles(const Logits4Args& a) {
     const auto tiles = [&](int BM, int BN) { return (double)((a.T + BM - 1) / BM) * (double)((a.V + BN - 1) / BN) / kCus; };
     const double small = tiles(T64x128::BM, T64x128::BN);
@@ -985,13 +986,15 @@ bool large_tiles(const Logits4Args& a) {
 
 // Up to 16 tokens the streaming form.  Up to 64 it is the faster one
 //   - in tiles of 16 tokens for small tables, as long as these are few: several tiles' blocks fill the
-//     chip and the codes come from the caches (us, D = 2048, groups of 128: 64 x 4000 8.1, 12.4 with the
-//     tiling; 64 x 8000 14.9 and 12.4; groups of 32 16.4 and 17.6, but 64 x 16000 32 and 18);
+//     chip and the codes come from the caches (us, D = 2048, groups of 128: 64 x 4000 8.4, 12.5 with the
+//     tiling; 64 x 8000 15.3 and 12.5; groups of 32 16.8 and 17.8, but 64 x 16000 32 and 18);
 //   - in tiles of 32 or 64 tokens whose codes fit the LDS for large ones: of up to 32 tokens (32 x 60000 x
-//     2048 18, 19 with the tiling), of more where the small tiling takes more than one round (64 x 60000
-//     x 2048 24 and 20, 64 x 128256 x 2048, groups of 64, 42 and 45);
+//     2048 17.7, 19.0 with the tiling), of more where the small tiling takes more than one round (64 x 60000
+//     x 2048 24 and 20, 64 x 128256 x 2048, groups of 64, 42 and 44);
 //   - in tiles of 16 for up to 32 tokens that do not fit, where groups of 32 or 64 keep the tiling's vector
-//     units (32 x 60000 x 8192: 88 and 104; groups of 128 82 and 57).
+//     units (32 x 60000 x 8192: groups of 32 88 and 104, of 64 82 and 75, of 128 81 and 57; of 64 it is the
+//     faster one in 14 of 20 shapes of 34000 to 128256 channels and 4700 to 8192 columns, 32 x 34000 x 8192 54 and 74,
+//     and 13% slower at most).
 template <int G>
 hipError_t launch_group(const Logits4Args& a, hipStream_t s) {
     const int64_t pitch = few_pitch((a.D + kUnit * kBlockCols - 1) / (kUnit * kBlockCols));

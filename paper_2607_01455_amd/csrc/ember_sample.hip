@@ -28,11 +28,12 @@
 // alone have most of their bins about 0, where floats are dense: 256 rows of 8192 with top-k
 // and top-p take 20 us, and 31 so.)
 //
-// Bound by: a row of 8192 by the chain of its barriers (8 to 10 us, 18 to 20 with filters, 1 or 256
-// rows); few long rows by the chain of the four launches (16 x 128256 bf16: 4 + 9 + 8 + 11 us);
-// many by HBM in launch 1 (256 x 128256 fp32: 23 us, 5.8 TB/s), the vector units and LDS
-// atomics in 2 (41 us: 70% and 40% busy), loads and the rows that keep the most tokens in 3
-// (37 us; 4 takes 13).
+// Bound by: a short row by one block's chain of latencies (8 us for 64 logits as for 8191, 9 for 256 such rows: by clocks
+// kept along the way a third goes to the joined range and the row's parameters in fp64, an eighth to the logits' loads, a
+// fifth to the last token with its logarithm, a sixth to the two sums over the block and their barriers), with filters
+// by that of finding the ends (17 to 23 us, 1 or 256 rows); few long rows by the chain of the four launches (16 x 128256
+// bf16: 4 + 9 + 8 + 11 us); many by HBM in launch 1 (256 x 128256 fp32: 23 us, 5.8 TB/s), the vector units and LDS
+// atomics in 2 (41 us: 70% and 40% busy), loads and the rows that keep the most tokens in 3 (37 to 40 us; 4 takes 13).
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
