@@ -291,7 +291,7 @@ struct Few4Params {
 // other tokens are neighbours on one XCD, whose L2 then has the codes.  The order of
 // a logit's sum depends on V and D, not on the number of tokens.
 // 128256 x 4096: 1 token, groups of 128, 44 to 48 us (271 MB, 5.6 to 6.1 TB/s; reading alone 6.9); 16 tokens,
-// groups of 32, 54 to 63, where no unit is full: the vector units work for 41% of the time (half of it on the sums'
+// groups of 32, 54 to 63, where no unit is full: the vector units work for 40% of the time (half of it on the sums'
 // scaling), the matrix units for 10%, and a wave's loads, operands, MFMAs and scaling follow each other; 64 x 100000 x
 // 1000, groups of 64, 26.
 template <typename C, int G, typename YT>
@@ -634,7 +634,7 @@ struct Tile4 {
 // between the next sum's MFMAs, each wave has all of the block's tokens (the codes' halves
 // are taken apart once), and the step barrier sits before the last tile of tokens, whose
 // operands are in registers by then.  1024 x 128256 x 4096, groups of 128, bf16 logits: 660 to
-// 720 us by card (the first dozen launches 715 to 750), 1.5 to 1.6 POPS (the int8 library product, without scales:
+// 720 us by card (the first dozen launches up to 780), 1.5 to 1.6 POPS (the int8 library product, without scales:
 // 2.0); the vector units have 55% of the time, the matrix units 36%, and they hardly overlap.
 template <typename C, int G, typename YT>
 __global__ __launch_bounds__(C::kThreads) void ember_logits_q4(Tile4Params p) {
