@@ -532,3 +532,17 @@ def test_rows_on_both_sides_of_the_store_limit(em, D, group, dtype):
         same[n // 3] = torch.isnan(Y[n // 3].float())
         assert same.all()
         assert torch.isnan(Y._base[:, D:].float()).all()
+
+
+@pytest.mark.parametrize("T", [1, 20, 70, 300])
+def test_sums_near_the_end_of_fp32(em, T):
+    """Sums of up to 2^124 before the token's scale (held times 16, below 2^128), exact: one group, powers of two."""
+    V, D = 600, 128
+    codes, Q, s = table(V, D, 128, 3)
+    Xq, _ = tokens(T, D, 5)
+    sums = Xq.double() @ codes.double().t().contiguous()
+    top = 123 - int(sums.abs().max().log2().floor())
+    s.fill_(2.0 ** top)
+    Y = mat(T, V, F)
+    em.ember_logits_q4(Xq, torch.full((T,), 2.0 ** -100, device=DEV), Q, s, Y, 128)
+    assert torch.equal(Y.double(), sums * 2.0 ** (top - 100))
